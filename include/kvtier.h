@@ -19,7 +19,8 @@
  *              = 1.5 MiB for L=48, Hkv=4 (the paper's block unit, Section 4).
  *              Each (block, layer, K|V, kv-head) run is bt*D*2 = 4 KiB.
  *   cold image img[L][2][Hkv][T_cap][D] per session, contiguous and
- *              layer-major, placed in the cold arena by the pool.
+ *              layer-major, placed in the cold arena by the pool
+ *              (KV_POOL_COLD_INT8: int8 codes and exponents, see there).
  *   block table: row of int32 physical block ids; logical block j of a
  *              session holds its tokens j*bt .. j*bt+bt-1.
  *
@@ -94,6 +95,25 @@ enum { KV_SESSION_FREE = 0, KV_SESSION_ACTIVE = 1, KV_SESSION_PAUSED = 2 };
  * victims' own appends and resumes by themselves). */
 #define KV_POOL_LRU_RESIDENCY 2u
 
+/* Pool flag: cold images in 8 bits. A pause or an eviction quantises each row
+ * (token, layer, K or V, kv-head; 128 values) as it writes the image, a resume
+ * or a fetch reads the row back into bf16. The image is then
+ *   int8  codes[L][2][Hkv][T_cap][D], followed by
+ *   uint8 exponents[L][2][Hkv][T_cap]
+ * (kv_image_token_bytes: 129 bytes per row in place of 256, so the cold tier
+ * holds nearly twice the tokens, and moves and writes half the bytes). With E
+ * the biased exponent of the row's largest finite magnitude, at least 1,
+ *   code  = round_to_even(x * 2^(133 - E)), held to [-127, 127];
+ *   value = code * 2^(E - 133), exactly a bf16;
+ * an error of at most half a step, 1/127 of the row's largest magnitude. A
+ * value that is not finite has code -128 and reads back as NaN. Packing what
+ * was read back gives the same codes, so a token keeps its values however
+ * often it goes out and comes back after the first time. Tokens already in the
+ * image are not rewritten, as in any pool. Everything else (hot blocks, tables,
+ * states, errors) is as without the flag; decode outputs differ across the
+ * first pause of a token by what the rounding changes. */
+#define KV_POOL_COLD_INT8 4u
+
 typedef struct kv_pool_config {
     int32_t num_layers;     /* L  (48 for Qwen3-Coder-30B-A3B)             */
     int32_t num_q_heads;    /* Hq (32); Hq / Hkv must be 1, 2, 4 or 8      */
@@ -109,7 +129,7 @@ typedef struct kv_pool_config {
     int64_t cold_bytes;     /* bytes in the cold arena                      */
     void *cold_base;        /* device, 256-B aligned                        */
     uint64_t alloc_seed;    /* seeds the shuffle of the initial free list   */
-    uint32_t flags;         /* KV_POOL_HOST_LOGIC_ONLY | KV_POOL_LRU_RESIDENCY */
+    uint32_t flags;         /* KV_POOL_* bits                               */
     uint32_t reserved;
 } kv_pool_config;
 
@@ -119,7 +139,8 @@ typedef struct kv_session_info {
     int64_t tokens;      /* T: tokens in the session's KV                  */
     int64_t capacity;    /* T_cap of its cold image                        */
     int64_t cold_valid;  /* tokens already valid in the cold image         */
-    void *image;         /* device address of img[L][2][Hkv][T_cap][D]     */
+    void *image;         /* device address of img[L][2][Hkv][T_cap][D]
+                          * (8-bit images: of the codes; the exponents follow) */
 } kv_session_info;
 
 typedef struct kv_pool_stats {
@@ -167,6 +188,10 @@ int64_t kv_block_bytes(const kv_pool_config *cfg);
  * model, Section 4). */
 int64_t kv_token_bytes(const kv_pool_config *cfg);
 
+/* Bytes of a token in a cold image: kv_token_bytes, or L * 2 * Hkv * (D + 1)
+ * with KV_POOL_COLD_INT8. */
+int64_t kv_image_token_bytes(const kv_pool_config *cfg);
+
 /* S(t): the most KV splits a decode call makes for one (session, head) of up
  * to t tokens, the factor by which the decode workspace scales (see
  * decode_attention). Each session of T tokens is cut into ceil(T/16) 16-token
@@ -179,7 +204,7 @@ int32_t kv_decode_splits(int64_t t);
  * is the paper's unit of agentic serving, whose context keeps growing
  * across turns (Section 2, "Agentic AI Serving"); its cold image is the
  * per-session region that data path 4 writes (Section 3). Reserves the
- * image (max_tokens * token bytes, rounded up to 256 B) in the cold arena
+ * image (max_tokens * kv_image_token_bytes, rounded up to 256 B) in the cold arena
  * (first fit). Errors: KV_ERR_NO_COLD_SPACE, too many sessions ->
  * KV_ERR_INVALID_ARG. */
 int session_create(kv_pool *pool, int64_t max_tokens, int32_t *sid_out);

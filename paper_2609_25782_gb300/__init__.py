@@ -23,7 +23,7 @@ class Pool:
                  num_q_heads: int = 32, num_kv_heads: int = 4, head_dim: int = 128,
                  block_tokens: int = 16, max_sessions: int = 64, max_batch: int = 64,
                  max_context: int = 32768, alloc_seed: int = 0, device: int = 0,
-                 lru_residency: bool = False):
+                 lru_residency: bool = False, cold_int8: bool = False):
         import torch
         self.device = torch.device("cuda", device)
         self.L, self.Hq, self.Hkv, self.D, self.bt = (num_layers, num_q_heads, num_kv_heads,
@@ -36,6 +36,7 @@ class Pool:
         self.token_bytes = kvtier.kv_token_bytes(probe)
         self.hot = torch.empty(num_hot_blocks * self.block_bytes // 2, dtype=torch.bfloat16,
                                device=self.device)
+        self.cold_int8 = cold_int8
         self.cold = torch.empty(max(cold_bytes, 256) // 2, dtype=torch.bfloat16, device=self.device)
         cfg = kvtier.make_config(num_layers=num_layers, num_q_heads=num_q_heads,
                                  num_kv_heads=num_kv_heads, head_dim=head_dim,
@@ -43,7 +44,8 @@ class Pool:
                                  max_batch=max_batch, device=device, max_context=max_context,
                                  num_hot_blocks=num_hot_blocks, hot_base=self.hot,
                                  cold_bytes=cold_bytes, cold_base=self.cold, alloc_seed=alloc_seed,
-                                 flags=kvtier.KV_POOL_LRU_RESIDENCY if lru_residency else 0)
+                                 flags=(kvtier.KV_POOL_LRU_RESIDENCY if lru_residency else 0) |
+                                 (kvtier.KV_POOL_COLD_INT8 if cold_int8 else 0))
         self.handle = kvtier.kv_pool_create(cfg)
         self.max_context = max_context
 
@@ -65,10 +67,24 @@ class Pool:
 
     def image(self, sid: int):
         """A session's cold image as [L][2][Hkv][T_cap][D] bf16 (a view)."""
+        if self.cold_int8:
+            raise ValueError("the pool's images hold 8-bit rows: image_int8")
         info = kvtier.session_info(self.handle, sid)
         off = (info.image - self.cold.data_ptr()) // 2
         n = self.L * 2 * self.Hkv * info.capacity * self.D
         return self.cold[off:off + n].view(self.L, 2, self.Hkv, info.capacity, self.D)
+
+    def image_int8(self, sid: int):
+        """A session's 8-bit cold image (views): int8 codes [L][2][Hkv][T_cap][D] and uint8
+        exponents [L][2][Hkv][T_cap]; value = code * 2^(exponent - 133), code -128 a NaN."""
+        import torch
+        if not self.cold_int8:
+            raise ValueError("the pool's images hold bf16 rows: image")
+        info = kvtier.session_info(self.handle, sid)
+        off, shape = info.image - self.cold.data_ptr(), (self.L, 2, self.Hkv, info.capacity)
+        rows = self.L * 2 * self.Hkv * info.capacity
+        flat = self.cold.view(torch.int8)[off:off + rows * (self.D + 1)]
+        return flat[:rows * self.D].view(*shape, self.D), flat[rows * self.D:].view(torch.uint8).view(shape)
 
     # C ABI forwards ------------------------------------------------------------
     def session_create(self, max_tokens: int) -> int:

@@ -1,18 +1,22 @@
 // Copy kernels of the hot/cold KV tiering hot path, for sm_103a.
 //
-//   migrate_kernel<false>  data path 2: resume-unpack, cold image -> blocks.
+//   migrate_kernel<false,> data path 2: resume-unpack, cold image -> blocks.
 //   resume_inline_kernel   the same for a resume of up to 2 048 blocks whose
 //                          ids ride in the launch (it also writes the row).
-//   migrate_kernel<true>   data path 4: pause-pack, blocks -> cold image,
+//   migrate_kernel<true,>  data path 4: pause-pack, blocks -> cold image,
 //                          tokens [t0, T) only (write-on-evict, Section 3).
 //   block_jobs_kernel<>    the same moves for explicit (slot, block, token
 //                          range) lists: residency-mode evictions and fetches.
+//   Each of these moves bytes, or (kInt8) quantises rows into 8-bit images and
+//   reads them back.
 //   append_kernel          data path 3: fresh tokens into the tail blocks.
 //   append_inline_kernel   the same with up to 2 048 new block ids in the launch.
 //   table_write_kernel / gather_tables_kernel: block-table bookkeeping.
 //
 // Hot pool: hot[NB][L][2][Hkv][bt][128] bf16. A (block, layer, K|V, head)
-// run is bt rows of 256 B. The image of a session is img[L][2][Hkv][T_cap][128].
+// run is bt rows of 256 B. The image of a session is img[L][2][Hkv][T_cap][128],
+// bf16; an 8-bit one holds int8 codes of that shape, then one exponent byte per
+// row, [L][2][Hkv][T_cap].
 #include <cstdint>
 
 #include "kvt_internal.h"
@@ -106,13 +110,168 @@ __device__ __forceinline__ void move_rows(const uint8_t *from, uint8_t *to, int 
         if (k * 32 < units) st_row(dst + k * 32, v[k], policy);
 }
 
+// An 8-bit row: E = the biased exponent of the row's largest finite magnitude
+// (at least 1), code = x * 2^(133 - E) rounded to nearest even and held to
+// [-127, 127], value = code * 2^(E - 133). |x| < 2^(E - 126), so the scaled
+// magnitude is below 128 (127.5 at most for a bf16 x, and 127 is half a step
+// from that as any rounding may be), and the largest code is at least 64 unless
+// the row is subnormal. A power of two for the step, and not largest / 127, makes
+// every step here exact but the one rounding: a code has seven bits and a sign,
+// bf16 eight significant bits, so the value read back is exactly a bf16, and
+// packing it again gives the same codes. A value that is not finite becomes code
+// -128 and reads back as NaN; the row's others keep theirs.
+constexpr uint32_t kBf16Inf = 0x7F80;
+
+__device__ __forceinline__ float exp2_bits(int biased) {   // 2^(biased - 127), biased in [-22, 254]
+    return __int_as_float(biased >= 1 ? biased << 23 : 1 << (biased + 22));
+}
+
+// A lane's 16 values of a row, eight lanes per row (kRowLanes, in lane order).
+constexpr int kRowLanes = kRowBytes / 32;
+
+// Codes of a lane's 16 values, four per word; the row's exponent in *exponent.
+__device__ __forceinline__ uint4 quantise(const Row32 &v, uint32_t *exponent) {
+    uint32_t top = 0;   // magnitudes in both halves of a word, as unsigned
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = __vmaxu2(top, v.w[k] & 0x7FFF7FFFu);
+#pragma unroll
+    for (int d = 1; d < kRowLanes; d <<= 1) top = __vmaxu2(top, __shfl_xor_sync(~0u, top, d));
+    uint32_t most = max(top & 0xFFFFu, top >> 16);
+    const bool odd = most >= kBf16Inf;   // the same in a row's eight lanes
+    if (__any_sync(~0u, odd)) {          // the largest finite one
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t lo = v.w[k] & 0x7FFFu, hi = v.w[k] >> 16 & 0x7FFFu;
+            m = max(m, max(lo < kBf16Inf ? lo : 0u, hi < kBf16Inf ? hi : 0u));
+        }
+#pragma unroll
+        for (int d = 1; d < kRowLanes; d <<= 1) m = max(m, __shfl_xor_sync(~0u, m, d));
+        most = m;
+    }
+    const int E = max(1, static_cast<int>(most >> 7));
+    *exponent = E;
+    // 2^(133 - E) is up to 2^132: two factors
+    const float s1 = exp2_bits(min(254, 260 - E)), s2 = exp2_bits(127 + max(0, 6 - E));
+    uint32_t c[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint32_t f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = v.w[2 * k + (i >> 1)];
+            const float x = __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
+            const float y = fminf(fmaxf(x * s1 * s2, -127.f), 127.f);
+            f[i] = __float_as_uint(y + 12582912.f);   // 1.5 * 2^23: the rounded integer in the low bits
+            if (odd && (w >> (i & 1 ? 16 : 0) & 0x7FFFu) >= kBf16Inf) f[i] = 0x80u;
+        }
+        c[k] = __byte_perm(__byte_perm(f[0], f[1], 0x0040), __byte_perm(f[2], f[3], 0x0040), 0x5410);
+    }
+    return make_uint4(c[0], c[1], c[2], c[3]);
+}
+
+// The 16 values of a lane's codes, exponent E.
+__device__ __forceinline__ Row32 values_of(const uint4 &codes, int E) {
+    const float step = exp2_bits(E - 6);
+    const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w};
+    Row32 v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t u = c[k] ^ 0x80808080u;   // code + 128
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)   // 2^23 + code + 128, exactly
+            x[i] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540 + i)) - 8388736.f) * step;
+        // The product is exactly a bf16: its upper half is all of it.
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            v.w[2 * k + i] = __byte_perm(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]), 0x7632);
+    }
+    // Code -128 alone has nothing but its sign bit: such words are rare.
+    const uint32_t nan4 = __vcmpeq4(c[0], 0x80808080u) | __vcmpeq4(c[1], 0x80808080u) |
+                          __vcmpeq4(c[2], 0x80808080u) | __vcmpeq4(c[3], 0x80808080u);
+    if (nan4) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t m = __vcmpeq4(c[k >> 1], 0x80808080u) >> (k & 1 ? 16 : 0);
+            if (m & 0xFFu) v.w[k] = (v.w[k] & 0xFFFF0000u) | 0x7FFFu;
+            if (m & 0xFF00u) v.w[k] = (v.w[k] & 0xFFFFu) | 0x7FFF0000u;
+        }
+    }
+    return v;
+}
+
+__device__ __forceinline__ uint4 ld_codes(const uint4 *p, uint64_t policy) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0,%1,%2,%3}, [%4], %5;"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p), "l"(policy));
+    return v;
+}
+
+__device__ __forceinline__ void st_codes(uint4 *p, const uint4 &v, uint64_t policy) {
+    asm volatile("st.global.L2::cache_hint.v4.u32 [%0], {%1,%2,%3,%4}, %5;" ::"l"(p), "r"(v.x),
+                 "r"(v.y), "r"(v.z), "r"(v.w), "l"(policy)
+                 : "memory");
+}
+
+// Up to one chunk of hot rows into (kPack) or out of an 8-bit image's codes and
+// exponents, by a warp: four rows a round, eight lanes each.
+template <bool kPack>
+__device__ __forceinline__ void move_rows8(uint8_t *hot, uint8_t *codes, uint8_t *exps, int rows,
+                                           int lane, uint64_t policy) {
+    Row32 *h = reinterpret_cast<Row32 *>(hot) + lane;
+    uint4 *c = reinterpret_cast<uint4 *>(codes) + lane;
+    constexpr int kRound = 32 / kRowLanes;   // rows a round
+    const int r0 = lane / kRowLanes;
+    if constexpr (kPack) {
+        Row32 v[kMigUnroll] = {};
+#pragma unroll
+        for (int k = 0; k < kMigUnroll; ++k)
+            if (k * kRound + r0 < rows) v[k] = ld_row(h + k * 32, policy);
+#pragma unroll
+        for (int k = 0; k < kMigUnroll; ++k) {
+            uint32_t e;
+            const uint4 q = quantise(v[k], &e);
+            if (k * kRound + r0 < rows) {
+                st_codes(c + k * 32, q, policy);
+                if (lane % kRowLanes == 0) exps[k * kRound + r0] = static_cast<uint8_t>(e);
+            }
+        }
+    } else {
+        uint4 q[kMigUnroll];
+        uint32_t e[kMigUnroll];
+#pragma unroll
+        for (int k = 0; k < kMigUnroll; ++k)
+            if (k * kRound + r0 < rows) {
+                q[k] = ld_codes(c + k * 32, policy);
+                e[k] = exps[k * kRound + r0];
+            }
+#pragma unroll
+        for (int k = 0; k < kMigUnroll; ++k)
+            if (k * kRound + r0 < rows) st_row(h + k * 32, values_of(q[k], e[k]), policy);
+    }
+}
+
+// Rows [row, row + n) of an image of `rows` rows to or from hot rows at hp.
+template <bool kPack, bool kInt8>
+__device__ __forceinline__ void move_image_rows(uint8_t *hp, uint8_t *img, int64_t rows, int64_t row,
+                                                int n, int lane, uint64_t policy) {
+    if constexpr (kInt8) {
+        move_rows8<kPack>(hp, img + row * kCodeBytes, img + rows * kCodeBytes + row, n, lane, policy);
+    } else {
+        uint8_t *ip = img + row * kRowBytes;
+        move_rows(kPack ? hp : ip, kPack ? ip : hp, n, lane, policy);
+    }
+}
+
 // K3 / K4: the chunks of the token range of every (layer, K|V, kv-head) run.
 // Both sides of a chunk are contiguous rows of 256 B. Items are ordered
 // run-major so that consecutive warps walk the image sequentially (the eight
 // runs of a block next to each other instead: 4.39 against 4.37 ms for the
 // sessions above).
 // The copy loop of a session's migration; block_of(j) gives logical block j's slot.
-template <bool kPack, typename BlockOf>
+template <bool kPack, bool kInt8, typename BlockOf>
 __device__ __forceinline__ void migrate_runs(const MigArgs &a, BlockOf block_of) {
     const Shape sh = a.s;
     const int runs = sh.L * 2 * sh.Hkv;
@@ -138,29 +297,30 @@ __device__ __forceinline__ void migrate_runs(const MigArgs &a, BlockOf block_of)
         const int t_hi = min(a.t_end, (q + 1) * kMigChunkTokens);
         uint8_t *hp = a.hot + ((static_cast<int64_t>(blk) * runs + c) * sh.bt + (t_lo - j * sh.bt)) *
                                   kRowBytes;
-        uint8_t *ip = a.img + (static_cast<int64_t>(c) * a.T_cap + t_lo) * kRowBytes;
-        move_rows(kPack ? hp : ip, kPack ? ip : hp, t_hi - t_lo, lane, policy);
+        move_image_rows<kPack, kInt8>(hp, a.img, runs * a.T_cap, static_cast<int64_t>(c) * a.T_cap + t_lo,
+                                      t_hi - t_lo, lane, policy);
     }
 }
 
-template <bool kPack>
+template <bool kPack, bool kInt8>
 __global__ void __launch_bounds__(kCopyThreads) migrate_kernel(const MigArgs a) {
-    migrate_runs<kPack>(a, [&](int j) { return a.table[j]; });
+    migrate_runs<kPack, kInt8>(a, [&](int j) { return a.table[j]; });
 }
 
 // Resume-unpack with the new block ids in the launch parameters: the grid
 // also writes them to the session's table row (read by later work only).
+template <bool kInt8>
 __global__ void __launch_bounds__(kCopyThreads) resume_inline_kernel(const __grid_constant__ ResumeArgs r) {
     const int nthreads = gridDim.x * blockDim.x;
     int32_t *row = const_cast<int32_t *>(r.m.table);   // the pool's own row: writable
     for (int j = blockIdx.x * blockDim.x + threadIdx.x; j < r.n; j += nthreads)
         row[j] = r.blocks[j];
-    migrate_runs<false>(r.m, [&](int j) { return j < r.n ? r.blocks[j] : -1; });
+    migrate_runs<false, kInt8>(r.m, [&](int j) { return j < r.n ? r.blocks[j] : -1; });
 }
 
 // K3'/K4': block-granular moves for the residency mode: one warp per chunk of a
 // (job, layer, K|V, kv-head) run; a job moves tokens [t0, t1) of one block.
-template <bool kPack>
+template <bool kPack, bool kInt8>
 __global__ void __launch_bounds__(kCopyThreads) block_jobs_kernel(const __grid_constant__ BlockJobs a) {
     const Shape sh = a.s;
     const int runs = sh.L * 2 * sh.Hkv;
@@ -185,9 +345,9 @@ __global__ void __launch_bounds__(kCopyThreads) block_jobs_kernel(const __grid_c
         const int t_hi = min(b.t1, (ch + 1) * kMigChunkTokens);
         if (t_hi <= t_lo) continue;
         uint8_t *hp = a.hot + ((static_cast<int64_t>(b.slot) * runs + c) * sh.bt + t_lo) * kRowBytes;
-        uint8_t *ip = b.img + (static_cast<int64_t>(c) * b.T_cap + static_cast<int64_t>(b.j) * sh.bt +
-                               t_lo) * kRowBytes;
-        move_rows(kPack ? hp : ip, kPack ? ip : hp, t_hi - t_lo, lane, policy);
+        move_image_rows<kPack, kInt8>(hp, b.img, static_cast<int64_t>(runs) * b.T_cap,
+                                      static_cast<int64_t>(c) * b.T_cap + static_cast<int64_t>(b.j) * sh.bt + t_lo,
+                                      t_hi - t_lo, lane, policy);
     }
 }
 
@@ -312,21 +472,24 @@ static int32_t moves_once(int64_t items) {
 cudaError_t launch_unpack(MigArgs a, int max_ctas, cudaStream_t st) {
     if (a.t_end <= a.t_begin) return cudaSuccess;
     a.once = moves_once(move_items(a));
-    migrate_kernel<false><<<item_grid(move_items(a), max_ctas), kCopyThreads, 0, st>>>(a);
+    const auto kernel = a.int8 ? migrate_kernel<false, true> : migrate_kernel<false, false>;
+    kernel<<<item_grid(move_items(a), max_ctas), kCopyThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 
 cudaError_t launch_unpack_inline(ResumeArgs &r, int max_ctas, cudaStream_t st) {
     if (r.m.t_end <= r.m.t_begin || r.n < 1 || r.n > kResumeInlineMax) return cudaErrorInvalidValue;
     r.m.once = moves_once(move_items(r.m));
-    resume_inline_kernel<<<item_grid(move_items(r.m), max_ctas), kCopyThreads, 0, st>>>(r);
+    const auto kernel = r.m.int8 ? resume_inline_kernel<true> : resume_inline_kernel<false>;
+    kernel<<<item_grid(move_items(r.m), max_ctas), kCopyThreads, 0, st>>>(r);
     return cudaGetLastError();
 }
 
 cudaError_t launch_pack(MigArgs a, int max_ctas, cudaStream_t st) {
     if (a.t_end <= a.t_begin) return cudaSuccess;
     a.once = moves_once(move_items(a));
-    migrate_kernel<true><<<item_grid(move_items(a), max_ctas), kCopyThreads, 0, st>>>(a);
+    const auto kernel = a.int8 ? migrate_kernel<true, true> : migrate_kernel<true, false>;
+    kernel<<<item_grid(move_items(a), max_ctas), kCopyThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 
@@ -358,10 +521,9 @@ cudaError_t launch_block_jobs(BlockJobs &a, bool pack, int max_ctas, cudaStream_
                           (a.s.bt / kMigChunkTokens);
     const unsigned grid = item_grid(items, max_ctas);
     a.once = moves_once(items);
-    if (pack)
-        block_jobs_kernel<true><<<grid, kCopyThreads, 0, st>>>(a);
-    else
-        block_jobs_kernel<false><<<grid, kCopyThreads, 0, st>>>(a);
+    const auto kernel = pack ? (a.int8 ? block_jobs_kernel<true, true> : block_jobs_kernel<true, false>)
+                             : (a.int8 ? block_jobs_kernel<false, true> : block_jobs_kernel<false, false>);
+    kernel<<<grid, kCopyThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 

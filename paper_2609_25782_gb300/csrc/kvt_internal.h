@@ -10,6 +10,7 @@ namespace kvt {
 
 constexpr int kHeadDim = 128;     // D; one token row of one head is 256 B
 constexpr int kRowBytes = kHeadDim * 2;
+constexpr int kCodeBytes = kHeadDim;   // the same row in an 8-bit image: its codes, and one exponent byte apart
 constexpr int kTileTokens = 16;   // tokens per decode tile (one mma M)
 constexpr int kMaxGroup = 8;      // Hq / Hkv handled by one CTA
 
@@ -93,6 +94,7 @@ struct MigArgs {
     int64_t T_cap;            // image rows per (layer, K|V, kv-head) run
     int32_t t_begin, t_end;   // tokens to move
     int32_t once;             // set by the launch: lines leave the L2 first
+    int32_t int8;             // the image holds 8-bit rows
     int32_t *err;
     Shape s;
 };
@@ -174,7 +176,7 @@ struct BlockJobs {
     int64_t table_stride;
     Shape s;
     int32_t n;
-    int32_t once;             // as in MigArgs
+    int32_t once, int8;       // as in MigArgs
     BlockJob job[kBlockJobsMax];
 };
 

@@ -103,6 +103,8 @@ struct kv_pool {
     kv_pool_config cfg{};
     bool host_only = false;
     int64_t block_bytes = 0, token_bytes = 0;
+    int64_t image_token_bytes = 0;       // of a token in a cold image
+    bool int8 = false;                   // KV_POOL_COLD_INT8
     int32_t table_stride = 0;            // max blocks per session
     int32_t max_splits = 0;              // split bound for max_context
     int64_t part_rows = 0;               // decode workspace capacity (partial rows)
@@ -170,7 +172,7 @@ struct kv_pool {
     }
 
     int64_t image_bytes(int64_t cap) const {
-        return (cap * token_bytes + 255) / 256 * 256;
+        return (cap * image_token_bytes + 255) / 256 * 256;
     }
 
     bool cold_alloc(int64_t bytes, int64_t *off) {
@@ -359,7 +361,7 @@ struct kv_pool {
         for (const Victim &x : v) {
             Session &s = sessions[x.sid];
             lru_out(x.sid);
-            if (x.t1 > x.t0) stats.bytes_packed += static_cast<int64_t>(x.t1 - x.t0) * token_bytes;
+            if (x.t1 > x.t0) stats.bytes_packed += static_cast<int64_t>(x.t1 - x.t0) * image_token_bytes;
             s.img_tok[x.j] = static_cast<int16_t>(x.t1);
             s.blocks[x.j] = -1;
             s.hot_count -= 1;
@@ -402,6 +404,7 @@ struct kv_pool {
             a.s = shape;
             a.n = static_cast<int32_t>(std::min<size_t>(kvt::kBlockJobsMax, jobs.size() - i));
             a.once = 0;
+            a.int8 = int8;
             std::copy(jobs.begin() + i, jobs.begin() + i + a.n, a.job);
             int rc = cuda(pack ? "pack launch" : "unpack launch",
                           [&] { return kvt::launch_block_jobs(a, pack, move_ctas(st), st); });
@@ -419,6 +422,7 @@ struct kv_pool {
         m.t_begin = 0;
         m.t_end = 0;
         m.once = 0;
+        m.int8 = int8;
         m.err = d_err;
         m.s = shape;
         return m;
@@ -431,6 +435,11 @@ const char *kv_last_error(void) { return g_last_error.c_str(); }
 
 int64_t kv_token_bytes(const kv_pool_config *c) {
     return c ? static_cast<int64_t>(c->num_layers) * 2 * c->num_kv_heads * c->head_dim * 2 : 0;
+}
+
+int64_t kv_image_token_bytes(const kv_pool_config *c) {
+    if (!c || !(c->flags & KV_POOL_COLD_INT8)) return kv_token_bytes(c);
+    return static_cast<int64_t>(c->num_layers) * 2 * c->num_kv_heads * (c->head_dim + 1);
 }
 
 int64_t kv_block_bytes(const kv_pool_config *c) {
@@ -472,7 +481,9 @@ int kv_pool_create(const kv_pool_config *cfg, kv_pool **out) {
     p->cfg = c;
     p->host_only = host_only;
     p->lru = (c.flags & KV_POOL_LRU_RESIDENCY) != 0;
+    p->int8 = (c.flags & KV_POOL_COLD_INT8) != 0;
     p->token_bytes = kv_token_bytes(&c);
+    p->image_token_bytes = kv_image_token_bytes(&c);
     p->block_bytes = kv_block_bytes(&c);
     p->table_stride = static_cast<int32_t>((c.max_context + c.block_tokens - 1) / c.block_tokens);
     p->max_splits = kvt::max_splits_for(static_cast<int64_t>(p->table_stride) * c.block_tokens);
@@ -689,7 +700,7 @@ static int lru_append(kv_pool *p, int32_t sid, const void *k, const void *v, int
     if (refetch) {
         s->blocks[tail] = got[0];
         s->hot_count += 1;
-        p->stats.bytes_unpacked += p->tokens_in_block(*s, tail) * p->token_bytes;
+        p->stats.bytes_unpacked += p->tokens_in_block(*s, tail) * p->image_token_bytes;
     }
     for (int64_t i = 0; i < fresh_n; ++i) {
         s->blocks.push_back(got[(refetch ? 1 : 0) + i]);
@@ -748,7 +759,7 @@ static int lru_resume(kv_pool *p, int32_t sid, cudaStream_t st) {
     s->ready_recorded = !p->host_only;
     p->stats.free_blocks -= need;
     p->stats.used_blocks += need;
-    p->stats.bytes_unpacked += fetched * p->token_bytes;
+    p->stats.bytes_unpacked += fetched * p->image_token_bytes;
     p->stats.resume_blocks_hit += static_cast<int64_t>(s->blocks.size()) - need;
     p->stats.resume_blocks_missed += need;
     p->stats.resumes += 1;
@@ -817,7 +828,7 @@ static int lru_fetch(kv_pool *p, const std::vector<int32_t> &uniq,
     }
     p->stats.free_blocks -= need;
     p->stats.used_blocks += need;
-    p->stats.bytes_unpacked += fetched * p->token_bytes;
+    p->stats.bytes_unpacked += fetched * p->image_token_bytes;
     *blocks = need;
     return KV_OK;
 }
@@ -1012,7 +1023,7 @@ int session_pause(kv_pool *p, int32_t sid, kv_stream_t stream_) {
     }
     p->stats.free_blocks += static_cast<int64_t>(s->blocks.size());
     p->stats.used_blocks -= static_cast<int64_t>(s->blocks.size());
-    p->stats.bytes_packed += (t1 - t0) * p->token_bytes;
+    p->stats.bytes_packed += (t1 - t0) * p->image_token_bytes;
     p->stats.pauses += 1;
     s->blocks.clear();
     s->cold_valid = t1;
@@ -1078,7 +1089,7 @@ int session_resume(kv_pool *p, int32_t sid, kv_stream_t stream_) {
     s->ready_recorded = !p->host_only;
     p->stats.free_blocks -= need;
     p->stats.used_blocks += need;
-    p->stats.bytes_unpacked += s->T * p->token_bytes;
+    p->stats.bytes_unpacked += s->T * p->image_token_bytes;
     p->stats.resumes += 1;
     return KV_OK;
 }
@@ -1284,7 +1295,7 @@ int kv_pool_batch_reserve(kv_pool *p, const int32_t *sids, int32_t B, int32_t *b
     }
     p->stats.free_blocks -= need;
     p->stats.used_blocks += need;
-    p->stats.bytes_unpacked += fetched * p->token_bytes;
+    p->stats.bytes_unpacked += fetched * p->image_token_bytes;
     p->stats.batch_blocks_fetched += static_cast<int64_t>(jobs.size());
     p->stats.bytes_appended += static_cast<int64_t>(B) * p->token_bytes;
     p->stats.appends += B;

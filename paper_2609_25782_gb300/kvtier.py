@@ -26,6 +26,7 @@ KV_ERR_DEVICE_CHECK = -6
 KV_SESSION_FREE, KV_SESSION_ACTIVE, KV_SESSION_PAUSED = 0, 1, 2
 KV_POOL_HOST_LOGIC_ONLY = 1
 KV_POOL_LRU_RESIDENCY = 2
+KV_POOL_COLD_INT8 = 4
 
 _ERR_NAMES = {v: k for k, v in globals().items() if k.startswith("KV_ERR_")}
 
@@ -40,6 +41,7 @@ EXPORTS = [
     "decode_attention_ex", "kv_pool_set_migration_limit", "kv_pool_batch_reserve",
     "decode_append_attention", "kv_pool_inject_decode_timeout", "kv_decode_splits",
     "session_block_table_device", "kv_pool_prefetch", "kv_pool_inject_stale_counter",
+    "kv_image_token_bytes",
 ]
 
 KV_DEVICE_BAD_BLOCK, KV_DEVICE_BAD_LENGTH, KV_DEVICE_TIMEOUT = 1, 2, 4
@@ -94,6 +96,7 @@ def _load():
         "kv_pool_destroy": [p],
         "kv_block_bytes": [C.POINTER(kv_pool_config)],
         "kv_token_bytes": [C.POINTER(kv_pool_config)],
+        "kv_image_token_bytes": [C.POINTER(kv_pool_config)],
         "kv_decode_splits": [i64],
         "session_create": [p, i64, C.POINTER(i32)],
         "session_create_paused": [p, i64, i64, C.POINTER(i32)],
@@ -129,6 +132,7 @@ def _load():
         f.restype = C.c_int
     L.kv_block_bytes.restype = i64
     L.kv_token_bytes.restype = i64
+    L.kv_image_token_bytes.restype = i64
     L.kv_last_error.restype = C.c_char_p
     return L
 
@@ -167,6 +171,10 @@ def kv_last_error() -> str:
 
 def kv_token_bytes(cfg: kv_pool_config) -> int:
     return int(lib.kv_token_bytes(C.byref(cfg)))
+
+
+def kv_image_token_bytes(cfg: kv_pool_config) -> int:
+    return int(lib.kv_image_token_bytes(C.byref(cfg)))
 
 
 def kv_block_bytes(cfg: kv_pool_config) -> int:
