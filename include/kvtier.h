@@ -8,7 +8,8 @@
  *   path 2  resume: cold image -> hot blocks ................ session_resume
  *   path 3  fresh KV written into hot blocks ................ session_append
  *           (or kv_pool_batch_reserve + decode_append_attention: one
- *           token per session and step, written by the decode kernel)
+ *           token per session and step, written by the decode kernel;
+ *           kv_pool_batch_reserve_tokens + prefill_attention: a turn's)
  *   path 4  eviction: hot blocks -> cold image .............. session_pause
  * The cold tier (high bandwidth flash in the paper) is a second device
  * allocation; its bandwidth, energy and endurance are not modelled.
@@ -295,6 +296,56 @@ int decode_append_attention(kv_pool *pool, int32_t layer, const void *q, const v
                             const int32_t *seq_lens, int32_t B, int32_t max_blocks, float scale,
                             float *out, uint32_t flags, kv_stream_t stream);
 
+/* Data paths 3 and 1 for a turn's context or a whole first prompt: attention of
+ * all new tokens of B sessions, packed one session after the other, over the
+ * tokens cached before them and, causally, over themselves. Their K and V are
+ * written into the slots that kv_pool_batch_reserve_tokens allocated
+ * (block_tables and seq_lens are its outputs). The paper has no passage on
+ * prefill; the fresh KV's way into HBM is Section 3's data path 3.
+ *   layer        0 .. L-1
+ *   q            device bf16 [total][Hq][D], the next token q_stride elements
+ *                on (0: contiguous), so that it may be a view of a projection
+ *                of q, k and v together
+ *   k_new, v_new device bf16 [total][Hkv][D], the next token kv_stride elements on
+ *   cu_new       device int32 [B + 1]: session b's tokens are rows cu_new[b] ..
+ *                cu_new[b + 1] - 1 (none: the session only keeps its place)
+ *   total        rows of q, k_new, v_new and out; 0 does nothing
+ *   block_tables device int32 [B][max_blocks]
+ *   seq_lens     device int32 [B]: tokens of the session with the new ones, at
+ *                most max_blocks * bt
+ *   out          device fp32 [total][Hq][D], or bf16 with KV_DECODE_OUT_BF16
+ * out[lo + i][h] = sum over t <= seq_len - n + i of softmax_t(scale * q . K[g][t])
+ * V[g][t] for the session's n new tokens at rows lo + i, g = h / (Hq/Hkv).
+ * q, k_new, v_new and out 16-byte aligned, the others 4-byte, strides multiples
+ * of 8. Scores, softmax statistics and sums are held in 32 bits, the weights in
+ * bf16 for the product with V. The new tokens' K and V have to be finite: a V
+ * that is not may reach rows that come before it. Tokens past seq_len in a block
+ * may hold anything. The result depends on the values, the lengths and the
+ * batch, and is the same from run to run. Offsets or lengths out of range set
+ * KV_DEVICE_BAD_LENGTH, and that session's rows are not written. */
+int prefill_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride,
+                      const void *k_new, const void *v_new, int64_t kv_stride, const int32_t *cu_new,
+                      int32_t total, const int32_t *block_tables, const int32_t *seq_lens, int32_t B,
+                      int32_t max_blocks, float scale, void *out, uint32_t flags, kv_stream_t stream);
+
+/* Path 1 for drafted tokens (speculative decoding; no passage): every draft
+ * attends to all seq_lens[b] cached tokens of its session (0 or more) and to
+ * those of the session's own drafts that its mask names: draft j if bit j of
+ * ancestors[row] is set, usually its ancestors in the draft tree and itself.
+ * k_draft and v_draft arrive with the call and are NOT written to the pool,
+ * whose tokens are immutable: the accepted ones are appended afterwards.
+ *   ancestors    device uint64 [total], 8-byte aligned; bits at or past the
+ *                session's number of drafts are ignored
+ *   cu_draft     device int32 [B + 1], at most 64 drafts per session
+ *   seq_lens     device int32 [B]: cached tokens, drafts not counted
+ * A draft that sees nothing (no cached token, no bit) gets zeros. All else as
+ * prefill_attention. */
+int tree_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride, const void *k_draft,
+                   const void *v_draft, int64_t kv_stride, const uint64_t *ancestors,
+                   const int32_t *cu_draft, int32_t total, const int32_t *block_tables,
+                   const int32_t *seq_lens, int32_t B, int32_t max_blocks, float scale, void *out,
+                   uint32_t flags, kv_stream_t stream);
+
 /* Data path 4 with write-on-evict (Section 3, "Memory hierarchy and write
  * policy"): copy tokens [cold_valid, T) of an ACTIVE session into its
  * image, set cold_valid = T, return its hot blocks to the end of the free
@@ -371,6 +422,16 @@ int kv_pool_batch_tables(kv_pool *pool, const int32_t *sids, int32_t B, int32_t 
  * bookkeeping and ignore the outputs. */
 int kv_pool_batch_reserve(kv_pool *pool, const int32_t *sids, int32_t B, int32_t *block_tables,
                           int32_t max_blocks, int32_t *seq_lens, kv_stream_t stream);
+
+/* kv_pool_batch_reserve with n_new[i] >= 0 new positions for member i (host
+ * array of B counts; blocks are popped as its tokens need them), for a call
+ * that writes a turn's whole context (prefill_attention) or, with counts of 1,
+ * a decode step. A member without new tokens keeps its length; one that is
+ * empty needs at least one. Same order of pops (a member's missing blocks, then
+ * its new blocks), same errors, all or nothing. */
+int kv_pool_batch_reserve_tokens(kv_pool *pool, const int32_t *sids, const int32_t *n_new, int32_t B,
+                                 int32_t *block_tables, int32_t max_blocks, int32_t *seq_lens,
+                                 kv_stream_t stream);
 
 /* Prefetch one step ahead of decode (Section 3, "Eviction, resume and
  * decode": decode reads a known set of blocks each step, so the next step's

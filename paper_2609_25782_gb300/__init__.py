@@ -119,9 +119,15 @@ class Pool:
         kvtier.kv_pool_batch_tables(self.handle, list(sids), block_tables, max_blocks, seq_lens,
                                     stream)
 
-    def batch_reserve(self, sids, block_tables, max_blocks: int, seq_lens, stream=None) -> None:
-        """One new position per session (filled by decode_append_attention),
-        then the batch's tables and lengths as batch_tables builds them."""
+    def batch_reserve(self, sids, block_tables, max_blocks: int, seq_lens, stream=None,
+                      counts=None) -> None:
+        """One new position per session (filled by decode_append_attention), or
+        counts[i] of them (filled by prefill_attention), then the batch's
+        tables and lengths as batch_tables builds them."""
+        if counts is not None:
+            kvtier.kv_pool_batch_reserve_tokens(self.handle, list(sids), list(counts), block_tables,
+                                                max_blocks, seq_lens, stream)
+            return
         kvtier.kv_pool_batch_reserve(self.handle, list(sids), block_tables, max_blocks, seq_lens,
                                      stream)
 
@@ -157,6 +163,52 @@ class Pool:
             (kvtier.KV_DECODE_OUT_BF16 if getattr(out, "dtype", None) == torch.bfloat16 else 0)
         kvtier.decode_append_attention(self.handle, layer, q, k_new, v_new, block_tables, seq_lens,
                                        B, max_blocks, scale, out, flags, stream)
+
+    @staticmethod
+    def _token_stride(x, heads: int, D: int, total: int) -> int:
+        """Elements from token to token of a bf16 [total][heads][D] tensor whose heads are contiguous."""
+        import torch
+        if x.dtype != torch.bfloat16 or tuple(x.shape) != (total, heads, D) or \
+                x.stride(2) != 1 or (heads > 1 and x.stride(1) != D):
+            raise ValueError(f"need bf16 [{total}][{heads}][{D}] with contiguous heads, "
+                             f"got {x.dtype} {tuple(x.shape)} strides {x.stride()}")
+        return x.stride(0) if total > 1 else 0
+
+    def _turn(self, q, k, v, out):
+        """Strides and flags of a call on [N][Hq][D] queries, checked."""
+        import torch
+        total = q.shape[0]
+        kv_stride = self._token_stride(k, self.Hkv, self.D, total)
+        if self._token_stride(v, self.Hkv, self.D, total) != kv_stride:
+            raise ValueError("k and v need the same token stride")
+        if tuple(out.shape) != (total, self.Hq, self.D) or not out.is_contiguous() or \
+                out.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"out must be contiguous fp32 or bf16 [{total}][{self.Hq}][{self.D}]")
+        return (self._token_stride(q, self.Hq, self.D, total), kv_stride, total,
+                kvtier.KV_DECODE_OUT_BF16 if out.dtype == torch.bfloat16 else 0)
+
+    def prefill_attention(self, layer: int, q, k_new, v_new, cu_new, block_tables, seq_lens, B: int,
+                          max_blocks: int, scale: float, out, stream=None) -> None:
+        """Causal attention of a turn's new tokens (or whole prompts), packed: session b has rows
+        cu_new[b]..cu_new[b+1]-1 of q [N][Hq][D] and k_new, v_new [N][Hkv][D] (bf16, any token
+        stride, so views of one projection will do), the newest of its seq_lens[b] tokens; K and V
+        go into the slots that batch_reserve(counts=...) allocated. out: fp32 or bf16."""
+        q_stride, kv_stride, total, flags = self._turn(q, k_new, v_new, out)
+        kvtier.prefill_attention(self.handle, layer, q, q_stride, k_new, v_new, kv_stride, cu_new,
+                                 total, block_tables, seq_lens, B, max_blocks, scale, out, flags,
+                                 stream)
+
+    def tree_attention(self, layer: int, q, k_draft, v_draft, ancestors, cu_draft, block_tables,
+                       seq_lens, B: int, max_blocks: int, scale: float, out, stream=None) -> None:
+        """Attention of drafted tokens (at most 64 per session, packed by cu_draft) over the
+        session's seq_lens[b] cached tokens and the drafts in ancestors [N] (64-bit masks over the
+        session's own drafts). Nothing is written to the pool."""
+        q_stride, kv_stride, total, flags = self._turn(q, k_draft, v_draft, out)
+        if ancestors.numel() != total or ancestors.element_size() != 8 or not ancestors.is_contiguous():
+            raise ValueError("one contiguous 64-bit mask per draft")
+        kvtier.tree_attention(self.handle, layer, q, q_stride, k_draft, v_draft, kv_stride, ancestors,
+                              cu_draft, total, block_tables, seq_lens, B, max_blocks, scale, out,
+                              flags, stream)
 
     def shuffle_free(self, seed: int) -> None:
         kvtier.kv_pool_shuffle_free(self.handle, seed)

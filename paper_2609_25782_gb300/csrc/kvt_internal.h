@@ -87,6 +87,27 @@ struct DecodeArgs {
     Shape s;
 };
 
+// Attention of the new tokens of B sessions (turn_kernels.cu): session b has rows
+// cu[b] .. cu[b + 1] - 1 of q, k_new, v_new and out. Without masks the rows are a
+// turn's context, the newest of the seq_lens[b] tokens, causal, and their K and V
+// are written into the pool; with masks they are drafts beyond them.
+constexpr int kMaxDrafts = 64;
+struct TurnArgs {
+    const uint16_t *q;               // [total][Hq][D] bf16, q_stride elements from token to token
+    const uint16_t *k_new, *v_new;   // [total][Hkv][D] bf16, kv_stride elements from token to token
+    const uint64_t *masks;           // [total], or null
+    const int32_t *cu;               // [B + 1]
+    const int32_t *tables;           // [B][max_blocks]
+    const int32_t *seq_lens;         // [B]
+    void *out;                       // [total][Hq][D], fp32 or (out_bf16) bf16
+    uint16_t *hot;
+    int32_t *err;
+    int64_t q_stride, kv_stride;
+    int32_t total, B, max_blocks, layer, out_bf16;
+    float scale_log2;                // scale * log2(e)
+    Shape s;
+};
+
 struct MigArgs {
     const int32_t *table;     // session's block-table row (device)
     uint8_t *hot;
@@ -213,6 +234,7 @@ cudaError_t prepare_kernels();  // per-device function attributes
 // split kernel's tile rings to the grid.
 cudaError_t launch_decode(const CUtensorMap &map, const DecodeArgs &a, int num_sms,
                           cudaStream_t st, bool overlap_previous);
+cudaError_t launch_turn(const TurnArgs &a, cudaStream_t st);
 // max_ctas > 0 caps the copy grids (migration_ctas).
 cudaError_t launch_unpack(MigArgs a, int max_ctas, cudaStream_t st);
 cudaError_t launch_unpack_inline(ResumeArgs &r, int max_ctas, cudaStream_t st);

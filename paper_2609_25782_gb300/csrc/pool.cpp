@@ -978,6 +978,84 @@ int decode_append_attention(kv_pool *p, int32_t layer, const void *q, const void
                        out, flags, stream);
 }
 
+// Several new tokens per session: a turn's context (masks == null) or drafts.
+static int turn_impl(kv_pool *p, int32_t layer, const void *q, int64_t q_stride, const void *k,
+                     const void *v, int64_t kv_stride, const uint64_t *masks, const int32_t *cu,
+                     int32_t total, const int32_t *block_tables, const int32_t *seq_lens, int32_t B,
+                     int32_t max_blocks, float scale, void *out, uint32_t flags, kv_stream_t stream_) {
+    if (flags & ~static_cast<uint32_t>(KV_DECODE_OUT_BF16))
+        return fail(KV_ERR_INVALID_ARG, "unknown flag");
+    if (!p) return fail(KV_ERR_INVALID_ARG, "null pool");
+    if (!cu || !block_tables || !seq_lens || (total != 0 && (!q || !k || !v || !out)))
+        return fail(KV_ERR_INVALID_ARG, "null pointer");
+    auto bits = [](const void *x) { return reinterpret_cast<uintptr_t>(x); };
+    if ((bits(q) | bits(k) | bits(v) | bits(out)) & 15)
+        return fail(KV_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+    if ((bits(cu) | bits(block_tables) | bits(seq_lens)) & 3 || bits(masks) & 7)
+        return fail(KV_ERR_INVALID_ARG, "offsets, block_tables and seq_lens need 4-byte, masks 8-byte alignment");
+    if (layer < 0 || layer >= p->cfg.num_layers) return fail(KV_ERR_INVALID_ARG, "bad layer");
+    if (B < 1 || B > 65535) return fail(KV_ERR_INVALID_ARG, "B out of range");
+    if (total < 0 || total > (1 << 28)) return fail(KV_ERR_INVALID_ARG, "token count out of range");
+    if (max_blocks < 1 || max_blocks > (1 << 26))
+        return fail(KV_ERR_INVALID_ARG, "max_blocks out of range");
+    const int64_t q_row = static_cast<int64_t>(p->cfg.num_q_heads) * kvt::kHeadDim;
+    const int64_t kv_row = static_cast<int64_t>(p->cfg.num_kv_heads) * kvt::kHeadDim;
+    if (q_stride == 0) q_stride = q_row;
+    if (kv_stride == 0) kv_stride = kv_row;
+    if (q_stride < q_row || kv_stride < kv_row || (q_stride | kv_stride) & 7 ||
+        q_stride > (int64_t(1) << 32) || kv_stride > (int64_t(1) << 32))
+        return fail(KV_ERR_INVALID_ARG, "token strides must be multiples of 8 and hold a token's heads");
+    if (!(scale == scale) || std::isinf(scale)) return fail(KV_ERR_INVALID_ARG, "scale not finite");
+    // arguments first, then the pool's state
+    if (p->host_only) return fail(KV_ERR_BAD_STATE, "attention on a host-logic-only pool");
+    if (total == 0) return KV_OK;
+    DeviceGuard dg(p->cfg.device, true);
+    kvt::TurnArgs a;
+    a.q = static_cast<const uint16_t *>(q);
+    a.k_new = static_cast<const uint16_t *>(k);
+    a.v_new = static_cast<const uint16_t *>(v);
+    a.masks = masks;
+    a.cu = cu;
+    a.tables = block_tables;
+    a.seq_lens = seq_lens;
+    a.out = out;
+    a.hot = static_cast<uint16_t *>(p->cfg.hot_base);
+    a.err = p->d_err;
+    a.q_stride = q_stride;
+    a.kv_stride = kv_stride;
+    a.total = total;
+    a.B = B;
+    a.max_blocks = max_blocks;
+    a.layer = layer;
+    a.out_bf16 = (flags & KV_DECODE_OUT_BF16) ? 1 : 0;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.s = p->shape;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream_);
+    int rc = p->cuda("attention launch", [&] { return kvt::launch_turn(a, st); });
+    if (rc) return rc;
+    p->decoded = true;
+    p->decode_stream = st;
+    return KV_OK;
+}
+
+int prefill_attention(kv_pool *p, int32_t layer, const void *q, int64_t q_stride, const void *k_new,
+                      const void *v_new, int64_t kv_stride, const int32_t *cu_new, int32_t total,
+                      const int32_t *block_tables, const int32_t *seq_lens, int32_t B,
+                      int32_t max_blocks, float scale, void *out, uint32_t flags, kv_stream_t stream) {
+    return turn_impl(p, layer, q, q_stride, k_new, v_new, kv_stride, nullptr, cu_new, total,
+                     block_tables, seq_lens, B, max_blocks, scale, out, flags, stream);
+}
+
+int tree_attention(kv_pool *p, int32_t layer, const void *q, int64_t q_stride, const void *k_draft,
+                   const void *v_draft, int64_t kv_stride, const uint64_t *ancestors,
+                   const int32_t *cu_draft, int32_t total, const int32_t *block_tables,
+                   const int32_t *seq_lens, int32_t B, int32_t max_blocks, float scale, void *out,
+                   uint32_t flags, kv_stream_t stream) {
+    if (!ancestors && total != 0) return fail(KV_ERR_INVALID_ARG, "null ancestors");
+    return turn_impl(p, layer, q, q_stride, k_draft, v_draft, kv_stride, ancestors, cu_draft, total,
+                     block_tables, seq_lens, B, max_blocks, scale, out, flags, stream);
+}
+
 int session_pause(kv_pool *p, int32_t sid, kv_stream_t stream_) {
     if (!p) return fail(KV_ERR_INVALID_ARG, "null pool");
     Session *s = p->session(sid);
@@ -1192,13 +1270,15 @@ int kv_pool_batch_tables(kv_pool *p, const int32_t *sids, int32_t B, int32_t *bl
     return gather_batch(p, sids, B, block_tables, max_blocks, seq_lens, st);
 }
 
-// Path 3 for one decode step: every member gets position T (a fresh block
-// when its tail block is full) and, in residency mode, its evicted blocks
+// Path 3 for one step: every member gets position T, or the next n (fresh
+// blocks where its tail block is full) and, in residency mode, its evicted blocks
 // back; victims come only from sessions outside the batch. The values
 // arrive with decode_append_attention. Free-list pops go in batch order:
-// a member's missing blocks (ascending), then its fresh block.
-int kv_pool_batch_reserve(kv_pool *p, const int32_t *sids, int32_t B, int32_t *block_tables,
-                          int32_t max_blocks, int32_t *seq_lens, kv_stream_t stream_) {
+// a member's missing blocks (ascending), then its fresh blocks.
+// counts: new positions per member, or null for one each.
+static int reserve_impl(kv_pool *p, const int32_t *sids, const int32_t *counts, int32_t B,
+                        int32_t *block_tables, int32_t max_blocks, int32_t *seq_lens,
+                        kv_stream_t stream_) {
     if (!p || !sids || B < 1) return fail(KV_ERR_INVALID_ARG, "bad argument");
     if (!p->host_only && (!block_tables || !seq_lens)) return fail(KV_ERR_INVALID_ARG, "null output");
     if ((reinterpret_cast<uintptr_t>(block_tables) | reinterpret_cast<uintptr_t>(seq_lens)) & 3)
@@ -1212,19 +1292,24 @@ int kv_pool_batch_reserve(kv_pool *p, const int32_t *sids, int32_t B, int32_t *b
         if (std::find(members.begin(), members.begin() + i, sids[i]) != members.begin() + i)
             return fail(KV_ERR_INVALID_ARG, "a session appears twice in the batch");
         if (s->state != KV_SESSION_ACTIVE) return fail(KV_ERR_BAD_STATE, "paused session in batch");
-        if (s->T + 1 > s->cap) return fail(KV_ERR_INVALID_ARG, "append past the session capacity");
-        if ((s->T + bt) / bt > max_blocks)
+        const int64_t n = counts ? counts[i] : 1;
+        if (n < 0 || s->T + n < 1)
+            return fail(KV_ERR_INVALID_ARG, "a negative count, or an empty session without new tokens");
+        if (s->T + n > s->cap) return fail(KV_ERR_INVALID_ARG, "append past the session capacity");
+        if ((s->T + n + bt - 1) / bt > max_blocks)
             return fail(KV_ERR_INVALID_ARG, "max_blocks shorter than a session's table");
     }
     std::vector<std::vector<int32_t>> miss(B);
-    std::vector<char> grow(B);
-    int64_t need = 0;
+    std::vector<int64_t> grow(B);    // new blocks at the row's end
+    int64_t need = 0, tokens = 0;
     for (int32_t i = 0; i < B; ++i) {
         const Session &s = p->sessions[sids[i]];
         if (p->lru)
             for (size_t j = 0; j < s.blocks.size(); ++j)
                 if (s.blocks[j] < 0) miss[i].push_back(static_cast<int32_t>(j));
-        grow[i] = (s.T % bt) == 0;
+        const int64_t n = counts ? counts[i] : 1;
+        grow[i] = (s.T + n + bt - 1) / bt - static_cast<int64_t>(s.blocks.size());
+        tokens += n;
         need += static_cast<int64_t>(miss[i].size()) + grow[i];
     }
     std::vector<Victim> vic;
@@ -1245,7 +1330,7 @@ int kv_pool_batch_reserve(kv_pool *p, const int32_t *sids, int32_t B, int32_t *b
             fetched += p->tokens_in_block(s, j);
             ++k;
         }
-        if (grow[i]) rows[i].push_back(got[k++]);
+        for (int64_t j = 0; j < grow[i]; ++j) rows[i].push_back(got[k++]);
     }
     // Slots that come off the free list (not from this call's victims) may
     // have been freed by a pause whose pack is still running.
@@ -1265,11 +1350,15 @@ int kv_pool_batch_reserve(kv_pool *p, const int32_t *sids, int32_t B, int32_t *b
         if (!miss[i].empty()) rc = p->wait_packed(sids[i], st);
     if (!rc) rc = p->run_jobs(jobs, false, st);
     // Fetched entries were written by their jobs; a new tail block's entry is
-    // written by the gather launch below (host-logic pools launch nothing).
+    // written by the gather launch below (host-logic pools launch nothing), those
+    // before it by launches of their own.
     std::vector<int32_t> new_blk(B, -1), lens(B), nblk(B);
     for (int32_t i = 0; i < B; ++i) {
+        const int64_t from = static_cast<int64_t>(rows[i].size()) - grow[i];
+        if (!rc && !p->host_only && grow[i] > 1)
+            rc = p->write_table(sids[i], rows[i].data() + from, from, grow[i] - 1, st);
         if (grow[i]) new_blk[i] = rows[i].back();
-        lens[i] = static_cast<int32_t>(p->sessions[sids[i]].T + 1);
+        lens[i] = static_cast<int32_t>(p->sessions[sids[i]].T + (counts ? counts[i] : 1));
         nblk[i] = static_cast<int32_t>(rows[i].size());
     }
     if (!rc && !p->host_only)
@@ -1285,8 +1374,8 @@ int kv_pool_batch_reserve(kv_pool *p, const int32_t *sids, int32_t B, int32_t *b
         Session &s = p->sessions[sids[i]];
         if (p->lru) p->lru_out(sids[i]);
         s.blocks = rows[i];
-        if (grow[i] && p->lru) s.img_tok.push_back(0);
-        s.T += 1;
+        if (p->lru) s.img_tok.resize(rows[i].size(), 0);
+        s.T += counts ? counts[i] : 1;
         if (p->lru) {
             s.hot_count += static_cast<int64_t>(miss[i].size()) + grow[i];
             s.last_use = stamp;
@@ -1297,9 +1386,21 @@ int kv_pool_batch_reserve(kv_pool *p, const int32_t *sids, int32_t B, int32_t *b
     p->stats.used_blocks += need;
     p->stats.bytes_unpacked += fetched * p->image_token_bytes;
     p->stats.batch_blocks_fetched += static_cast<int64_t>(jobs.size());
-    p->stats.bytes_appended += static_cast<int64_t>(B) * p->token_bytes;
+    p->stats.bytes_appended += tokens * p->token_bytes;
     p->stats.appends += B;
     return KV_OK;
+}
+
+int kv_pool_batch_reserve(kv_pool *p, const int32_t *sids, int32_t B, int32_t *block_tables,
+                          int32_t max_blocks, int32_t *seq_lens, kv_stream_t stream) {
+    return reserve_impl(p, sids, nullptr, B, block_tables, max_blocks, seq_lens, stream);
+}
+
+int kv_pool_batch_reserve_tokens(kv_pool *p, const int32_t *sids, const int32_t *n_new, int32_t B,
+                                 int32_t *block_tables, int32_t max_blocks, int32_t *seq_lens,
+                                 kv_stream_t stream) {
+    if (!n_new) return fail(KV_ERR_INVALID_ARG, "null n_new");
+    return reserve_impl(p, sids, n_new, B, block_tables, max_blocks, seq_lens, stream);
 }
 
 // One step ahead of decode (Section 3, "Eviction, resume and decode": decode

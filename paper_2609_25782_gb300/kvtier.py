@@ -41,7 +41,7 @@ EXPORTS = [
     "decode_attention_ex", "kv_pool_set_migration_limit", "kv_pool_batch_reserve",
     "decode_append_attention", "kv_pool_inject_decode_timeout", "kv_decode_splits",
     "session_block_table_device", "kv_pool_prefetch", "kv_pool_inject_stale_counter",
-    "kv_image_token_bytes",
+    "kv_image_token_bytes", "kv_pool_batch_reserve_tokens", "prefill_attention", "tree_attention",
 ]
 
 KV_DEVICE_BAD_BLOCK, KV_DEVICE_BAD_LENGTH, KV_DEVICE_TIMEOUT = 1, 2, 4
@@ -103,6 +103,11 @@ def _load():
         "session_destroy": [p, i32],
         "session_append": [p, i32, p, p, i32, p],
         "kv_pool_batch_reserve": [p, p, i32, p, i32, p, p],
+        "kv_pool_batch_reserve_tokens": [p, p, p, i32, p, i32, p, p],
+        "prefill_attention": [p, i32, p, i64, p, p, i64, p, i32, p, p, i32, i32, C.c_float, p,
+                              C.c_uint32, p],
+        "tree_attention": [p, i32, p, i64, p, p, i64, p, p, i32, p, p, i32, i32, C.c_float, p,
+                           C.c_uint32, p],
         "kv_pool_prefetch": [p, p, i32, p, i32, p],
         "decode_append_attention": [p, i32, p, p, p, p, p, i32, i32, C.c_float, p, C.c_uint32, p],
         "decode_attention": [p, i32, p, p, p, i32, i32, C.c_float, p, p],
@@ -290,6 +295,34 @@ def kv_pool_batch_reserve(pool: int, sids, block_tables, max_blocks: int, seq_le
     arr = (C.c_int32 * len(sids))(*sids)
     _check(lib.kv_pool_batch_reserve(pool, arr, len(sids), _addr(block_tables), max_blocks,
                                      _addr(seq_lens), _stream(stream)), "kv_pool_batch_reserve")
+
+
+def kv_pool_batch_reserve_tokens(pool: int, sids, n_new, block_tables, max_blocks: int, seq_lens,
+                                 stream=None) -> None:
+    if len(n_new) != len(sids):
+        raise ValueError("one count per session")
+    arr, counts = (C.c_int32 * len(sids))(*sids), (C.c_int32 * len(sids))(*n_new)
+    _check(lib.kv_pool_batch_reserve_tokens(pool, arr, counts, len(sids), _addr(block_tables),
+                                            max_blocks, _addr(seq_lens), _stream(stream)),
+           "kv_pool_batch_reserve_tokens")
+
+
+def prefill_attention(pool: int, layer: int, q, q_stride: int, k_new, v_new, kv_stride: int, cu_new,
+                      total: int, block_tables, seq_lens, B: int, max_blocks: int, scale: float,
+                      out, flags: int = 0, stream=None) -> None:
+    _check(lib.prefill_attention(pool, layer, _addr(q), q_stride, _addr(k_new), _addr(v_new),
+                                 kv_stride, _addr(cu_new), total, _addr(block_tables),
+                                 _addr(seq_lens), B, max_blocks, scale, _addr(out), flags,
+                                 _stream(stream)), "prefill_attention")
+
+
+def tree_attention(pool: int, layer: int, q, q_stride: int, k_draft, v_draft, kv_stride: int,
+                   ancestors, cu_draft, total: int, block_tables, seq_lens, B: int, max_blocks: int,
+                   scale: float, out, flags: int = 0, stream=None) -> None:
+    _check(lib.tree_attention(pool, layer, _addr(q), q_stride, _addr(k_draft), _addr(v_draft),
+                              kv_stride, _addr(ancestors), _addr(cu_draft), total,
+                              _addr(block_tables), _addr(seq_lens), B, max_blocks, scale, _addr(out),
+                              flags, _stream(stream)), "tree_attention")
 
 
 def kv_pool_prefetch(pool: int, sids, busy=(), stream=None) -> None:
