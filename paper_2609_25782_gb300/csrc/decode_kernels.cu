@@ -1181,8 +1181,8 @@ __global__ void __launch_bounds__(128) decode_combine_shared_kernel(const Decode
 
 }  // namespace
 
-bool encode_hot_tensor_map(CUtensorMap *map, void *hot_base, int64_t rows, int64_t run_rows,
-                           const char **why) {
+bool encode_bf16_map(CUtensorMap *map, void *base, int rank, const cuuint64_t *dims,
+                     const cuuint64_t *strides, const cuuint32_t *box, const char **why) {
     // Resolved once; a function-local static is initialised exactly once even
     // when pools are created, or allocation-free decodes issued, on several
     // host threads at the same moment.
@@ -1199,6 +1199,19 @@ bool encode_hot_tensor_map(CUtensorMap *map, void *hot_base, int64_t rows, int64
         *why = "cuTensorMapEncodeTiled entry point unavailable";
         return false;
     }
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, base, dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        *why = "cuTensorMapEncodeTiled rejected a tensor";
+        return false;
+    }
+    return true;
+}
+
+bool encode_hot_tensor_map(CUtensorMap *map, void *hot_base, int64_t rows, int64_t run_rows,
+                           const char **why) {
     // A 4-D view of the pool: (64 columns, row, column half, K|V) with byte
     // strides (2, 256, 128, run_rows * 256). A tile is one box of it: 16 rows
     // of both halves of K and of V, landing in shared memory as [K|V][half]
@@ -1207,15 +1220,7 @@ bool encode_hot_tensor_map(CUtensorMap *map, void *hot_base, int64_t rows, int64
     cuuint64_t strides[3] = {static_cast<cuuint64_t>(kRowBytes), 128,
                              static_cast<cuuint64_t>(run_rows) * kRowBytes};
     cuuint32_t box[4] = {64, kTileTokens, 2, 2};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, hot_base, dims, strides, box, estr,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        *why = "cuTensorMapEncodeTiled rejected the hot pool";
-        return false;
-    }
-    return true;
+    return encode_bf16_map(map, hot_base, 4, dims, strides, box, why);
 }
 
 template <int kWarps, int kStages, int kSub, Form kForm = kAny>

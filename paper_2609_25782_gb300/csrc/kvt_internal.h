@@ -1,5 +1,5 @@
 // Internal interface between the pool runtime (pool.cpp) and the kernels
-// (decode_kernels.cu, copy_kernels.cu). Not part of the C ABI.
+// (decode_kernels.cu, turn_kernels.cu, copy_kernels.cu). Not part of the C ABI.
 #pragma once
 
 #include <cuda.h>
@@ -104,7 +104,13 @@ struct TurnArgs {
     int32_t *err;
     int64_t q_stride, kv_stride;
     int32_t total, B, max_blocks, layer, out_bf16;
+    int32_t negate;                  // set by the launch: a negative scale's sign
     float scale_log2;                // scale * log2(e)
+    // Workspace for items that are cut into pieces, of 2 slots per CTA of the launch
+    // (turn_part_floats, turn_counters; counters are zero between calls).
+    float *part;
+    int32_t *part_counters;
+    int32_t part_slots;
     Shape s;
 };
 
@@ -223,7 +229,10 @@ struct GatherArgs {
     int32_t new_blk[kGatherMax];   // >= 0: also store it as the row's last entry (nblk-1)
 };
 
-// Host launchers (decode_kernels.cu, copy_kernels.cu). Each returns the launch's CUDA status.
+// Host launchers (decode_kernels.cu, turn_kernels.cu, copy_kernels.cu). Each returns the launch's CUDA status.
+// A bf16 tensor map with the 128-byte swizzle; strides in bytes, from the second dimension on.
+bool encode_bf16_map(CUtensorMap *map, void *base, int rank, const cuuint64_t *dims,
+                     const cuuint64_t *strides, const cuuint32_t *box, const char **why);
 // The decode kernel's tensor map of the hot pool: rows of 128 bf16, and
 // run_rows (Hkv * bt) rows between a (block, layer) K run and its V run.
 bool encode_hot_tensor_map(CUtensorMap *map, void *hot_base, int64_t rows, int64_t run_rows,
@@ -234,7 +243,11 @@ cudaError_t prepare_kernels();  // per-device function attributes
 // split kernel's tile rings to the grid.
 cudaError_t launch_decode(const CUtensorMap &map, const DecodeArgs &a, int num_sms,
                           cudaStream_t st, bool overlap_previous);
-cudaError_t launch_turn(const TurnArgs &a, cudaStream_t st);
+cudaError_t launch_turn(TurnArgs a, const CUtensorMap &hot, cudaStream_t st);
+cudaError_t prepare_turn_kernel();
+bool encode_turn_hot_map(CUtensorMap *map, void *hot_base, int64_t rows, const char **why);
+int64_t turn_part_floats(int ctas);
+int64_t turn_counters(int ctas);
 // max_ctas > 0 caps the copy grids (migration_ctas).
 cudaError_t launch_unpack(MigArgs a, int max_ctas, cudaStream_t st);
 cudaError_t launch_unpack_inline(ResumeArgs &r, int max_ctas, cudaStream_t st);
