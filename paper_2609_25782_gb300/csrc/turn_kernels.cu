@@ -31,7 +31,7 @@ constexpr int kThreads = 384;
 constexpr int kCopyWarp = 8, kMmaWarp = 9;          // 10 and 11 only make up a warpgroup
 // Registers per thread: at launch, then of the softmax warps and of the others. A softmax thread
 // keeps its row's 128 scores; the shares add up to what the CTA was launched with.
-constexpr int kRegsLaunch = 168, kRegsSoftmax = 216, kRegsOther = 72;
+constexpr int kRegsLaunch = 168, kRegsSoftmax = 200, kRegsOther = 104;
 static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * kRegsLaunch, "a larger share would wait forever");
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s
 
@@ -547,80 +547,133 @@ struct Stats {
     float m, l;   // running maximum of the scaled scores (base 2), sum of the weights
 };
 
-// A key tile's weights of this thread's row: S from tensor memory, P back over it.
+// Two values at a time.
+__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
+    uint64_t y;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "r"(lo), "r"(hi));
+    return y;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) {
+    uint64_t w;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(w) : "l"(x), "l"(y), "l"(z));
+    return w;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
+    uint64_t w;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(w) : "l"(x), "l"(y));
+    return w;
+}
+__device__ __forceinline__ float2 halves(uint64_t x) {
+    float2 y;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(y.x), "=f"(y.y) : "l"(x));
+    return y;
+}
+
+__device__ __forceinline__ float top_of(const uint32_t (&x)[32], float top) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(x[i]));
+    return top;
+}
+
+// The running maximum after a tile whose largest scaled score is `top`; O follows where it moves.
+// A row that sees nothing yet keeps m = -infinity.
+__device__ __forceinline__ void move_top(float top, uint32_t o_addr, bool first, Stats &st) {
+    if (!__any_sync(~0u, top > st.m + kLazyLog2)) return;
+    const float m = fmaxf(st.m, top);
+    const float c = m == -INFINITY ? 1.f : ex2(st.m - m);
+    st.m = m;
+    st.l *= c;
+    if (first) return;
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+        uint32_t o[32];
+        tmem_load(o, o_addr + i * 32);
+        tmem_wait(o);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * c);
+        tmem_store(o_addr + i * 32, o);
+    }
+}
+
+// Weights ex2(x * scale - ref) of 32 scores, in bf16 to tensor memory; their sum (of the unrounded
+// ones) is added to `sum`.
+__device__ __forceinline__ void put_weights(const uint32_t (&x)[32], uint64_t scale, uint64_t ref, uint32_t p_addr,
+                                            uint64_t &sum) {
+    uint32_t p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float2 e = halves(fma2(pair_of(x[2 * i], x[2 * i + 1]), scale, ref));
+        const float y0 = ex2(e.x), y1 = ex2(e.y);
+        sum = add2(sum, pair_of(__float_as_uint(y0), __float_as_uint(y1)));
+        p[i] = pack_bf16(y0, y1);
+    }
+    tmem_store16(p_addr, p);
+}
+
+// Scores of which the row sees those in `sees`; the others become -infinity, weight 0.
+__device__ __forceinline__ void hide(uint32_t (&x)[32], uint32_t sees) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        if (!(sees >> i & 1)) x[i] = 0xFF800000u;
+}
+
+// A key tile's weights of this thread's row: S from tensor memory, P back over it (16 columns
+// of P for 32 of S, so a chunk's weights never reach scores that are still to be read).
 __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, int t, int token, uint64_t mask,
                                              uint32_t s_addr, uint32_t o_addr, bool first, Stats &st) {
     const int keys = keys_of(r, t);
     const bool own = t >= r.cached_tiles;
-    const int j0 = own ? (t - r.cached_tiles) * kTurnKeys : 0;
-    // Keys of the tile that the row sees: the first `seen` of them, or (drafts) those of its mask.
+    // Keys of the tile that the row sees: the first `seen` of them, of drafts those in its mask.
     int seen = keys;
-    if (own && !a.masks) seen = min(keys, token + 1 - j0);
-    const int chunks = (keys + 31) / 32;
-    uint32_t x[4][32];
+    if (own && !a.masks) seen = min(keys, token + 1 - (t - r.cached_tiles) * kTurnKeys);
+    const uint64_t scale = pair_of(__float_as_uint(a.scale_log2), __float_as_uint(a.scale_log2));
+    uint64_t sum = 0;
+    if (__all_sync(~0u, seen == kTurnKeys) && !(own && a.masks)) {
+        uint32_t x[4][32];
+        tmem_load(x[0], s_addr);
+        tmem_load(x[1], s_addr + 32);
+        tmem_wait(x[0]);
+        tmem_wait(x[1]);
+        tmem_load(x[2], s_addr + 64);
+        tmem_load(x[3], s_addr + 96);
+        const float half = top_of(x[1], top_of(x[0], -INFINITY));
+        tmem_wait(x[2]);
+        tmem_wait(x[3]);
+        move_top(top_of(x[3], top_of(x[2], half)) * a.scale_log2, o_addr, first, st);
+        const uint32_t minus = __float_as_uint(st.m == -INFINITY ? 0.f : -st.m);
+        const uint64_t ref = pair_of(minus, minus);
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (c < chunks) tmem_load(x[c], s_addr + c * 32);
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (c < chunks) tmem_wait(x[c]);
-    const bool masked = keys < kTurnKeys || (own && (a.masks || __any_sync(~0u, seen < keys)));
-    if (masked) {
-        const bool bits = own && a.masks;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (c < chunks) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int k = c * 32 + i;
-                    const bool sees = k < seen && !(bits && !(c < 2 && (mask >> (k & 63) & 1)));
-                    if (!sees) x[c][i] = 0xFF800000u;   // -infinity
-                }
-            }
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (c < chunks) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(x[c][i]));
+        for (int c = 0; c < 4; ++c) put_weights(x[c], scale, ref, s_addr + c * 16, sum);
+    } else {
+        const uint64_t bits = own && a.masks ? mask : ~0ull;   // drafts are at most 64 keys
+        const int chunks = (keys + 31) / 32;
+        auto sees = [&](int c) {
+            const int n = seen - c * 32;
+            return (n >= 32 ? ~0u : n > 0 ? (1u << n) - 1 : 0u) & (c < 2 ? static_cast<uint32_t>(bits >> (c * 32)) : ~0u);
+        };
+        float top = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < chunks; ++c) {
+            uint32_t x[32];
+            tmem_load(x, s_addr + c * 32);
+            tmem_wait(x);
+            hide(x, sees(c));
+            top = top_of(x, top);
         }
-    top *= a.scale_log2;
-    // A row that sees nothing yet keeps m = -infinity, and weights of 0 by ex2(-infinity).
-    if (__any_sync(~0u, top > st.m + kLazyLog2)) {
-        const float m = fmaxf(st.m, top);
-        const float c = m == -INFINITY ? 1.f : ex2(st.m - m);
-        st.m = m;
-        st.l *= c;
-        if (!first) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t o[32];
-                tmem_load(o, o_addr + i * 32);
-                tmem_wait(o);
-#pragma unroll
-                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * c);
-                tmem_store(o_addr + i * 32, o);
-            }
+        move_top(top * a.scale_log2, o_addr, first, st);
+        const uint32_t minus = __float_as_uint(st.m == -INFINITY ? 0.f : -st.m);
+        const uint64_t ref = pair_of(minus, minus);
+#pragma unroll 1
+        for (int c = 0; c < chunks; ++c) {
+            uint32_t x[32];
+            tmem_load(x, s_addr + c * 32);
+            tmem_wait(x);
+            hide(x, sees(c));
+            put_weights(x, scale, ref, s_addr + c * 16, sum);
         }
     }
-    const float ref = st.m == -INFINITY ? 0.f : st.m;
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (c < chunks) {
-            uint32_t p[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float y0 = ex2(__fmaf_rn(__uint_as_float(x[c][2 * i]), a.scale_log2, -ref));
-                const float y1 = ex2(__fmaf_rn(__uint_as_float(x[c][2 * i + 1]), a.scale_log2, -ref));
-                sum[0] += y0;
-                sum[1] += y1;
-                p[i] = pack_bf16(y0, y1);
-            }
-            tmem_store16(s_addr + c * 16, p);
-        }
-    st.l += sum[0] + sum[1];
+    const float2 y = halves(sum);
+    st.l += y.x + y.y;
     tmem_stored();
 }
 
@@ -649,22 +702,23 @@ __device__ __forceinline__ float2 *part_ml(const TurnArgs &a, int slot, int stre
            (static_cast<int64_t>(slot) * 2 + stream) * kTurnRows;
 }
 
-// The item's output rows of this stream, from tensor memory: O times `scale_o`, and (other != 0) the other
-// stream's times `scale_other`.
-template <typename Put>
-__device__ __forceinline__ void read_o(uint32_t o_addr, float scale_o, uint32_t other, float scale_other, Put put) {
+// The item's output row of this thread, from tensor memory, 32 columns at a time: O times `w`, and
+// (kTwo) the other stream's, at `other`, times `w_other`.
+template <bool kTwo, typename Put>
+__device__ __forceinline__ void read_o(uint32_t o_addr, float w, uint32_t other, float w_other, Put put) {
 #pragma unroll 1
     for (int d = 0; d < kHeadDim; d += 32) {
-        uint32_t o[32], z[32];
+        uint32_t o[32];
         float y[32];
         tmem_load(o, o_addr + d);
-        if (other) tmem_load(z, other + d);
         tmem_wait(o);
-        if (other) tmem_wait(z);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            y[i] = __uint_as_float(o[i]) * scale_o;
-            if (other) y[i] = __fmaf_rn(__uint_as_float(z[i]), scale_other, y[i]);
+        for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(o[i]) * w;
+        if constexpr (kTwo) {
+            tmem_load(o, other + d);
+            tmem_wait(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] = __fmaf_rn(__uint_as_float(o[i]), w_other, y[i]);
         }
         put(d, y);
     }
@@ -748,22 +802,26 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
         if (!(r.narrow && stream == 1)) {
             if (whole) {
                 const float inv = st.l > 0.f || st.l != st.l ? __frcp_rn(st.l) : 0.f;   // nothing seen: zeros
-                if (ok) read_o(o_addr, w * inv, other, w_other * inv, [&](int d, const float (&y)[32]) {
+                const auto put = [&](int d, const float (&y)[32]) {
                     if (live) store_out(a, out_row, d, y);
-                });
+                };
+                if (ok && other) read_o<true>(o_addr, w * inv, other, w_other * inv, put);
+                else if (ok) read_o<false>(o_addr, w * inv, 0, 0.f, put);
             } else {
                 int c0, c1;
                 turn_item_pieces(sm.plan.W, sm.plan.pieces, r.t0 > 0 ? sm.plan.begin_at : sm.plan.end_at, r.tiles,
                                  turn_tile_cost(s, r.x, r.pair), &c0, &c1);
                 const int slot = r.t0 > 0 ? 2 * blockIdx.x : 2 * blockIdx.x + 1;
                 float4 *po = part_o(a, slot, stream);
-                if (ok) read_o(o_addr, w, other, w_other, [&](int d, const float (&y)[32]) {
+                const auto put = [&](int d, const float (&y)[32]) {
                     if (!live) return;
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         po[(d / 4 + i) * kTurnRows + row] =
                             make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-                });
+                };
+                if (ok && other) read_o<true>(o_addr, w, other, w_other, put);
+                else if (ok) read_o<false>(o_addr, w, 0, 0.f, put);
                 if (live) part_ml(a, slot, stream)[row] = make_float2(st.m, st.l);
                 __threadfence();
                 sync_threads(1 + stream, kTurnRows);
