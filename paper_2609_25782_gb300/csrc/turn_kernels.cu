@@ -471,6 +471,28 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
 
 // ---- matrix products -----------------------------------------------------------------------
 
+// S = Q K^T. The steps' operands lie a constant apart: one addition per step and operand, so that the
+// issuing thread keeps up with the tensor cores (64 cycles a step).
+__device__ __forceinline__ void product_qk(uint32_t d, uint32_t q, uint32_t k, uint32_t form) {
+    const uint64_t a = operand(q, 16), b = operand(k, 16);
+#pragma unroll
+    for (int i = 0; i < kHeadDim / 16; ++i) {
+        const int off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;
+        mma_ss(d, a + off, b + off, form, i > 0);
+    }
+}
+// O += P V over 16 * steps keys, or O = P V.
+__device__ __forceinline__ void product_pv(uint32_t d, uint32_t p, uint32_t v, int steps, bool add) {
+    const uint64_t b = operand(v, kHalfBytes);
+    const uint32_t form = mma_form(kHeadDim, true, false);
+    if (steps == kTurnKeys / 16) {
+#pragma unroll
+        for (int i = 0; i < kTurnKeys / 16; ++i) mma_ts(d, p + i * 8, b + i * (16 * 128 >> 4), form, i > 0 || add);
+    } else {
+        for (int i = 0; i < steps; ++i) mma_ts(d, p + i * 8, b + i * (16 * 128 >> 4), form, i > 0 || add);
+    }
+}
+
 // One thread. Ring position of the n-th tile of the piece: K at 2n, V at 2n + 1.
 __device__ void mma_role(const TurnArgs &a, Smem &sm) {
     const uint32_t tmem = sm.tmem;
@@ -500,11 +522,8 @@ __device__ void mma_role(const TurnArgs &a, Smem &sm) {
             if (!ok) return;
             p_phase[s] ^= 1;
             fence_after();
-            const int steps = (keys_of(r, r.t0 + i) + 15) / 16;
-            const uint32_t v = smem_u32(sm.kv[st]);
-            for (int k = 0; k < steps; ++k)
-                mma_ts(tmem + kColO + s * kColStream, tmem + kColS + s * kColStream + k * 8,
-                       operand(v + k * 16 * 128, kHalfBytes), mma_form(kHeadDim, true, false), j >= 2 || k > 0);
+            product_pv(tmem + kColO + s * kColStream, tmem + kColS + s * kColStream, smem_u32(sm.kv[st]),
+                       (keys_of(r, r.t0 + i) + 15) / 16, j >= 2);
             if (r.narrow || s == 1) mma_commit(&sm.kv_empty[st]);
         };
         for (int j = 0; ok && j < jobs; ++j) {
@@ -515,12 +534,8 @@ __device__ void mma_role(const TurnArgs &a, Smem &sm) {
             if (ok && (r.narrow || s == 0)) ok = mbar_wait(sm, &sm.kv_full[st], parity);
             if (!ok) break;
             fence_after();
-            const uint32_t form = mma_form((keys_of(r, r.t0 + i) + 15) / 16 * 16, false, negate);
-            const uint32_t q = smem_u32(sm.q[r.narrow ? 0 : s]), k = smem_u32(sm.kv[st]);
-            for (int d = 0; d < kHeadDim / 16; ++d) {
-                const uint32_t off = (d >> 2) * kHalfBytes + (d & 3) * 32;
-                mma_ss(tmem + kColS + s * kColStream, operand(q + off, 16), operand(k + off, 16), form, d > 0);
-            }
+            product_qk(tmem + kColS + s * kColStream, smem_u32(sm.q[r.narrow ? 0 : s]), smem_u32(sm.kv[st]),
+                       mma_form((keys_of(r, r.t0 + i) + 15) / 16 * 16, false, negate));
             mma_commit(&sm.s_full[s]);
             if (r.narrow || s == 1) mma_commit(&sm.kv_empty[st]);
         }
@@ -569,11 +584,16 @@ __device__ __forceinline__ float2 halves(uint64_t x) {
     return y;
 }
 
-__device__ __forceinline__ float top_of(const uint32_t (&x)[32], float top) {
+// Four running maxima, so that no instruction waits for the one before it.
+struct Tops {
+    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    __device__ __forceinline__ void add(const uint32_t (&x)[32]) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(x[i]));
-    return top;
-}
+        for (int i = 0; i < 32; i += 2)
+            t[i / 2 % 4] = fmaxf(t[i / 2 % 4], fmaxf(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
+    }
+    __device__ __forceinline__ float all() const { return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])); }
+};
 
 // The running maximum after a tile whose largest scaled score is `top`; O follows where it moves.
 // A row that sees nothing yet keeps m = -infinity.
@@ -598,13 +618,13 @@ __device__ __forceinline__ void move_top(float top, uint32_t o_addr, bool first,
 // Weights ex2(x * scale - ref) of 32 scores, in bf16 to tensor memory; their sum (of the unrounded
 // ones) is added to `sum`.
 __device__ __forceinline__ void put_weights(const uint32_t (&x)[32], uint64_t scale, uint64_t ref, uint32_t p_addr,
-                                            uint64_t &sum) {
+                                            uint64_t (&sum)[4]) {
     uint32_t p[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const float2 e = halves(fma2(pair_of(x[2 * i], x[2 * i + 1]), scale, ref));
         const float y0 = ex2(e.x), y1 = ex2(e.y);
-        sum = add2(sum, pair_of(__float_as_uint(y0), __float_as_uint(y1)));
+        sum[i % 4] = add2(sum[i % 4], pair_of(__float_as_uint(y0), __float_as_uint(y1)));
         p[i] = pack_bf16(y0, y1);
     }
     tmem_store16(p_addr, p);
@@ -627,7 +647,8 @@ __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, in
     int seen = keys;
     if (own && !a.masks) seen = min(keys, token + 1 - (t - r.cached_tiles) * kTurnKeys);
     const uint64_t scale = pair_of(__float_as_uint(a.scale_log2), __float_as_uint(a.scale_log2));
-    uint64_t sum = 0;
+    uint64_t sum[4] = {0, 0, 0, 0};
+    Tops top;
     if (__all_sync(~0u, seen == kTurnKeys) && !(own && a.masks)) {
         uint32_t x[4][32];
         tmem_load(x[0], s_addr);
@@ -636,10 +657,13 @@ __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, in
         tmem_wait(x[1]);
         tmem_load(x[2], s_addr + 64);
         tmem_load(x[3], s_addr + 96);
-        const float half = top_of(x[1], top_of(x[0], -INFINITY));
+        top.add(x[0]);
+        top.add(x[1]);
         tmem_wait(x[2]);
         tmem_wait(x[3]);
-        move_top(top_of(x[3], top_of(x[2], half)) * a.scale_log2, o_addr, first, st);
+        top.add(x[2]);
+        top.add(x[3]);
+        move_top(top.all() * a.scale_log2, o_addr, first, st);
         const uint32_t minus = __float_as_uint(st.m == -INFINITY ? 0.f : -st.m);
         const uint64_t ref = pair_of(minus, minus);
 #pragma unroll
@@ -651,16 +675,15 @@ __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, in
             const int n = seen - c * 32;
             return (n >= 32 ? ~0u : n > 0 ? (1u << n) - 1 : 0u) & (c < 2 ? static_cast<uint32_t>(bits >> (c * 32)) : ~0u);
         };
-        float top = -INFINITY;
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c) {
             uint32_t x[32];
             tmem_load(x, s_addr + c * 32);
             tmem_wait(x);
             hide(x, sees(c));
-            top = top_of(x, top);
+            top.add(x);
         }
-        move_top(top * a.scale_log2, o_addr, first, st);
+        move_top(top.all() * a.scale_log2, o_addr, first, st);
         const uint32_t minus = __float_as_uint(st.m == -INFINITY ? 0.f : -st.m);
         const uint64_t ref = pair_of(minus, minus);
 #pragma unroll 1
@@ -672,7 +695,7 @@ __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, in
             put_weights(x, scale, ref, s_addr + c * 16, sum);
         }
     }
-    const float2 y = halves(sum);
+    const float2 y = halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
     st.l += y.x + y.y;
     tmem_stored();
 }
