@@ -493,61 +493,94 @@ __device__ __forceinline__ void product_pv(uint32_t d, uint32_t p, uint32_t v, i
     }
 }
 
-// One thread. Ring position of the n-th tile of the piece: K at 2n, V at 2n + 1.
+// A stage of the ring and the parity of its present round, two stages further at each step: K tiles
+// have the even places, V tiles the odd ones.
+struct Cursor {
+    int stage;
+    uint32_t parity;
+    __device__ __forceinline__ void next() {
+        stage += 2;
+        if (stage >= kStages) {
+            stage -= kStages;
+            parity ^= 1;
+        }
+    }
+};
+
+// One lane of the warp.
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }
+
+// The whole warp walks and waits, one lane issues: control flow and operands are the same in all lanes,
+// which the compiler has to see (votes, shuffles) to keep them in uniform registers. With one lane
+// doing everything each step moved its operands there first: 90 cycles a step, 64 of the tensor cores'.
 __device__ void mma_role(const TurnArgs &a, Smem &sm) {
-    const uint32_t tmem = sm.tmem;
+    const uint32_t tmem = uniform(sm.tmem);
     const bool negate = a.negate != 0;
     uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-    int64_t base = 0;   // tiles of the runs before
+    Cursor at_k = {0, 0}, at_v = {1, 0};
     bool ok = true;
-    auto ring = [&](int64_t pos, uint32_t *parity) {
-        *parity = static_cast<uint32_t>(pos / kStages) & 1;
-        return static_cast<int>(pos % kStages);
-    };
+    auto wait = [&](uint64_t *bar, uint32_t parity) { ok = __all_sync(~0u, mbar_wait(sm, bar, parity)); };
     Walk walk(sm.plan);
     Run r;
-    while (ok && walk.next(a, sm.plan, r)) {
-        const int tiles = r.t1 - r.t0, jobs = r.narrow ? tiles : 2 * tiles;
-        for (int s = 0; ok && s < (r.narrow ? 1 : 2); ++s) {
-            ok = mbar_wait(sm, &sm.q_full[s], q_phase[s]);
+    while (ok && __all_sync(~0u, walk.next(a, sm.plan, r))) {
+        const int tiles = uniform(r.t1 - r.t0), t0 = uniform(r.t0), cached_tiles = uniform(r.cached_tiles);
+        const int cached_keys = uniform(r.x.P), own_keys = uniform(r.own_keys);
+        const bool narrow = uniform(r.narrow);
+        const int jobs = narrow ? tiles : 2 * tiles;
+        auto steps_of = [&](int i) {   // of 16 keys, of the run's tile i
+            const int t = t0 + i;
+            const int left = t < cached_tiles ? cached_keys - t * kTurnKeys : own_keys - (t - cached_tiles) * kTurnKeys;
+            return left >= kTurnKeys ? kTurnKeys / 16 : (left + 15) / 16;
+        };
+        for (int s = 0; ok && s < (narrow ? 1 : 2); ++s) {
+            wait(&sm.q_full[s], q_phase[s]);
             q_phase[s] ^= 1;
         }
         // O_s += P_s V of job j
         auto pv = [&](int j) {
-            const int s = j & 1, i = r.narrow ? j : j >> 1;
-            uint32_t parity;
-            const int st = ring(2 * (base + i) + 1, &parity);
-            if (r.narrow || s == 0) ok = ok && mbar_wait(sm, &sm.kv_full[st], parity);
-            ok = ok && mbar_wait(sm, &sm.p_full[s], p_phase[s]);
+            const int s = j & 1;
+            if (narrow || s == 0) wait(&sm.kv_full[at_v.stage], at_v.parity);
+            if (ok) wait(&sm.p_full[s], p_phase[s]);
             if (!ok) return;
             p_phase[s] ^= 1;
             fence_after();
-            product_pv(tmem + kColO + s * kColStream, tmem + kColS + s * kColStream, smem_u32(sm.kv[st]),
-                       (keys_of(r, r.t0 + i) + 15) / 16, j >= 2);
-            if (r.narrow || s == 1) mma_commit(&sm.kv_empty[st]);
+            const int steps = steps_of(narrow ? j : j >> 1);
+            if (elected()) {
+                product_pv(tmem + kColO + s * kColStream, tmem + kColS + s * kColStream,
+                           smem_u32(sm.kv[at_v.stage]), steps, j >= 2);
+                if (narrow || s == 1) mma_commit(&sm.kv_empty[at_v.stage]);
+                if (j + 2 >= jobs) mma_commit(&sm.o_full[s]);
+            }
+            __syncwarp();
+            if (narrow || s == 1) at_v.next();
         };
         for (int j = 0; ok && j < jobs; ++j) {
-            const int s = j & 1, i = r.narrow ? j : j >> 1;
+            const int s = j & 1;
             if (j >= 2) pv(j - 2);
-            uint32_t parity;
-            const int st = ring(2 * (base + i), &parity);
-            if (ok && (r.narrow || s == 0)) ok = mbar_wait(sm, &sm.kv_full[st], parity);
+            if (ok && (narrow || s == 0)) wait(&sm.kv_full[at_k.stage], at_k.parity);
             if (!ok) break;
             fence_after();
-            product_qk(tmem + kColS + s * kColStream, smem_u32(sm.q[r.narrow ? 0 : s]), smem_u32(sm.kv[st]),
-                       mma_form((keys_of(r, r.t0 + i) + 15) / 16 * 16, false, negate));
-            mma_commit(&sm.s_full[s]);
-            if (r.narrow || s == 1) mma_commit(&sm.kv_empty[st]);
+            const int steps = steps_of(narrow ? j : j >> 1);
+            if (elected()) {
+                product_qk(tmem + kColS + s * kColStream, smem_u32(sm.q[narrow ? 0 : s]),
+                           smem_u32(sm.kv[at_k.stage]), mma_form(16 * steps, false, negate));
+                mma_commit(&sm.s_full[s]);
+                if (narrow || s == 1) mma_commit(&sm.kv_empty[at_k.stage]);
+                if (j == jobs - 1) mma_commit(&sm.q_empty);
+            }
+            __syncwarp();
+            if (narrow || s == 1) at_k.next();
         }
-        if (ok) mma_commit(&sm.q_empty);
-        for (int j = jobs < 2 ? 0 : jobs - 2; ok && j < jobs; ++j) {
-            pv(j);
-            if (ok) mma_commit(&sm.o_full[j & 1]);
-        }
-        base += tiles;
+        for (int j = jobs < 2 ? 0 : jobs - 2; ok && j < jobs; ++j) pv(j);
     }
     // Nothing of the tensor cores' is left behind.
-    mma_commit(&sm.drained);
+    if (elected()) mma_commit(&sm.drained);
+    __syncwarp();
     const unsigned long long t0 = global_ns();
     while (!mbar_try(&sm.drained, 0) && global_ns() - t0 < kWaitLimitNs) {}
 }
@@ -935,7 +968,7 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
         } else {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
             if (warp == kCopyWarp) copy_role(a, maps, sm, lane);
-            else if (warp == kMmaWarp && lane == 0) mma_role(a, sm);
+            else if (warp == kMmaWarp) mma_role(a, sm);
         }
     }
     __syncwarp();
