@@ -243,9 +243,9 @@ cudaError_t prepare_kernels();  // per-device function attributes
 // split kernel's tile rings to the grid.
 cudaError_t launch_decode(const CUtensorMap &map, const DecodeArgs &a, int num_sms,
                           cudaStream_t st, bool overlap_previous);
-cudaError_t launch_turn(TurnArgs a, const CUtensorMap &hot, cudaStream_t st);
+cudaError_t launch_turn(TurnArgs a, const CUtensorMap hot[2], cudaStream_t st);
 cudaError_t prepare_turn_kernel();
-bool encode_turn_hot_map(CUtensorMap *map, void *hot_base, int64_t rows, const char **why);
+bool encode_turn_hot_maps(CUtensorMap maps[2], void *hot_base, int64_t rows, int bt, const char **why);
 int64_t turn_part_floats(int ctas);
 int64_t turn_counters(int ctas);
 // max_ctas > 0 caps the copy grids (migration_ctas).

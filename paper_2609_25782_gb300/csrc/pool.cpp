@@ -134,7 +134,7 @@ struct kv_pool {
     float *d_turn_part = nullptr;        // partial results of prefill_attention and tree_attention
     int32_t *d_turn_counters = nullptr;  // right after d_counters' counter_count decode ones
     int64_t turn_counter_count = 0;
-    CUtensorMap tmap{}, turn_map{};
+    CUtensorMap tmap{}, turn_maps[2]{};
 
     Fence fences[kFenceSlots];
     int next_fence = 0;
@@ -552,7 +552,7 @@ int kv_pool_create(const kv_pool_config *cfg, kv_pool **out) {
         if (!kvt::encode_hot_tensor_map(&p->tmap, c.hot_base, rows,
                                         static_cast<int64_t>(c.num_kv_heads) * c.block_tokens, &why))
             return bail(fail(KV_ERR_CUDA, why));
-        if (!kvt::encode_turn_hot_map(&p->turn_map, c.hot_base, rows, &why))
+        if (!kvt::encode_turn_hot_maps(p->turn_maps, c.hot_base, rows, c.block_tokens, &why))
             return bail(fail(KV_ERR_CUDA, why));
         if (cudaDeviceSynchronize() != cudaSuccess)
             return bail(fail(KV_ERR_CUDA, "device synchronise after pool set-up failed"));
@@ -1045,7 +1045,7 @@ static int turn_impl(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     a.part_slots = 2 * p->num_sms;
     a.s = p->shape;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream_);
-    int rc = p->cuda("attention launch", [&] { return kvt::launch_turn(a, p->turn_map, st); });
+    int rc = p->cuda("attention launch", [&] { return kvt::launch_turn(a, p->turn_maps, st); });
     if (rc) return rc;
     p->decoded = true;
     p->decode_stream = st;

@@ -12,8 +12,8 @@
 //             memory, running maximum and sum in 32 bits, weights back to tensor
 //             memory in bf16; at the end the output
 //   8         copies: q tiles and key tiles (TMA, 128-byte swizzle)
-//   9         matrix products (tcgen05): S = Q K^T from shared memory, O += P V
-//             with P from tensor memory
+//   9, 10     matrix products (tcgen05) of stream 0 and 1: S = Q K^T from shared
+//             memory, O += P V with P from tensor memory
 // The tensor cores work on one stream while the other's softmax runs.
 #include <cuda_bf16.h>
 
@@ -24,11 +24,16 @@ namespace kvt {
 namespace {
 
 constexpr int kTileBytes = kTurnKeys * kRowBytes;   // a key or row tile, 32 KB
-constexpr int kHalfBytes = kTileBytes / 2;          // its columns 0-63, then 64-127: 128 rows of 128 B
-constexpr int kBoxRows = 16;                        // rows of one copy
+// Its rows' halves (columns 0-63 and 64-127, 128 B each) lie in one of two orders. Whole: all rows'
+// first halves, then all second ones; a q tile, or a tile of the call's own tokens, is one copy or two.
+// Grouped: eight rows' first halves, their second halves, the next eight rows'; so a block of the
+// pool is one copy, whatever its place in the tile.
+constexpr int kHalfWhole = kTileBytes / 2, kHalfGrouped = 1024;   // bytes from a row's half to the other
+constexpr int kGroupWhole = 1024, kGroupGrouped = 2048;           // bytes from eight rows to the next
+constexpr int kBoxRows = 16;                        // rows that a copy at the end of the keys has
 constexpr int kStages = 5;                          // K or V tiles in flight
 constexpr int kThreads = 384;
-constexpr int kCopyWarp = 8, kMmaWarp = 9;          // 10 and 11 only make up a warpgroup
+constexpr int kCopyWarp = 8, kMmaWarp = 9;          // and 10; 11 only makes up a warpgroup
 // Registers per thread: at launch, then of the softmax warps and of the others. A softmax thread
 // keeps its row's 128 scores; the shares add up to what the CTA was launched with.
 constexpr int kRegsLaunch = 168, kRegsSoftmax = 200, kRegsOther = 104;
@@ -49,8 +54,11 @@ struct Plan {
 struct alignas(1024) Smem {
     uint8_t q[2][kTileBytes];
     uint8_t kv[kStages][kTileBytes];
-    uint64_t kv_full[kStages], kv_empty[kStages];
-    uint64_t q_full[2], q_empty, s_full[2], p_full[2], o_full[2], drained;
+    // The ring's copies have landed: two barriers a stage, for its even and its odd rounds. A stream of a
+    // narrow item does not look at the other's tiles, so it may ask for a stage's next round while the
+    // present one is still on its way; with one barrier, a parity, that would pass as done.
+    uint64_t kv_full[2 * kStages], kv_empty[kStages];
+    uint64_t q_full[2], q_empty, s_full[2], p_full[2], o_full[2], drained[2];
     Plan plan;
     float other_m[kTurnRows], other_l[kTurnRows];   // narrow items: stream 1's statistics
     uint32_t tmem;
@@ -61,7 +69,9 @@ constexpr int kSmemBytes = sizeof(Smem) + 1024;     // and the way to a 1 024-by
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of a CTA");
 
 struct Maps {
-    CUtensorMap q, k, v, hot;
+    CUtensorMap q;                       // [token][head] rows, a half row tile a copy
+    CUtensorMap k, v, k_whole, v_whole;  // kBoxRows rows' halves a copy, or a tile
+    CUtensorMap hot, hot_block;          // kBoxRows grouped rows a copy, or a block
 };
 
 // ---- instructions ------------------------------------------------------------------------
@@ -109,28 +119,20 @@ __device__ __forceinline__ bool mbar_wait(Smem &sm, uint64_t *bar, uint32_t pari
     return true;
 }
 
-__device__ __forceinline__ void copy_box3(void *dst, const CUtensorMap *map, int row, int half, uint64_t *bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(half), "r"(smem_u32(bar))
-        : "memory");
-}
-__device__ __forceinline__ void copy_box4(void *dst, const CUtensorMap *map, int head, int token, int half,
-                                          uint64_t *bar) {
+__device__ __forceinline__ void copy_box(void *dst, const CUtensorMap *map, int c1, int c2, int c3, uint64_t *bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
         " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(head), "r"(token), "r"(half), "r"(smem_u32(bar))
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar))
         : "memory");
 }
 
-// Shared-memory operand, 128-byte swizzle. Q and K have their inner (summed) dimension contiguous:
-// groups of 8 rows are 1 024 bytes apart. V is summed over its rows: 8 keys are 1 024 bytes
-// apart, its two column halves kHalfBytes.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading) {
-    return static_cast<uint64_t>(addr >> 4 & 0x3FFF) | static_cast<uint64_t>(leading >> 4) << 16 |
-           static_cast<uint64_t>(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+// Shared-memory operand, 128-byte swizzle: rows of 128 B in groups of eight, `group` bytes from one to
+// the next. An operand that is summed over its rows (V) has its two column halves `half` bytes apart;
+// where the sum runs along the rows (Q, K) that field is not used.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t half, uint32_t group) {
+    return static_cast<uint64_t>(addr >> 4 & 0x3FFF) | static_cast<uint64_t>(half >> 4) << 16 |
+           static_cast<uint64_t>(group >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 // bf16 x bf16 -> fp32, 128 rows; n columns, the right operand transposed for V, the left negated.
 __device__ __forceinline__ uint32_t mma_form(int n, bool v, bool negate) {
@@ -158,6 +160,14 @@ __device__ __forceinline__ void mma_commit(uint64_t *bar) {
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// One lane of the warp.
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }
 
 #define KVT_R8(x, o) "=r"(x[o]), "=r"(x[o + 1]), "=r"(x[o + 2]), "=r"(x[o + 3]), "=r"(x[o + 4]), "=r"(x[o + 5]), \
         "=r"(x[o + 6]), "=r"(x[o + 7])
@@ -366,56 +376,90 @@ __device__ __forceinline__ int keys_of(const Run &r, int t) {
 
 // ---- copies ------------------------------------------------------------------------------
 
-// One K (kv = 0) or V tile into a stage, by the copy warp: groups of 16 keys by TMA, two boxes each
-// (the column halves, kHalfBytes apart). Keys past the last full group come by plain loads, rows up
-// to the group's end are cleared: what they hold in memory may be anything, and a weight of 0 does not
-// make a NaN go away in the product with V.
-__device__ __forceinline__ void copy_key_tile(const TurnArgs &a, const Maps &maps, const Run &r, int t, int kv,
-                                              uint8_t *stage, uint64_t *full, int lane) {
+// Lane l's row of the pool (below 2^31) for key tile t: K of its keys 16 l and on, where there are any.
+__device__ __forceinline__ int pool_row(const TurnArgs &a, const Run &r, int t, int lane) {
     const Shape &sh = a.s;
-    const int keys = keys_of(r, t), groups = keys / kBoxRows, rest = keys % kBoxRows;
-    const bool cached = t < r.cached_tiles;
-    const int k0 = (cached ? t : t - r.cached_tiles) * kTurnKeys;
-    // Lane l has group l / 2, column half l % 2.
-    const int group = lane >> 1, half = lane & 1;
-    int row = 0;   // of the pool: below 2^31
-    if (cached && group * kBoxRows < keys) {
-        const int pos = k0 + group * kBoxRows, j = pos / sh.bt;
-        int blk = a.tables[static_cast<int64_t>(r.b) * a.max_blocks + j];
-        if (blk < 0 || blk >= sh.num_blocks) {
-            atomicOr(a.err, kErrBadBlock);
-            blk = 0;   // the result is wrong, the access is not
-        }
-        row = (((blk * sh.L + a.layer) * 2 + kv) * sh.Hkv + r.g) * sh.bt + pos - j * sh.bt;
+    const int pos = t * kTurnKeys + lane * kBoxRows;
+    if (t >= r.cached_tiles || lane >= kTurnKeys / kBoxRows || pos >= r.x.P) return 0;
+    const int j = sh.bt == 64 ? pos >> 6 : pos >> 4;
+    int blk = a.tables[static_cast<int64_t>(r.b) * a.max_blocks + j];
+    if (blk < 0 || blk >= sh.num_blocks) {
+        atomicOr(a.err, kErrBadBlock);
+        blk = 0;   // the result is wrong, the access is not
     }
-    if (rest) {
-        const int first = __shfl_sync(~0u, row, 2 * groups);
-        const uint16_t *src;
-        int64_t step;
-        if (cached) {
-            src = a.hot + static_cast<int64_t>(first) * kHeadDim;
-            step = kHeadDim;
-        } else {
-            src = (kv ? a.v_new : a.k_new) + (r.x.lo + k0 + groups * kBoxRows) * a.kv_stride + r.g * kHeadDim;
-            step = a.kv_stride;
-        }
+    return ((blk * sh.L + a.layer) * 2 * sh.Hkv + r.g) * sh.bt + pos - j * sh.bt;
+}
+
+// The keys past the last full group of 16, by plain loads; rows up to the group's end are cleared: what
+// they hold in memory may be anything, and a weight of 0 does not make a NaN go away in the product with V.
+__device__ __forceinline__ void copy_rest(const uint16_t *src, int64_t step, int rest, uint8_t *stage, int row0,
+                                          int half, int group, int lane) {
 #pragma unroll
-        for (int i = 0; i < kBoxRows * 16 / 32; ++i) {
-            const int rr = i * 2 + (lane >> 4), u = lane & 15;   // row of the group, 16-byte unit of the row
-            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (rr < rest) x = *reinterpret_cast<const uint4 *>(src + rr * step + u * 8);
-            *reinterpret_cast<uint4 *>(stage + (u >> 3) * kHalfBytes + (groups * kBoxRows + rr) * 128 +
-                                       (((u & 7) ^ (rr & 7)) << 4)) = x;
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
+    for (int i = 0; i < kBoxRows * 16 / 32; ++i) {
+        const int rr = i * 2 + (lane >> 4), u = lane & 15;   // row, 16-byte unit of the row
+        const int row = row0 + rr;
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (rr < rest) x = *reinterpret_cast<const uint4 *>(src + rr * step + u * 8);
+        *reinterpret_cast<uint4 *>(stage + (row >> 3) * group + (u >> 3) * half + (row & 7) * 128 +
+                                   (((u & 7) ^ (row & 7)) << 4)) = x;
     }
-    if (lane == 0) mbar_expect(full, groups * kBoxRows * kRowBytes);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
-    if (group < groups) {
-        uint8_t *dst = stage + half * kHalfBytes + group * kBoxRows * 128;
-        if (cached) copy_box3(dst, &maps.hot, row, half, full);
-        else copy_box4(dst, kv ? &maps.v : &maps.k, r.g, r.x.lo + k0 + group * kBoxRows, half, full);
+}
+
+// The K (kv = 0) or V tile of cached keys, grouped, by the copy warp; row: pool_row's.
+__device__ __forceinline__ void copy_cached(const TurnArgs &a, const Maps &maps, int keys, int row, int kv,
+                                            uint8_t *stage, uint64_t *full, int lane) {
+    const int groups = keys / kBoxRows, rest = keys % kBoxRows;
+    row += kv * a.s.Hkv * a.s.bt;
+    if (rest) {
+        const int first = __shfl_sync(~0u, row, groups);
+        copy_rest(a.hot + static_cast<int64_t>(first) * kHeadDim, kHeadDim, rest, stage, groups * kBoxRows,
+                  kHalfGrouped, kGroupGrouped, lane);
+    }
+    const bool leader = elected();
+    if (leader) mbar_expect(full, groups * kBoxRows * kRowBytes);
+    // Coordinates: (column, row of eight, half, eight rows)
+    int i = 0;
+    if (a.s.bt == 64)   // whole blocks
+        for (; i + 4 <= groups; i += 4) {
+            const int at = __shfl_sync(~0u, row, i) >> 3;
+            if (leader) copy_box(stage + i * 2 * kGroupGrouped, &maps.hot_block, 0, 0, at, full);
+        }
+    if (i == 0 && groups == kTurnKeys / kBoxRows) {
+#pragma unroll
+        for (int k = 0; k < kTurnKeys / kBoxRows; ++k) {
+            const int at = __shfl_sync(~0u, row, k) >> 3;
+            if (leader) copy_box(stage + k * 2 * kGroupGrouped, &maps.hot, 0, 0, at, full);
+        }
+    } else {
+        for (; i < groups; ++i) {
+            const int at = __shfl_sync(~0u, row, i) >> 3;
+            if (leader) copy_box(stage + i * 2 * kGroupGrouped, &maps.hot, 0, 0, at, full);
+        }
+    }
+    __syncwarp();
+}
+
+// The same of the call's own keys from row `first` on, whole.
+__device__ __forceinline__ void copy_own(const TurnArgs &a, const Maps &maps, int keys, int first, int g, int kv,
+                                         uint8_t *stage, uint64_t *full, int lane) {
+    const int groups = keys / kBoxRows, rest = keys % kBoxRows;
+    if (rest)
+        copy_rest((kv ? a.v_new : a.k_new) + (static_cast<int64_t>(first) + groups * kBoxRows) * a.kv_stride +
+                      g * kHeadDim,
+                  a.kv_stride, rest, stage, groups * kBoxRows, kHalfWhole, kGroupWhole, lane);
+    if (elected()) {
+        mbar_expect(full, groups * kBoxRows * kRowBytes);
+        // Coordinates: (column, head, token, half), or (column, token, half, head)
+        if (groups == kTurnKeys / kBoxRows) {
+            copy_box(stage, kv ? &maps.v_whole : &maps.k_whole, first, 0, g, full);
+        } else {
+            for (int i = 0; i < groups; ++i)
+                for (int half = 0; half < 2; ++half)
+                    copy_box(stage + half * kHalfWhole + i * kBoxRows * 128, kv ? &maps.v : &maps.k, g,
+                             first + i * kBoxRows, half, full);
+        }
     }
     __syncwarp();
 }
@@ -425,10 +469,11 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
     const int G = a.s.Hq / a.s.Hkv;
     int stage = 0, round = 0, items = 0, pairs = 0;
     uint32_t filled = 0;   // copies issued so far, saturating at kStages
-    bool ok = true;   // the same in all lanes until the last copy is out
+    bool ok = true;        // the same in all lanes until the last copy is out
     Walk walk(sm.plan);
     Run r;
     while (ok && walk.next(a, sm.plan, r)) {
+        int row = pool_row(a, r, r.t0, lane);
         if (items > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.q_empty, (items - 1) & 1));
         if (!ok) break;
         ++items;
@@ -436,30 +481,40 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
         pairs += tiles - 1;
         if (lane < tiles) mbar_expect(&sm.q_full[lane], kTileBytes);
         __syncwarp();
-        if (lane < 2 * tiles)
-            copy_box4(sm.q[lane >> 1] + (lane & 1) * kHalfBytes, &maps.q, r.g * G,
-                      r.x.lo + (2 * r.pair + (lane >> 1)) * s.tokens, lane & 1, &sm.q_full[lane >> 1]);
+        if (lane < 2 * tiles)   // coordinates: (column, head, token, half)
+            copy_box(sm.q[lane >> 1] + (lane & 1) * kHalfWhole, &maps.q, r.g * G,
+                     r.x.lo + (2 * r.pair + (lane >> 1)) * s.tokens, lane & 1, &sm.q_full[lane >> 1]);
         __syncwarp();
-        for (int t = r.t0; ok && t < r.t1; ++t)
+        for (int t = r.t0; ok && t < r.t1; ++t) {
+            const int keys = keys_of(r, t);
+            int next = 0;   // the next tile's block ids are on their way while this one's copies go out
             for (int kv = 0; kv < 2; ++kv) {
                 if (round > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.kv_empty[stage], (round - 1) & 1));
                 if (!ok) break;
-                copy_key_tile(a, maps, r, t, kv, sm.kv[stage], &sm.kv_full[stage], lane);
+                if (kv == 0 && t + 1 < r.t1) next = pool_row(a, r, t + 1, lane);
+                uint64_t *full = &sm.kv_full[stage + (round & 1) * kStages];
+                if (t < r.cached_tiles)
+                    copy_cached(a, maps, keys, row, kv, sm.kv[stage], full, lane);
+                else
+                    copy_own(a, maps, keys, r.x.lo + (t - r.cached_tiles) * kTurnKeys, r.g, kv, sm.kv[stage], full,
+                             lane);
                 if (filled < kStages) ++filled;
                 if (++stage == kStages) {
                     stage = 0;
                     ++round;
                 }
             }
+            row = next;
+        }
     }
     // Every copy lands before the CTA ends, whatever became of the other roles; with all well,
     // every stage has been given back as well.
     for (uint32_t i = 0; i < filled; ++i) {
         const bool now = static_cast<int>(i) < stage;   // filled in this round, or in the one before
-        const uint32_t parity = (now ? round : round - 1) & 1;
-        if (ok) ok = mbar_wait(sm, &sm.kv_empty[i], parity);
+        const int last = now ? round : round - 1;
+        if (ok) ok = mbar_wait(sm, &sm.kv_empty[i], last & 1);
         const unsigned long long t0 = global_ns();
-        while (!mbar_try(&sm.kv_full[i], parity) && global_ns() - t0 < kWaitLimitNs) {}
+        while (!mbar_try(&sm.kv_full[i + (last & 1) * kStages], last >> 1 & 1) && global_ns() - t0 < kWaitLimitNs) {}
     }
     if (ok && items > 0) ok = mbar_wait(sm, &sm.q_empty, (items - 1) & 1);
     for (int i = 0; !ok && i < 2; ++i) {   // and the last q tiles
@@ -473,56 +528,38 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
 
 // S = Q K^T. The steps' operands lie a constant apart: one addition per step and operand, so that the
 // issuing thread keeps up with the tensor cores (64 cycles a step).
+template <bool kGrouped>
 __device__ __forceinline__ void product_qk(uint32_t d, uint32_t q, uint32_t k, uint32_t form) {
-    const uint64_t a = operand(q, 16), b = operand(k, 16);
+    const uint64_t a = operand(q, 16, kGroupWhole), b = operand(k, 16, kGrouped ? kGroupGrouped : kGroupWhole);
 #pragma unroll
-    for (int i = 0; i < kHeadDim / 16; ++i) {
-        const int off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;
-        mma_ss(d, a + off, b + off, form, i > 0);
-    }
+    for (int i = 0; i < kHeadDim / 16; ++i)
+        mma_ss(d, a + (((i >> 2) * kHalfWhole + (i & 3) * 32) >> 4),
+               b + (((i >> 2) * (kGrouped ? kHalfGrouped : kHalfWhole) + (i & 3) * 32) >> 4), form, i > 0);
 }
 // O += P V over 16 * steps keys, or O = P V.
+template <bool kGrouped>
 __device__ __forceinline__ void product_pv(uint32_t d, uint32_t p, uint32_t v, int steps, bool add) {
-    const uint64_t b = operand(v, kHalfBytes);
+    const uint64_t b = kGrouped ? operand(v, kHalfGrouped, kGroupGrouped) : operand(v, kHalfWhole, kGroupWhole);
+    constexpr int kStep = 2 * (kGrouped ? kGroupGrouped : kGroupWhole) >> 4;
     const uint32_t form = mma_form(kHeadDim, true, false);
     if (steps == kTurnKeys / 16) {
 #pragma unroll
-        for (int i = 0; i < kTurnKeys / 16; ++i) mma_ts(d, p + i * 8, b + i * (16 * 128 >> 4), form, i > 0 || add);
+        for (int i = 0; i < kTurnKeys / 16; ++i) mma_ts(d, p + i * 8, b + i * kStep, form, i > 0 || add);
     } else {
-        for (int i = 0; i < steps; ++i) mma_ts(d, p + i * 8, b + i * (16 * 128 >> 4), form, i > 0 || add);
+        for (int i = 0; i < steps; ++i) mma_ts(d, p + i * 8, b + i * kStep, form, i > 0 || add);
     }
 }
 
-// A stage of the ring and the parity of its present round, two stages further at each step: K tiles
-// have the even places, V tiles the odd ones.
-struct Cursor {
-    int stage;
-    uint32_t parity;
-    __device__ __forceinline__ void next() {
-        stage += 2;
-        if (stage >= kStages) {
-            stage -= kStages;
-            parity ^= 1;
-        }
-    }
-};
-
-// One lane of the warp.
-__device__ __forceinline__ bool elected() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
-}
-__device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }
-
-// The whole warp walks and waits, one lane issues: control flow and operands are the same in all lanes,
-// which the compiler has to see (votes, shuffles) to keep them in uniform registers. With one lane
-// doing everything each step moved its operands there first: 90 cycles a step, 64 of the tensor cores'.
-__device__ void mma_role(const TurnArgs &a, Smem &sm) {
+// The products of one stream. The whole warp walks and waits, one lane issues: control flow and operands
+// are the same in all lanes, which the compiler has to see (votes, shuffles) to keep them in uniform
+// registers; with one lane doing everything a step took 90 cycles to issue. Each stream has a warp, so
+// that one's waits do not stand in the way of the other's products.
+__device__ void mma_role(const TurnArgs &a, Smem &sm, int stream) {
     const uint32_t tmem = uniform(sm.tmem);
+    const uint32_t s_col = tmem + kColS + stream * kColStream, o_col = tmem + kColO + stream * kColStream;
     const bool negate = a.negate != 0;
-    uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-    Cursor at_k = {0, 0}, at_v = {1, 0};
+    uint32_t items = 0, pairs = 0, p_phase = 0;
+    uint32_t base = 0;   // tiles of the runs before: tile n has K at place 2n of the ring's sequence, V at 2n + 1
     bool ok = true;
     auto wait = [&](uint64_t *bar, uint32_t parity) { ok = __all_sync(~0u, mbar_wait(sm, bar, parity)); };
     Walk walk(sm.plan);
@@ -531,58 +568,67 @@ __device__ void mma_role(const TurnArgs &a, Smem &sm) {
         const int tiles = uniform(r.t1 - r.t0), t0 = uniform(r.t0), cached_tiles = uniform(r.cached_tiles);
         const int cached_keys = uniform(r.x.P), own_keys = uniform(r.own_keys);
         const bool narrow = uniform(r.narrow);
-        const int jobs = narrow ? tiles : 2 * tiles;
+        const int by = narrow ? 2 : 1, first = narrow ? stream : 0;
         auto steps_of = [&](int i) {   // of 16 keys, of the run's tile i
             const int t = t0 + i;
             const int left = t < cached_tiles ? cached_keys - t * kTurnKeys : own_keys - (t - cached_tiles) * kTurnKeys;
             return left >= kTurnKeys ? kTurnKeys / 16 : (left + 15) / 16;
         };
-        for (int s = 0; ok && s < (narrow ? 1 : 2); ++s) {
-            wait(&sm.q_full[s], q_phase[s]);
-            q_phase[s] ^= 1;
-        }
-        // O_s += P_s V of job j
-        auto pv = [&](int j) {
-            const int s = j & 1;
-            if (narrow || s == 0) wait(&sm.kv_full[at_v.stage], at_v.parity);
-            if (ok) wait(&sm.p_full[s], p_phase[s]);
+        // A stage goes back to the copies once both streams' products are done with it; a narrow item's
+        // tile has one stream.
+        auto give_back = [&](int stage) {
+            mma_commit(&sm.kv_empty[stage]);
+            if (narrow) mma_commit(&sm.kv_empty[stage]);
+        };
+        const int q = narrow ? 0 : stream;
+        wait(&sm.q_full[q], (q ? pairs : items) & 1);
+        ++items;
+        pairs += !narrow;
+        // O += P V of the run's tile i
+        auto pv = [&](int i) {
+            const uint32_t place = 2 * (base + i) + 1;
+            const int stage = place % kStages;
+            wait(&sm.kv_full[place % (2 * kStages)], place / (2 * kStages) & 1);
+            if (ok) wait(&sm.p_full[stream], p_phase);
             if (!ok) return;
-            p_phase[s] ^= 1;
+            p_phase ^= 1;
             fence_after();
-            const int steps = steps_of(narrow ? j : j >> 1);
+            const int steps = steps_of(i);
             if (elected()) {
-                product_pv(tmem + kColO + s * kColStream, tmem + kColS + s * kColStream,
-                           smem_u32(sm.kv[at_v.stage]), steps, j >= 2);
-                if (narrow || s == 1) mma_commit(&sm.kv_empty[at_v.stage]);
-                if (j + 2 >= jobs) mma_commit(&sm.o_full[s]);
+                if (t0 + i < cached_tiles) product_pv<true>(o_col, s_col, smem_u32(sm.kv[stage]), steps, i > first);
+                else product_pv<false>(o_col, s_col, smem_u32(sm.kv[stage]), steps, i > first);
+                give_back(stage);
+                if (i + by >= tiles) mma_commit(&sm.o_full[stream]);
             }
             __syncwarp();
-            if (narrow || s == 1) at_v.next();
         };
-        for (int j = 0; ok && j < jobs; ++j) {
-            const int s = j & 1;
-            if (j >= 2) pv(j - 2);
-            if (ok && (narrow || s == 0)) wait(&sm.kv_full[at_k.stage], at_k.parity);
+        for (int i = first; ok && i < tiles; i += by) {
+            const uint32_t place = 2 * (base + i);
+            const int stage = place % kStages;
+            wait(&sm.kv_full[place % (2 * kStages)], place / (2 * kStages) & 1);
+            if (ok && i > first) pv(i - by);
             if (!ok) break;
             fence_after();
-            const int steps = steps_of(narrow ? j : j >> 1);
+            const uint32_t form = mma_form(16 * steps_of(i), false, negate);
             if (elected()) {
-                product_qk(tmem + kColS + s * kColStream, smem_u32(sm.q[narrow ? 0 : s]),
-                           smem_u32(sm.kv[at_k.stage]), mma_form(16 * steps, false, negate));
-                mma_commit(&sm.s_full[s]);
-                if (narrow || s == 1) mma_commit(&sm.kv_empty[at_k.stage]);
-                if (j == jobs - 1) mma_commit(&sm.q_empty);
+                if (t0 + i < cached_tiles) product_qk<true>(s_col, smem_u32(sm.q[q]), smem_u32(sm.kv[stage]), form);
+                else product_qk<false>(s_col, smem_u32(sm.q[q]), smem_u32(sm.kv[stage]), form);
+                mma_commit(&sm.s_full[stream]);
+                give_back(stage);
             }
             __syncwarp();
-            if (narrow || s == 1) at_k.next();
         }
-        for (int j = jobs < 2 ? 0 : jobs - 2; ok && j < jobs; ++j) pv(j);
+        if (ok && elected()) mma_commit(&sm.q_empty);
+        __syncwarp();
+        const int jobs = tiles > first ? (tiles - first + by - 1) / by : 0;
+        if (ok && jobs > 0) pv(first + (jobs - 1) * by);
+        base += tiles;
     }
     // Nothing of the tensor cores' is left behind.
-    if (elected()) mma_commit(&sm.drained);
+    if (elected()) mma_commit(&sm.drained[stream]);
     __syncwarp();
     const unsigned long long t0 = global_ns();
-    while (!mbar_try(&sm.drained, 0) && global_ns() - t0 < kWaitLimitNs) {}
+    while (!mbar_try(&sm.drained[stream], 0) && global_ns() - t0 < kWaitLimitNs) {}
 }
 
 // ---- softmax -------------------------------------------------------------------------------
@@ -832,7 +878,8 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
             if (!ok) break;
             softmax_tile(a, r, t, token, mask, s_addr, o_addr, t == t_first, st);
             fence_before();
-            mbar_arrive(&sm.p_full[stream]);
+            __syncwarp();
+            if (row % 32 == 0) mbar_arrive(&sm.p_full[stream]);
         }
         if (ok && t_first < r.t1) wait(&sm.o_full[stream], o_phase);
         // A narrow item: stream 0 takes both streams' results together.
@@ -939,16 +986,17 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&sm.kv_full[i], 1);
-            mbar_init(&sm.kv_empty[i], 1);
+            mbar_init(&sm.kv_full[i + kStages], 1);
+            mbar_init(&sm.kv_empty[i], 2);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&sm.q_full[s], 1);
             mbar_init(&sm.s_full[s], 1);
-            mbar_init(&sm.p_full[s], kTurnRows);
+            mbar_init(&sm.p_full[s], kTurnRows / 32);
             mbar_init(&sm.o_full[s], 1);
+            mbar_init(&sm.drained[s], 1);
         }
-        mbar_init(&sm.q_empty, 1);
-        mbar_init(&sm.drained, 1);
+        mbar_init(&sm.q_empty, 2);
         sm.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -968,7 +1016,7 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
         } else {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
             if (warp == kCopyWarp) copy_role(a, maps, sm, lane);
-            else if (warp == kMmaWarp) mma_role(a, sm);
+            else if (warp < kMmaWarp + 2) mma_role(a, sm, warp - kMmaWarp);
         }
     }
     __syncwarp();
@@ -986,31 +1034,39 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
 int64_t turn_part_floats(int ctas) { return int64_t(2) * ctas * 2 * kTurnRows * (kHeadDim + 2); }
 int64_t turn_counters(int ctas) { return int64_t(2) * ctas; }
 
-bool encode_turn_hot_map(CUtensorMap *map, void *hot_base, int64_t rows, const char **why) {
-    const cuuint64_t dims[3] = {64, static_cast<cuuint64_t>(rows), 2};
-    const cuuint64_t strides[2] = {kRowBytes, 128};
-    const cuuint32_t box[3] = {64, kBoxRows, 1};
-    return encode_bf16_map(map, hot_base, 3, dims, strides, box, why);
+bool encode_turn_hot_maps(CUtensorMap maps[2], void *hot_base, int64_t rows, int bt, const char **why) {
+    // [eight rows][half][row of eight][64 columns]; a block's rows start at a multiple of 16
+    const cuuint64_t dims[4] = {64, 8, 2, static_cast<cuuint64_t>(rows / 8)};
+    const cuuint64_t strides[3] = {kRowBytes, 128, 8 * kRowBytes};
+    const cuuint32_t part[4] = {64, 8, 2, kBoxRows / 8}, block[4] = {64, 8, 2, static_cast<cuuint32_t>(bt / 8)};
+    return encode_bf16_map(&maps[0], hot_base, 4, dims, strides, part, why) &&
+           encode_bf16_map(&maps[1], hot_base, 4, dims, strides, block, why);
 }
 
-cudaError_t launch_turn(TurnArgs a, const CUtensorMap &hot, cudaStream_t st) {
+cudaError_t launch_turn(TurnArgs a, const CUtensorMap hot[2], cudaStream_t st) {
     if (a.total < 1) return cudaSuccess;
     const int G = a.s.Hq / a.s.Hkv;
     Maps maps;
-    maps.hot = hot;
-    const cuuint64_t n = static_cast<cuuint64_t>(a.total);
-    // [token][head][column half][64 columns], the halves outermost
-    const cuuint64_t q_dims[4] = {64, static_cast<cuuint64_t>(a.s.Hq), n, 2};
-    const cuuint64_t q_strides[3] = {kRowBytes, static_cast<cuuint64_t>(a.q_stride) * 2, 128};
-    const cuuint32_t q_box[4] = {64, static_cast<cuuint32_t>(G), static_cast<cuuint32_t>(kTurnRows / G), 1};
-    const cuuint64_t kv_dims[4] = {64, static_cast<cuuint64_t>(a.s.Hkv), n, 2};
-    const cuuint64_t kv_strides[3] = {kRowBytes, static_cast<cuuint64_t>(a.kv_stride) * 2, 128};
-    const cuuint32_t kv_box[4] = {64, 1, kBoxRows, 1};
+    maps.hot = hot[0];
+    maps.hot_block = hot[1];
+    const cuuint64_t n = static_cast<cuuint64_t>(a.total), hkv = static_cast<cuuint64_t>(a.s.Hkv);
+    const cuuint64_t q_step = static_cast<cuuint64_t>(a.q_stride) * 2, kv_step = static_cast<cuuint64_t>(a.kv_stride) * 2;
     const char *why = nullptr;
-    if (!encode_bf16_map(&maps.q, const_cast<uint16_t *>(a.q), 4, q_dims, q_strides, q_box, &why) ||
-        !encode_bf16_map(&maps.k, const_cast<uint16_t *>(a.k_new), 4, kv_dims, kv_strides, kv_box, &why) ||
-        !encode_bf16_map(&maps.v, const_cast<uint16_t *>(a.v_new), 4, kv_dims, kv_strides, kv_box, &why))
-        return cudaErrorInvalidValue;
+    auto encode = [&](CUtensorMap *map, const uint16_t *base, const cuuint64_t (&dims)[4], const cuuint64_t (&strides)[3],
+                      const cuuint32_t (&box)[4]) {
+        return encode_bf16_map(map, const_cast<uint16_t *>(base), 4, dims, strides, box, &why);
+    };
+    // [half][token][head][64 columns], and for whole tiles [head][half][token][64 columns]
+    const cuuint32_t per_tile = static_cast<cuuint32_t>(kTurnRows / G);
+    bool ok = encode(&maps.q, a.q, {64, static_cast<cuuint64_t>(a.s.Hq), n, 2}, {kRowBytes, q_step, 128},
+                     {64, static_cast<cuuint32_t>(G), per_tile, 1});
+    for (int kv = 0; ok && kv < 2; ++kv) {
+        const uint16_t *base = kv ? a.v_new : a.k_new;
+        ok = encode(kv ? &maps.v : &maps.k, base, {64, hkv, n, 2}, {kRowBytes, kv_step, 128}, {64, 1, kBoxRows, 1}) &&
+             encode(kv ? &maps.v_whole : &maps.k_whole, base, {64, n, 2, hkv}, {kv_step, 128, kRowBytes},
+                    {64, kTurnKeys, 2, 1});
+    }
+    if (!ok) return cudaErrorInvalidValue;
     // The scores' sign goes into the product, so that the largest score is the largest scaled one; a
     // scale of 0 (all weights equal) stays a positive one, which masked scores keep apart.
     a.negate = a.scale_log2 < 0.f;

@@ -95,6 +95,23 @@ def test_same_from_run_to_run_and_on_other_streams(cuda_dev, kind):
         assert torch.equal(c.out, first)
 
 
+@pytest.mark.parametrize("kind,hq,hkv,bt", [("tree", 32, 4, 16), ("tree", 32, 8, 64), ("prefill", 32, 8, 64)])
+def test_many_calls_in_a_row(cuda_dev, kind, hq, hkv, bt):
+    """Hundreds of calls queued behind each other, of items that fill one row tile and items that fill
+    two: the same output every time, no wait that runs out."""
+    n = [20, 31, 32, 52, 16, 60, 29, 7, 58, 33] * 2
+    p = [500 + 397 * i for i in range(20)]
+    c = Call(kind, n, p, hq=hq, hkv=hkv, bt=bt, seed=26, q_std=2.0)
+    first = c.run().clone()
+    outs = [torch.empty_like(c.out) for _ in range(8)]
+    for _ in range(40):
+        for o in outs:
+            c.out = o
+            c.run()
+        assert all(torch.equal(o, first) for o in outs)
+    assert c.pool.check_device() == 0
+
+
 def test_prefill_of_one_token_is_the_decode_step(cuda_dev):
     """n = 1 over the same cache: the decode kernel's result, both within their rounding."""
     p = [77, 1, 2000]
