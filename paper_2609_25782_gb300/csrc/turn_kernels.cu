@@ -63,6 +63,7 @@ struct alignas(1024) Smem {
     float other_m[kTurnRows], other_l[kTurnRows];   // narrow items: stream 1's statistics
     uint32_t tmem;
     int32_t abort;
+    int32_t issuing;                 // a stream's products are going out
     int32_t last[2];
 };
 constexpr int kSmemBytes = sizeof(Smem) + 1024;     // and the way to a 1 024-byte boundary
@@ -376,18 +377,20 @@ __device__ __forceinline__ int keys_of(const Run &r, int t) {
 
 // ---- copies ------------------------------------------------------------------------------
 
-// Lane l's row of the pool (below 2^31) for key tile t: K of its keys 16 l and on, where there are any.
-__device__ __forceinline__ int pool_row(const TurnArgs &a, const Run &r, int t, int lane) {
-    const Shape &sh = a.s;
+// Lane l's block of key tile t: that of its keys 16 l and on, where there are any.
+__device__ __forceinline__ int block_id(const TurnArgs &a, const Run &r, int t, int lane) {
     const int pos = t * kTurnKeys + lane * kBoxRows;
     if (t >= r.cached_tiles || lane >= kTurnKeys / kBoxRows || pos >= r.x.P) return 0;
-    const int j = sh.bt == 64 ? pos >> 6 : pos >> 4;
-    int blk = a.tables[static_cast<int64_t>(r.b) * a.max_blocks + j];
+    return a.tables[static_cast<int64_t>(r.b) * a.max_blocks + (a.s.bt == 64 ? pos >> 6 : pos >> 4)];
+}
+// The row of the pool (below 2^31) of those keys' K.
+__device__ __forceinline__ int pool_row(const TurnArgs &a, const Run &r, int t, int blk, int lane) {
+    const Shape &sh = a.s;
     if (blk < 0 || blk >= sh.num_blocks) {
         atomicOr(a.err, kErrBadBlock);
         blk = 0;   // the result is wrong, the access is not
     }
-    return ((blk * sh.L + a.layer) * 2 * sh.Hkv + r.g) * sh.bt + pos - j * sh.bt;
+    return ((blk * sh.L + a.layer) * 2 * sh.Hkv + r.g) * sh.bt + ((t * kTurnKeys + lane * kBoxRows) & (sh.bt - 1));
 }
 
 // The keys past the last full group of 16, by plain loads; rows up to the group's end are cleared: what
@@ -473,7 +476,7 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
     Walk walk(sm.plan);
     Run r;
     while (ok && walk.next(a, sm.plan, r)) {
-        int row = pool_row(a, r, r.t0, lane);
+        int blk = block_id(a, r, r.t0, lane);
         if (items > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.q_empty, (items - 1) & 1));
         if (!ok) break;
         ++items;
@@ -487,11 +490,12 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
         __syncwarp();
         for (int t = r.t0; ok && t < r.t1; ++t) {
             const int keys = keys_of(r, t);
-            int next = 0;   // the next tile's block ids are on their way while this one's copies go out
+            const int row = pool_row(a, r, t, blk, lane);
+            // The next tile's block ids are on their way while this one's copies go out.
+            if (t + 1 < r.t1) blk = block_id(a, r, t + 1, lane);
             for (int kv = 0; kv < 2; ++kv) {
                 if (round > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.kv_empty[stage], (round - 1) & 1));
                 if (!ok) break;
-                if (kv == 0 && t + 1 < r.t1) next = pool_row(a, r, t + 1, lane);
                 uint64_t *full = &sm.kv_full[stage + (round & 1) * kStages];
                 if (t < r.cached_tiles)
                     copy_cached(a, maps, keys, row, kv, sm.kv[stage], full, lane);
@@ -504,7 +508,6 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
                     ++round;
                 }
             }
-            row = next;
         }
     }
     // Every copy lands before the CTA ends, whatever became of the other roles; with all well,
@@ -536,7 +539,7 @@ __device__ __forceinline__ void product_qk(uint32_t d, uint32_t q, uint32_t k, u
         mma_ss(d, a + (((i >> 2) * kHalfWhole + (i & 3) * 32) >> 4),
                b + (((i >> 2) * (kGrouped ? kHalfGrouped : kHalfWhole) + (i & 3) * 32) >> 4), form, i > 0);
 }
-// O += P V over 16 * steps keys, or O = P V.
+// O += P V over 16 * steps keys, or (!add) O = P V.
 template <bool kGrouped>
 __device__ __forceinline__ void product_pv(uint32_t d, uint32_t p, uint32_t v, int steps, bool add) {
     const uint64_t b = kGrouped ? operand(v, kHalfGrouped, kGroupGrouped) : operand(v, kHalfWhole, kGroupWhole);
@@ -584,44 +587,71 @@ __device__ void mma_role(const TurnArgs &a, Smem &sm, int stream) {
         wait(&sm.q_full[q], (q ? pairs : items) & 1);
         ++items;
         pairs += !narrow;
-        // O += P V of the run's tile i
-        auto pv = [&](int i) {
-            const uint32_t place = 2 * (base + i) + 1;
-            const int stage = place % kStages;
-            wait(&sm.kv_full[place % (2 * kStages)], place / (2 * kStages) & 1);
-            if (ok) wait(&sm.p_full[stream], p_phase);
-            if (!ok) return;
-            p_phase ^= 1;
-            fence_after();
-            const int steps = steps_of(i);
-            if (elected()) {
-                if (t0 + i < cached_tiles) product_pv<true>(o_col, s_col, smem_u32(sm.kv[stage]), steps, i > first);
-                else product_pv<false>(o_col, s_col, smem_u32(sm.kv[stage]), steps, i > first);
-                give_back(stage);
-                if (i + by >= tiles) mma_commit(&sm.o_full[stream]);
-            }
-            __syncwarp();
+        // Place of the run's tile i in the ring's sequence: its stage, and the wait for it.
+        auto landed = [&](uint32_t place) {
+            if (ok) wait(&sm.kv_full[place % (2 * kStages)], place / (2 * kStages) & 1);
         };
-        for (int i = first; ok && i < tiles; i += by) {
-            const uint32_t place = 2 * (base + i);
-            const int stage = place % kStages;
-            wait(&sm.kv_full[place % (2 * kStages)], place / (2 * kStages) & 1);
-            if (ok && i > first) pv(i - by);
-            if (!ok) break;
-            fence_after();
-            const uint32_t form = mma_form(16 * steps_of(i), false, negate);
-            if (elected()) {
-                if (t0 + i < cached_tiles) product_qk<true>(s_col, smem_u32(sm.q[q]), smem_u32(sm.kv[stage]), form);
-                else product_qk<false>(s_col, smem_u32(sm.q[q]), smem_u32(sm.kv[stage]), form);
-                mma_commit(&sm.s_full[stream]);
-                give_back(stage);
-            }
-            __syncwarp();
-        }
-        if (ok && elected()) mma_commit(&sm.q_empty);
+        auto weights = [&] {
+            if (ok) wait(&sm.p_full[stream], p_phase);
+            p_phase ^= 1;
+        };
+        auto issue_pv = [&](int i) {   // O += P V of the run's tile i
+            const int stage = (2 * (base + i) + 1) % kStages, steps = steps_of(i);
+            const uint32_t v = smem_u32(sm.kv[stage]);
+            if (t0 + i < cached_tiles) product_pv<true>(o_col, s_col, v, steps, i > first);
+            else product_pv<false>(o_col, s_col, v, steps, i > first);
+            give_back(stage);
+            if (i + by >= tiles) mma_commit(&sm.o_full[stream]);
+        };
+        auto issue_qk = [&](int i) {   // S = Q K^T
+            const int stage = 2 * (base + i) % kStages;
+            const uint32_t k = smem_u32(sm.kv[stage]), form = mma_form(16 * steps_of(i), false, negate);
+            if (t0 + i < cached_tiles) product_qk<true>(s_col, smem_u32(sm.q[q]), k, form);
+            else product_qk<false>(s_col, smem_u32(sm.q[q]), k, form);
+            mma_commit(&sm.s_full[stream]);
+            give_back(stage);
+            if (i + by >= tiles) mma_commit(&sm.q_empty);
+        };
+        if (first >= tiles && elected()) mma_commit(&sm.q_empty);   // no tile for this stream
         __syncwarp();
-        const int jobs = tiles > first ? (tiles - first + by - 1) / by : 0;
-        if (ok && jobs > 0) pv(first + (jobs - 1) * by);
+        // Step i: the products with V of tile i - by, then those with K of tile i, whose scores take the weights' place.
+        for (int i = first; ok && first < tiles && i < tiles + by; i += by) {
+            const bool has_v = i > first, has_k = i < tiles;
+            if (narrow) {
+                // Such an item waits for HBM: V's stage is given back before K is asked for.
+                if (has_v) {
+                    landed(2 * (base + i - by) + 1);
+                    weights();
+                    fence_after();
+                    if (ok && elected()) issue_pv(i - by);
+                    __syncwarp();
+                }
+                if (has_k) {
+                    landed(2 * (base + i));
+                    fence_after();
+                    if (ok && elected()) issue_qk(i);
+                    __syncwarp();
+                }
+            } else {
+                // A pair's waits for its weights; K is there by then. One stream's products go out without
+                // the other's between them: taking turns step by step, both streams' softmax would wait for
+                // both products, and then both products for the softmax.
+                if (has_k) landed(2 * (base + i));
+                if (has_v) {
+                    landed(2 * (base + i - by) + 1);
+                    weights();
+                }
+                fence_after();
+                if (ok && elected()) {
+                    // (Order is all that this decides: past the limit, which no holder needs, they mix.)
+                    for (int n = 0; n < 1 << 16 && atomicCAS_block(&sm.issuing, 0, 1) != 0; ++n) {}
+                    if (has_v) issue_pv(i - by);
+                    if (has_k) issue_qk(i);
+                    atomicExch_block(&sm.issuing, 0);
+                }
+                __syncwarp();
+            }
+        }
         base += tiles;
     }
     // Nothing of the tensor cores' is left behind.
@@ -716,6 +746,14 @@ __device__ __forceinline__ void hide(uint32_t (&x)[32], uint32_t sees) {
         if (!(sees >> i & 1)) x[i] = 0xFF800000u;
 }
 
+// What this warp has put into tensor memory is there, for the products.
+__device__ __forceinline__ void weights_there(uint64_t *bar) {
+    tmem_stored();
+    fence_before();
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) mbar_arrive(bar);
+}
+
 // A key tile's weights of this thread's row: S from tensor memory, P back over it (16 columns
 // of P for 32 of S, so a chunk's weights never reach scores that are still to be read).
 __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, int t, int token, uint64_t mask,
@@ -776,7 +814,6 @@ __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, in
     }
     const float2 y = halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
     st.l += y.x + y.y;
-    tmem_stored();
 }
 
 // 32 values of an output row from column d0.
@@ -877,9 +914,7 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
             wait(&sm.s_full[stream], s_phase);
             if (!ok) break;
             softmax_tile(a, r, t, token, mask, s_addr, o_addr, t == t_first, st);
-            fence_before();
-            __syncwarp();
-            if (row % 32 == 0) mbar_arrive(&sm.p_full[stream]);
+            weights_there(&sm.p_full[stream]);
         }
         if (ok && t_first < r.t1) wait(&sm.o_full[stream], o_phase);
         // A narrow item: stream 0 takes both streams' results together.
@@ -998,6 +1033,7 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
         }
         mbar_init(&sm.q_empty, 2);
         sm.abort = 0;
+        sm.issuing = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMmaWarp) {
