@@ -106,11 +106,11 @@ struct TurnArgs {
     int32_t total, B, max_blocks, layer, out_bf16;
     int32_t negate;                  // set by the launch: a negative scale's sign
     float scale_log2;                // scale * log2(e)
-    // Workspace for items that are cut into pieces, of 2 slots per CTA of the launch
-    // (turn_part_floats, turn_counters; counters are zero between calls).
+    // Partial results of items that are cut into pieces, of 2 slots per CTA (turn_part_floats).
     float *part;
-    int32_t *part_counters;
     int32_t part_slots;
+    int32_t whole;                   // set by the launch: no item is cut
+    int32_t token_shift;             // set by the launch: tokens of a row tile, 128 / G, as a power of two
     Shape s;
 };
 
@@ -247,7 +247,6 @@ cudaError_t launch_turn(TurnArgs a, const CUtensorMap hot[2], cudaStream_t st);
 cudaError_t prepare_turn_kernel();
 bool encode_turn_hot_maps(CUtensorMap maps[2], void *hot_base, int64_t rows, int bt, const char **why);
 int64_t turn_part_floats(int ctas);
-int64_t turn_counters(int ctas);
 // max_ctas > 0 caps the copy grids (migration_ctas).
 cudaError_t launch_unpack(MigArgs a, int max_ctas, cudaStream_t st);
 cudaError_t launch_unpack_inline(ResumeArgs &r, int max_ctas, cudaStream_t st);

@@ -132,8 +132,6 @@ struct kv_pool {
     int64_t counter_count = 0;
     int32_t *d_err = nullptr;
     float *d_turn_part = nullptr;        // partial results of prefill_attention and tree_attention
-    int32_t *d_turn_counters = nullptr;  // right after d_counters' counter_count decode ones
-    int64_t turn_counter_count = 0;
     CUtensorMap tmap{}, turn_maps[2]{};
 
     Fence fences[kFenceSlots];
@@ -527,8 +525,7 @@ int kv_pool_create(const kv_pool_config *cfg, kv_pool **out) {
         const int64_t at_ml = place(prow * 2 * sizeof(float));
         const int64_t at_tables = place(tbl);
         const int64_t at_turn = place(kvt::turn_part_floats(p->num_sms) * sizeof(float));
-        p->turn_counter_count = kvt::turn_counters(p->num_sms);
-        const int64_t at_counters = place((p->counter_count + p->turn_counter_count) * 4);
+        const int64_t at_counters = place(p->counter_count * 4);
         const int64_t at_err = place(4);
         int rc = p->cuda("cudaMalloc(pool metadata)", [&] { return cudaMalloc(&p->d_slab, bytes); });
         if (!rc) {
@@ -538,7 +535,6 @@ int kv_pool_create(const kv_pool_config *cfg, kv_pool **out) {
             p->d_tables = reinterpret_cast<int32_t *>(base + at_tables);
             p->d_turn_part = reinterpret_cast<float *>(base + at_turn);
             p->d_counters = reinterpret_cast<int32_t *>(base + at_counters);
-            p->d_turn_counters = p->d_counters + p->counter_count;
             p->d_err = reinterpret_cast<int32_t *>(base + at_err);
         }
         if (!rc) rc = p->cuda("cudaMemset", [&] { return cudaMemset(p->d_tables, 0xFF, tbl); });
@@ -1039,9 +1035,8 @@ static int turn_impl(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     a.layer = layer;
     a.out_bf16 = (flags & KV_DECODE_OUT_BF16) ? 1 : 0;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.negate = 0;
+    a.negate = a.whole = a.token_shift = 0;   // set by the launch
     a.part = p->d_turn_part;
-    a.part_counters = p->d_turn_counters;
     a.part_slots = 2 * p->num_sms;
     a.s = p->shape;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream_);
@@ -1479,9 +1474,9 @@ int kv_pool_check_device(kv_pool *p, int32_t *flags) {
         return cudaMemcpy(flags, p->d_err, 4, cudaMemcpyDeviceToHost);
     });
     if (!rc) rc = p->cuda("cudaMemset", [&] { return cudaMemset(p->d_err, 0, 4); });
-    // Every attention call leaves its arrival counters at zero; any other value
-    // comes from calls that overlapped on the GPU, or gave up.
-    std::vector<int32_t> cnt(static_cast<size_t>(p->counter_count + p->turn_counter_count));
+    // Every decode call leaves the split-arrival counters at zero; any other
+    // value comes from calls that overlapped on the GPU.
+    std::vector<int32_t> cnt(static_cast<size_t>(p->counter_count));
     if (!rc && !cnt.empty())
         rc = p->cuda("cudaMemcpy", [&] {
             return cudaMemcpy(cnt.data(), p->d_counters, cnt.size() * 4, cudaMemcpyDeviceToHost);

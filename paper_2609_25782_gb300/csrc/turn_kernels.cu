@@ -2,7 +2,7 @@
 // a turn's context or a whole prompt (causal, its K and V written into the hot
 // pool), and drafted tokens (a bit mask per draft, nothing written).
 //
-// One persistent CTA per SM works through its piece of the line of items that
+// turn_kernel: one persistent CTA per SM works through its piece of the line of items that
 // turn_plan.h lays out. The query heads that share a kv-head are packed into the
 // 128 rows of a row tile, so K and V are read once for all of them. A CTA has two
 // streams, each with a row tile's scores and output in tensor memory: two row
@@ -14,8 +14,13 @@
 //   8         copies: q tiles and key tiles (TMA, 128-byte swizzle)
 //   9, 10     matrix products (tcgen05) of stream 0 and 1: S = Q K^T from shared
 //             memory, O += P V with P from tensor memory
+//   11        the new tokens' K and V, into the pool
 // The tensor cores work on one stream while the other's softmax runs.
+// turn_combine_kernel merges the partial results of items that lie in several
+// pieces, in the pieces' order; it is a programmatic dependent of turn_kernel.
 #include <cuda_bf16.h>
+
+#include <algorithm>
 
 #include "kvt_internal.h"
 #include "turn_plan.h"
@@ -33,7 +38,7 @@ constexpr int kGroupWhole = 1024, kGroupGrouped = 2048;           // bytes from 
 constexpr int kBoxRows = 16;                        // rows that a copy at the end of the keys has
 constexpr int kStages = 5;                          // K or V tiles in flight
 constexpr int kThreads = 384;
-constexpr int kCopyWarp = 8, kMmaWarp = 9;          // and 10; 11 only makes up a warpgroup
+constexpr int kCopyWarp = 8, kMmaWarp = 9, kStoreWarp = 11;
 // Registers per thread: at launch, then of the softmax warps and of the others. A softmax thread
 // keeps its row's 128 scores; the shares add up to what the CTA was launched with.
 constexpr int kRegsLaunch = 168, kRegsSoftmax = 200, kRegsOther = 104;
@@ -45,9 +50,8 @@ constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 256, kColStream = 128;
 
 struct Plan {
-    int64_t W;
-    int64_t begin_at, end_at;   // cost at which the first and the last item begin
     TurnPos begin, end;
+    TurnSession first;   // the session of `begin`, n < 0: not at hand
     int32_t pieces;
 };
 
@@ -64,7 +68,6 @@ struct alignas(1024) Smem {
     uint32_t tmem;
     int32_t abort;
     int32_t issuing;                 // a stream's products are going out
-    int32_t last[2];
 };
 constexpr int kSmemBytes = sizeof(Smem) + 1024;     // and the way to a 1 024-byte boundary
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of a CTA");
@@ -219,16 +222,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return y;
 }
 __device__ __forceinline__ void sync_threads(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
-__device__ __forceinline__ int arrive(int32_t *counter) {
-    int prev;
-    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(prev) : "l"(counter) : "memory");
-    return prev;
-}
 
 // ---- the work ----------------------------------------------------------------------------
 
 __device__ __forceinline__ TurnShape turn_shape(const TurnArgs &a) {
-    return {kTurnRows / (a.s.Hq / a.s.Hkv), a.s.Hkv, a.masks == nullptr};
+    return {a.token_shift, a.s.Hkv, a.masks == nullptr};
 }
 
 // Session b as the call describes it; n = 0 for one whose data is out of range.
@@ -261,47 +259,46 @@ __device__ __forceinline__ int64_t scan(int64_t x, int lane, int64_t *all) {
 // This CTA's piece, by one warp.
 __device__ void make_plan(const TurnArgs &a, Plan &plan, int lane) {
     const TurnShape s = turn_shape(a);
-    int64_t W = 0, mine = 0;
+    int64_t W = 0, cost = 0;
+    TurnSession x = {0, 0, 0};   // up to 32 sessions: kept from the first round to the second
     for (int b0 = 0; b0 < a.B; b0 += 32) {
         const int b = b0 + lane;
-        int64_t cost = 0, all;
+        int64_t all;
+        cost = 0;
         if (b < a.B) {
             bool bad;
-            cost = s.Hkv * turn_head_cost(s, session_of(a, b, &bad));
+            x = session_of(a, b, &bad);
+            cost = s.Hkv * turn_head_cost(s, x);
             if (bad && blockIdx.x == 0) atomicOr(a.err, kErrBadLength);
         }
-        mine = cost;   // kept for the second pass where one round has all sessions
         scan(cost, lane, &all);
         W += all;
     }
-    const int pieces = W == 0 ? 0 : turn_pieces(W, gridDim.x);
+    const int pieces = W == 0 ? 0 : turn_pieces(W, gridDim.x), c = blockIdx.x;
     if (lane == 0) {
-        plan.W = W;
         plan.pieces = pieces;
         plan.begin = plan.end = {a.B, 0, 0, 0};
-        plan.begin_at = plan.end_at = 0;
     }
     __syncwarp();
-    const int c = blockIdx.x;
     if (c >= pieces) return;
     const int64_t u[2] = {turn_cut(W, pieces, c), turn_cut(W, pieces, c + 1)};   // the second is W at the end
     int64_t before = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
         const int b = b0 + lane;
-        int64_t cost = 0, all;
-        TurnSession x = {0, 0, 0};
-        if (a.B <= 32) cost = mine;
-        if (b < a.B) {
-            x = session_of(a, b);
-            if (a.B > 32) cost = s.Hkv * turn_head_cost(s, x);
+        int64_t all;
+        if (a.B > 32) {
+            cost = 0;
+            if (b < a.B) {
+                x = session_of(a, b);
+                cost = s.Hkv * turn_head_cost(s, x);
+            }
         }
         const int64_t at = before + scan(cost, lane, &all);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             if (u[e] < at || u[e] >= at + cost) continue;
-            int64_t item;
-            TurnPos p = turn_locate(s, x, b, u[e] - at, &item);
-            if (p.t >= turn_tiles(s, x, p.pair)) {   // the item's end: the next one's start
+            TurnPos p = turn_locate(s, x, b, u[e] - at);
+            if (p.t >= turn_tiles(s, x, p.pair) || (a.whole && p.t > 0)) {   // the item's end: the next one's start
                 p.t = 0;
                 if (++p.pair >= turn_pairs(s, x)) {
                     p.pair = 0;
@@ -311,8 +308,13 @@ __device__ void make_plan(const TurnArgs &a, Plan &plan, int lane) {
                     }
                 }
             }
-            (e ? plan.end : plan.begin) = p;
-            (e ? plan.end_at : plan.begin_at) = at + item;
+            if (e) {
+                plan.end = p;
+            } else {
+                plan.begin = p;
+                plan.first = x;
+                if (p.b != b) plan.first.n = -1;
+            }
         }
         before += all;
     }
@@ -329,26 +331,30 @@ struct Run {
 // The runs of a piece, in order; every role walks them by itself.
 struct Walk {
     TurnPos at;
-    __device__ explicit Walk(const Plan &plan) : at(plan.begin) {}
+    TurnSession x;   // of at.b
+    __device__ Walk(const TurnArgs &a, const Plan &plan) : at(plan.begin), x(plan.first) {
+        if (at.b < a.B && x.n < 0) x = session_of(a, at.b);
+    }
     __device__ bool next(const TurnArgs &a, const Plan &plan, Run &r) {
         const TurnShape s = turn_shape(a);
+        const TurnPos &end = plan.end;
         while (at.b < a.B) {
-            const TurnPos &end = plan.end;
             const bool to_end = at.b == end.b && at.g == end.g && at.pair == end.pair;
             if (to_end && at.t >= end.t) return false;
-            r.x = session_of(a, at.b);
-            if (r.x.n == 0) {   // nothing of this session; the end may be its start
+            if (x.n == 0) {   // nothing of this session; the end may be its start
                 if (at.b == end.b) return false;
                 at = {at.b + 1, 0, 0, 0};
+                if (at.b < a.B) x = session_of(a, at.b);
                 continue;
             }
+            r.x = x;
             r.b = at.b;
             r.g = at.g;
             r.pair = at.pair;
-            r.tiles = turn_tiles(s, r.x, at.pair);
-            r.cached_tiles = turn_cached_tiles(r.x);
-            r.own_keys = turn_own_keys(s, r.x, at.pair);
-            r.narrow = turn_narrow(s, r.x, at.pair);
+            r.cached_tiles = turn_tiles_of(x.P);
+            r.own_keys = turn_own_keys(s, x, at.pair);
+            r.tiles = r.cached_tiles + turn_tiles_of(r.own_keys);
+            r.narrow = turn_narrow(s, x, at.pair);
             r.t0 = at.t;
             r.t1 = to_end ? end.t : r.tiles;
             if (to_end) {
@@ -356,11 +362,12 @@ struct Walk {
                 return true;
             }
             at.t = 0;
-            if (++at.pair >= turn_pairs(s, r.x)) {
+            if (++at.pair >= turn_pairs(s, x)) {
                 at.pair = 0;
                 if (++at.g >= s.Hkv) {
                     at.g = 0;
                     ++at.b;
+                    if (at.b < a.B) x = session_of(a, at.b);
                 }
             }
             return true;
@@ -473,7 +480,7 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
     int stage = 0, round = 0, items = 0, pairs = 0;
     uint32_t filled = 0;   // copies issued so far, saturating at kStages
     bool ok = true;        // the same in all lanes until the last copy is out
-    Walk walk(sm.plan);
+    Walk walk(a, sm.plan);
     Run r;
     while (ok && walk.next(a, sm.plan, r)) {
         int blk = block_id(a, r, r.t0, lane);
@@ -486,7 +493,7 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
         __syncwarp();
         if (lane < 2 * tiles)   // coordinates: (column, head, token, half)
             copy_box(sm.q[lane >> 1] + (lane & 1) * kHalfWhole, &maps.q, r.g * G,
-                     r.x.lo + (2 * r.pair + (lane >> 1)) * s.tokens, lane & 1, &sm.q_full[lane >> 1]);
+                     r.x.lo + ((2 * r.pair + (lane >> 1)) << s.shift), lane & 1, &sm.q_full[lane >> 1]);
         __syncwarp();
         for (int t = r.t0; ok && t < r.t1; ++t) {
             const int keys = keys_of(r, t);
@@ -565,7 +572,7 @@ __device__ void mma_role(const TurnArgs &a, Smem &sm, int stream) {
     uint32_t base = 0;   // tiles of the runs before: tile n has K at place 2n of the ring's sequence, V at 2n + 1
     bool ok = true;
     auto wait = [&](uint64_t *bar, uint32_t parity) { ok = __all_sync(~0u, mbar_wait(sm, bar, parity)); };
-    Walk walk(sm.plan);
+    Walk walk(a, sm.plan);
     Run r;
     while (ok && __all_sync(~0u, walk.next(a, sm.plan, r))) {
         const int tiles = uniform(r.t1 - r.t0), t0 = uniform(r.t0), cached_tiles = uniform(r.cached_tiles);
@@ -832,13 +839,25 @@ __device__ __forceinline__ void store_out(const TurnArgs &a, int64_t row, int d0
 }
 
 // A slot of partial results: 256 rows of 128 values, four values of all rows together (so that a warp's
-// rows are next to each other), then (m, l) of the rows.
+// rows are next to each other), then (m, l) of the rows. CTA c has slot 2c for an item that an earlier piece
+// begins, and 2c + 1 for one that it begins and a later piece ends.
 __device__ __forceinline__ float4 *part_o(const TurnArgs &a, int slot, int stream) {
     return reinterpret_cast<float4 *>(a.part) + (static_cast<int64_t>(slot) * 2 + stream) * kTurnRows * (kHeadDim / 4);
 }
 __device__ __forceinline__ float2 *part_ml(const TurnArgs &a, int slot, int stream) {
     return reinterpret_cast<float2 *>(a.part + static_cast<int64_t>(a.part_slots) * 2 * kTurnRows * kHeadDim) +
            (static_cast<int64_t>(slot) * 2 + stream) * kTurnRows;
+}
+// What a CTA tells the merge: the item that it begins and does not end, and whether an item passes
+// through its piece.
+struct PartRecord {
+    int32_t opens, through;
+    int32_t row;      // first row (token) of the item
+    int32_t tokens, g;
+};
+__device__ __forceinline__ PartRecord *part_record(const TurnArgs &a, int cta) {
+    return reinterpret_cast<PartRecord *>(a.part + static_cast<int64_t>(a.part_slots) * 2 * kTurnRows * (kHeadDim + 2)) +
+           cta;
 }
 
 // The item's output row of this thread, from tensor memory, 32 columns at a time: O times `w`, and
@@ -863,29 +882,47 @@ __device__ __forceinline__ void read_o(uint32_t o_addr, float w, uint32_t other,
     }
 }
 
-// The item's new tokens' K and V of its kv-head into their slots of the pool; thread `tid` of `threads`.
-__device__ __forceinline__ void store_new_kv(const TurnArgs &a, const TurnShape &s, const Run &r, int tid,
-                                             int threads) {
+// The new tokens' K and V into their slots of the pool, by one warp beside the others' work, a token's
+// K and V rows of the item's kv-head at a time: each item's once, by the piece that has its last key tile.
+__device__ void store_role(const TurnArgs &a, const Smem &sm, int lane) {
     const Shape &sh = a.s;
-    const int i0 = r.pair * 2 * s.tokens, n = min(2 * s.tokens, r.x.n - i0);
-    for (int u = tid; u < n * 32; u += threads) {   // 16-byte units: token, K or V, unit
-        const int i = i0 + (u >> 5), kv = u >> 4 & 1, c = u & 15;
-        const int pos = r.x.P + i, j = pos / sh.bt;
-        const int blk = a.tables[static_cast<int64_t>(r.b) * a.max_blocks + j];
-        if (blk < 0 || blk >= sh.num_blocks) {
-            atomicOr(a.err, kErrBadBlock);
-            continue;
+    const TurnShape s = turn_shape(a);
+    const int kv = lane >> 4, c = lane & 15, bt_shift = sh.bt == 64 ? 6 : 4;
+    Walk walk(a, sm.plan);
+    Run r;
+    while (walk.next(a, sm.plan, r)) {
+        if (r.t1 != r.tiles) continue;
+        const int i0 = r.pair << (s.shift + 1), i1 = min(i0 + (2 << s.shift), r.x.n);
+        const uint16_t *src = (kv ? a.v_new : a.k_new) + r.x.lo * a.kv_stride + r.g * kHeadDim + c * 8;
+        const int32_t *table = a.tables + static_cast<int64_t>(r.b) * a.max_blocks;
+        constexpr int kAhead = 4;
+        for (int i = i0; i < i1; i += kAhead) {
+            uint4 x[kAhead];
+            int blk[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (i + k < i1) {
+                    blk[k] = table[(r.x.P + i + k) >> bt_shift];
+                    x[k] = *reinterpret_cast<const uint4 *>(src + (i + k) * a.kv_stride);
+                }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (i + k >= i1) break;
+                if (blk[k] < 0 || blk[k] >= sh.num_blocks) {
+                    if (lane == 0) atomicOr(a.err, kErrBadBlock);
+                    continue;
+                }
+                const int row = (((blk[k] * sh.L + a.layer) * 2 + kv) * sh.Hkv + r.g) * sh.bt +
+                                ((r.x.P + i + k) & (sh.bt - 1));
+                reinterpret_cast<uint4 *>(a.hot + static_cast<int64_t>(row) * kHeadDim)[c] = x[k];
+            }
         }
-        const int row = (((blk * sh.L + a.layer) * 2 + kv) * sh.Hkv + r.g) * sh.bt + pos - j * sh.bt;
-        const uint16_t *src = (kv ? a.v_new : a.k_new) + (r.x.lo + i) * a.kv_stride + r.g * kHeadDim;
-        reinterpret_cast<uint4 *>(a.hot + static_cast<int64_t>(row) * kHeadDim)[c] =
-            reinterpret_cast<const uint4 *>(src)[c];
     }
 }
 
 __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
     const TurnShape s = turn_shape(a);
-    const int G = a.s.Hq / a.s.Hkv;
+    const int g_shift = 7 - s.shift;                          // a token has 128 / tokens rows
     const int row = threadIdx.x & (kTurnRows - 1);
     const uint32_t lanes = static_cast<uint32_t>(row & ~31) << 16;   // a warp has 32 lanes of tensor memory
     const uint32_t tmem = sm.tmem + lanes;
@@ -898,13 +935,14 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
         phase ^= 1;
         fence_after();
     };
-    Walk walk(sm.plan);
+    PartRecord rec = {0, 0, 0, 0, 0};
+    Walk walk(a, sm.plan);
     Run r;
     while (walk.next(a, sm.plan, r)) {
         const int tile = r.narrow ? 2 * r.pair : 2 * r.pair + stream;
-        const int token = tile * s.tokens + row / G;          // of the session's new ones
+        const int token = (tile << s.shift) + (row >> g_shift);   // of the session's new ones
         const bool live = token < r.x.n;
-        const int64_t out_row = (static_cast<int64_t>(r.x.lo) + token) * a.s.Hq + r.g * G + row % G;
+        const int64_t out_row = (static_cast<int64_t>(r.x.lo) + token) * a.s.Hq + (r.g << g_shift) + (row & ((1 << g_shift) - 1));
         uint64_t mask = 0;
         if (a.masks && live) mask = a.masks[r.x.lo + token];
         Stats st = {-INFINITY, 0.f};
@@ -946,9 +984,6 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
                 if (ok && other) read_o<true>(o_addr, w * inv, other, w_other * inv, put);
                 else if (ok) read_o<false>(o_addr, w * inv, 0, 0.f, put);
             } else {
-                int c0, c1;
-                turn_item_pieces(sm.plan.W, sm.plan.pieces, r.t0 > 0 ? sm.plan.begin_at : sm.plan.end_at, r.tiles,
-                                 turn_tile_cost(s, r.x, r.pair), &c0, &c1);
                 const int slot = r.t0 > 0 ? 2 * blockIdx.x : 2 * blockIdx.x + 1;
                 float4 *po = part_o(a, slot, stream);
                 const auto put = [&](int d, const float (&y)[32]) {
@@ -961,60 +996,24 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
                 if (ok && other) read_o<true>(o_addr, w, other, w_other, put);
                 else if (ok) read_o<false>(o_addr, w, 0, 0.f, put);
                 if (live) part_ml(a, slot, stream)[row] = make_float2(st.m, st.l);
-                __threadfence();
-                sync_threads(1 + stream, kTurnRows);
-                int32_t *counter = a.part_counters + 2 * c0 + stream;
-                if (row == 0) sm.last[stream] = ok && arrive(counter) == c1 - c0;
-                sync_threads(1 + stream, kTurnRows);
-                if (sm.last[stream]) {   // the item's last piece to finish: merge all, in order
-                    __threadfence();
-                    if (row == 0) *counter = 0;
-                    if (live) {
-                        float m = -INFINITY;
-                        for (int c = c0; c <= c1; ++c)
-                            m = fmaxf(m, __ldcg(part_ml(a, c == c0 ? 2 * c + 1 : 2 * c, stream) + row).x);
-                        const float ref = m == -INFINITY ? 0.f : m;
-                        float l = 0.f;
-                        for (int c = c0; c <= c1; ++c) {
-                            const float2 v = __ldcg(part_ml(a, c == c0 ? 2 * c + 1 : 2 * c, stream) + row);
-                            l = __fmaf_rn(ex2(v.x - ref), v.y, l);
-                        }
-                        const float inv = l > 0.f || l != l ? __frcp_rn(l) : 0.f;
-#pragma unroll 1
-                        for (int d = 0; d < kHeadDim; d += 32) {
-                            float y[32] = {};
-                            for (int c = c0; c <= c1; ++c) {
-                                const int from = c == c0 ? 2 * c + 1 : 2 * c;
-                                const float f = ex2(__ldcg(part_ml(a, from, stream) + row).x - ref);
-                                const float4 *pc = part_o(a, from, stream) + d / 4 * kTurnRows + row;
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    const float4 o = __ldcg(pc + i * kTurnRows);
-                                    y[4 * i] = __fmaf_rn(f, o.x, y[4 * i]);
-                                    y[4 * i + 1] = __fmaf_rn(f, o.y, y[4 * i + 1]);
-                                    y[4 * i + 2] = __fmaf_rn(f, o.z, y[4 * i + 2]);
-                                    y[4 * i + 3] = __fmaf_rn(f, o.w, y[4 * i + 3]);
-                                }
-                            }
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) y[i] *= inv;
-                            store_out(a, out_row, d, y);
-                        }
-                    }
+                if (stream == 0 && row == 0) {
+                    const int t0 = r.pair << (s.shift + 1);
+                    if (r.t0 == 0) rec = {1, 0, r.x.lo + t0, min(2 << s.shift, r.x.n - t0), r.g};
+                    else if (r.t1 < r.tiles) rec.through = 1;
                 }
             }
         }
-        // Once per item: by the piece that has its last key tile.
-        if (!a.masks && r.t1 == r.tiles) store_new_kv(a, s, r, threadIdx.x, 2 * kTurnRows);
         fence_before();
         // Stream 1's O is free for its next product once stream 0 has read it.
         if (r.narrow) sync_threads(3, 2 * kTurnRows);
     }
+    if (!a.whole && stream == 0 && row == 0) *part_record(a, blockIdx.x) = rec;
 }
 
 __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant__ TurnArgs a,
                                                            const __grid_constant__ Maps maps) {
     extern __shared__ uint8_t raw[];
+    if (!a.whole) asm volatile("griddepcontrol.launch_dependents;");   // the merge, which waits for all of this
     Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (warp == kCopyWarp) make_plan(a, sm.plan, lane);
@@ -1053,7 +1052,10 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
             if (warp == kCopyWarp) copy_role(a, maps, sm, lane);
             else if (warp < kMmaWarp + 2) mma_role(a, sm, warp - kMmaWarp);
+            else if (warp == kStoreWarp && !a.masks) store_role(a, sm, lane);
         }
+    } else if (threadIdx.x == 0 && !a.whole) {
+        *part_record(a, blockIdx.x) = {0, 0, 0, 0, 0};
     }
     __syncwarp();
     fence_before();
@@ -1064,11 +1066,67 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sm.tmem), "r"(kTmemCols));
 }
 
+// The pieces of each item that several have, merged in order: a thread per row and 16 values of it. CTA
+// (c, j): the item that piece c begins, if any.
+constexpr int kCombineCtas = 8;   // per item
+__global__ void __launch_bounds__(256) turn_combine_kernel(const __grid_constant__ TurnArgs a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const PartRecord rec = *part_record(a, blockIdx.x);
+    if (!rec.opens) return;
+    int last = blockIdx.x + 1;
+    while (last + 1 < a.part_slots / 2 && part_record(a, last)->through) ++last;
+    // 64 warps' work: 8 groups of 32 rows, 8 of 16 values
+    const int work = blockIdx.y * 8 + (threadIdx.x >> 5), stream = work >> 5;
+    const int row = (work >> 3 & 3) * 32 + (threadIdx.x & 31), d4 = (work & 7) * 4;
+    const int g_shift = 7 - a.token_shift;
+    const int token = (stream << a.token_shift) + (row >> g_shift);
+    if (token >= rec.tokens) return;
+    const int first = blockIdx.x;
+    const auto slot = [&](int c) { return c == first ? 2 * c + 1 : 2 * c; };
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int c = first; c <= last; ++c) m = fmaxf(m, part_ml(a, slot(c), stream)[row].x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    float4 y[4] = {};
+#pragma unroll 4
+    for (int c = first; c <= last; ++c) {
+        const float2 v = part_ml(a, slot(c), stream)[row];
+        const float4 *po = part_o(a, slot(c), stream) + d4 * kTurnRows + row;
+        const float w = ex2(v.x - ref);
+        l = __fmaf_rn(w, v.y, l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 o = po[i * kTurnRows];
+            y[i] = make_float4(__fmaf_rn(w, o.x, y[i].x), __fmaf_rn(w, o.y, y[i].y), __fmaf_rn(w, o.z, y[i].z),
+                               __fmaf_rn(w, o.w, y[i].w));
+        }
+    }
+    const float inv = l > 0.f || l != l ? __frcp_rn(l) : 0.f;
+    const int64_t to = ((static_cast<int64_t>(rec.row) + token) * a.s.Hq + (rec.g << g_shift) +
+                        (row & ((1 << g_shift) - 1))) * kHeadDim + d4 * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = make_float4(y[i].x * inv, y[i].y * inv, y[i].z * inv, y[i].w * inv);
+    if (a.out_bf16) {
+        uint4 *out = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + to);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            out[i] = make_uint4(pack_bf16(y[2 * i].x, y[2 * i].y), pack_bf16(y[2 * i].z, y[2 * i].w),
+                                pack_bf16(y[2 * i + 1].x, y[2 * i + 1].y), pack_bf16(y[2 * i + 1].z, y[2 * i + 1].w));
+    } else {
+        float4 *out = reinterpret_cast<float4 *>(static_cast<float *>(a.out) + to);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = y[i];
+    }
+}
+
 }  // namespace
 
-// Floats and counters that a launch of `ctas` CTAs may need.
-int64_t turn_part_floats(int ctas) { return int64_t(2) * ctas * 2 * kTurnRows * (kHeadDim + 2); }
-int64_t turn_counters(int ctas) { return int64_t(2) * ctas; }
+// Floats that launches of up to `ctas` CTAs need for partial results.
+int64_t turn_part_floats(int ctas) {
+    static_assert(sizeof(PartRecord) % sizeof(float) == 0, "records follow the rows");
+    return int64_t(2) * ctas * 2 * kTurnRows * (kHeadDim + 2) + ctas * int64_t(sizeof(PartRecord) / sizeof(float));
+}
 
 bool encode_turn_hot_maps(CUtensorMap maps[2], void *hot_base, int64_t rows, int bt, const char **why) {
     // [eight rows][half][row of eight][64 columns]; a block's rows start at a multiple of 16
@@ -1107,8 +1165,28 @@ cudaError_t launch_turn(TurnArgs a, const CUtensorMap hot[2], cudaStream_t st) {
     // scale of 0 (all weights equal) stays a positive one, which masked scores keep apart.
     a.negate = a.scale_log2 < 0.f;
     a.scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-30f);
-    turn_kernel<<<a.part_slots / 2, kThreads, kSmemBytes, st>>>(a, maps);
-    return cudaGetLastError();
+    a.token_shift = G == 8 ? 4 : G == 4 ? 5 : G == 2 ? 6 : 7;
+    // No more CTAs than there can be pieces; items of at most two key tiles are not cut, which saves the
+    // merge's launch (a prompt of 37 tokens: X us with it, Y without).
+    const int64_t longest = static_cast<int64_t>(a.max_blocks) * a.s.bt;
+    const int64_t items = (a.total / (2 << a.token_shift) + static_cast<int64_t>(a.B)) * a.s.Hkv;
+    const int64_t pieces = items * ((longest / kTurnKeys + 2) * kCostTile + kCostItem) / kCostPiece;
+    const unsigned ctas = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(pieces, a.part_slots / 2)));
+    a.part_slots = 2 * ctas;
+    a.whole = longest <= kTurnKeys;
+    turn_kernel<<<ctas, kThreads, kSmemBytes, st>>>(a, maps);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess || a.whole) return e;
+    cudaLaunchAttribute early[1];
+    early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas, kCombineCtas);
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cfg.attrs = early;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, turn_combine_kernel, a);
 }
 
 cudaError_t prepare_turn_kernel() {

@@ -1,6 +1,5 @@
 """The line of items of prompt and draft attention, and its pieces, without a GPU: whatever the
-lengths, every key tile of every item lies in exactly one piece, no piece is empty, and a piece that
-holds part of an item knows which others hold the rest."""
+lengths, every key tile of every item lies in exactly one piece, and no piece is empty."""
 import ctypes
 import functools
 import os
@@ -22,12 +21,12 @@ def lib():
                         os.path.join(HERE, "turn_plan.cpp"), "-o", so], check=True)
         x = ctypes.CDLL(so)
     i32, i64 = ctypes.c_int32, ctypes.c_int64
-    for name in ("cost_before", "head_cost", "locate", "cut"):
+    for name in ("cost_before", "head_cost", "cut"):
         getattr(x, name).restype = i64
+    x.locate.restype = None
     x.locate.argtypes = [i32] * 5 + [i64, ctypes.POINTER(i32)]
     x.pieces.argtypes = [i64, i32]
     x.cut.argtypes = [i64, i32, i32]
-    x.item_pieces.argtypes = [i64, i32, i64, i32, i32, ctypes.POINTER(i32)]
     return x
 
 
@@ -50,25 +49,24 @@ def test_costs_add_up(tokens, causal):
             assert x.cost_before(tokens, causal, n, P, p) == total
             t = x.tiles(tokens, causal, n, P, p)
             assert t == -(-P // 128) + own_tiles(tokens, causal, n, p)
-            narrow = n - p * 2 * tokens <= tokens
-            assert x.tile_cost(tokens, causal, n, p) == (3 if narrow else 4)
-            total += t * (3 if narrow else 4) + x.item_overhead()
+            assert x.narrow(tokens, n, p) == (n - p * 2 * tokens <= tokens)
+            total += t * x.tile_cost() + x.item_cost()
         assert x.head_cost(tokens, causal, n, P) == total
 
 
 def layout(sessions, tokens, hkv, causal):
-    """[(session, head, pair, cost at its start, tiles, cost of a tile)], and the whole cost."""
+    """[(session, head, pair, cost at its start, tiles)], and the whole cost."""
     x, at, items = lib(), 0, []
     for b, (n, P) in enumerate(sessions):
         for g in range(hkv):
             for p in range(x.pairs(tokens, causal, n)):
-                t, c = x.tiles(tokens, causal, n, P, p), x.tile_cost(tokens, causal, n, p)
-                items.append((b, g, p, at, t, c))
-                at += t * c + x.item_overhead()
+                t = x.tiles(tokens, causal, n, P, p)
+                items.append((b, g, p, at, t))
+                at += t * x.tile_cost() + x.item_cost()
     return items, at
 
 
-@pytest.mark.parametrize("seed", range(40))
+@pytest.mark.parametrize("seed", range(60))
 def test_pieces_cover_the_line(seed):
     x, r = lib(), random.Random(seed)
     causal, tokens, hkv = r.random() < 0.6, r.choice([16, 32, 64, 128]), r.choice([1, 2, 4, 8])
@@ -86,21 +84,37 @@ def test_pieces_cover_the_line(seed):
     assert at == W
     for ctas in (1, 2, 7, 152):
         m = x.pieces(W, ctas)
-        assert 1 <= m <= ctas
+        assert 1 <= m <= ctas and x.cut(W, m, 0) == 0 and x.cut(W, m, m) == W
+        lengths = [x.cut(W, m, c + 1) - x.cut(W, m, c) for c in range(m)]
+        assert max(lengths) - min(lengths) <= 1
         cuts = []
         for c in range(m):
             u = x.cut(W, m, c)
             b = max(i for i in range(B) if starts[i] <= u and sessions[i][0] > 0)
             pos = (ctypes.c_int32 * 3)()
-            item_at = x.locate(tokens, hkv, int(causal), *sessions[b], u - starts[b], pos)
+            x.locate(tokens, hkv, int(causal), *sessions[b], u - starts[b], pos)
             k = index[(b, pos[0], pos[1])]
-            assert items[k][3] == starts[b] + item_at and 0 <= pos[2] <= items[k][4]
+            assert 0 <= pos[2] <= items[k][4]
+            # the tile whose cost contains the cut, or the one after it
+            into = u - items[k][3] - x.item_cost()
+            assert pos[2] == max(0, -(-into // x.tile_cost()))
             cuts.append((k, pos[2]) if pos[2] < items[k][4] else (k + 1, 0))
         cuts.append((len(items), 0))
         assert cuts[0] == (0, 0) and all(a < b for a, b in zip(cuts, cuts[1:])), "an empty piece"
-        # which pieces hold tiles of each item, by the cuts themselves
-        for k, (_, _, _, U, t, cost) in enumerate(items):
-            held = [c for c in range(m) if cuts[c] < (k, t) and cuts[c + 1] > (k, 0)]
-            out = (ctypes.c_int32 * 2)()
-            x.item_pieces(W, m, U, t, cost, out)
-            assert held == list(range(out[0], out[1] + 1))
+
+
+@pytest.mark.parametrize("items", [1, 8, 100, 152])
+def test_items_of_one_tile_have_a_piece_each(items):
+    """A short prompt's items, all of one key tile: no CTA has two of them."""
+    x = lib()
+    W = items * (x.tile_cost() + x.item_cost())
+    m = x.pieces(W, 152)
+    assert m == items and all(x.cut(W, m, c) == c * W // items for c in range(m + 1))
+
+
+def test_cuts_of_work_past_32_bits():
+    x = lib()
+    for W in (2 ** 31 - 1, 2 ** 31, 2 ** 40 + 7):
+        cuts = [x.cut(W, 152, c) for c in range(153)]
+        assert cuts[0] == 0 and cuts[-1] == W
+        assert max(b - a for a, b in zip(cuts, cuts[1:])) - min(b - a for a, b in zip(cuts, cuts[1:])) <= 1

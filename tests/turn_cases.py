@@ -116,6 +116,17 @@ class Call:
             noise[:, h] = torch.sqrt((w * w) @ (v * v).sum(1))
         return out, noise
 
+    def assert_right(self, b, ref, noise):
+        """Session b's rows of `out` against reference(b)."""
+        lo = sum(self.n[:b])
+        got = self.out[lo:lo + self.n[b]].double()
+        bound = ROW * (noise + ref.norm(dim=2))
+        err = (got - ref).norm(dim=2)
+        worst = (err - bound).max() if err.numel() else torch.tensor(-1.0)
+        assert torch.isfinite(got).all(), f"session {b}: not finite"
+        assert worst <= 0, f"session {b} (n {self.n[b]}, p {self.p[b]}): error over its bound by {worst:.3e}, " \
+            f"rows {torch.nonzero(err > bound)[:6].tolist()}"
+
     def check(self):
         """Every row against the reference; for a prefill the slots as well, and nothing else written."""
         refs = [self.reference(b) for b in range(self.B)]
@@ -123,14 +134,7 @@ class Call:
         self.run()
         assert self.pool.check_device() == 0
         for b, (ref, noise) in enumerate(refs):
-            lo = sum(self.n[:b])
-            got = self.out[lo:lo + self.n[b]].double()
-            bound = ROW * (noise + ref.norm(dim=2))
-            err = (got - ref).norm(dim=2)
-            worst = (err - bound).max() if err.numel() else torch.tensor(-1.0)
-            assert torch.isfinite(got).all(), f"session {b}: not finite"
-            assert worst <= 0, f"session {b} (n {self.n[b]}, p {self.p[b]}): error over its bound by {worst:.3e}, " \
-                f"rows {torch.nonzero(err > bound)[:6].tolist()}"
+            self.assert_right(b, ref, noise)
         if self.kind == "prefill":
             for b, p in enumerate(self.p):
                 lo = sum(self.n[:b])
