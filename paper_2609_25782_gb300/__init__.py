@@ -29,6 +29,8 @@ class Pool:
         self.L, self.Hq, self.Hkv, self.D, self.bt = (num_layers, num_q_heads, num_kv_heads,
                                                       head_dim, block_tokens)
         self.num_hot_blocks = num_hot_blocks
+        self._bf16 = torch.bfloat16
+        self._out_flags = {torch.float32: 0, torch.bfloat16: kvtier.KV_DECODE_OUT_BF16}
         probe = kvtier.make_config(num_layers=num_layers, num_q_heads=num_q_heads,
                                    num_kv_heads=num_kv_heads, head_dim=head_dim,
                                    block_tokens=block_tokens, num_hot_blocks=num_hot_blocks)
@@ -164,28 +166,24 @@ class Pool:
         kvtier.decode_append_attention(self.handle, layer, q, k_new, v_new, block_tables, seq_lens,
                                        B, max_blocks, scale, out, flags, stream)
 
-    @staticmethod
-    def _token_stride(x, heads: int, D: int, total: int) -> int:
-        """Elements from token to token of a bf16 [total][heads][D] tensor whose heads are contiguous."""
-        import torch
-        if x.dtype != torch.bfloat16 or tuple(x.shape) != (total, heads, D) or \
-                x.stride(2) != 1 or (heads > 1 and x.stride(1) != D):
-            raise ValueError(f"need bf16 [{total}][{heads}][{D}] with contiguous heads, "
-                             f"got {x.dtype} {tuple(x.shape)} strides {x.stride()}")
-        return x.stride(0) if total > 1 else 0
-
     def _turn(self, q, k, v, out):
-        """Strides and flags of a call on [N][Hq][D] queries, checked."""
-        import torch
-        total = q.shape[0]
-        kv_stride = self._token_stride(k, self.Hkv, self.D, total)
-        if self._token_stride(v, self.Hkv, self.D, total) != kv_stride:
-            raise ValueError("k and v need the same token stride")
-        if tuple(out.shape) != (total, self.Hq, self.D) or not out.is_contiguous() or \
-                out.dtype not in (torch.float32, torch.bfloat16):
-            raise ValueError(f"out must be contiguous fp32 or bf16 [{total}][{self.Hq}][{self.D}]")
-        return (self._token_stride(q, self.Hq, self.D, total), kv_stride, total,
-                kvtier.KV_DECODE_OUT_BF16 if out.dtype == torch.bfloat16 else 0)
+        """(token strides of q and of k and v, tokens, flags) of a call on packed tokens, checked:
+        bf16 [N][heads][D] each, heads contiguous, any token stride (k and v the same)."""
+        total, D = len(q), self.D
+        kv_shape = (total, self.Hkv, D)
+        q_stride, kv_stride = q.stride(), k.stride()
+        if q.dtype is not self._bf16 or k.dtype is not self._bf16 or v.dtype is not self._bf16 or \
+                q.shape != (total, self.Hq, D) or k.shape != kv_shape or v.shape != kv_shape or \
+                q_stride[2] != 1 or (q_stride[1] != D and self.Hq > 1) or kv_stride != v.stride() or \
+                kv_stride[2] != 1 or (kv_stride[1] != D and self.Hkv > 1):
+            raise ValueError(f"need bf16 q [{total}][{self.Hq}][{D}], k and v {list(kv_shape)} with contiguous heads "
+                             "and one token stride for k and v, got " +
+                             ", ".join(f"{x.dtype} {tuple(x.shape)} strides {x.stride()}" for x in (q, k, v)))
+        if out.shape != q.shape or not out.is_contiguous() or out.dtype not in self._out_flags:
+            raise ValueError(f"out must be contiguous fp32 or bf16 [{total}][{self.Hq}][{D}]")
+        if total < 2:   # the stride of a single token says nothing
+            return 0, 0, total, self._out_flags[out.dtype]
+        return q_stride[0], kv_stride[0], total, self._out_flags[out.dtype]
 
     def prefill_attention(self, layer: int, q, k_new, v_new, cu_new, block_tables, seq_lens, B: int,
                           max_blocks: int, scale: float, out, stream=None) -> None:
@@ -194,9 +192,9 @@ class Pool:
         stride, so views of one projection will do), the newest of its seq_lens[b] tokens; K and V
         go into the slots that batch_reserve(counts=...) allocated. out: fp32 or bf16."""
         q_stride, kv_stride, total, flags = self._turn(q, k_new, v_new, out)
-        kvtier.prefill_attention(self.handle, layer, q, q_stride, k_new, v_new, kv_stride, cu_new,
-                                 total, block_tables, seq_lens, B, max_blocks, scale, out, flags,
-                                 stream)
+        kvtier.prefill_attention(self.handle, layer, q.data_ptr(), q_stride, k_new.data_ptr(),
+                                 v_new.data_ptr(), kv_stride, cu_new, total, block_tables, seq_lens,
+                                 B, max_blocks, scale, out.data_ptr(), flags, stream)
 
     def tree_attention(self, layer: int, q, k_draft, v_draft, ancestors, cu_draft, block_tables,
                        seq_lens, B: int, max_blocks: int, scale: float, out, stream=None) -> None:
@@ -206,9 +204,10 @@ class Pool:
         q_stride, kv_stride, total, flags = self._turn(q, k_draft, v_draft, out)
         if ancestors.numel() != total or ancestors.element_size() != 8 or not ancestors.is_contiguous():
             raise ValueError("one contiguous 64-bit mask per draft")
-        kvtier.tree_attention(self.handle, layer, q, q_stride, k_draft, v_draft, kv_stride, ancestors,
-                              cu_draft, total, block_tables, seq_lens, B, max_blocks, scale, out,
-                              flags, stream)
+        kvtier.tree_attention(self.handle, layer, q.data_ptr(), q_stride, k_draft.data_ptr(),
+                              v_draft.data_ptr(), kv_stride, ancestors.data_ptr(), cu_draft, total,
+                              block_tables, seq_lens, B, max_blocks, scale, out.data_ptr(), flags,
+                              stream)
 
     def shuffle_free(self, seed: int) -> None:
         kvtier.kv_pool_shuffle_free(self.handle, seed)

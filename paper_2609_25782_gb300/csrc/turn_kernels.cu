@@ -41,7 +41,7 @@ constexpr int kThreads = 384;
 constexpr int kCopyWarp = 8, kMmaWarp = 9, kStoreWarp = 11;
 // Registers per thread: at launch, then of the softmax warps and of the others. A softmax thread
 // keeps its row's 128 scores; the shares add up to what the CTA was launched with.
-constexpr int kRegsLaunch = 168, kRegsSoftmax = 200, kRegsOther = 104;
+constexpr int kRegsLaunch = 168, kRegsSoftmax = 192, kRegsOther = 120;
 static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * kRegsLaunch, "a larger share would wait forever");
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s
 
@@ -180,7 +180,7 @@ __device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }
 #define KVT_RW8(x, o) "+r"(x[o]), "+r"(x[o + 1]), "+r"(x[o + 2]), "+r"(x[o + 3]), "+r"(x[o + 4]), "+r"(x[o + 5]), \
         "+r"(x[o + 6]), "+r"(x[o + 7])
 
-// 32 columns of this thread's row. The values are there after tmem_wait on them.
+// 32 or 16 columns of this thread's row. The values are there after tmem_wait on them.
 __device__ __forceinline__ void tmem_load(uint32_t (&x)[32], uint32_t addr) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -190,24 +190,31 @@ __device__ __forceinline__ void tmem_load(uint32_t (&x)[32], uint32_t addr) {
         : "r"(addr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_load(uint32_t (&x)[16], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : KVT_R8(x, 0), KVT_R8(x, 8)
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&x)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : KVT_RW8(x, 0), KVT_RW8(x, 8)::"memory");
+}
 __device__ __forceinline__ void tmem_wait(uint32_t (&x)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : KVT_RW8(x, 0), KVT_RW8(x, 8), KVT_RW8(x, 16), KVT_RW8(x, 24)::"memory");
 }
-__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&x)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
-        "%28,%29,%30,%31};" ::KVT_U8(x, 0),
-        KVT_U8(x, 8), KVT_U8(x, 16), KVT_U8(x, 24), "r"(addr)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&x)[16]) {
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&x)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
         "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::KVT_U8(x, 0),
         KVT_U8(x, 8), "r"(addr)
         : "memory");
+}
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&x)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::KVT_U8(x, 0), "r"(addr)
+                 : "memory");
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -489,11 +496,14 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
         ++items;
         const int tiles = r.narrow ? 1 : 2;
         pairs += tiles - 1;
-        if (lane < tiles) mbar_expect(&sm.q_full[lane], kTileBytes);
-        __syncwarp();
-        if (lane < 2 * tiles)   // coordinates: (column, head, token, half)
-            copy_box(sm.q[lane >> 1] + (lane & 1) * kHalfWhole, &maps.q, r.g * G,
-                     r.x.lo + ((2 * r.pair + (lane >> 1)) << s.shift), lane & 1, &sm.q_full[lane >> 1]);
+        if (elected())   // coordinates: (column, head, token, half)
+#pragma unroll 1
+            for (int i = 0; i < tiles; ++i) {
+                const int token = r.x.lo + ((2 * r.pair + i) << s.shift);
+                mbar_expect(&sm.q_full[i], kTileBytes);
+                copy_box(sm.q[i], &maps.q, r.g * G, token, 0, &sm.q_full[i]);
+                copy_box(sm.q[i] + kHalfWhole, &maps.q, r.g * G, token, 1, &sm.q_full[i]);
+            }
         __syncwarp();
         for (int t = r.t0; ok && t < r.t1; ++t) {
             const int keys = keys_of(r, t);
@@ -538,25 +548,25 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
 
 // S = Q K^T. The steps' operands lie a constant apart: one addition per step and operand, so that the
 // issuing thread keeps up with the tensor cores (64 cycles a step).
-template <bool kGrouped>
-__device__ __forceinline__ void product_qk(uint32_t d, uint32_t q, uint32_t k, uint32_t form) {
-    const uint64_t a = operand(q, 16, kGroupWhole), b = operand(k, 16, kGrouped ? kGroupGrouped : kGroupWhole);
+__device__ __forceinline__ void product_qk(uint32_t d, uint32_t q, uint32_t k, bool grouped, uint32_t form) {
+    const uint64_t a = operand(q, 16, kGroupWhole), b = operand(k, 16, grouped ? kGroupGrouped : kGroupWhole);
+    const uint32_t half = (grouped ? kHalfGrouped : kHalfWhole) >> 4;
 #pragma unroll
     for (int i = 0; i < kHeadDim / 16; ++i)
-        mma_ss(d, a + (((i >> 2) * kHalfWhole + (i & 3) * 32) >> 4),
-               b + (((i >> 2) * (kGrouped ? kHalfGrouped : kHalfWhole) + (i & 3) * 32) >> 4), form, i > 0);
+        mma_ss(d, a + (((i >> 2) * kHalfWhole + (i & 3) * 32) >> 4), b + ((i >> 2) * half + ((i & 3) * 32 >> 4)), form,
+               i > 0);
 }
 // O += P V over 16 * steps keys, or (!add) O = P V.
-template <bool kGrouped>
-__device__ __forceinline__ void product_pv(uint32_t d, uint32_t p, uint32_t v, int steps, bool add) {
-    const uint64_t b = kGrouped ? operand(v, kHalfGrouped, kGroupGrouped) : operand(v, kHalfWhole, kGroupWhole);
-    constexpr int kStep = 2 * (kGrouped ? kGroupGrouped : kGroupWhole) >> 4;
+__device__ __forceinline__ void product_pv(uint32_t d, uint32_t p, uint32_t v, bool grouped, int steps, bool add) {
+    uint64_t b = grouped ? operand(v, kHalfGrouped, kGroupGrouped) : operand(v, kHalfWhole, kGroupWhole);
+    const uint32_t step = 2 * (grouped ? kGroupGrouped : kGroupWhole) >> 4;
     const uint32_t form = mma_form(kHeadDim, true, false);
     if (steps == kTurnKeys / 16) {
 #pragma unroll
-        for (int i = 0; i < kTurnKeys / 16; ++i) mma_ts(d, p + i * 8, b + i * kStep, form, i > 0 || add);
+        for (int i = 0; i < kTurnKeys / 16; ++i) mma_ts(d, p + i * 8, b + i * step, form, i > 0 || add);
     } else {
-        for (int i = 0; i < steps; ++i) mma_ts(d, p + i * 8, b + i * kStep, form, i > 0 || add);
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i, b += step) mma_ts(d, p + i * 8, b, form, i > 0 || add);
     }
 }
 
@@ -605,16 +615,14 @@ __device__ void mma_role(const TurnArgs &a, Smem &sm, int stream) {
         auto issue_pv = [&](int i) {   // O += P V of the run's tile i
             const int stage = (2 * (base + i) + 1) % kStages, steps = steps_of(i);
             const uint32_t v = smem_u32(sm.kv[stage]);
-            if (t0 + i < cached_tiles) product_pv<true>(o_col, s_col, v, steps, i > first);
-            else product_pv<false>(o_col, s_col, v, steps, i > first);
+            product_pv(o_col, s_col, v, t0 + i < cached_tiles, steps, i > first);
             give_back(stage);
             if (i + by >= tiles) mma_commit(&sm.o_full[stream]);
         };
         auto issue_qk = [&](int i) {   // S = Q K^T
             const int stage = 2 * (base + i) % kStages;
             const uint32_t k = smem_u32(sm.kv[stage]), form = mma_form(16 * steps_of(i), false, negate);
-            if (t0 + i < cached_tiles) product_qk<true>(s_col, smem_u32(sm.q[q]), k, form);
-            else product_qk<false>(s_col, smem_u32(sm.q[q]), k, form);
+            product_qk(s_col, smem_u32(sm.q[q]), k, t0 + i < cached_tiles, form);
             mma_commit(&sm.s_full[stream]);
             give_back(stage);
             if (i + by >= tiles) mma_commit(&sm.q_empty);
@@ -703,9 +711,10 @@ __device__ __forceinline__ float2 halves(uint64_t x) {
 // Four running maxima, so that no instruction waits for the one before it.
 struct Tops {
     float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    __device__ __forceinline__ void add(const uint32_t (&x)[32]) {
+    template <int kN>
+    __device__ __forceinline__ void add(const uint32_t (&x)[kN]) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 2)
+        for (int i = 0; i < kN; i += 2)
             t[i / 2 % 4] = fmaxf(t[i / 2 % 4], fmaxf(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
     }
     __device__ __forceinline__ float all() const { return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])); }
@@ -721,35 +730,36 @@ __device__ __forceinline__ void move_top(float top, uint32_t o_addr, bool first,
     st.l *= c;
     if (first) return;
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) {
-        uint32_t o[32];
-        tmem_load(o, o_addr + i * 32);
+    for (int i = 0; i < kHeadDim; i += 16) {
+        uint32_t o[16];
+        tmem_load(o, o_addr + i);
         tmem_wait(o);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * c);
-        tmem_store(o_addr + i * 32, o);
+        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * c);
+        tmem_store(o_addr + i, o);
     }
 }
 
-// Weights ex2(x * scale - ref) of 32 scores, in bf16 to tensor memory; their sum (of the unrounded
-// ones) is added to `sum`.
-__device__ __forceinline__ void put_weights(const uint32_t (&x)[32], uint64_t scale, uint64_t ref, uint32_t p_addr,
+// Weights ex2(x * scale - ref) of scores, in bf16 to tensor memory; their sums (of the unrounded
+// ones) are added to `sum`.
+template <int kN>
+__device__ __forceinline__ void put_weights(const uint32_t (&x)[kN], uint64_t scale, uint64_t ref, uint32_t p_addr,
                                             uint64_t (&sum)[4]) {
-    uint32_t p[16];
+    uint32_t p[kN / 2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < kN / 2; ++i) {
         const float2 e = halves(fma2(pair_of(x[2 * i], x[2 * i + 1]), scale, ref));
         const float y0 = ex2(e.x), y1 = ex2(e.y);
         sum[i % 4] = add2(sum[i % 4], pair_of(__float_as_uint(y0), __float_as_uint(y1)));
         p[i] = pack_bf16(y0, y1);
     }
-    tmem_store16(p_addr, p);
+    tmem_store(p_addr, p);
 }
 
 // Scores of which the row sees those in `sees`; the others become -infinity, weight 0.
-__device__ __forceinline__ void hide(uint32_t (&x)[32], uint32_t sees) {
+__device__ __forceinline__ void hide(uint32_t (&x)[16], uint32_t sees) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
+    for (int i = 0; i < 16; ++i)
         if (!(sees >> i & 1)) x[i] = 0xFF800000u;
 }
 
@@ -761,8 +771,8 @@ __device__ __forceinline__ void weights_there(uint64_t *bar) {
     if (threadIdx.x % 32 == 0) mbar_arrive(bar);
 }
 
-// A key tile's weights of this thread's row: S from tensor memory, P back over it (16 columns
-// of P for 32 of S, so a chunk's weights never reach scores that are still to be read).
+// A key tile's weights of this thread's row: S from tensor memory, P back over it (8 columns
+// of P for 16 of S, so a chunk's weights never reach scores that are still to be read).
 __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, int t, int token, uint64_t mask,
                                              uint32_t s_addr, uint32_t o_addr, bool first, Stats &st) {
     const int keys = keys_of(r, t);
@@ -793,16 +803,18 @@ __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, in
 #pragma unroll
         for (int c = 0; c < 4; ++c) put_weights(x[c], scale, ref, s_addr + c * 16, sum);
     } else {
+        // 16 at a time: such tiles are an item's last, and short code that is run once or twice a call
+        // comes from the instruction caches sooner than its results from the arithmetic.
         const uint64_t bits = own && a.masks ? mask : ~0ull;   // drafts are at most 64 keys
-        const int chunks = (keys + 31) / 32;
+        const int chunks = (keys + 15) / 16;
         auto sees = [&](int c) {
-            const int n = seen - c * 32;
-            return (n >= 32 ? ~0u : n > 0 ? (1u << n) - 1 : 0u) & (c < 2 ? static_cast<uint32_t>(bits >> (c * 32)) : ~0u);
+            const int n = seen - c * 16;
+            return (n >= 16 ? ~0u : n > 0 ? (1u << n) - 1 : 0u) & (c < 4 ? static_cast<uint32_t>(bits >> (c * 16)) : ~0u);
         };
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c) {
-            uint32_t x[32];
-            tmem_load(x, s_addr + c * 32);
+            uint32_t x[16];
+            tmem_load(x, s_addr + c * 16);
             tmem_wait(x);
             hide(x, sees(c));
             top.add(x);
@@ -812,30 +824,15 @@ __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, in
         const uint64_t ref = pair_of(minus, minus);
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c) {
-            uint32_t x[32];
-            tmem_load(x, s_addr + c * 32);
+            uint32_t x[16];
+            tmem_load(x, s_addr + c * 16);
             tmem_wait(x);
             hide(x, sees(c));
-            put_weights(x, scale, ref, s_addr + c * 16, sum);
+            put_weights(x, scale, ref, s_addr + c * 8, sum);
         }
     }
     const float2 y = halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
     st.l += y.x + y.y;
-}
-
-// 32 values of an output row from column d0.
-__device__ __forceinline__ void store_out(const TurnArgs &a, int64_t row, int d0, const float (&y)[32]) {
-    if (a.out_bf16) {
-        uint4 *to = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + row * kHeadDim + d0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            to[i] = make_uint4(pack_bf16(y[8 * i], y[8 * i + 1]), pack_bf16(y[8 * i + 2], y[8 * i + 3]),
-                               pack_bf16(y[8 * i + 4], y[8 * i + 5]), pack_bf16(y[8 * i + 6], y[8 * i + 7]));
-    } else {
-        float4 *to = reinterpret_cast<float4 *>(static_cast<float *>(a.out) + row * kHeadDim + d0);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) to[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-    }
 }
 
 // A slot of partial results: 256 rows of 128 values, four values of all rows together (so that a warp's
@@ -858,28 +855,6 @@ struct PartRecord {
 __device__ __forceinline__ PartRecord *part_record(const TurnArgs &a, int cta) {
     return reinterpret_cast<PartRecord *>(a.part + static_cast<int64_t>(a.part_slots) * 2 * kTurnRows * (kHeadDim + 2)) +
            cta;
-}
-
-// The item's output row of this thread, from tensor memory, 32 columns at a time: O times `w`, and
-// (kTwo) the other stream's, at `other`, times `w_other`.
-template <bool kTwo, typename Put>
-__device__ __forceinline__ void read_o(uint32_t o_addr, float w, uint32_t other, float w_other, Put put) {
-#pragma unroll 1
-    for (int d = 0; d < kHeadDim; d += 32) {
-        uint32_t o[32];
-        float y[32];
-        tmem_load(o, o_addr + d);
-        tmem_wait(o);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(o[i]) * w;
-        if constexpr (kTwo) {
-            tmem_load(o, other + d);
-            tmem_wait(o);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = __fmaf_rn(__uint_as_float(o[i]), w_other, y[i]);
-        }
-        put(d, y);
-    }
 }
 
 // The new tokens' K and V into their slots of the pool, by one warp beside the others' work, a token's
@@ -974,33 +949,53 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
                 other = tmem + kColO + kColStream;
             }
         }
-        const bool whole = r.t0 == 0 && r.t1 == r.tiles;
         if (!(r.narrow && stream == 1)) {
+            const bool whole = r.t0 == 0 && r.t1 == r.tiles;
+            const int slot = r.t0 > 0 ? 2 * blockIdx.x : 2 * blockIdx.x + 1;
             if (whole) {
                 const float inv = st.l > 0.f || st.l != st.l ? __frcp_rn(st.l) : 0.f;   // nothing seen: zeros
-                const auto put = [&](int d, const float (&y)[32]) {
-                    if (live) store_out(a, out_row, d, y);
-                };
-                if (ok && other) read_o<true>(o_addr, w * inv, other, w_other * inv, put);
-                else if (ok) read_o<false>(o_addr, w * inv, 0, 0.f, put);
+                w *= inv;
+                w_other *= inv;
             } else {
-                const int slot = r.t0 > 0 ? 2 * blockIdx.x : 2 * blockIdx.x + 1;
-                float4 *po = part_o(a, slot, stream);
-                const auto put = [&](int d, const float (&y)[32]) {
-                    if (!live) return;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        po[(d / 4 + i) * kTurnRows + row] =
-                            make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-                };
-                if (ok && other) read_o<true>(o_addr, w, other, w_other, put);
-                else if (ok) read_o<false>(o_addr, w, 0, 0.f, put);
                 if (live) part_ml(a, slot, stream)[row] = make_float2(st.m, st.l);
                 if (stream == 0 && row == 0) {
                     const int t0 = r.pair << (s.shift + 1);
                     if (r.t0 == 0) rec = {1, 0, r.x.lo + t0, min(2 << s.shift, r.x.n - t0), r.g};
                     else if (r.t1 < r.tiles) rec.through = 1;
                 }
+            }
+            // The row from tensor memory, 16 columns at a time (short code, as above).
+            float4 *po = part_o(a, slot, stream) + row;
+#pragma unroll 1
+            for (int d = 0; ok && d < kHeadDim; d += 16) {
+                uint32_t o[16];
+                float y[16];
+                tmem_load(o, o_addr + d);
+                tmem_wait(o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(o[i]) * w;
+                if (other) {
+                    tmem_load(o, other + d);
+                    tmem_wait(o);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) y[i] = __fmaf_rn(__uint_as_float(o[i]), w_other, y[i]);
+                }
+                if (live && whole && a.out_bf16) {
+                    uint4 *to = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + out_row * kHeadDim + d);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        to[i] = make_uint4(pack_bf16(y[8 * i], y[8 * i + 1]), pack_bf16(y[8 * i + 2], y[8 * i + 3]),
+                                           pack_bf16(y[8 * i + 4], y[8 * i + 5]), pack_bf16(y[8 * i + 6], y[8 * i + 7]));
+                } else if (live) {
+                    // four values to the output row, or to all rows' four
+                    float4 *to = whole ? reinterpret_cast<float4 *>(static_cast<float *>(a.out) + out_row * kHeadDim + d)
+                                       : po + d / 4 * kTurnRows;
+                    const int step = whole ? 1 : kTurnRows;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        to[i * step] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                }
+                __syncwarp();
             }
         }
         fence_before();
@@ -1016,6 +1011,8 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
     if (!a.whole) asm volatile("griddepcontrol.launch_dependents;");   // the merge, which waits for all of this
     Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp == kStoreWarp && lane < sizeof(Maps) / sizeof(CUtensorMap))
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<const CUtensorMap *>(&maps) + lane) : "memory");
     if (warp == kCopyWarp) make_plan(a, sm.plan, lane);
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
