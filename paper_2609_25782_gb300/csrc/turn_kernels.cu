@@ -198,6 +198,16 @@ __device__ __forceinline__ void tmem_load(uint32_t (&x)[16], uint32_t addr) {
         : "r"(addr)
         : "memory");
 }
+// 32 columns of 16 rows (from the address's lane on) shared out as a matrix fragment: lane l has columns
+// 8 g + 2 (l % 4) and the next of rows l / 4, in x[4 g] and x[4 g + 1], and l / 4 + 8, in the two after.
+__device__ __forceinline__ void tmem_load_rows(uint32_t (&x)[16], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : KVT_R8(x, 0), KVT_R8(x, 8)
+        : "r"(addr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_wait(uint32_t (&x)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" : KVT_RW8(x, 0), KVT_RW8(x, 8)::"memory");
 }
@@ -835,11 +845,10 @@ __device__ __forceinline__ void softmax_tile(const TurnArgs &a, const Run &r, in
     st.l += y.x + y.y;
 }
 
-// A slot of partial results: 256 rows of 128 values, four values of all rows together (so that a warp's
-// rows are next to each other), then (m, l) of the rows. CTA c has slot 2c for an item that an earlier piece
-// begins, and 2c + 1 for one that it begins and a later piece ends.
-__device__ __forceinline__ float4 *part_o(const TurnArgs &a, int slot, int stream) {
-    return reinterpret_cast<float4 *>(a.part) + (static_cast<int64_t>(slot) * 2 + stream) * kTurnRows * (kHeadDim / 4);
+// A slot of partial results: 256 rows of 128 values; behind all slots, (m, l) of the rows. CTA c has slot 2c
+// for an item that an earlier piece begins, and 2c + 1 for one that it begins and a later piece ends.
+__device__ __forceinline__ float *part_o(const TurnArgs &a, int slot, int stream) {
+    return a.part + (static_cast<int64_t>(slot) * 2 + stream) * kTurnRows * kHeadDim;
 }
 __device__ __forceinline__ float2 *part_ml(const TurnArgs &a, int slot, int stream) {
     return reinterpret_cast<float2 *>(a.part + static_cast<int64_t>(a.part_slots) * 2 * kTurnRows * kHeadDim) +
@@ -855,6 +864,16 @@ struct PartRecord {
 __device__ __forceinline__ PartRecord *part_record(const TurnArgs &a, int cta) {
     return reinterpret_cast<PartRecord *>(a.part + static_cast<int64_t>(a.part_slots) * 2 * kTurnRows * (kHeadDim + 2)) +
            cta;
+}
+
+// Words w[g] of four lanes, of 16-byte units g = 0 .. 3 that the lanes hold a word each of: lane q of the
+// four gets unit q whole.
+__device__ __forceinline__ uint4 units_of(const uint32_t (&w)[4], int lane) {
+    const bool odd = lane & 1, high = lane & 2;
+    const uint32_t t0 = __shfl_xor_sync(~0u, odd ? w[0] : w[1], 1), t1 = __shfl_xor_sync(~0u, odd ? w[2] : w[3], 1);
+    const uint32_t c0 = odd ? t0 : w[0], c1 = odd ? w[1] : t0, c2 = odd ? t1 : w[2], c3 = odd ? w[3] : t1;
+    const uint32_t s0 = __shfl_xor_sync(~0u, high ? c0 : c2, 2), s1 = __shfl_xor_sync(~0u, high ? c1 : c3, 2);
+    return high ? make_uint4(s0, s1, c2, c3) : make_uint4(c0, c1, s0, s1);
 }
 
 // The new tokens' K and V into their slots of the pool, by one warp beside the others' work, a token's
@@ -917,7 +936,6 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
         const int tile = r.narrow ? 2 * r.pair : 2 * r.pair + stream;
         const int token = (tile << s.shift) + (row >> g_shift);   // of the session's new ones
         const bool live = token < r.x.n;
-        const int64_t out_row = (static_cast<int64_t>(r.x.lo) + token) * a.s.Hq + (r.g << g_shift) + (row & ((1 << g_shift) - 1));
         uint64_t mask = 0;
         if (a.masks && live) mask = a.masks[r.x.lo + token];
         Stats st = {-INFINITY, 0.f};
@@ -964,38 +982,53 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
                     else if (r.t1 < r.tiles) rec.through = 1;
                 }
             }
-            // The row from tensor memory, 16 columns at a time (short code, as above).
-            float4 *po = part_o(a, slot, stream) + row;
+            // The rows from tensor memory, 16 rows by 32 columns at a time, so that a store has the 64 or
+            // 32 bytes of eight rows; with a row per thread each store had 16 bytes of 32 rows, and an
+            // item's end took 6 700 cycles (2 000). Short code, as above.
+            const int lane = row & 31;
 #pragma unroll 1
-            for (int d = 0; ok && d < kHeadDim; d += 16) {
-                uint32_t o[16];
-                float y[16];
-                tmem_load(o, o_addr + d);
-                tmem_wait(o);
+            for (int part = 0; ok && part < 8; ++part) {
+                const int half = part >> 2 << 4, d = (part & 3) * 32;   // first row of the warp's, first column
+                uint32_t x[16];
+                float y[16], scale[2], scale_other[2];
+                tmem_load_rows(x, o_addr + (half << 16) + d);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(o[i]) * w;
+                for (int i = 0; i < 2; ++i) {   // this thread's rows: half + lane / 4, and 8 on
+                    scale[i] = __shfl_sync(~0u, w, half + i * 8 + (lane >> 2));
+                    scale_other[i] = __shfl_sync(~0u, w_other, half + i * 8 + (lane >> 2));
+                }
+                tmem_wait(x);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(x[i]) * scale[i >> 1 & 1];
                 if (other) {
-                    tmem_load(o, other + d);
-                    tmem_wait(o);
+                    tmem_load_rows(x, other + (half << 16) + d);
+                    tmem_wait(x);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) y[i] = __fmaf_rn(__uint_as_float(o[i]), w_other, y[i]);
+                    for (int i = 0; i < 16; ++i) y[i] = __fmaf_rn(__uint_as_float(x[i]), scale_other[i >> 1 & 1], y[i]);
                 }
-                if (live && whole && a.out_bf16) {
-                    uint4 *to = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + out_row * kHeadDim + d);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        to[i] = make_uint4(pack_bf16(y[8 * i], y[8 * i + 1]), pack_bf16(y[8 * i + 2], y[8 * i + 3]),
-                                           pack_bf16(y[8 * i + 4], y[8 * i + 5]), pack_bf16(y[8 * i + 6], y[8 * i + 7]));
-                } else if (live) {
-                    // four values to the output row, or to all rows' four
-                    float4 *to = whole ? reinterpret_cast<float4 *>(static_cast<float *>(a.out) + out_row * kHeadDim + d)
-                                       : po + d / 4 * kTurnRows;
-                    const int step = whole ? 1 : kTurnRows;
+                for (int i = 0; i < 2; ++i) {
+                    const int its = (row & ~31) + half + i * 8 + (lane >> 2);
+                    const int t = (tile << s.shift) + (its >> g_shift);
+                    const bool there = t < r.x.n;
+                    const int64_t to = (static_cast<int64_t>(r.x.lo) + t) * a.s.Hq + (r.g << g_shift) +
+                                       (its & ((1 << g_shift) - 1));
+                    if (whole && a.out_bf16) {
+                        uint32_t v[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        to[i * step] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                        for (int g = 0; g < 4; ++g) v[g] = pack_bf16(y[4 * g + 2 * i], y[4 * g + 2 * i + 1]);
+                        const uint4 unit = units_of(v, lane);
+                        if (there)
+                            reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + to * kHeadDim + d)[lane & 3] = unit;
+                    } else if (there) {
+                        float2 *f = reinterpret_cast<float2 *>((whole ? static_cast<float *>(a.out) + to * kHeadDim
+                                                                      : part_o(a, slot, stream) + its * kHeadDim) + d) +
+                                    (lane & 3);
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) f[g * 4] = make_float2(y[4 * g + 2 * i], y[4 * g + 2 * i + 1]);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
         }
         fence_before();
@@ -1063,57 +1096,77 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sm.tmem), "r"(kTmemCols));
 }
 
-// The pieces of each item that several have, merged in order: a thread per row and 16 values of it. CTA
-// (c, j): the item that piece c begins, if any.
-constexpr int kCombineCtas = 8;   // per item
-__global__ void __launch_bounds__(256) turn_combine_kernel(const __grid_constant__ TurnArgs a) {
+// The pieces of each item that several have, merged in order: a warp for up to four of its rows, 64 apart,
+// a lane for four values of each. CTA (c, j): the item that piece c begins, if any. Loads are what takes
+// the time: the statistics of up to 32 pieces come in one round, a lane each, and the values 16 at a time.
+constexpr int kCombineCtas = 8, kCombineWarps = 8;
+constexpr int kCombineRows = 2 * kTurnRows / (kCombineCtas * kCombineWarps);
+__global__ void __launch_bounds__(kCombineWarps * 32) turn_combine_kernel(const __grid_constant__ TurnArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const PartRecord rec = *part_record(a, blockIdx.x);
+    const int first = blockIdx.x, lane = threadIdx.x & 31, g_shift = 7 - a.token_shift;
+    const PartRecord rec = *part_record(a, first);
     if (!rec.opens) return;
-    int last = blockIdx.x + 1;
+    const int row0 = blockIdx.y * kCombineWarps + (threadIdx.x >> 5), rows = rec.tokens << g_shift;
+    if (row0 >= rows) return;
+    int last = first + 1;
     while (last + 1 < a.part_slots / 2 && part_record(a, last)->through) ++last;
-    // 64 warps' work: 8 groups of 32 rows, 8 of 16 values
-    const int work = blockIdx.y * 8 + (threadIdx.x >> 5), stream = work >> 5;
-    const int row = (work >> 3 & 3) * 32 + (threadIdx.x & 31), d4 = (work & 7) * 4;
-    const int g_shift = 7 - a.token_shift;
-    const int token = (stream << a.token_shift) + (row >> g_shift);
-    if (token >= rec.tokens) return;
-    const int first = blockIdx.x;
     const auto slot = [&](int c) { return c == first ? 2 * c + 1 : 2 * c; };
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int c = first; c <= last; ++c) m = fmaxf(m, part_ml(a, slot(c), stream)[row].x);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    float4 y[4] = {};
-#pragma unroll 4
-    for (int c = first; c <= last; ++c) {
-        const float2 v = part_ml(a, slot(c), stream)[row];
-        const float4 *po = part_o(a, slot(c), stream) + d4 * kTurnRows + row;
-        const float w = ex2(v.x - ref);
-        l = __fmaf_rn(w, v.y, l);
+    constexpr int kApart = kCombineCtas * kCombineWarps;
+    const auto stream_of = [&](int i) { return (row0 + i * kApart) / kTurnRows; };
+    const auto row_of = [&](int i) { return (row0 + i * kApart) % kTurnRows; };
+    float m[kCombineRows], l[kCombineRows];
+    float4 y[kCombineRows];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 o = po[i * kTurnRows];
-            y[i] = make_float4(__fmaf_rn(w, o.x, y[i].x), __fmaf_rn(w, o.y, y[i].y), __fmaf_rn(w, o.z, y[i].z),
-                               __fmaf_rn(w, o.w, y[i].w));
-        }
+    for (int i = 0; i < kCombineRows; ++i) {
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+        y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    const float inv = l > 0.f || l != l ? __frcp_rn(l) : 0.f;
-    const int64_t to = ((static_cast<int64_t>(rec.row) + token) * a.s.Hq + (rec.g << g_shift) +
-                        (row & ((1 << g_shift) - 1))) * kHeadDim + d4 * 4;
+    for (int c0 = first; c0 <= last; c0 += 32) {
+        const int n = min(32, last + 1 - c0);
+        float weight[kCombineRows];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = make_float4(y[i].x * inv, y[i].y * inv, y[i].z * inv, y[i].w * inv);
-    if (a.out_bf16) {
-        uint4 *out = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + to);
+        for (int i = 0; i < kCombineRows; ++i) {
+            float2 v = make_float2(-INFINITY, 0.f);
+            if (lane < n && row0 + i * kApart < rows) v = part_ml(a, slot(c0 + lane), stream_of(i))[row_of(i)];
+            float top = v.x;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            out[i] = make_uint4(pack_bf16(y[2 * i].x, y[2 * i].y), pack_bf16(y[2 * i].z, y[2 * i].w),
-                                pack_bf16(y[2 * i + 1].x, y[2 * i + 1].y), pack_bf16(y[2 * i + 1].z, y[2 * i + 1].w));
-    } else {
-        float4 *out = reinterpret_cast<float4 *>(static_cast<float *>(a.out) + to);
+            for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+            top = fmaxf(top, m[i]);
+            const float ref = top == -INFINITY ? 0.f : top, c = ex2(m[i] - ref);   // of the pieces before
+            weight[i] = ex2(v.x - ref);
+            float sum = weight[i] * v.y;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) out[i] = y[i];
+            for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+            m[i] = top;
+            l[i] = __fmaf_rn(l[i], c, sum);
+            y[i] = make_float4(y[i].x * c, y[i].y * c, y[i].z * c, y[i].w * c);
+        }
+#pragma unroll 4
+        for (int k = 0; k < n; ++k)
+#pragma unroll
+            for (int i = 0; i < kCombineRows; ++i) {
+                const float w = __shfl_sync(~0u, weight[i], k);
+                if (row0 + i * kApart >= rows) continue;
+                const float4 x = reinterpret_cast<const float4 *>(part_o(a, slot(c0 + k), stream_of(i)) +
+                                                                  row_of(i) * kHeadDim)[lane];
+                y[i] = make_float4(__fmaf_rn(w, x.x, y[i].x), __fmaf_rn(w, x.y, y[i].y), __fmaf_rn(w, x.z, y[i].z),
+                                   __fmaf_rn(w, x.w, y[i].w));
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < kCombineRows; ++i) {
+        const int row = row0 + i * kApart;
+        if (row >= rows) break;
+        const float inv = l[i] > 0.f || l[i] != l[i] ? __frcp_rn(l[i]) : 0.f;   // nothing seen: zeros
+        const int64_t to = ((static_cast<int64_t>(rec.row) + (row >> g_shift)) * a.s.Hq + (rec.g << g_shift) +
+                            (row & ((1 << g_shift) - 1))) * kHeadDim;
+        const float4 z = make_float4(y[i].x * inv, y[i].y * inv, y[i].z * inv, y[i].w * inv);
+        if (a.out_bf16)
+            reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + to)[lane] =
+                make_uint2(pack_bf16(z.x, z.y), pack_bf16(z.z, z.w));
+        else
+            reinterpret_cast<float4 *>(static_cast<float *>(a.out) + to)[lane] = z;
     }
 }
 
