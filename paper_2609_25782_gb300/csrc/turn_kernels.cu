@@ -11,7 +11,7 @@
 //   0-3, 4-7  softmax of stream 0 and 1, a thread per row: scores from tensor
 //             memory, running maximum and sum in 32 bits, weights back to tensor
 //             memory in bf16; at the end the output
-//   8         copies: q tiles and key tiles (TMA, 128-byte swizzle)
+//   8         the plan, then copies: q tiles and key tiles (TMA, 128-byte swizzle)
 //   9, 10     matrix products (tcgen05) of stream 0 and 1: S = Q K^T from shared
 //             memory, O += P V with P from tensor memory
 //   11        the new tokens' K and V, into the pool
@@ -49,10 +49,18 @@ constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 256, kColStream = 128;
 
+// A run of key tiles t0 .. t1 - 1 of one item; tiles 0: no more runs.
+struct alignas(16) Run {
+    int32_t lo, n, P, b;   // the session: first row, new tokens, cached ones, its number
+    int32_t g, pair, t0, t1;
+    int32_t tiles, cached_tiles, own_keys, narrow;
+};
+constexpr int kRuns = 4;        // runs that the copies may be ahead of the other roles
+constexpr int kRunReaders = 11;   // warps: softmax, products, store
+
 struct Plan {
     TurnPos begin, end;
     TurnSession first;   // the session of `begin`, n < 0: not at hand
-    int32_t pieces;
 };
 
 struct alignas(1024) Smem {
@@ -63,6 +71,8 @@ struct alignas(1024) Smem {
     // present one is still on its way; with one barrier, a parity, that would pass as done.
     uint64_t kv_full[2 * kStages], kv_empty[kStages];
     uint64_t q_full[2], q_empty, s_full[2], p_full[2], o_full[2], drained[2];
+    uint64_t run_full[kRuns], run_empty[kRuns], other_ready, other_free;
+    Run runs[kRuns];
     Plan plan;
     float other_m[kTurnRows], other_l[kTurnRows];   // narrow items: stream 1's statistics
     uint32_t tmem;
@@ -113,6 +123,7 @@ __device__ __forceinline__ bool mbar_try(uint64_t *bar, uint32_t parity) {
 __device__ __forceinline__ bool mbar_wait(Smem &sm, uint64_t *bar, uint32_t parity) {
     if (mbar_try(bar, parity)) return true;
     const unsigned long long t0 = global_ns();
+#pragma unroll 1
     while (!mbar_try(bar, parity)) {
         if (*reinterpret_cast<volatile int32_t *>(&sm.abort)) return false;
         if (global_ns() - t0 > kWaitLimitNs) {
@@ -238,7 +249,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
     return y;
 }
-__device__ __forceinline__ void sync_threads(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 
 // ---- the work ----------------------------------------------------------------------------
 
@@ -273,129 +283,125 @@ __device__ __forceinline__ int64_t scan(int64_t x, int lane, int64_t *all) {
     return y - x;
 }
 
-// This CTA's piece, by one warp.
+// This CTA's piece, by one warp. (Short code: a call runs it once.)
 __device__ void make_plan(const TurnArgs &a, Plan &plan, int lane) {
     const TurnShape s = turn_shape(a);
-    int64_t W = 0, cost = 0;
-    TurnSession x = {0, 0, 0};   // up to 32 sessions: kept from the first round to the second
-    for (int b0 = 0; b0 < a.B; b0 += 32) {
-        const int b = b0 + lane;
-        int64_t all;
-        cost = 0;
-        if (b < a.B) {
-            bool bad;
-            x = session_of(a, b, &bad);
-            cost = s.Hkv * turn_head_cost(s, x);
-            if (bad && blockIdx.x == 0) atomicOr(a.err, kErrBadLength);
-        }
-        scan(cost, lane, &all);
-        W += all;
-    }
-    const int pieces = W == 0 ? 0 : turn_pieces(W, gridDim.x), c = blockIdx.x;
-    if (lane == 0) {
-        plan.pieces = pieces;
-        plan.begin = plan.end = {a.B, 0, 0, 0};
-    }
-    __syncwarp();
-    if (c >= pieces) return;
-    const int64_t u[2] = {turn_cut(W, pieces, c), turn_cut(W, pieces, c + 1)};   // the second is W at the end
-    int64_t before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 32) {
-        const int b = b0 + lane;
-        int64_t all;
-        if (a.B > 32) {
-            cost = 0;
-            if (b < a.B) {
-                x = session_of(a, b);
-                cost = s.Hkv * turn_head_cost(s, x);
-            }
-        }
-        const int64_t at = before + scan(cost, lane, &all);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            if (u[e] < at || u[e] >= at + cost) continue;
-            TurnPos p = turn_locate(s, x, b, u[e] - at);
-            if (p.t >= turn_tiles(s, x, p.pair) || (a.whole && p.t > 0)) {   // the item's end: the next one's start
-                p.t = 0;
-                if (++p.pair >= turn_pairs(s, x)) {
-                    p.pair = 0;
-                    if (++p.g >= s.Hkv) {
-                        p.g = 0;
-                        ++p.b;   // an empty session here is passed over by the walk
-                    }
+    int64_t cost = 0, u[2] = {0, 0};
+    TurnSession x = {0, 0, 0};   // up to 32 sessions: kept from the first pass to the second
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        int64_t before = 0;
+#pragma unroll 1
+        for (int b0 = 0; b0 < a.B; b0 += 32) {
+            const int b = b0 + lane;
+            if (pass == 0 || a.B > 32) {
+                cost = 0;
+                if (b < a.B) {
+                    bool bad;
+                    x = session_of(a, b, &bad);
+                    cost = s.Hkv * turn_head_cost(s, x);
+                    if (bad && blockIdx.x == 0) atomicOr(a.err, kErrBadLength);
                 }
             }
-            if (e) {
-                plan.end = p;
-            } else {
-                plan.begin = p;
-                plan.first = x;
-                if (p.b != b) plan.first.n = -1;
+            int64_t all;
+            const int64_t at = before + scan(cost, lane, &all);
+            before += all;
+#pragma unroll 1
+            for (int e = 0; pass == 1 && e < 2; ++e) {
+                const int64_t o = (e ? u[1] : u[0]) - at;
+                if (o < 0 || o >= cost) continue;
+                TurnPos p = turn_locate(s, x, b, o);
+                if (p.t >= turn_tiles(s, x, p.pair) || (a.whole && p.t > 0)) {   // the item's end: the next one's start
+                    p.t = 0;
+                    if (++p.pair >= turn_pairs(s, x)) {
+                        p.pair = 0;
+                        if (++p.g >= s.Hkv) {
+                            p.g = 0;
+                            ++p.b;   // an empty session here is passed over by the walk
+                        }
+                    }
+                }
+                if (e) {
+                    plan.end = p;
+                } else {
+                    plan.begin = p;
+                    plan.first = x;
+                    if (p.b != b) plan.first.n = -1;
+                }
             }
         }
-        before += all;
+        if (pass == 0) {
+            const int pieces = before == 0 ? 0 : turn_pieces(before, gridDim.x), c = blockIdx.x;
+            if (lane == 0) plan.begin = plan.end = {a.B, 0, 0, 0};   // no piece; a last piece's end
+            __syncwarp();
+            if (c >= pieces) return;
+            u[0] = turn_cut(before, pieces, c);
+            u[1] = turn_cut(before, pieces, c + 1);
+        }
     }
     __syncwarp();
 }
 
-// A run of key tiles t0 .. t1 - 1 of one item.
-struct Run {
-    TurnSession x;
-    int b, g, pair, t0, t1, tiles, cached_tiles, own_keys;
-    bool narrow;
-};
-
-// The runs of a piece, in order; every role walks them by itself.
+// The runs of a piece, in order.
 struct Walk {
-    TurnPos at;
+    TurnPos at, end;
     TurnSession x;   // of at.b
-    __device__ Walk(const TurnArgs &a, const Plan &plan) : at(plan.begin), x(plan.first) {
+    __device__ Walk(const TurnArgs &a, const Plan &plan) : at(plan.begin), end(plan.end), x(plan.first) {
         if (at.b < a.B && x.n < 0) x = session_of(a, at.b);
     }
-    __device__ bool next(const TurnArgs &a, const Plan &plan, Run &r) {
+    __device__ bool next(const TurnArgs &a, Run &r) {
         const TurnShape s = turn_shape(a);
-        const TurnPos &end = plan.end;
         while (at.b < a.B) {
             const bool to_end = at.b == end.b && at.g == end.g && at.pair == end.pair;
-            if (to_end && at.t >= end.t) return false;
-            if (x.n == 0) {   // nothing of this session; the end may be its start
-                if (at.b == end.b) return false;
-                at = {at.b + 1, 0, 0, 0};
-                if (at.b < a.B) x = session_of(a, at.b);
-                continue;
-            }
-            r.x = x;
-            r.b = at.b;
-            r.g = at.g;
-            r.pair = at.pair;
-            r.cached_tiles = turn_tiles_of(x.P);
-            r.own_keys = turn_own_keys(s, x, at.pair);
-            r.tiles = r.cached_tiles + turn_tiles_of(r.own_keys);
-            r.narrow = turn_narrow(s, x, at.pair);
-            r.t0 = at.t;
-            r.t1 = to_end ? end.t : r.tiles;
-            if (to_end) {
-                at.t = end.t;
-                return true;
-            }
-            at.t = 0;
-            if (++at.pair >= turn_pairs(s, x)) {
+            if ((to_end && at.t >= end.t) || (x.n == 0 && at.b == end.b)) return false;
+            if (x.n > 0) {
+                r.lo = x.lo;
+                r.n = x.n;
+                r.P = x.P;
+                r.b = at.b;
+                r.g = at.g;
+                r.pair = at.pair;
+                r.cached_tiles = turn_tiles_of(x.P);
+                r.own_keys = turn_own_keys(s, x, at.pair);
+                r.tiles = r.cached_tiles + turn_tiles_of(r.own_keys);
+                r.narrow = turn_narrow(s, x, at.pair);
+                r.t0 = at.t;
+                r.t1 = to_end ? end.t : r.tiles;
+                at.t = r.t1;
+                if (to_end) return true;
+                at.t = 0;
+                if (++at.pair < turn_pairs(s, x)) return true;
                 at.pair = 0;
-                if (++at.g >= s.Hkv) {
-                    at.g = 0;
-                    ++at.b;
-                    if (at.b < a.B) x = session_of(a, at.b);
-                }
+                if (++at.g < s.Hkv) return true;
             }
-            return true;
+            const bool any = x.n > 0;   // else nothing of this session: the next one
+            at = {at.b + 1, 0, 0, 0};
+            if (at.b < a.B) x = session_of(a, at.b);
+            if (any) return true;
         }
         return false;
     }
 };
 
+// The runs as the copies' warp publishes them, for a warp of another role. Each is read once, then given back.
+struct Reader {
+    uint32_t count = 0;
+    __device__ bool next(Smem &sm, Run &r) {
+        const int slot = count % kRuns;
+        if (!__all_sync(~0u, mbar_wait(sm, &sm.run_full[slot], count / kRuns & 1))) return false;
+        r = sm.runs[slot];
+        return r.tiles > 0;
+    }
+    __device__ void done(Smem &sm) {
+        __syncwarp();
+        if (threadIdx.x % 32 == 0) mbar_arrive(&sm.run_empty[count % kRuns]);
+        ++count;
+    }
+};
+
 // Keys of key tile t of an item.
 __device__ __forceinline__ int keys_of(const Run &r, int t) {
-    const int left = t < r.cached_tiles ? r.x.P - t * kTurnKeys : r.own_keys - (t - r.cached_tiles) * kTurnKeys;
+    const int left = t < r.cached_tiles ? r.P - t * kTurnKeys : r.own_keys - (t - r.cached_tiles) * kTurnKeys;
     return min(left, kTurnKeys);
 }
 
@@ -404,7 +410,7 @@ __device__ __forceinline__ int keys_of(const Run &r, int t) {
 // Lane l's block of key tile t: that of its keys 16 l and on, where there are any.
 __device__ __forceinline__ int block_id(const TurnArgs &a, const Run &r, int t, int lane) {
     const int pos = t * kTurnKeys + lane * kBoxRows;
-    if (t >= r.cached_tiles || lane >= kTurnKeys / kBoxRows || pos >= r.x.P) return 0;
+    if (t >= r.cached_tiles || lane >= kTurnKeys / kBoxRows || pos >= r.P) return 0;
     return a.tables[static_cast<int64_t>(r.b) * a.max_blocks + (a.s.bt == 64 ? pos >> 6 : pos >> 4)];
 }
 // The row of the pool (below 2^31) of those keys' K.
@@ -421,9 +427,9 @@ __device__ __forceinline__ int pool_row(const TurnArgs &a, const Run &r, int t, 
 // they hold in memory may be anything, and a weight of 0 does not make a NaN go away in the product with V.
 __device__ __forceinline__ void copy_rest(const uint16_t *src, int64_t step, int rest, uint8_t *stage, int row0,
                                           int half, int group, int lane) {
-#pragma unroll
-    for (int i = 0; i < kBoxRows * 16 / 32; ++i) {
-        const int rr = i * 2 + (lane >> 4), u = lane & 15;   // row, 16-byte unit of the row
+    const int u = lane & 15;   // 16-byte unit of the row
+#pragma unroll 4
+    for (int rr = lane >> 4; rr < kBoxRows; rr += 2) {
         const int row = row0 + rr;
         uint4 x = make_uint4(0u, 0u, 0u, 0u);
         if (rr < rest) x = *reinterpret_cast<const uint4 *>(src + rr * step + u * 8);
@@ -434,58 +440,55 @@ __device__ __forceinline__ void copy_rest(const uint16_t *src, int64_t step, int
     __syncwarp();
 }
 
-// The K (kv = 0) or V tile of cached keys, grouped, by the copy warp; row: pool_row's.
-__device__ __forceinline__ void copy_cached(const TurnArgs &a, const Maps &maps, int keys, int row, int kv,
-                                            uint8_t *stage, uint64_t *full, int lane) {
-    const int groups = keys / kBoxRows, rest = keys % kBoxRows;
+// A K (kv = 0) or V tile into a stage, by the warp: cached keys grouped, a copy per block (row:
+// pool_row's), the call's own whole, one copy for a full tile.
+__device__ __forceinline__ void copy_tile(const TurnArgs &a, const Maps &maps, const Run &r, int t, int row, int kv,
+                                          uint8_t *stage, uint64_t *full, int lane) {
+    const int keys = keys_of(r, t), groups = keys / kBoxRows, rest = keys % kBoxRows;
+    const bool cached = t < r.cached_tiles;
+    const int first = r.lo + (t - r.cached_tiles) * kTurnKeys;   // own keys: row of k_new and v_new
     row += kv * a.s.Hkv * a.s.bt;
     if (rest) {
-        const int first = __shfl_sync(~0u, row, groups);
-        copy_rest(a.hot + static_cast<int64_t>(first) * kHeadDim, kHeadDim, rest, stage, groups * kBoxRows,
-                  kHalfGrouped, kGroupGrouped, lane);
+        const int at = __shfl_sync(~0u, row, groups);
+        const uint16_t *src = cached ? a.hot + static_cast<int64_t>(at) * kHeadDim
+                                     : (kv ? a.v_new : a.k_new) +
+                                           (static_cast<int64_t>(first) + groups * kBoxRows) * a.kv_stride + r.g * kHeadDim;
+        copy_rest(src, cached ? kHeadDim : a.kv_stride, rest, stage, groups * kBoxRows,
+                  cached ? kHalfGrouped : kHalfWhole, cached ? kGroupGrouped : kGroupWhole, lane);
     }
     const bool leader = elected();
     if (leader) mbar_expect(full, groups * kBoxRows * kRowBytes);
-    // Coordinates: (column, row of eight, half, eight rows)
-    int i = 0;
-    if (a.s.bt == 64)   // whole blocks
-        for (; i + 4 <= groups; i += 4) {
-            const int at = __shfl_sync(~0u, row, i) >> 3;
-            if (leader) copy_box(stage + i * 2 * kGroupGrouped, &maps.hot_block, 0, 0, at, full);
-        }
-    if (i == 0 && groups == kTurnKeys / kBoxRows) {
+    // Each copy names its map by itself: with the map selected before, a copy took three times as long to issue.
+    if (cached) {   // coordinates: (column, row of eight, half, eight rows)
+        int i = 0;
+        if (a.s.bt == 64)   // whole blocks
+            for (; i + 4 <= groups; i += 4) {
+                const int at = __shfl_sync(~0u, row, i) >> 3;
+                if (leader) copy_box(stage + i * 2 * kGroupGrouped, &maps.hot_block, 0, 0, at, full);
+            }
+        if (i == 0 && groups == kTurnKeys / kBoxRows) {
 #pragma unroll
-        for (int k = 0; k < kTurnKeys / kBoxRows; ++k) {
-            const int at = __shfl_sync(~0u, row, k) >> 3;
-            if (leader) copy_box(stage + k * 2 * kGroupGrouped, &maps.hot, 0, 0, at, full);
-        }
-    } else {
-        for (; i < groups; ++i) {
-            const int at = __shfl_sync(~0u, row, i) >> 3;
-            if (leader) copy_box(stage + i * 2 * kGroupGrouped, &maps.hot, 0, 0, at, full);
-        }
-    }
-    __syncwarp();
-}
-
-// The same of the call's own keys from row `first` on, whole.
-__device__ __forceinline__ void copy_own(const TurnArgs &a, const Maps &maps, int keys, int first, int g, int kv,
-                                         uint8_t *stage, uint64_t *full, int lane) {
-    const int groups = keys / kBoxRows, rest = keys % kBoxRows;
-    if (rest)
-        copy_rest((kv ? a.v_new : a.k_new) + (static_cast<int64_t>(first) + groups * kBoxRows) * a.kv_stride +
-                      g * kHeadDim,
-                  a.kv_stride, rest, stage, groups * kBoxRows, kHalfWhole, kGroupWhole, lane);
-    if (elected()) {
-        mbar_expect(full, groups * kBoxRows * kRowBytes);
-        // Coordinates: (column, head, token, half), or (column, token, half, head)
-        if (groups == kTurnKeys / kBoxRows) {
-            copy_box(stage, kv ? &maps.v_whole : &maps.k_whole, first, 0, g, full);
+            for (int k = 0; k < kTurnKeys / kBoxRows; ++k) {
+                const int at = __shfl_sync(~0u, row, k) >> 3;
+                if (leader) copy_box(stage + k * 2 * kGroupGrouped, &maps.hot, 0, 0, at, full);
+            }
         } else {
-            for (int i = 0; i < groups; ++i)
-                for (int half = 0; half < 2; ++half)
-                    copy_box(stage + half * kHalfWhole + i * kBoxRows * 128, kv ? &maps.v : &maps.k, g,
-                             first + i * kBoxRows, half, full);
+            for (; i < groups; ++i) {
+                const int at = __shfl_sync(~0u, row, i) >> 3;
+                if (leader) copy_box(stage + i * 2 * kGroupGrouped, &maps.hot, 0, 0, at, full);
+            }
+        }
+    } else if (leader) {
+        if (groups == kTurnKeys / kBoxRows) {   // (column, token, half, head)
+            if (kv) copy_box(stage, &maps.v_whole, first, 0, r.g, full);
+            else copy_box(stage, &maps.k_whole, first, 0, r.g, full);
+        } else {                                // (column, head, token, half)
+#pragma unroll 1
+            for (int i = 0; i < 2 * groups; ++i) {
+                uint8_t *to = stage + (i & 1) * kHalfWhole + (i >> 1) * kBoxRows * 128;
+                if (kv) copy_box(to, &maps.v, r.g, first + (i >> 1) * kBoxRows, i & 1, full);
+                else copy_box(to, &maps.k, r.g, first + (i >> 1) * kBoxRows, i & 1, full);
+            }
         }
     }
     __syncwarp();
@@ -493,42 +496,47 @@ __device__ __forceinline__ void copy_own(const TurnArgs &a, const Maps &maps, in
 
 __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lane) {
     const TurnShape s = turn_shape(a);
-    const int G = a.s.Hq / a.s.Hkv;
     int stage = 0, round = 0, items = 0, pairs = 0;
-    uint32_t filled = 0;   // copies issued so far, saturating at kStages
-    bool ok = true;        // the same in all lanes until the last copy is out
+    uint32_t filled = 0, runs = 0;   // copies issued so far, saturating at kStages; runs published
+    bool ok = true;                  // the same in all lanes until the last copy is out
     Walk walk(a, sm.plan);
-    Run r;
-    while (ok && walk.next(a, sm.plan, r)) {
+#pragma unroll 1
+    while (ok) {
+        Run r;
+        r.tiles = 0;
+        const bool more = walk.next(a, r);
+        if (runs >= kRuns)
+            ok = __all_sync(~0u, mbar_wait(sm, &sm.run_empty[runs % kRuns], (runs / kRuns - 1) & 1));
+        if (ok && lane == 0) {
+            sm.runs[runs % kRuns] = r;
+            mbar_arrive(&sm.run_full[runs % kRuns]);
+        }
+        ++runs;
+        if (!more) break;
         int blk = block_id(a, r, r.t0, lane);
-        if (items > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.q_empty, (items - 1) & 1));
+        if (ok && items > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.q_empty, (items - 1) & 1));
         if (!ok) break;
         ++items;
-        const int tiles = r.narrow ? 1 : 2;
-        pairs += tiles - 1;
+        pairs += !r.narrow;
         if (elected())   // coordinates: (column, head, token, half)
 #pragma unroll 1
-            for (int i = 0; i < tiles; ++i) {
-                const int token = r.x.lo + ((2 * r.pair + i) << s.shift);
+            for (int i = 0; i < (r.narrow ? 1 : 2); ++i) {
+                const int token = r.lo + ((2 * r.pair + i) << s.shift);
                 mbar_expect(&sm.q_full[i], kTileBytes);
-                copy_box(sm.q[i], &maps.q, r.g * G, token, 0, &sm.q_full[i]);
-                copy_box(sm.q[i] + kHalfWhole, &maps.q, r.g * G, token, 1, &sm.q_full[i]);
+                copy_box(sm.q[i], &maps.q, r.g << (7 - s.shift), token, 0, &sm.q_full[i]);
+                copy_box(sm.q[i] + kHalfWhole, &maps.q, r.g << (7 - s.shift), token, 1, &sm.q_full[i]);
             }
         __syncwarp();
+#pragma unroll 1
         for (int t = r.t0; ok && t < r.t1; ++t) {
-            const int keys = keys_of(r, t);
             const int row = pool_row(a, r, t, blk, lane);
             // The next tile's block ids are on their way while this one's copies go out.
             if (t + 1 < r.t1) blk = block_id(a, r, t + 1, lane);
+#pragma unroll 1
             for (int kv = 0; kv < 2; ++kv) {
                 if (round > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.kv_empty[stage], (round - 1) & 1));
                 if (!ok) break;
-                uint64_t *full = &sm.kv_full[stage + (round & 1) * kStages];
-                if (t < r.cached_tiles)
-                    copy_cached(a, maps, keys, row, kv, sm.kv[stage], full, lane);
-                else
-                    copy_own(a, maps, keys, r.x.lo + (t - r.cached_tiles) * kTurnKeys, r.g, kv, sm.kv[stage], full,
-                             lane);
+                copy_tile(a, maps, r, t, row, kv, sm.kv[stage], &sm.kv_full[stage + (round & 1) * kStages], lane);
                 if (filled < kStages) ++filled;
                 if (++stage == kStages) {
                     stage = 0;
@@ -539,6 +547,7 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
     }
     // Every copy lands before the CTA ends, whatever became of the other roles; with all well,
     // every stage has been given back as well.
+#pragma unroll 1
     for (uint32_t i = 0; i < filled; ++i) {
         const bool now = static_cast<int>(i) < stage;   // filled in this round, or in the one before
         const int last = now ? round : round - 1;
@@ -547,6 +556,7 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
         while (!mbar_try(&sm.kv_full[i + (last & 1) * kStages], last >> 1 & 1) && global_ns() - t0 < kWaitLimitNs) {}
     }
     if (ok && items > 0) ok = mbar_wait(sm, &sm.q_empty, (items - 1) & 1);
+#pragma unroll 1
     for (int i = 0; !ok && i < 2; ++i) {   // and the last q tiles
         const int loads = i ? pairs : items;
         const unsigned long long t0 = global_ns();
@@ -592,12 +602,14 @@ __device__ void mma_role(const TurnArgs &a, Smem &sm, int stream) {
     uint32_t base = 0;   // tiles of the runs before: tile n has K at place 2n of the ring's sequence, V at 2n + 1
     bool ok = true;
     auto wait = [&](uint64_t *bar, uint32_t parity) { ok = __all_sync(~0u, mbar_wait(sm, bar, parity)); };
-    Walk walk(a, sm.plan);
+    Reader reader;
     Run r;
-    while (ok && __all_sync(~0u, walk.next(a, sm.plan, r))) {
+#pragma unroll 1
+    while (ok && reader.next(sm, r)) {
         const int tiles = uniform(r.t1 - r.t0), t0 = uniform(r.t0), cached_tiles = uniform(r.cached_tiles);
-        const int cached_keys = uniform(r.x.P), own_keys = uniform(r.own_keys);
+        const int cached_keys = uniform(r.P), own_keys = uniform(r.own_keys);
         const bool narrow = uniform(r.narrow);
+        reader.done(sm);
         const int by = narrow ? 2 : 1, first = narrow ? stream : 0;
         auto steps_of = [&](int i) {   // of 16 keys, of the run's tile i
             const int t = t0 + i;
@@ -618,64 +630,51 @@ __device__ void mma_role(const TurnArgs &a, Smem &sm, int stream) {
         auto landed = [&](uint32_t place) {
             if (ok) wait(&sm.kv_full[place % (2 * kStages)], place / (2 * kStages) & 1);
         };
-        auto weights = [&] {
-            if (ok) wait(&sm.p_full[stream], p_phase);
-            p_phase ^= 1;
-        };
-        auto issue_pv = [&](int i) {   // O += P V of the run's tile i
-            const int stage = (2 * (base + i) + 1) % kStages, steps = steps_of(i);
-            const uint32_t v = smem_u32(sm.kv[stage]);
-            product_pv(o_col, s_col, v, t0 + i < cached_tiles, steps, i > first);
-            give_back(stage);
-            if (i + by >= tiles) mma_commit(&sm.o_full[stream]);
-        };
-        auto issue_qk = [&](int i) {   // S = Q K^T
-            const int stage = 2 * (base + i) % kStages;
-            const uint32_t k = smem_u32(sm.kv[stage]), form = mma_form(16 * steps_of(i), false, negate);
-            product_qk(s_col, smem_u32(sm.q[q]), k, t0 + i < cached_tiles, form);
-            mma_commit(&sm.s_full[stream]);
-            give_back(stage);
-            if (i + by >= tiles) mma_commit(&sm.q_empty);
-        };
         if (first >= tiles && elected()) mma_commit(&sm.q_empty);   // no tile for this stream
         __syncwarp();
-        // Step i: the products with V of tile i - by, then those with K of tile i, whose scores take the weights' place.
+        // Step i: the products with V of tile i - by, then those with K of tile i, whose scores take the weights'
+        // place.
+#pragma unroll 1
         for (int i = first; ok && first < tiles && i < tiles + by; i += by) {
             const bool has_v = i > first, has_k = i < tiles;
-            if (narrow) {
-                // Such an item waits for HBM: V's stage is given back before K is asked for.
-                if (has_v) {
-                    landed(2 * (base + i - by) + 1);
-                    weights();
-                    fence_after();
-                    if (ok && elected()) issue_pv(i - by);
-                    __syncwarp();
-                }
-                if (has_k) {
-                    landed(2 * (base + i));
-                    fence_after();
-                    if (ok && elected()) issue_qk(i);
-                    __syncwarp();
-                }
-            } else {
-                // A pair's waits for its weights; K is there by then. One stream's products go out without
-                // the other's between them: taking turns step by step, both streams' softmax would wait for
-                // both products, and then both products for the softmax.
-                if (has_k) landed(2 * (base + i));
-                if (has_v) {
-                    landed(2 * (base + i - by) + 1);
-                    weights();
-                }
-                fence_after();
-                if (ok && elected()) {
-                    // (Order is all that this decides: past the limit, which no holder needs, they mix.)
-                    for (int n = 0; n < 1 << 16 && atomicCAS_block(&sm.issuing, 0, 1) != 0; ++n) {}
-                    if (has_v) issue_pv(i - by);
-                    if (has_k) issue_qk(i);
-                    atomicExch_block(&sm.issuing, 0);
-                }
-                __syncwarp();
+            const uint32_t k_place = 2 * (base + i), v_place = 2 * (base + i - by) + 1;
+            // A pair's products wait for their weights; K is there by then. One stream's go out without the
+            // other's between them: taking turns step by step, both streams' softmax would wait for both
+            // products, and then both products for the softmax. (Order is all that the lock decides: past the
+            // limit, which no holder needs, they mix.) A narrow item waits for HBM: V's stage is given back
+            // before K is asked for.
+            if (!narrow && has_k) landed(k_place);
+            if (has_v) {
+                landed(v_place);
+                if (ok) wait(&sm.p_full[stream], p_phase);
+                p_phase ^= 1;
             }
+            fence_after();
+            const bool leader = elected();
+            if (ok && leader && !narrow)
+                for (int n = 0; n < 1 << 16 && atomicCAS_block(&sm.issuing, 0, 1) != 0; ++n) {}
+            if (ok && leader && has_v) {   // O += P V
+                const int stage = v_place % kStages;
+                product_pv(o_col, s_col, smem_u32(sm.kv[stage]), t0 + i - by < cached_tiles, steps_of(i - by),
+                           i - by > first);
+                give_back(stage);
+                if (!has_k) mma_commit(&sm.o_full[stream]);
+            }
+            __syncwarp();
+            if (narrow && has_k) {
+                landed(k_place);
+                fence_after();
+            }
+            if (ok && leader && has_k) {   // S = Q K^T
+                const int stage = k_place % kStages;
+                product_qk(s_col, smem_u32(sm.q[q]), smem_u32(sm.kv[stage]), t0 + i < cached_tiles,
+                           mma_form(16 * steps_of(i), false, negate));
+                mma_commit(&sm.s_full[stream]);
+                give_back(stage);
+                if (i + by >= tiles) mma_commit(&sm.q_empty);
+            }
+            if (ok && leader && !narrow) atomicExch_block(&sm.issuing, 0);
+            __syncwarp();
         }
         base += tiles;
     }
@@ -773,9 +772,8 @@ __device__ __forceinline__ void hide(uint32_t (&x)[16], uint32_t sees) {
         if (!(sees >> i & 1)) x[i] = 0xFF800000u;
 }
 
-// What this warp has put into tensor memory is there, for the products.
-__device__ __forceinline__ void weights_there(uint64_t *bar) {
-    tmem_stored();
+// This warp is done with tensor memory and what it has written up to here.
+__device__ __forceinline__ void warp_done(uint64_t *bar) {
     fence_before();
     __syncwarp();
     if (threadIdx.x % 32 == 0) mbar_arrive(bar);
@@ -878,25 +876,27 @@ __device__ __forceinline__ uint4 units_of(const uint32_t (&w)[4], int lane) {
 
 // The new tokens' K and V into their slots of the pool, by one warp beside the others' work, a token's
 // K and V rows of the item's kv-head at a time: each item's once, by the piece that has its last key tile.
-__device__ void store_role(const TurnArgs &a, const Smem &sm, int lane) {
+__device__ void store_role(const TurnArgs &a, Smem &sm, int lane) {
     const Shape &sh = a.s;
     const TurnShape s = turn_shape(a);
     const int kv = lane >> 4, c = lane & 15, bt_shift = sh.bt == 64 ? 6 : 4;
-    Walk walk(a, sm.plan);
+    Reader reader;
     Run r;
-    while (walk.next(a, sm.plan, r)) {
-        if (r.t1 != r.tiles) continue;
-        const int i0 = r.pair << (s.shift + 1), i1 = min(i0 + (2 << s.shift), r.x.n);
-        const uint16_t *src = (kv ? a.v_new : a.k_new) + r.x.lo * a.kv_stride + r.g * kHeadDim + c * 8;
+#pragma unroll 1
+    for (; reader.next(sm, r); reader.done(sm)) {
+        if (a.masks || r.t1 != r.tiles) continue;
+        const int i0 = r.pair << (s.shift + 1), i1 = min(i0 + (2 << s.shift), r.n);
+        const uint16_t *src = (kv ? a.v_new : a.k_new) + r.lo * a.kv_stride + r.g * kHeadDim + c * 8;
         const int32_t *table = a.tables + static_cast<int64_t>(r.b) * a.max_blocks;
         constexpr int kAhead = 4;
+#pragma unroll 1
         for (int i = i0; i < i1; i += kAhead) {
             uint4 x[kAhead];
             int blk[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
                 if (i + k < i1) {
-                    blk[k] = table[(r.x.P + i + k) >> bt_shift];
+                    blk[k] = table[(r.P + i + k) >> bt_shift];
                     x[k] = *reinterpret_cast<const uint4 *>(src + (i + k) * a.kv_stride);
                 }
 #pragma unroll
@@ -907,7 +907,7 @@ __device__ void store_role(const TurnArgs &a, const Smem &sm, int lane) {
                     continue;
                 }
                 const int row = (((blk[k] * sh.L + a.layer) * 2 + kv) * sh.Hkv + r.g) * sh.bt +
-                                ((r.x.P + i + k) & (sh.bt - 1));
+                                ((r.P + i + k) & (sh.bt - 1));
                 reinterpret_cast<uint4 *>(a.hot + static_cast<int64_t>(row) * kHeadDim)[c] = x[k];
             }
         }
@@ -921,23 +921,23 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
     const uint32_t lanes = static_cast<uint32_t>(row & ~31) << 16;   // a warp has 32 lanes of tensor memory
     const uint32_t tmem = sm.tmem + lanes;
     const uint32_t s_addr = tmem + kColS + stream * kColStream, o_addr = tmem + kColO + stream * kColStream;
-    uint32_t s_phase = 0, o_phase = 0;
-    // A wait that ran out ends this warp's work, but not its walk: the barriers below count on every warp.
-    bool ok = true;
+    uint32_t s_phase = 0, o_phase = 0, other_phase = 0;
+    bool ok = true;   // the same in a warp's lanes
     auto wait = [&](uint64_t *bar, uint32_t &phase) {
         ok = __all_sync(~0u, ok && mbar_wait(sm, bar, phase));
         phase ^= 1;
         fence_after();
     };
     PartRecord rec = {0, 0, 0, 0, 0};
-    Walk walk(a, sm.plan);
+    Reader reader;
     Run r;
-    while (walk.next(a, sm.plan, r)) {
+#pragma unroll 1
+    for (; ok && reader.next(sm, r); reader.done(sm)) {
         const int tile = r.narrow ? 2 * r.pair : 2 * r.pair + stream;
         const int token = (tile << s.shift) + (row >> g_shift);   // of the session's new ones
-        const bool live = token < r.x.n;
+        const bool live = token < r.n;
         uint64_t mask = 0;
-        if (a.masks && live) mask = a.masks[r.x.lo + token];
+        if (a.masks && live) mask = a.masks[r.lo + token];
         Stats st = {-INFINITY, 0.f};
         const int step = r.narrow ? 2 : 1;
         const int t_first = r.narrow ? r.t0 + stream : r.t0;
@@ -945,7 +945,8 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
             wait(&sm.s_full[stream], s_phase);
             if (!ok) break;
             softmax_tile(a, r, t, token, mask, s_addr, o_addr, t == t_first, st);
-            weights_there(&sm.p_full[stream]);
+            tmem_stored();
+            warp_done(&sm.p_full[stream]);
         }
         if (ok && t_first < r.t1) wait(&sm.o_full[stream], o_phase);
         // A narrow item: stream 0 takes both streams' results together.
@@ -955,9 +956,12 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
             if (stream == 1) {
                 sm.other_m[row] = st.m;
                 sm.other_l[row] = st.l;
+                warp_done(&sm.other_ready);
+                wait(&sm.other_free, other_phase);   // before the next product into this O
+                continue;
             }
-            sync_threads(3, 2 * kTurnRows);
-            if (stream == 0 && r.t1 - r.t0 > 1) {
+            wait(&sm.other_ready, other_phase);
+            if (r.t1 - r.t0 > 1) {
                 const float m1 = sm.other_m[row], l1 = sm.other_l[row], m = fmaxf(st.m, m1);
                 const float ref = m == -INFINITY ? 0.f : m;
                 w = ex2(st.m - ref);
@@ -967,7 +971,7 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
                 other = tmem + kColO + kColStream;
             }
         }
-        if (!(r.narrow && stream == 1)) {
+        {
             const bool whole = r.t0 == 0 && r.t1 == r.tiles;
             const int slot = r.t0 > 0 ? 2 * blockIdx.x : 2 * blockIdx.x + 1;
             if (whole) {
@@ -978,7 +982,7 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
                 if (live) part_ml(a, slot, stream)[row] = make_float2(st.m, st.l);
                 if (stream == 0 && row == 0) {
                     const int t0 = r.pair << (s.shift + 1);
-                    if (r.t0 == 0) rec = {1, 0, r.x.lo + t0, min(2 << s.shift, r.x.n - t0), r.g};
+                    if (r.t0 == 0) rec = {1, 0, r.lo + t0, min(2 << s.shift, r.n - t0), r.g};
                     else if (r.t1 < r.tiles) rec.through = 1;
                 }
             }
@@ -986,9 +990,11 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
             // 32 bytes of eight rows; with a row per thread each store had 16 bytes of 32 rows, and an
             // item's end took 6 700 cycles (2 000). Short code, as above.
             const int lane = row & 31;
-#pragma unroll 1
-            for (int part = 0; ok && part < 8; ++part) {
+            const uint32_t some = __ballot_sync(~0u, live);
+#pragma unroll 2
+            for (int part = 0; part < 8; ++part) {
                 const int half = part >> 2 << 4, d = (part & 3) * 32;   // first row of the warp's, first column
+                if (!ok || !(some >> half & 0xFFFFu)) continue;
                 uint32_t x[16];
                 float y[16], scale[2], scale_other[2];
                 tmem_load_rows(x, o_addr + (half << 16) + d);
@@ -1010,8 +1016,8 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
                 for (int i = 0; i < 2; ++i) {
                     const int its = (row & ~31) + half + i * 8 + (lane >> 2);
                     const int t = (tile << s.shift) + (its >> g_shift);
-                    const bool there = t < r.x.n;
-                    const int64_t to = (static_cast<int64_t>(r.x.lo) + t) * a.s.Hq + (r.g << g_shift) +
+                    const bool there = t < r.n;
+                    const int64_t to = (static_cast<int64_t>(r.lo) + t) * a.s.Hq + (r.g << g_shift) +
                                        (its & ((1 << g_shift) - 1));
                     if (whole && a.out_bf16) {
                         uint32_t v[4];
@@ -1032,8 +1038,7 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
             }
         }
         fence_before();
-        // Stream 1's O is free for its next product once stream 0 has read it.
-        if (r.narrow) sync_threads(3, 2 * kTurnRows);
+        if (r.narrow) warp_done(&sm.other_free);
     }
     if (!a.whole && stream == 0 && row == 0) *part_record(a, blockIdx.x) = rec;
 }
@@ -1046,8 +1051,7 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (warp == kStoreWarp && lane < sizeof(Maps) / sizeof(CUtensorMap))
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<const CUtensorMap *>(&maps) + lane) : "memory");
-    if (warp == kCopyWarp) make_plan(a, sm.plan, lane);
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 32) {   // a warp that has nothing else to do yet
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&sm.kv_full[i], 1);
             mbar_init(&sm.kv_full[i + kStages], 1);
@@ -1060,11 +1064,18 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
             mbar_init(&sm.o_full[s], 1);
             mbar_init(&sm.drained[s], 1);
         }
+        for (int i = 0; i < kRuns; ++i) {
+            mbar_init(&sm.run_full[i], 1);
+            mbar_init(&sm.run_empty[i], kRunReaders);
+        }
+        mbar_init(&sm.other_ready, kTurnRows / 32);
+        mbar_init(&sm.other_free, kTurnRows / 32);
         mbar_init(&sm.q_empty, 2);
         sm.abort = 0;
         sm.issuing = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == kCopyWarp) make_plan(a, sm.plan, lane);
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)),
                      "r"(kTmemCols)
@@ -1074,18 +1085,14 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
     fence_before();
     __syncthreads();
     fence_after();
-    if (blockIdx.x < sm.plan.pieces) {
-        if (warp < 8) {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-            softmax_role(a, sm, warp >> 2);
-        } else {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-            if (warp == kCopyWarp) copy_role(a, maps, sm, lane);
-            else if (warp < kMmaWarp + 2) mma_role(a, sm, warp - kMmaWarp);
-            else if (warp == kStoreWarp && !a.masks) store_role(a, sm, lane);
-        }
-    } else if (threadIdx.x == 0 && !a.whole) {
-        *part_record(a, blockIdx.x) = {0, 0, 0, 0, 0};
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+        softmax_role(a, sm, warp >> 2);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+        if (warp == kCopyWarp) copy_role(a, maps, sm, lane);
+        else if (warp < kMmaWarp + 2) mma_role(a, sm, warp - kMmaWarp);
+        else store_role(a, sm, lane);
     }
     __syncwarp();
     fence_before();
@@ -1108,8 +1115,15 @@ __global__ void __launch_bounds__(kCombineWarps * 32) turn_combine_kernel(const 
     if (!rec.opens) return;
     const int row0 = blockIdx.y * kCombineWarps + (threadIdx.x >> 5), rows = rec.tokens << g_shift;
     if (row0 >= rows) return;
-    int last = first + 1;
-    while (last + 1 < a.part_slots / 2 && part_record(a, last)->through) ++last;
+    int last = first + 1;   // the first piece that the item does not pass through
+    for (;; last += 32) {
+        const int c = last + lane;
+        const uint32_t ends = __ballot_sync(~0u, c >= a.part_slots / 2 || !part_record(a, c)->through);
+        if (ends) {
+            last += __ffs(ends) - 1;
+            break;
+        }
+    }
     const auto slot = [&](int c) { return c == first ? 2 * c + 1 : 2 * c; };
     constexpr int kApart = kCombineCtas * kCombineWarps;
     const auto stream_of = [&](int i) { return (row0 + i * kApart) / kTurnRows; };
