@@ -991,47 +991,58 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
             // item's end took 6 700 cycles (2 000). Short code, as above.
             const int lane = row & 31;
             const uint32_t some = __ballot_sync(~0u, live);
-#pragma unroll 2
-            for (int part = 0; part < 8; ++part) {
-                const int half = part >> 2 << 4, d = (part & 3) * 32;   // first row of the warp's, first column
+            const bool bf16 = whole && a.out_bf16;
+#pragma unroll 1
+            for (int half = 0; half < 32; half += 16) {
                 if (!ok || !(some >> half & 0xFFFFu)) continue;
-                uint32_t x[16];
-                float y[16], scale[2], scale_other[2];
-                tmem_load_rows(x, o_addr + (half << 16) + d);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {   // this thread's rows: half + lane / 4, and 8 on
-                    scale[i] = __shfl_sync(~0u, w, half + i * 8 + (lane >> 2));
-                    scale_other[i] = __shfl_sync(~0u, w_other, half + i * 8 + (lane >> 2));
-                }
-                tmem_wait(x);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(x[i]) * scale[i >> 1 & 1];
-                if (other) {
-                    tmem_load_rows(x, other + (half << 16) + d);
-                    tmem_wait(x);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) y[i] = __fmaf_rn(__uint_as_float(x[i]), scale_other[i >> 1 & 1], y[i]);
-                }
+                // This thread's rows, lane / 4 and 8 on: factors, and where their values go.
+                float scale[2], scale_other[2];
+                bool there[2];
+                uint8_t *to[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int its = (row & ~31) + half + i * 8 + (lane >> 2);
+                    const int from = half + i * 8 + (lane >> 2), its = (row & ~31) + from;
                     const int t = (tile << s.shift) + (its >> g_shift);
-                    const bool there = t < r.n;
-                    const int64_t to = (static_cast<int64_t>(r.lo) + t) * a.s.Hq + (r.g << g_shift) +
-                                       (its & ((1 << g_shift) - 1));
-                    if (whole && a.out_bf16) {
-                        uint32_t v[4];
+                    const int64_t o_row = (static_cast<int64_t>(r.lo) + t) * a.s.Hq + (r.g << g_shift) +
+                                          (its & ((1 << g_shift) - 1));
+                    scale[i] = __shfl_sync(~0u, w, from);
+                    scale_other[i] = __shfl_sync(~0u, w_other, from);
+                    there[i] = t < r.n;
+                    to[i] = bf16    ? static_cast<uint8_t *>(a.out) + o_row * kRowBytes + (lane & 3) * 16
+                            : whole ? static_cast<uint8_t *>(a.out) + o_row * (2 * kRowBytes) + (lane & 3) * 8
+                                    : reinterpret_cast<uint8_t *>(part_o(a, slot, stream) + its * kHeadDim) + (lane & 3) * 8;
+                }
+#pragma unroll 2
+                for (int d = 0; d < kHeadDim; d += 32) {
+                    uint32_t x[16];
+                    float y[16];
+                    tmem_load_rows(x, o_addr + (half << 16) + d);
+                    tmem_wait(x);
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) v[g] = pack_bf16(y[4 * g + 2 * i], y[4 * g + 2 * i + 1]);
-                        const uint4 unit = units_of(v, lane);
-                        if (there)
-                            reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + to * kHeadDim + d)[lane & 3] = unit;
-                    } else if (there) {
-                        float2 *f = reinterpret_cast<float2 *>((whole ? static_cast<float *>(a.out) + to * kHeadDim
-                                                                      : part_o(a, slot, stream) + its * kHeadDim) + d) +
-                                    (lane & 3);
+                    for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(x[i]) * scale[i >> 1 & 1];
+                    if (other) {
+                        tmem_load_rows(x, other + (half << 16) + d);
+                        tmem_wait(x);
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) f[g * 4] = make_float2(y[4 * g + 2 * i], y[4 * g + 2 * i + 1]);
+                        for (int i = 0; i < 16; ++i) y[i] = __fmaf_rn(__uint_as_float(x[i]), scale_other[i >> 1 & 1], y[i]);
+                    }
+                    if (bf16) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) v[g] = pack_bf16(y[4 * g + 2 * i], y[4 * g + 2 * i + 1]);
+                            const uint4 unit = units_of(v, lane);
+                            if (there[i]) *reinterpret_cast<uint4 *>(to[i] + d * 2) = unit;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int g = 0; g < 4; ++g)
+                                if (there[i])
+                                    *reinterpret_cast<float2 *>(to[i] + d * 4 + g * 32) =
+                                        make_float2(y[4 * g + 2 * i], y[4 * g + 2 * i + 1]);
                     }
                     __syncwarp();
                 }
