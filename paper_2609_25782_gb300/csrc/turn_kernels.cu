@@ -428,13 +428,17 @@ __device__ __forceinline__ int pool_row(const TurnArgs &a, const Run &r, int t, 
 __device__ __forceinline__ void copy_rest(const uint16_t *src, int64_t step, int rest, uint8_t *stage, int row0,
                                           int half, int group, int lane) {
     const int u = lane & 15;   // 16-byte unit of the row
-#pragma unroll 4
-    for (int rr = lane >> 4; rr < kBoxRows; rr += 2) {
-        const int row = row0 + rr;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (rr < rest) x = *reinterpret_cast<const uint4 *>(src + rr * step + u * 8);
+    constexpr int kEach = kBoxRows / 2;
+    uint4 x[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)   // no branch, so that all are on their way together
+        x[i] = *reinterpret_cast<const uint4 *>(src + min(2 * i + (lane >> 4), rest - 1) * step + u * 8);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int rr = 2 * i + (lane >> 4), row = row0 + rr;
+        if (rr >= rest) x[i] = make_uint4(0u, 0u, 0u, 0u);
         *reinterpret_cast<uint4 *>(stage + (row >> 3) * group + (u >> 3) * half + (row & 7) * 128 +
-                                   (((u & 7) ^ (row & 7)) << 4)) = x;
+                                   (((u & 7) ^ (row & 7)) << 4)) = x[i];
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
