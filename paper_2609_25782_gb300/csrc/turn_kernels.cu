@@ -41,7 +41,7 @@ constexpr int kThreads = 384;
 constexpr int kCopyWarp = 8, kMmaWarp = 9, kStoreWarp = 11;
 // Registers per thread: at launch, then of the softmax warps and of the others. A softmax thread
 // keeps its row's 128 scores; the shares add up to what the CTA was launched with.
-constexpr int kRegsLaunch = 168, kRegsSoftmax = 192, kRegsOther = 120;
+constexpr int kRegsLaunch = 168, kRegsSoftmax = 184, kRegsOther = 136;
 static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * kRegsLaunch, "a larger share would wait forever");
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s
 
@@ -83,7 +83,7 @@ constexpr int kSmemBytes = sizeof(Smem) + 1024;     // and the way to a 1 024-by
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of a CTA");
 
 struct Maps {
-    CUtensorMap q;                       // [token][head] rows, a half row tile a copy
+    CUtensorMap q;                       // [half][token][head] rows, a row tile a copy
     CUtensorMap k, v, k_whole, v_whole;  // kBoxRows rows' halves a copy, or a tile
     CUtensorMap hot, hot_block;          // kBoxRows grouped rows a copy, or a block
 };
@@ -423,45 +423,40 @@ __device__ __forceinline__ int pool_row(const TurnArgs &a, const Run &r, int t, 
     return ((blk * sh.L + a.layer) * 2 * sh.Hkv + r.g) * sh.bt + ((t * kTurnKeys + lane * kBoxRows) & (sh.bt - 1));
 }
 
-// The keys past the last full group of 16, by plain loads; rows up to the group's end are cleared: what
-// they hold in memory may be anything, and a weight of 0 does not make a NaN go away in the product with V.
-__device__ __forceinline__ void copy_rest(const uint16_t *src, int64_t step, int rest, uint8_t *stage, int row0,
-                                          int half, int group, int lane) {
-    const int u = lane & 15;   // 16-byte unit of the row
-    constexpr int kEach = kBoxRows / 2;
-    uint4 x[kEach];
+// The keys past a tile's last full group of 16 come by plain loads, and rows up to the group's end are
+// cleared: what they hold in memory may be anything, and a weight of 0 does not make a NaN go away in the
+// product with V. A lane has 16 bytes of every other row. The loads go out before the copies wait for a
+// stage: one after the other, or after that wait, they held up every item's end by thousands of cycles.
+constexpr int kRestRows = kBoxRows / 2;
+struct Rest {
+    uint4 x[kRestRows];
+};
+__device__ __forceinline__ void load_rest(Rest &r, const uint16_t *src, int64_t step, int rest, int lane) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)   // no branch, so that all are on their way together
-        x[i] = *reinterpret_cast<const uint4 *>(src + min(2 * i + (lane >> 4), rest - 1) * step + u * 8);
+    for (int i = 0; i < kRestRows; ++i)   // no branch, so that all are on their way together
+        r.x[i] = *reinterpret_cast<const uint4 *>(src + min(2 * i + (lane >> 4), rest - 1) * step + (lane & 15) * 8);
+}
+__device__ __forceinline__ void store_rest(Rest &r, int rest, uint8_t *stage, int row0, bool grouped, int lane) {
+    const int u = lane & 15, half = grouped ? kHalfGrouped : kHalfWhole, group = grouped ? kGroupGrouped : kGroupWhole;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
+    for (int i = 0; i < kRestRows; ++i) {
         const int rr = 2 * i + (lane >> 4), row = row0 + rr;
-        if (rr >= rest) x[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (rr >= rest) r.x[i] = make_uint4(0u, 0u, 0u, 0u);
         *reinterpret_cast<uint4 *>(stage + (row >> 3) * group + (u >> 3) * half + (row & 7) * 128 +
-                                   (((u & 7) ^ (row & 7)) << 4)) = x[i];
+                                   (((u & 7) ^ (row & 7)) << 4)) = r.x[i];
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
 }
 
-// A K (kv = 0) or V tile into a stage, by the warp: cached keys grouped, a copy per block (row:
-// pool_row's), the call's own whole, one copy for a full tile.
-__device__ __forceinline__ void copy_tile(const TurnArgs &a, const Maps &maps, const Run &r, int t, int row, int kv,
-                                          uint8_t *stage, uint64_t *full, int lane) {
-    const int keys = keys_of(r, t), groups = keys / kBoxRows, rest = keys % kBoxRows;
-    const bool cached = t < r.cached_tiles;
-    const int first = r.lo + (t - r.cached_tiles) * kTurnKeys;   // own keys: row of k_new and v_new
-    row += kv * a.s.Hkv * a.s.bt;
-    if (rest) {
-        const int at = __shfl_sync(~0u, row, groups);
-        const uint16_t *src = cached ? a.hot + static_cast<int64_t>(at) * kHeadDim
-                                     : (kv ? a.v_new : a.k_new) +
-                                           (static_cast<int64_t>(first) + groups * kBoxRows) * a.kv_stride + r.g * kHeadDim;
-        copy_rest(src, cached ? kHeadDim : a.kv_stride, rest, stage, groups * kBoxRows,
-                  cached ? kHalfGrouped : kHalfWhole, cached ? kGroupGrouped : kGroupWhole, lane);
-    }
+// The full groups of a K (kv = 0) or V tile into a stage, by the warp: cached keys grouped, a copy per
+// block (row: that of the lane's keys), the call's own whole.
+__device__ __forceinline__ void copy_groups(const TurnArgs &a, const Maps &maps, const Run &r, int groups, int rest, bool cached,
+                                            int first, int row, int kv, uint8_t *stage, uint64_t *full) {
     const bool leader = elected();
-    if (leader) mbar_expect(full, groups * kBoxRows * kRowBytes);
+    // Own keys that fill their groups come in one copy; rows past them, of later tokens or other sessions,
+    // are not read.
+    if (leader) mbar_expect(full, cached || rest ? groups * kBoxRows * kRowBytes : kTileBytes);
     // Each copy names its map by itself: with the map selected before, a copy took three times as long to issue.
     if (cached) {   // coordinates: (column, row of eight, half, eight rows)
         int i = 0;
@@ -483,7 +478,7 @@ __device__ __forceinline__ void copy_tile(const TurnArgs &a, const Maps &maps, c
             }
         }
     } else if (leader) {
-        if (groups == kTurnKeys / kBoxRows) {   // (column, token, half, head)
+        if (!rest) {                            // (column, token, half, head)
             if (kv) copy_box(stage, &maps.v_whole, first, 0, r.g, full);
             else copy_box(stage, &maps.k_whole, first, 0, r.g, full);
         } else {                                // (column, head, token, half)
@@ -525,22 +520,38 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
         if (elected())   // coordinates: (column, head, token, half)
 #pragma unroll 1
             for (int i = 0; i < (r.narrow ? 1 : 2); ++i) {
-                const int token = r.lo + ((2 * r.pair + i) << s.shift);
                 mbar_expect(&sm.q_full[i], kTileBytes);
-                copy_box(sm.q[i], &maps.q, r.g << (7 - s.shift), token, 0, &sm.q_full[i]);
-                copy_box(sm.q[i] + kHalfWhole, &maps.q, r.g << (7 - s.shift), token, 1, &sm.q_full[i]);
+                copy_box(sm.q[i], &maps.q, r.g << (7 - s.shift), r.lo + ((2 * r.pair + i) << s.shift), 0, &sm.q_full[i]);
             }
         __syncwarp();
 #pragma unroll 1
         for (int t = r.t0; ok && t < r.t1; ++t) {
-            const int row = pool_row(a, r, t, blk, lane);
+            const int keys = keys_of(r, t), groups = keys / kBoxRows, rest = keys % kBoxRows;
+            const bool cached = t < r.cached_tiles;
+            const int first = r.lo + (t - r.cached_tiles) * kTurnKeys;   // own keys: row of k_new and v_new
+            const int row = pool_row(a, r, t, blk, lane), v_rows = a.s.Hkv * a.s.bt;
+            Rest extra;
+            const uint16_t *rest_k = nullptr, *rest_v = nullptr;
+            const int64_t step = cached ? kHeadDim : a.kv_stride;
+            if (rest) {
+                const int at = __shfl_sync(~0u, row, groups);
+                const int64_t own = (static_cast<int64_t>(first) + groups * kBoxRows) * a.kv_stride + r.g * kHeadDim;
+                rest_k = cached ? a.hot + static_cast<int64_t>(at) * kHeadDim : a.k_new + own;
+                rest_v = cached ? rest_k + static_cast<int64_t>(v_rows) * kHeadDim : a.v_new + own;
+                load_rest(extra, rest_k, step, rest, lane);
+            }
             // The next tile's block ids are on their way while this one's copies go out.
             if (t + 1 < r.t1) blk = block_id(a, r, t + 1, lane);
 #pragma unroll 1
             for (int kv = 0; kv < 2; ++kv) {
-                if (round > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.kv_empty[stage], (round - 1) & 1));
+                if (ok && round > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.kv_empty[stage], (round - 1) & 1));
                 if (!ok) break;
-                copy_tile(a, maps, r, t, row, kv, sm.kv[stage], &sm.kv_full[stage + (round & 1) * kStages], lane);
+                if (rest) {
+                    store_rest(extra, rest, sm.kv[stage], groups * kBoxRows, cached, lane);
+                    if (kv == 0) load_rest(extra, rest_v, step, rest, lane);
+                }
+                copy_groups(a, maps, r, groups, rest, cached, first, row + kv * v_rows, kv, sm.kv[stage],
+                            &sm.kv_full[stage + (round & 1) * kStages]);
                 if (filled < kStages) ++filled;
                 if (++stage == kStages) {
                     stage = 0;
@@ -1232,7 +1243,7 @@ cudaError_t launch_turn(TurnArgs a, const CUtensorMap hot[2], cudaStream_t st) {
     // [half][token][head][64 columns], and for whole tiles [head][half][token][64 columns]
     const cuuint32_t per_tile = static_cast<cuuint32_t>(kTurnRows / G);
     bool ok = encode(&maps.q, a.q, {64, static_cast<cuuint64_t>(a.s.Hq), n, 2}, {kRowBytes, q_step, 128},
-                     {64, static_cast<cuuint32_t>(G), per_tile, 1});
+                     {64, static_cast<cuuint32_t>(G), per_tile, 2});
     for (int kv = 0; ok && kv < 2; ++kv) {
         const uint16_t *base = kv ? a.v_new : a.k_new;
         ok = encode(kv ? &maps.v : &maps.k, base, {64, hkv, n, 2}, {kRowBytes, kv_step, 128}, {64, 1, kBoxRows, 1}) &&
