@@ -1027,7 +1027,7 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
                             : whole ? static_cast<uint8_t *>(a.out) + o_row * (2 * kRowBytes) + (lane & 3) * 8
                                     : reinterpret_cast<uint8_t *>(part_o(a, slot, stream) + its * kHeadDim) + (lane & 3) * 8;
                 }
-#pragma unroll 2
+#pragma unroll 1
                 for (int d = 0; d < kHeadDim; d += 32) {
                     uint32_t x[16];
                     float y[16];
