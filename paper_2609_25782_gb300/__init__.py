@@ -29,6 +29,9 @@ class Pool:
         self.L, self.Hq, self.Hkv, self.D, self.bt = (num_layers, num_q_heads, num_kv_heads,
                                                       head_dim, block_tokens)
         self.num_hot_blocks = num_hot_blocks
+        # The calls that a model makes per layer go to the library by the shortest way: a call on a few
+        # tokens takes the GPU about as long as the host.
+        self._prefill, self._tree = kvtier.lib.prefill_attention, kvtier.lib.tree_attention
         self._bf16 = torch.bfloat16
         self._out_flags = {torch.float32: 0, torch.bfloat16: kvtier.KV_DECODE_OUT_BF16}
         probe = kvtier.make_config(num_layers=num_layers, num_q_heads=num_q_heads,
@@ -192,9 +195,12 @@ class Pool:
         stride, so views of one projection will do), the newest of its seq_lens[b] tokens; K and V
         go into the slots that batch_reserve(counts=...) allocated. out: fp32 or bf16."""
         q_stride, kv_stride, total, flags = self._turn(q, k_new, v_new, out)
-        kvtier.prefill_attention(self.handle, layer, q.data_ptr(), q_stride, k_new.data_ptr(),
-                                 v_new.data_ptr(), kv_stride, cu_new, total, block_tables, seq_lens,
-                                 B, max_blocks, scale, out.data_ptr(), flags, stream)
+        rc = self._prefill(self.handle, layer, q.data_ptr(), q_stride, k_new.data_ptr(),
+                           v_new.data_ptr(), kv_stride, cu_new.data_ptr(), total,
+                           block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, scale,
+                           out.data_ptr(), flags, None if stream is None else stream.cuda_stream)
+        if rc:
+            kvtier.raise_last(rc, "prefill_attention")
 
     def tree_attention(self, layer: int, q, k_draft, v_draft, ancestors, cu_draft, block_tables,
                        seq_lens, B: int, max_blocks: int, scale: float, out, stream=None) -> None:
@@ -204,10 +210,12 @@ class Pool:
         q_stride, kv_stride, total, flags = self._turn(q, k_draft, v_draft, out)
         if ancestors.numel() != total or ancestors.element_size() != 8 or not ancestors.is_contiguous():
             raise ValueError("one contiguous 64-bit mask per draft")
-        kvtier.tree_attention(self.handle, layer, q.data_ptr(), q_stride, k_draft.data_ptr(),
-                              v_draft.data_ptr(), kv_stride, ancestors.data_ptr(), cu_draft, total,
-                              block_tables, seq_lens, B, max_blocks, scale, out.data_ptr(), flags,
-                              stream)
+        rc = self._tree(self.handle, layer, q.data_ptr(), q_stride, k_draft.data_ptr(),
+                        v_draft.data_ptr(), kv_stride, ancestors.data_ptr(), cu_draft.data_ptr(), total,
+                        block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, scale,
+                        out.data_ptr(), flags, None if stream is None else stream.cuda_stream)
+        if rc:
+            kvtier.raise_last(rc, "tree_attention")
 
     def shuffle_free(self, seed: int) -> None:
         kvtier.kv_pool_shuffle_free(self.handle, seed)

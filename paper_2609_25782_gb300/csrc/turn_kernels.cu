@@ -252,7 +252,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 // ---- the work ----------------------------------------------------------------------------
 
-__device__ __forceinline__ TurnShape turn_shape(const TurnArgs &a) {
+__host__ __device__ __forceinline__ TurnShape turn_shape(const TurnArgs &a) {
     return {a.token_shift, a.s.Hkv, a.masks == nullptr};
 }
 
@@ -272,11 +272,12 @@ __device__ __forceinline__ TurnSession session_of(const TurnArgs &a, int b, bool
 }
 
 // Sum of x over the lanes before this one, and over all.
-__device__ __forceinline__ int64_t scan(int64_t x, int lane, int64_t *all) {
-    int64_t y = x;
+template <typename I>
+__device__ __forceinline__ I scan(I x, int lane, I *all) {
+    I y = x;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int64_t z = __shfl_up_sync(~0u, y, d);
+        const I z = __shfl_up_sync(~0u, y, d);
         if (lane >= d) y += z;
     }
     *all = __shfl_sync(~0u, y, 31);
@@ -284,33 +285,35 @@ __device__ __forceinline__ int64_t scan(int64_t x, int lane, int64_t *all) {
 }
 
 // This CTA's piece, by one warp. (Short code: a call runs it once.)
-__device__ void make_plan(const TurnArgs &a, Plan &plan, int lane) {
+template <typename I>
+__device__ __forceinline__ void make_plan(const TurnArgs &a, Plan &plan, int lane) {
     const TurnShape s = turn_shape(a);
-    int64_t cost = 0, u[2] = {0, 0};
+    I cost = 0, head = 0, u[2] = {0, 0};
     TurnSession x = {0, 0, 0};   // up to 32 sessions: kept from the first pass to the second
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
-        int64_t before = 0;
+        I before = 0;
 #pragma unroll 1
         for (int b0 = 0; b0 < a.B; b0 += 32) {
             const int b = b0 + lane;
             if (pass == 0 || a.B > 32) {
-                cost = 0;
+                head = 0;
                 if (b < a.B) {
                     bool bad;
                     x = session_of(a, b, &bad);
-                    cost = s.Hkv * turn_head_cost(s, x);
+                    head = turn_head_cost<I>(s, x);
                     if (bad && blockIdx.x == 0) atomicOr(a.err, kErrBadLength);
                 }
             }
-            int64_t all;
-            const int64_t at = before + scan(cost, lane, &all);
+            I all;
+            cost = s.Hkv * head;
+            const I at = before + scan(cost, lane, &all);
             before += all;
 #pragma unroll 1
             for (int e = 0; pass == 1 && e < 2; ++e) {
-                const int64_t o = (e ? u[1] : u[0]) - at;
+                const I o = (e ? u[1] : u[0]) - at;
                 if (o < 0 || o >= cost) continue;
-                TurnPos p = turn_locate(s, x, b, o);
+                TurnPos p = turn_locate<I>(s, x, b, head, o);
                 if (p.t >= turn_tiles(s, x, p.pair) || (a.whole && p.t > 0)) {   // the item's end: the next one's start
                     p.t = 0;
                     if (++p.pair >= turn_pairs(s, x)) {
@@ -1101,7 +1104,10 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
         sm.issuing = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kCopyWarp) make_plan(a, sm.plan, lane);
+    if (warp == kCopyWarp) {
+        if (a.small) make_plan<int32_t>(a, sm.plan, lane);
+        else make_plan<int64_t>(a, sm.plan, lane);
+    }
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)),
                      "r"(kTmemCols)
@@ -1136,24 +1142,33 @@ constexpr int kCombineCtas = 8, kCombineWarps = 8;
 constexpr int kCombineRows = 2 * kTurnRows / (kCombineCtas * kCombineWarps);
 __global__ void __launch_bounds__(kCombineWarps * 32) turn_combine_kernel(const __grid_constant__ TurnArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int first = blockIdx.x, lane = threadIdx.x & 31, g_shift = 7 - a.token_shift;
-    const PartRecord rec = *part_record(a, first);
-    if (!rec.opens) return;
-    const int row0 = blockIdx.y * kCombineWarps + (threadIdx.x >> 5), rows = rec.tokens << g_shift;
-    if (row0 >= rows) return;
-    int last = first + 1;   // the first piece that the item does not pass through
-    for (;; last += 32) {
-        const int c = last + lane;
-        const uint32_t ends = __ballot_sync(~0u, c >= a.part_slots / 2 || !part_record(a, c)->through);
-        if (ends) {
-            last += __ffs(ends) - 1;
-            break;
-        }
-    }
+    const int first = blockIdx.x, lane = threadIdx.x & 31, g_shift = 7 - a.token_shift, ctas = a.part_slots / 2;
+    const int row0 = blockIdx.y * kCombineWarps + (threadIdx.x >> 5);
     const auto slot = [&](int c) { return c == first ? 2 * c + 1 : 2 * c; };
     constexpr int kApart = kCombineCtas * kCombineWarps;
     const auto stream_of = [&](int i) { return (row0 + i * kApart) / kTurnRows; };
     const auto row_of = [&](int i) { return (row0 + i * kApart) % kTurnRows; };
+    // The record, the ends of up to 32 pieces and the rows' statistics in them (if they are the item's) in one
+    // round; a slot that no piece has written is not used.
+    const PartRecord rec = *part_record(a, first);
+    bool ends = first + 1 + lane >= ctas || !part_record(a, first + 1 + lane)->through;
+    float2 stats[kCombineRows];
+#pragma unroll
+    for (int i = 0; i < kCombineRows; ++i)
+        stats[i] = part_ml(a, slot(min(first + lane, ctas - 1)), stream_of(i))[row_of(i)];
+    if (!rec.opens) return;
+    const int rows = rec.tokens << g_shift;
+    if (row0 >= rows) return;
+    int last = first + 1;   // the first piece that the item does not pass through
+    for (;;) {
+        const uint32_t any = __ballot_sync(~0u, ends);
+        if (any) {
+            last += __ffs(any) - 1;
+            break;
+        }
+        last += 32;
+        ends = last + lane >= ctas || !part_record(a, last + lane)->through;
+    }
     float m[kCombineRows], l[kCombineRows];
     float4 y[kCombineRows];
 #pragma unroll
@@ -1168,7 +1183,8 @@ __global__ void __launch_bounds__(kCombineWarps * 32) turn_combine_kernel(const 
 #pragma unroll
         for (int i = 0; i < kCombineRows; ++i) {
             float2 v = make_float2(-INFINITY, 0.f);
-            if (lane < n && row0 + i * kApart < rows) v = part_ml(a, slot(c0 + lane), stream_of(i))[row_of(i)];
+            if (lane < n && row0 + i * kApart < rows)
+                v = c0 == first ? stats[i] : part_ml(a, slot(c0 + lane), stream_of(i))[row_of(i)];
             float top = v.x;
 #pragma unroll
             for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
@@ -1259,8 +1275,8 @@ cudaError_t launch_turn(TurnArgs a, const CUtensorMap hot[2], cudaStream_t st) {
     // No more CTAs than there can be pieces; items of at most two key tiles are not cut, which saves the
     // merge's launch (a prompt of 37 tokens: X us with it, Y without).
     const int64_t longest = static_cast<int64_t>(a.max_blocks) * a.s.bt;
-    const int64_t items = (a.total / (2 << a.token_shift) + static_cast<int64_t>(a.B)) * a.s.Hkv;
-    const int64_t pieces = items * ((longest / kTurnKeys + 2) * kCostTile + kCostItem) / kCostPiece;
+    const int64_t bound = turn_cost_bound(turn_shape(a), a.total, a.B, longest), pieces = bound / kCostPiece;
+    a.small = bound < int64_t(1) << 30;
     const unsigned ctas = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(pieces, a.part_slots / 2)));
     a.part_slots = 2 * ctas;
     a.whole = longest <= kTurnKeys;

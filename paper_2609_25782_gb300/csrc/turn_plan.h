@@ -63,55 +63,66 @@ KVT_PLAN int turn_own_keys(const TurnShape &s, const TurnSession &x, int pair) {
 KVT_PLAN int turn_tiles(const TurnShape &s, const TurnSession &x, int pair) {
     return turn_tiles_of(x.P) + turn_tiles_of(turn_own_keys(s, x, pair));
 }
-KVT_PLAN int64_t turn_item_cost(const TurnShape &s, const TurnSession &x, int pair) {
-    return static_cast<int64_t>(kCostTile) * turn_tiles(s, x, pair) + kCostItem;
+// Costs are counted in I, 32 bits where all of a call's fit them (the device has no others; a plan in 64
+// bits takes twice as long).
+template <typename I>
+KVT_PLAN I turn_item_cost(const TurnShape &s, const TurnSession &x, int pair) {
+    return static_cast<I>(kCostTile) * turn_tiles(s, x, pair) + kCostItem;
 }
 // Cost of the first p pairs of a kv-head, p below the number of pairs: all of
 // them full, so the own key tiles of a causal pair i are ceil((i + 1) * 2 tokens / 128).
-KVT_PLAN int64_t turn_cost_before(const TurnShape &s, const TurnSession &x, int64_t p) {
-    int64_t own;
+template <typename I>
+KVT_PLAN I turn_cost_before(const TurnShape &s, const TurnSession &x, I p) {
+    I own;
     if (!s.causal) {
         own = p * turn_tiles_of(x.n);
     } else if ((2 << s.shift) >= kTurnKeys) {
         own = (2 << s.shift) / kTurnKeys * (p * (p + 1) / 2);
     } else {
         const int r_shift = 6 - s.shift;   // 128 / (2 tokens) pairs a key tile
-        const int64_t a = p >> r_shift;
+        const I a = p >> r_shift;
         own = ((a * (a + 1) / 2) << r_shift) + (p - (a << r_shift)) * (a + 1);
     }
     return kCostTile * (p * turn_tiles_of(x.P) + own) + kCostItem * p;
 }
-KVT_PLAN int64_t turn_head_cost(const TurnShape &s, const TurnSession &x) {
+template <typename I>
+KVT_PLAN I turn_head_cost(const TurnShape &s, const TurnSession &x) {
     const int pairs = turn_pairs(s, x);
-    return pairs == 0 ? 0 : turn_cost_before(s, x, pairs - 1) + turn_item_cost(s, x, pairs - 1);
+    return pairs == 0 ? 0 : turn_cost_before<I>(s, x, pairs - 1) + turn_item_cost<I>(s, x, pairs - 1);
+}
+// No call's cost is above this, and none of its parts.
+KVT_PLAN int64_t turn_cost_bound(const TurnShape &s, int64_t total, int64_t B, int64_t longest) {
+    return ((total >> (s.shift + 1)) + B) * s.Hkv * ((longest / kTurnKeys + 2) * kCostTile + kCostItem);
 }
 
 // Pieces that work of cost W makes, and where piece c begins: the first W % pieces
 // are one longer than the others.
-KVT_PLAN int turn_pieces(int64_t W, int ctas) {
-    const int64_t n = W / kCostPiece;
+template <typename I>
+KVT_PLAN int turn_pieces(I W, int ctas) {
+    const I n = W / kCostPiece;
     return n < 1 ? 1 : n < ctas ? static_cast<int>(n) : ctas;
 }
-KVT_PLAN int64_t turn_cut(int64_t W, int pieces, int c) {
-    const int64_t each = W >> 31 ? W / pieces : static_cast<uint32_t>(W) / static_cast<uint32_t>(pieces);
-    const int64_t longer = W - each * pieces;
+template <typename I>
+KVT_PLAN I turn_cut(I W, int pieces, int c) {
+    const I each = W >> 30 ? W / pieces : static_cast<I>(static_cast<uint32_t>(W) / static_cast<uint32_t>(pieces));
+    const I longer = W - each * pieces;
     return each * c + (c < longer ? c : longer);
 }
 
-// The key tile at cost o of session b's work (o below Hkv times its head cost). t may be the item's
+// The key tile at cost o of session b's work (o below Hkv times `head`, its head cost). t may be the item's
 // number of key tiles: its end.
-KVT_PLAN TurnPos turn_locate(const TurnShape &s, const TurnSession &x, int b, int64_t o) {
-    const int64_t head = turn_head_cost(s, x);
+template <typename I>
+KVT_PLAN TurnPos turn_locate(const TurnShape &s, const TurnSession &x, int b, I head, I o) {
     TurnPos p = {b, 0, 0, 0};
     for (; o >= head; o -= head) ++p.g;      // at most 8 kv-heads
     int lo = 0, hi = turn_pairs(s, x) - 1;   // the last pair that begins at or before o
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
-        if (turn_cost_before(s, x, mid) <= o) lo = mid;
+        if (turn_cost_before<I>(s, x, mid) <= o) lo = mid;
         else hi = mid - 1;
     }
     p.pair = lo;
-    const int64_t in = o - turn_cost_before(s, x, lo) - kCostItem;
+    const I in = o - turn_cost_before<I>(s, x, lo) - kCostItem;
     p.t = in <= 0 ? 0 : static_cast<int>((in + kCostTile - 1) / kCostTile);
     return p;
 }

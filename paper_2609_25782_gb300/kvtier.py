@@ -165,9 +165,14 @@ def _stream(s) -> int | None:
     return s.cuda_stream
 
 
+def raise_last(rc: int, where: str) -> None:
+    """The error that the call `where` on this thread has just returned."""
+    raise KVError(rc, where, kv_last_error())
+
+
 def _check(rc: int, where: str) -> None:
     if rc != KV_OK:
-        raise KVError(rc, where, kv_last_error())
+        raise_last(rc, where)
 
 
 def kv_last_error() -> str:

@@ -21,12 +21,14 @@ def lib():
                         os.path.join(HERE, "turn_plan.cpp"), "-o", so], check=True)
         x = ctypes.CDLL(so)
     i32, i64 = ctypes.c_int32, ctypes.c_int64
-    for name in ("cost_before", "head_cost", "cut"):
+    for name in ("cost_before", "head_cost", "head_cost_32", "cut", "cut_32", "cost_bound"):
         getattr(x, name).restype = i64
-    x.locate.restype = None
-    x.locate.argtypes = [i32] * 5 + [i64, ctypes.POINTER(i32)]
+    for name in ("locate", "locate_32"):
+        getattr(x, name).restype = None
+        getattr(x, name).argtypes = [i32] * 5 + [i64, ctypes.POINTER(i32)]
     x.pieces.argtypes = [i64, i32]
-    x.cut.argtypes = [i64, i32, i32]
+    x.cut.argtypes = x.cut_32.argtypes = [i64, i32, i32]
+    x.cost_bound.argtypes = [i32, i32, i64, i64, i64]
     return x
 
 
@@ -51,7 +53,7 @@ def test_costs_add_up(tokens, causal):
             assert t == -(-P // 128) + own_tiles(tokens, causal, n, p)
             assert x.narrow(tokens, n, p) == (n - p * 2 * tokens <= tokens)
             total += t * x.tile_cost() + x.item_cost()
-        assert x.head_cost(tokens, causal, n, P) == total
+        assert x.head_cost(tokens, causal, n, P) == x.head_cost_32(tokens, causal, n, P) == total
 
 
 def layout(sessions, tokens, hkv, causal):
@@ -82,6 +84,8 @@ def test_pieces_cover_the_line(seed):
         starts.append(at)
         at += hkv * x.head_cost(tokens, int(causal), n, P)
     assert at == W
+    longest = max(P + (n if causal else 0) for n, P in sessions)
+    assert W <= x.cost_bound(tokens, hkv, sum(n for n, _ in sessions), B, longest) < 2 ** 30
     for ctas in (1, 2, 7, 152):
         m = x.pieces(W, ctas)
         assert 1 <= m <= ctas and x.cut(W, m, 0) == 0 and x.cut(W, m, m) == W
@@ -93,6 +97,9 @@ def test_pieces_cover_the_line(seed):
             b = max(i for i in range(B) if starts[i] <= u and sessions[i][0] > 0)
             pos = (ctypes.c_int32 * 3)()
             x.locate(tokens, hkv, int(causal), *sessions[b], u - starts[b], pos)
+            again = (ctypes.c_int32 * 3)()
+            x.locate_32(tokens, hkv, int(causal), *sessions[b], u - starts[b], again)
+            assert list(pos) == list(again) and x.cut_32(W, m, c) == u
             k = index[(b, pos[0], pos[1])]
             assert 0 <= pos[2] <= items[k][4]
             # the tile whose cost contains the cut, or the one after it

@@ -16,19 +16,35 @@ int32_t tiles(int tokens, int causal, int n, int P, int pair) {
     return turn_tiles(shape(tokens, 1, causal), {n, P, 0}, pair);
 }
 int64_t cost_before(int tokens, int causal, int n, int P, int pair) {
-    return turn_cost_before(shape(tokens, 1, causal), {n, P, 0}, pair);
+    return turn_cost_before<int64_t>(shape(tokens, 1, causal), {n, P, 0}, pair);
 }
 int64_t head_cost(int tokens, int causal, int n, int P) {
-    return turn_head_cost(shape(tokens, 1, causal), {n, P, 0});
+    return turn_head_cost<int64_t>(shape(tokens, 1, causal), {n, P, 0});
 }
-void locate(int tokens, int Hkv, int causal, int n, int P, int64_t o, int32_t *pos) {
-    const TurnPos p = turn_locate(shape(tokens, Hkv, causal), {n, P, 0}, 0, o);
+int64_t head_cost_32(int tokens, int causal, int n, int P) {
+    return turn_head_cost<int32_t>(shape(tokens, 1, causal), {n, P, 0});
+}
+int64_t cost_bound(int tokens, int Hkv, int64_t total, int64_t B, int64_t longest) {
+    return turn_cost_bound(shape(tokens, Hkv, 1), total, B, longest);
+}
+static void put(const TurnPos &p, int32_t *pos) {
     pos[0] = p.g;
     pos[1] = p.pair;
     pos[2] = p.t;
 }
+void locate(int tokens, int Hkv, int causal, int n, int P, int64_t o, int32_t *pos) {
+    const TurnShape s = shape(tokens, Hkv, causal);
+    const TurnSession x = {n, P, 0};
+    put(turn_locate<int64_t>(s, x, 0, turn_head_cost<int64_t>(s, x), o), pos);
+}
+void locate_32(int tokens, int Hkv, int causal, int n, int P, int64_t o, int32_t *pos) {
+    const TurnShape s = shape(tokens, Hkv, causal);
+    const TurnSession x = {n, P, 0};
+    put(turn_locate<int32_t>(s, x, 0, turn_head_cost<int32_t>(s, x), static_cast<int32_t>(o)), pos);
+}
 int32_t pieces(int64_t W, int ctas) { return turn_pieces(W, ctas); }
 int64_t cut(int64_t W, int n, int c) { return turn_cut(W, n, c); }
+int64_t cut_32(int64_t W, int n, int c) { return turn_cut(static_cast<int32_t>(W), n, c); }
 int32_t tile_cost() { return kCostTile; }
 int32_t item_cost() { return kCostItem; }
 }
