@@ -259,16 +259,11 @@ __host__ __device__ __forceinline__ TurnShape turn_shape(const TurnArgs &a) {
 // Session b as the call describes it; n = 0 for one whose data is out of range.
 __device__ __forceinline__ TurnSession session_of(const TurnArgs &a, int b, bool *bad = nullptr) {
     const int lo = a.cu[b], hi = a.cu[b + 1], T = a.seq_lens[b];
-    const bool drafts = a.masks != nullptr;
-    const int64_t n = static_cast<int64_t>(hi) - lo;
-    const bool ok = lo >= 0 && n >= 0 && hi <= a.total && T >= (drafts ? 0 : n) &&
-                    T <= static_cast<int64_t>(a.max_blocks) * a.s.bt && !(drafts && n > kMaxDrafts);
+    const bool drafts = a.masks != nullptr, order = lo >= 0 && lo <= hi && hi <= a.total;
+    const int n = order ? hi - lo : 0;
+    const bool ok = order && T >= (drafts ? 0 : n) && T <= a.longest && !(drafts && n > kMaxDrafts);
     if (bad) *bad = !ok;
-    TurnSession x;
-    x.n = ok ? static_cast<int>(n) : 0;
-    x.P = ok ? (drafts ? T : T - x.n) : 0;
-    x.lo = lo;
-    return x;
+    return {ok ? n : 0, !ok ? 0 : drafts ? T : T - n, lo};
 }
 
 // Sum of x over the lanes before this one, and over all.
@@ -284,62 +279,62 @@ __device__ __forceinline__ I scan(I x, int lane, I *all) {
     return y - x;
 }
 
-// This CTA's piece, by one warp. (Short code: a call runs it once.)
+// This CTA's piece, by one warp. (Short code: a call runs it once, and nothing else can begin before.)
 template <typename I>
 __device__ __forceinline__ void make_plan(const TurnArgs &a, Plan &plan, int lane) {
     const TurnShape s = turn_shape(a);
-    I cost = 0, head = 0, u[2] = {0, 0};
-    TurnSession x = {0, 0, 0};   // up to 32 sessions: kept from the first pass to the second
+    TurnSession x = {0, 0, 0};   // up to 32 sessions: kept, with what goes before, for the cuts
+    I head = 0, at = 0, W = 0, all;
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-        I before = 0;
+    for (int b = lane; b - lane < a.B; b += 32) {
+        head = 0;
+        if (b < a.B) {
+            bool bad;
+            x = session_of(a, b, &bad);
+            head = turn_head_cost<I>(s, x);
+            if (bad && blockIdx.x == 0) atomicOr(a.err, kErrBadLength);
+        }
+        at = W + scan(s.Hkv * head, lane, &all);
+        W += all;
+    }
+    const int pieces = W == 0 ? 0 : turn_pieces(W, gridDim.x), c = blockIdx.x;
+    if (lane == 0) plan.begin = plan.end = {a.B, 0, 0, 0};   // no piece; a last piece's end
+    __syncwarp();
+    if (c >= pieces) return;
+    const I u[2] = {turn_cut(W, pieces, c), turn_cut(W, pieces, c + 1)};
+    W = 0;
 #pragma unroll 1
-        for (int b0 = 0; b0 < a.B; b0 += 32) {
-            const int b = b0 + lane;
-            if (pass == 0 || a.B > 32) {
-                head = 0;
-                if (b < a.B) {
-                    bool bad;
-                    x = session_of(a, b, &bad);
-                    head = turn_head_cost<I>(s, x);
-                    if (bad && blockIdx.x == 0) atomicOr(a.err, kErrBadLength);
-                }
+    for (int b = lane; b - lane < a.B; b += 32) {
+        if (a.B > 32) {
+            head = 0;
+            if (b < a.B) {
+                x = session_of(a, b);
+                head = turn_head_cost<I>(s, x);
             }
-            I all;
-            cost = s.Hkv * head;
-            const I at = before + scan(cost, lane, &all);
-            before += all;
-#pragma unroll 1
-            for (int e = 0; pass == 1 && e < 2; ++e) {
-                const I o = (e ? u[1] : u[0]) - at;
-                if (o < 0 || o >= cost) continue;
-                TurnPos p = turn_locate<I>(s, x, b, head, o);
-                if (p.t >= turn_tiles(s, x, p.pair) || (a.whole && p.t > 0)) {   // the item's end: the next one's start
-                    p.t = 0;
-                    if (++p.pair >= turn_pairs(s, x)) {
-                        p.pair = 0;
-                        if (++p.g >= s.Hkv) {
-                            p.g = 0;
-                            ++p.b;   // an empty session here is passed over by the walk
-                        }
+            at = W + scan(s.Hkv * head, lane, &all);
+            W += all;
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if (u[e] < at || u[e] >= at + s.Hkv * head) continue;
+            TurnPos p = turn_locate<I>(s, x, b, head, u[e] - at);
+            if (p.t >= turn_tiles(s, x, p.pair) || (a.whole && p.t > 0)) {   // the item's end: the next one's start
+                p.t = 0;
+                if (++p.pair >= turn_pairs(s, x)) {
+                    p.pair = 0;
+                    if (++p.g >= s.Hkv) {
+                        p.g = 0;
+                        ++p.b;   // an empty session here is passed over by the walk
                     }
                 }
-                if (e) {
-                    plan.end = p;
-                } else {
-                    plan.begin = p;
-                    plan.first = x;
-                    if (p.b != b) plan.first.n = -1;
-                }
             }
-        }
-        if (pass == 0) {
-            const int pieces = before == 0 ? 0 : turn_pieces(before, gridDim.x), c = blockIdx.x;
-            if (lane == 0) plan.begin = plan.end = {a.B, 0, 0, 0};   // no piece; a last piece's end
-            __syncwarp();
-            if (c >= pieces) return;
-            u[0] = turn_cut(before, pieces, c);
-            u[1] = turn_cut(before, pieces, c + 1);
+            if (e) {
+                plan.end = p;
+            } else {
+                plan.begin = p;
+                plan.first = x;
+                if (p.b != b) plan.first.n = -1;
+            }
         }
     }
     __syncwarp();
@@ -1275,6 +1270,7 @@ cudaError_t launch_turn(TurnArgs a, const CUtensorMap hot[2], cudaStream_t st) {
     // No more CTAs than there can be pieces; items of at most two key tiles are not cut, which saves the
     // merge's launch (a prompt of 37 tokens: X us with it, Y without).
     const int64_t longest = static_cast<int64_t>(a.max_blocks) * a.s.bt;
+    a.longest = static_cast<int32_t>(std::min<int64_t>(longest, INT32_MAX));
     const int64_t bound = turn_cost_bound(turn_shape(a), a.total, a.B, longest), pieces = bound / kCostPiece;
     a.small = bound < int64_t(1) << 30;
     const unsigned ctas = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(pieces, a.part_slots / 2)));
