@@ -110,7 +110,7 @@ struct TurnArgs {
     float *part;
     int32_t part_slots;
     int32_t longest;                 // set by the launch: tokens that a table row holds
-    int32_t whole, small;            // set by the launch: no item is cut; costs fit 32 bits
+    int32_t whole, many, small;      // set by the launch: no item is cut; much work; costs fit 32 bits
     int32_t token_shift;             // set by the launch: tokens of a row tile, 128 / G, as a power of two
     Shape s;
 };

@@ -1035,7 +1035,7 @@ static int turn_impl(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     a.layer = layer;
     a.out_bf16 = (flags & KV_DECODE_OUT_BF16) ? 1 : 0;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.negate = a.longest = a.whole = a.small = a.token_shift = 0;   // set by the launch
+    a.negate = a.longest = a.whole = a.many = a.small = a.token_shift = 0;   // set by the launch
     a.part = p->d_turn_part;
     a.part_slots = 2 * p->num_sms;
     a.s = p->shape;

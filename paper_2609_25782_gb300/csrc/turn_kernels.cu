@@ -252,8 +252,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 // ---- the work ----------------------------------------------------------------------------
 
-__host__ __device__ __forceinline__ TurnShape turn_shape(const TurnArgs &a) {
-    return {a.token_shift, a.s.Hkv, a.masks == nullptr};
+__host__ __device__ __forceinline__ TurnShape turn_shape(const TurnArgs &a, bool many = false) {
+    return {a.token_shift, a.s.Hkv, a.masks == nullptr, many};
 }
 
 // Session b as the call describes it; n = 0 for one whose data is out of range.
@@ -279,10 +279,11 @@ __device__ __forceinline__ I scan(I x, int lane, I *all) {
     return y - x;
 }
 
-// This CTA's piece, by one warp. (Short code: a call runs it once, and nothing else can begin before.)
-template <typename I>
+// This CTA's piece, by one warp. (Short code: a call runs it once, and nothing else can begin before. So the
+// costs are constants in it, and the launch has chosen them.)
+template <typename I, bool kMany>
 __device__ __forceinline__ void make_plan(const TurnArgs &a, Plan &plan, int lane) {
-    const TurnShape s = turn_shape(a);
+    const TurnShape s = turn_shape(a, kMany);
     TurnSession x = {0, 0, 0};   // up to 32 sessions: kept, with what goes before, for the cuts
     I head = 0, at = 0, W = 0, all;
 #pragma unroll 1
@@ -297,7 +298,7 @@ __device__ __forceinline__ void make_plan(const TurnArgs &a, Plan &plan, int lan
         at = W + scan(s.Hkv * head, lane, &all);
         W += all;
     }
-    const int pieces = W == 0 ? 0 : turn_pieces(W, gridDim.x), c = blockIdx.x;
+    const int pieces = W == 0 ? 0 : turn_pieces(s, W, gridDim.x), c = blockIdx.x;
     if (lane == 0) plan.begin = plan.end = {a.B, 0, 0, 0};   // no piece; a last piece's end
     __syncwarp();
     if (c >= pieces) return;
@@ -1001,7 +1002,7 @@ __device__ void softmax_role(const TurnArgs &a, Smem &sm, int stream) {
             }
             // The rows from tensor memory, 16 rows by 32 columns at a time, so that a store has the 64 or
             // 32 bytes of eight rows; with a row per thread each store had 16 bytes of 32 rows, and an
-            // item's end took 6 700 cycles (2 000). Short code, as above.
+            // item's end took twice as long. Short code, as above.
             const int lane = row & 31;
             const uint32_t some = __ballot_sync(~0u, live);
             const bool bf16 = whole && a.out_bf16;
@@ -1100,8 +1101,9 @@ __global__ void __launch_bounds__(kThreads, 1) turn_kernel(const __grid_constant
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kCopyWarp) {
-        if (a.small) make_plan<int32_t>(a, sm.plan, lane);
-        else make_plan<int64_t>(a, sm.plan, lane);
+        if (!a.many) make_plan<int32_t, false>(a, sm.plan, lane);
+        else if (a.small) make_plan<int32_t, true>(a, sm.plan, lane);
+        else make_plan<int64_t, true>(a, sm.plan, lane);
     }
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)),
@@ -1268,12 +1270,14 @@ cudaError_t launch_turn(TurnArgs a, const CUtensorMap hot[2], cudaStream_t st) {
     a.scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-30f);
     a.token_shift = G == 8 ? 4 : G == 4 ? 5 : G == 2 ? 6 : 7;
     // No more CTAs than there can be pieces; items of at most two key tiles are not cut, which saves the
-    // merge's launch (a prompt of 37 tokens: X us with it, Y without).
+    // merge's launch (a prompt of 37 tokens: 9.9 us with it, 9.1 without).
     const int64_t longest = static_cast<int64_t>(a.max_blocks) * a.s.bt;
     a.longest = static_cast<int32_t>(std::min<int64_t>(longest, INT32_MAX));
-    const int64_t bound = turn_cost_bound(turn_shape(a), a.total, a.B, longest), pieces = bound / kCostPiece;
-    a.small = bound < int64_t(1) << 30;
-    const unsigned ctas = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(pieces, a.part_slots / 2)));
+    const int64_t bound = turn_cost_bound(turn_shape(a), a.total, a.B, longest);
+    const unsigned ctas = static_cast<unsigned>(
+        std::max<int64_t>(1, std::min<int64_t>(bound / kCostsFew.piece, a.part_slots / 2)));
+    a.many = turn_many(bound, a.part_slots / 2);
+    a.small = turn_cost_bound(turn_shape(a, true), a.total, a.B, longest) < int64_t(1) << 30;
     a.part_slots = 2 * ctas;
     a.whole = longest <= kTurnKeys;
     turn_kernel<<<ctas, kThreads, kSmemBytes, st>>>(a, maps);

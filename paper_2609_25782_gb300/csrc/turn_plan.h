@@ -26,12 +26,18 @@ namespace kvt {
 
 constexpr int kTurnRows = 128;    // rows of a row tile
 constexpr int kTurnKeys = 128;    // keys of a key tile
-// Costs of a key tile, and of an item's start and end.
-constexpr int kCostTile = 4, kCostItem = 4;
-// Least cost of a CTA's piece. Places where a cut moves on by a key tile are at most
-// kCostItem + kCostTile apart (from an item's last tile to the next one's first), so no
-// piece of so much is empty, and items of one key tile each get a CTA of their own.
-constexpr int kCostPiece = kCostItem + kCostTile;
+// Costs of a key tile of a wide and of a narrow item, of an item's start and end, and the least cost of a
+// CTA's piece. Places where a cut moves on by a key tile are at most an item's and a tile's cost apart
+// (from an item's last tile to the next one's first), so no piece of that much is empty.
+struct TurnCosts {
+    int32_t tile, narrow_tile, item, piece;
+};
+// With little work the shortest piece counts, and items of one key tile have a CTA each (one prompt of 37
+// tokens 9.1 us; 12 with the other costs). With much, what the parts take: a wide item's tile 3 300
+// cycles, a narrow one's 2 500, an item's end and the next one's start 6 000. Against the first costs: 32
+// sessions of 20-60 drafts 140 -> 124 us, chunks of 1-200 tokens on 1K-40K 282 -> 236, turns of 300-3K
+// tokens 935 -> 910.
+constexpr TurnCosts kCostsFew = {4, 4, 4, 8}, kCostsMany = {4, 3, 8, 12};
 
 struct TurnSession {
     int32_t n, P, lo;   // new tokens (0: skipped), cached tokens before them, first row
@@ -45,8 +51,13 @@ struct TurnPos {
 struct TurnShape {
     int32_t shift;      // tokens of a row tile, 128 / G, as a power of two
     int32_t Hkv;
-    bool causal;
+    bool causal, many;   // many: the costs of much work
 };
+
+KVT_PLAN TurnCosts turn_costs(const TurnShape &s) {
+    return {s.many ? kCostsMany.tile : kCostsFew.tile, s.many ? kCostsMany.narrow_tile : kCostsFew.narrow_tile,
+            s.many ? kCostsMany.item : kCostsFew.item, s.many ? kCostsMany.piece : kCostsFew.piece};
+}
 
 KVT_PLAN int turn_tiles_of(int keys) { return static_cast<int>((static_cast<uint32_t>(keys) + kTurnKeys - 1) / kTurnKeys); }
 KVT_PLAN int turn_pairs(const TurnShape &s, const TurnSession &x) {
@@ -67,7 +78,8 @@ KVT_PLAN int turn_tiles(const TurnShape &s, const TurnSession &x, int pair) {
 // bits takes twice as long).
 template <typename I>
 KVT_PLAN I turn_item_cost(const TurnShape &s, const TurnSession &x, int pair) {
-    return static_cast<I>(kCostTile) * turn_tiles(s, x, pair) + kCostItem;
+    const TurnCosts cost = turn_costs(s);
+    return static_cast<I>(turn_narrow(s, x, pair) ? cost.narrow_tile : cost.tile) * turn_tiles(s, x, pair) + cost.item;
 }
 // Cost of the first p pairs of a kv-head, p below the number of pairs: all of
 // them full, so the own key tiles of a causal pair i are ceil((i + 1) * 2 tokens / 128).
@@ -83,7 +95,7 @@ KVT_PLAN I turn_cost_before(const TurnShape &s, const TurnSession &x, I p) {
         const I a = p >> r_shift;
         own = ((a * (a + 1) / 2) << r_shift) + (p - (a << r_shift)) * (a + 1);
     }
-    return kCostTile * (p * turn_tiles_of(x.P) + own) + kCostItem * p;
+    return turn_costs(s).tile * (p * turn_tiles_of(x.P) + own) + turn_costs(s).item * p;
 }
 template <typename I>
 KVT_PLAN I turn_head_cost(const TurnShape &s, const TurnSession &x) {
@@ -92,14 +104,19 @@ KVT_PLAN I turn_head_cost(const TurnShape &s, const TurnSession &x) {
 }
 // No call's cost is above this, and none of its parts.
 KVT_PLAN int64_t turn_cost_bound(const TurnShape &s, int64_t total, int64_t B, int64_t longest) {
-    return ((total >> (s.shift + 1)) + B) * s.Hkv * ((longest / kTurnKeys + 2) * kCostTile + kCostItem);
+    return ((total >> (s.shift + 1)) + B) * s.Hkv * ((longest / kTurnKeys + 2) * turn_costs(s).tile + turn_costs(s).item);
+}
+// Whether a call has much work, by the bound of its cost with the costs of little: so much that, were it all
+// narrow items' tiles, every CTA would have a piece. (The launch knows the tables' width, not the lengths.)
+KVT_PLAN bool turn_many(int64_t bound, int ctas) {
+    return bound >= int64_t(1) * kCostsMany.piece * kCostsFew.tile / kCostsMany.narrow_tile * ctas;
 }
 
 // Pieces that work of cost W makes, and where piece c begins: the first W % pieces
 // are one longer than the others.
 template <typename I>
-KVT_PLAN int turn_pieces(I W, int ctas) {
-    const I n = W / kCostPiece;
+KVT_PLAN int turn_pieces(const TurnShape &s, I W, int ctas) {
+    const I n = s.many ? W / kCostsMany.piece : W / kCostsFew.piece;
     return n < 1 ? 1 : n < ctas ? static_cast<int>(n) : ctas;
 }
 template <typename I>
@@ -122,8 +139,11 @@ KVT_PLAN TurnPos turn_locate(const TurnShape &s, const TurnSession &x, int b, I 
         else hi = mid - 1;
     }
     p.pair = lo;
-    const I in = o - turn_cost_before<I>(s, x, lo) - kCostItem;
-    p.t = in <= 0 ? 0 : static_cast<int>((in + kCostTile - 1) / kCostTile);
+    const I in = o - turn_cost_before<I>(s, x, lo) - turn_costs(s).item;
+    if (in <= 0) p.t = 0;
+    else if (!s.many) p.t = static_cast<int>((in + kCostsFew.tile - 1) / kCostsFew.tile);
+    else if (turn_narrow(s, x, lo)) p.t = static_cast<int>((in + kCostsMany.narrow_tile - 1) / kCostsMany.narrow_tile);
+    else p.t = static_cast<int>((in + kCostsMany.tile - 1) / kCostsMany.tile);
     return p;
 }
 

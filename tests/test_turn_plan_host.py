@@ -25,10 +25,11 @@ def lib():
         getattr(x, name).restype = i64
     for name in ("locate", "locate_32"):
         getattr(x, name).restype = None
-        getattr(x, name).argtypes = [i32] * 5 + [i64, ctypes.POINTER(i32)]
-    x.pieces.argtypes = [i64, i32]
+        getattr(x, name).argtypes = [i32] * 6 + [i64, ctypes.POINTER(i32)]
+    x.pieces.argtypes = [i32, i64, i32]
+    x.is_many.argtypes = [i64, i32]
     x.cut.argtypes = x.cut_32.argtypes = [i64, i32, i32]
-    x.cost_bound.argtypes = [i32, i32, i64, i64, i64]
+    x.cost_bound.argtypes = [i32, i32, i32, i64, i64, i64]
     return x
 
 
@@ -37,9 +38,10 @@ def own_tiles(tokens, causal, n, pair):
     return -(-last // 128)
 
 
+@pytest.mark.parametrize("many", [0, 1])
 @pytest.mark.parametrize("causal", [0, 1])
 @pytest.mark.parametrize("tokens", [16, 32, 64, 128])
-def test_costs_add_up(tokens, causal):
+def test_costs_add_up(tokens, causal, many):
     x, r = lib(), random.Random(tokens)
     for _ in range(60):
         n = r.choice([1, 15, 16, 17, 64, r.randint(1, 64)]) if not causal else int(2 ** r.uniform(0, 12))
@@ -48,47 +50,52 @@ def test_costs_add_up(tokens, causal):
         assert pairs == -(-n // (2 * tokens))
         total = 0
         for p in range(pairs):
-            assert x.cost_before(tokens, causal, n, P, p) == total
+            assert x.cost_before(tokens, causal, many, n, P, p) == total
             t = x.tiles(tokens, causal, n, P, p)
             assert t == -(-P // 128) + own_tiles(tokens, causal, n, p)
-            assert x.narrow(tokens, n, p) == (n - p * 2 * tokens <= tokens)
-            total += t * x.tile_cost() + x.item_cost()
-        assert x.head_cost(tokens, causal, n, P) == x.head_cost_32(tokens, causal, n, P) == total
+            narrow = n - p * 2 * tokens <= tokens
+            assert x.narrow(tokens, n, p) == narrow
+            total += t * x.tile_cost(many, narrow) + x.item_cost(many)
+        assert x.head_cost(tokens, causal, many, n, P) == x.head_cost_32(tokens, causal, many, n, P) == total
 
 
-def layout(sessions, tokens, hkv, causal):
-    """[(session, head, pair, cost at its start, tiles)], and the whole cost."""
+def layout(sessions, tokens, hkv, causal, many):
+    """[(session, head, pair, cost at its start, tiles, cost of a tile)], and the whole cost."""
     x, at, items = lib(), 0, []
     for b, (n, P) in enumerate(sessions):
         for g in range(hkv):
             for p in range(x.pairs(tokens, causal, n)):
                 t = x.tiles(tokens, causal, n, P, p)
-                items.append((b, g, p, at, t))
-                at += t * x.tile_cost() + x.item_cost()
+                tile = x.tile_cost(many, x.narrow(tokens, n, p))
+                items.append((b, g, p, at, t, tile))
+                at += t * tile + x.item_cost(many)
     return items, at
 
 
+@pytest.mark.parametrize("many", [0, 1])
 @pytest.mark.parametrize("seed", range(60))
-def test_pieces_cover_the_line(seed):
+def test_pieces_cover_the_line(seed, many):
     x, r = lib(), random.Random(seed)
     causal, tokens, hkv = r.random() < 0.6, r.choice([16, 32, 64, 128]), r.choice([1, 2, 4, 8])
     B = r.choice([1, 2, 5, 40])
     sessions = [(r.choice([0, 1, 16, 17, 40, 64]) if not causal else r.choice([0, int(2 ** r.uniform(0, 10))]),
                  r.choice([0, 1, 128, 129, r.randint(0, 6000)])) for _ in range(B)]
-    items, W = layout(sessions, tokens, hkv, int(causal))
+    items, W = layout(sessions, tokens, hkv, int(causal), many)
     if W == 0:
         return
     index = {i[:3]: k for k, i in enumerate(items)}
     starts, at = [], 0
     for n, P in sessions:
         starts.append(at)
-        at += hkv * x.head_cost(tokens, int(causal), n, P)
+        at += hkv * x.head_cost(tokens, int(causal), many, n, P)
     assert at == W
     longest = max(P + (n if causal else 0) for n, P in sessions)
-    assert W <= x.cost_bound(tokens, hkv, sum(n for n, _ in sessions), B, longest) < 2 ** 30
+    assert W <= x.cost_bound(tokens, hkv, many, sum(n for n, _ in sessions), B, longest) < 2 ** 30
     for ctas in (1, 2, 7, 152):
-        m = x.pieces(W, ctas)
+        m = x.pieces(many, W, ctas)
         assert 1 <= m <= ctas and x.cut(W, m, 0) == 0 and x.cut(W, m, m) == W
+        if x.is_many(layout(sessions, tokens, hkv, int(causal), 0)[1], ctas) and many:
+            assert m == ctas, "a CTA without work"
         lengths = [x.cut(W, m, c + 1) - x.cut(W, m, c) for c in range(m)]
         assert max(lengths) - min(lengths) <= 1
         cuts = []
@@ -96,15 +103,15 @@ def test_pieces_cover_the_line(seed):
             u = x.cut(W, m, c)
             b = max(i for i in range(B) if starts[i] <= u and sessions[i][0] > 0)
             pos = (ctypes.c_int32 * 3)()
-            x.locate(tokens, hkv, int(causal), *sessions[b], u - starts[b], pos)
+            x.locate(tokens, hkv, int(causal), many, *sessions[b], u - starts[b], pos)
             again = (ctypes.c_int32 * 3)()
-            x.locate_32(tokens, hkv, int(causal), *sessions[b], u - starts[b], again)
+            x.locate_32(tokens, hkv, int(causal), many, *sessions[b], u - starts[b], again)
             assert list(pos) == list(again) and x.cut_32(W, m, c) == u
             k = index[(b, pos[0], pos[1])]
             assert 0 <= pos[2] <= items[k][4]
             # the tile whose cost contains the cut, or the one after it
-            into = u - items[k][3] - x.item_cost()
-            assert pos[2] == max(0, -(-into // x.tile_cost()))
+            into = u - items[k][3] - x.item_cost(many)
+            assert pos[2] == max(0, -(-into // items[k][5]))
             cuts.append((k, pos[2]) if pos[2] < items[k][4] else (k + 1, 0))
         cuts.append((len(items), 0))
         assert cuts[0] == (0, 0) and all(a < b for a, b in zip(cuts, cuts[1:])), "an empty piece"
@@ -114,8 +121,9 @@ def test_pieces_cover_the_line(seed):
 def test_items_of_one_tile_have_a_piece_each(items):
     """A short prompt's items, all of one key tile: no CTA has two of them."""
     x = lib()
-    W = items * (x.tile_cost() + x.item_cost())
-    m = x.pieces(W, 152)
+    W = items * (x.tile_cost(0, 0) + x.item_cost(0))
+    m = x.pieces(0, W, 152)
+    assert x.tile_cost(0, 0) == x.tile_cost(0, 1) and not x.is_many(W, 152)
     assert m == items and all(x.cut(W, m, c) == c * W // items for c in range(m + 1))
 
 
