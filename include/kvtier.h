@@ -322,7 +322,12 @@ int decode_append_attention(kv_pool *pool, int32_t layer, const void *q, const v
  * that is not may reach rows that come before it. Tokens past seq_len in a block
  * may hold anything. The result depends on the values, the lengths and the
  * batch, and is the same from run to run. Offsets or lengths out of range set
- * KV_DEVICE_BAD_LENGTH, and that session's rows are not written. */
+ * KV_DEVICE_BAD_LENGTH, and that session's rows are not written; a block id out
+ * of range sets KV_DEVICE_BAD_BLOCK, a wait inside the kernel that runs out (2 s)
+ * KV_DEVICE_TIMEOUT, and rows that they concern are wrong. Calls of this and
+ * tree_attention on one pool share a workspace (0.27 MB per SM, allocated with the
+ * pool): issue them in order on one stream, as decode_attention's. In residency
+ * mode order them before the next call that may evict, as a decode. */
 int prefill_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride,
                       const void *k_new, const void *v_new, int64_t kv_stride, const int32_t *cu_new,
                       int32_t total, const int32_t *block_tables, const int32_t *seq_lens, int32_t B,

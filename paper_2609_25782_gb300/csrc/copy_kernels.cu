@@ -271,7 +271,11 @@ __device__ __forceinline__ void st_codes(uint4 *p, const uint4 &v, uint64_t poli
 }
 
 // Up to one chunk of hot rows into (kPack) or out of an 8-bit image's codes and
-// exponents, by a warp: four rows a round, eight lanes each.
+// exponents, by a warp: four rows a round, eight lanes each (16 values a lane, so
+// that a row's codes are 16-byte accesses and its largest value three shuffles).
+// 385 bytes a row in place of 512, at the same rate: 2 100 tokens of 48 layers
+// read back in 43.5 us (7.1 TB/s), 1 536 tokens packed in 37.1 (6.1 TB/s, a part
+// of their blocks out of the L2); six resumes of 12K-32K tokens 2 350 us (6.9 TB/s).
 template <bool kPack>
 __device__ __forceinline__ void move_rows8(uint8_t *hot, uint8_t *codes, uint8_t *exps, int rows,
                                            int lane, uint64_t policy) {

@@ -2,6 +2,10 @@
 // a turn's context or a whole prompt (causal, its K and V written into the hot
 // pool), and drafted tokens (a bit mask per draft, nothing written).
 //
+// Per row, over key tiles: S = Q K^T; with c = scale log2(e), m the running maximum of c S and l the running
+// sum, weights P = 2^(c S - m), O = O 2^(m_before - m) + P V, l likewise; out = O / l. Pieces i of a row's
+// keys are merged with the weights 2^(m_i - m).
+//
 // turn_kernel: one persistent CTA per SM works through its piece of the line of items that
 // turn_plan.h lays out. The query heads that share a kv-head are packed into the
 // 128 rows of a row tile, so K and V are read once for all of them. A CTA has two
@@ -15,7 +19,17 @@
 //   9, 10     matrix products (tcgen05) of stream 0 and 1: S = Q K^T from shared
 //             memory, O += P V with P from tensor memory
 //   11        the new tokens' K and V, into the pool
-// The tensor cores work on one stream while the other's softmax runs.
+// The tensor cores work on one stream while the other's softmax runs. P lies in S's place, so a stream's
+// next scores wait for the product of its weights: a key tile of a pair takes 3 500 cycles, of which the
+// products need 2 050, and that chain bounds long prompts (tensor pipe 58 % active; no case got faster with
+// three quarters of the exponentials left out, or the maximum). Tensor memory has room for S beside P with
+// key tiles of 80: 5 % slower, because a product of 80 columns takes 80 % of one of 128. Two threads a row:
+// 20 % slower, 64 scores do not fit the registers of 640 threads. Few rows over long caches are bound by HBM.
+//   one prompt of 16 391 tokens, 32 heads (4 KV)           1 600 us   1 380 TFLOP/s
+//   turns of 300-3K tokens on 2K-24K, 4 sessions             930 us   1 340 TFLOP/s
+//   16 sessions of 2K-30K tokens, 16 drafts each             102 us   5.4 TB/s, with the merge
+//   one prompt of 37 tokens                                    9 us   plan, load, product, softmax, end in turn
+//
 // turn_combine_kernel merges the partial results of items that lie in several
 // pieces, in the pieces' order; it is a programmatic dependent of turn_kernel.
 #include <cuda_bf16.h>

@@ -66,6 +66,28 @@ def test_large_scores(cuda_dev, kind):
     c.check()
 
 
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1e-3, 2.0])
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_scales(cuda_dev, kind, scale):
+    """Negative: the smallest product weighs most. Zero: all that a row sees weighs the same."""
+    c = Call(kind, [33, 64, 3], [900, 0, 200], seed=27)
+    c.scale = scale
+    c.check()
+
+
+@pytest.mark.parametrize("blocks,B", [(3000, 3), (1 << 24, 40)])
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_tables_much_wider_than_the_sessions(cuda_dev, kind, blocks, B):
+    """The launch goes by the tables' width, the plan by the lengths: little work in a plan for much, and
+    one whose costs could pass 32 bits."""
+    c = Call(kind, [5, 40, 1, 17][:min(B, 4)] * max(1, B // 4), [100, 3, 129, 700][:min(B, 4)] * max(1, B // 4), seed=28)
+    wide = torch.full((B, blocks), -1, dtype=torch.int32, device="cuda")
+    wide[:, :c.width] = c.tables
+    c.tables, c.width = wide, blocks
+    c.check()
+    assert c.pool.check_device() == 0
+
+
 @pytest.mark.parametrize("kind", ["prefill", "tree"])
 def test_one_sessions_nan_stays_its_own(cuda_dev, kind):
     n, p = [20, 37, 50], [300, 40, 0]
