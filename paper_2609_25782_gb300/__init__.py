@@ -172,7 +172,7 @@ class Pool:
     def _turn(self, q, k, v, out):
         """(token strides of q and of k and v, tokens, flags) of a call on packed tokens, checked:
         bf16 [N][heads][D] each, heads contiguous, any token stride (k and v the same)."""
-        total, D = len(q), self.D
+        total, D = q.shape[0], self.D
         kv_shape = (total, self.Hkv, D)
         q_stride, kv_stride = q.stride(), k.stride()
         if q.dtype is not self._bf16 or k.dtype is not self._bf16 or v.dtype is not self._bf16 or \
