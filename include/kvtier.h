@@ -502,14 +502,15 @@ int kv_pool_set_migration_limit(kv_pool *pool, int32_t max_ctas);
  * n <= 0 disarms. */
 int kv_pool_inject_cuda_failure(kv_pool *pool, int32_t n);
 
-/* Test hook for the decode kernel's bounded waits: with on != 0, the next
+/* Test hook for the attention kernels' bounded waits: with on != 0, the next
  * decode call makes warp 0 of one CTA (split 0, kv-head 0, first row) expect
- * 16 bytes more than its first tile copy delivers. Every copy still lands;
- * that one wait runs out after its 2 s limit, the kernel sets
- * KV_DEVICE_TIMEOUT, waits (bounded) for the warp's other copies and
- * finishes. That call's output for the row is undefined; the CUDA context
- * stays usable and kv_pool_check_device reports the flag. Disarms itself
- * after one call. */
+ * 16 bytes more than its first tile copy delivers; if prefill_attention or
+ * tree_attention comes next, its first CTA does, for its first key tile. Every
+ * copy still lands; that one wait runs out after its 2 s limit, the kernel sets
+ * KV_DEVICE_TIMEOUT, waits (bounded) for the other copies and finishes. That
+ * call's output for the rows concerned is undefined; the CUDA context stays
+ * usable and kv_pool_check_device reports the flag. Disarms itself after one
+ * call. */
 int kv_pool_inject_decode_timeout(kv_pool *pool, int32_t on);
 
 /* Test hook for the counter check: synchronises the device and sets the

@@ -109,6 +109,7 @@ struct TurnArgs {
     // Partial results of items that are cut into pieces, of 2 slots per CTA (turn_part_floats).
     float *part;
     int32_t part_slots;
+    int32_t inject_extra_tx;         // test hook: extra bytes expected on one copy (0 normally)
     int32_t longest;                 // set by the launch: tokens that a table row holds
     int32_t whole, many, small;      // set by the launch: no item is cut; much work; costs fit 32 bits
     int32_t token_shift;             // set by the launch: tokens of a row tile, 128 / G, as a power of two

@@ -140,7 +140,7 @@ struct kv_pool {
 
     kv_pool_stats stats{};
     int32_t inject_countdown = 0;
-    bool inject_timeout = false;   // kv_pool_inject_decode_timeout, next decode only
+    bool inject_timeout = false;   // kv_pool_inject_decode_timeout, next attention call only
 
     // Residency mode (KV_POOL_LRU_RESIDENCY): sessions holding hot blocks,
     // ordered by (last use, sid); the first one is the least recently used.
@@ -1035,6 +1035,7 @@ static int turn_impl(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     a.layer = layer;
     a.out_bf16 = (flags & KV_DECODE_OUT_BF16) ? 1 : 0;
     a.scale_log2 = scale * 1.4426950408889634f;
+    a.inject_extra_tx = p->inject_timeout ? 16 : 0;
     a.negate = a.longest = a.whole = a.many = a.small = a.token_shift = 0;   // set by the launch
     a.part = p->d_turn_part;
     a.part_slots = 2 * p->num_sms;
@@ -1042,6 +1043,7 @@ static int turn_impl(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream_);
     int rc = p->cuda("attention launch", [&] { return kvt::launch_turn(a, p->turn_maps, st); });
     if (rc) return rc;
+    p->inject_timeout = false;
     p->decoded = true;
     p->decode_stream = st;
     return KV_OK;

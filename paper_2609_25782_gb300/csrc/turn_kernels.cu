@@ -512,6 +512,12 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
     uint32_t filled = 0, runs = 0;   // copies issued so far, saturating at kStages; runs published
     bool ok = true;                  // the same in all lanes until the last copy is out
     Walk walk(a, sm.plan);
+    // (A test of the bounded waits, 0 in normal calls: the first copy's barrier expects more than comes.)
+    if (a.inject_extra_tx && blockIdx.x == 0 && lane == 0)
+        asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(&sm.kv_full[0])),
+                     "r"(a.inject_extra_tx)
+                     : "memory");
+    __syncwarp();
 #pragma unroll 1
     while (ok) {
         Run r;
