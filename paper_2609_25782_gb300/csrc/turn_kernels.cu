@@ -156,6 +156,20 @@ __device__ __forceinline__ void copy_box(void *dst, const CUtensorMap *map, int 
         : "memory");
 }
 
+// The same, its lines the first to leave the L2.
+__device__ __forceinline__ uint64_t policy_once() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void copy_box_once(void *dst, const CUtensorMap *map, int c3, uint64_t *bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1, {%2, %2, %2, %3}], [%4], %5;" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(c3), "r"(smem_u32(bar)), "l"(policy)
+        : "memory");
+}
+
 // Shared-memory operand, 128-byte swizzle: rows of 128 B in groups of eight, `group` bytes from one to
 // the next. An operand that is summed over its rows (V) has its two column halves `half` bytes apart;
 // where the sum runs along the rows (Q, K) that field is not used.
@@ -465,30 +479,38 @@ __device__ __forceinline__ void store_rest(Rest &r, int rest, uint8_t *stage, in
 // The full groups of a K (kv = 0) or V tile into a stage, by the warp: cached keys grouped, a copy per
 // block (row: that of the lane's keys), the call's own whole.
 __device__ __forceinline__ void copy_groups(const TurnArgs &a, const Maps &maps, const Run &r, int groups, int rest, bool cached,
-                                            int first, int row, int kv, uint8_t *stage, uint64_t *full) {
+                                            int first, int row, int kv, uint8_t *stage, uint64_t *full, bool once) {
     const bool leader = elected();
     // Own keys that fill their groups come in one copy; rows past them, of later tokens or other sessions,
     // are not read.
     if (leader) mbar_expect(full, cached || rest ? groups * kBoxRows * kRowBytes : kTileBytes);
     // Each copy names its map by itself: with the map selected before, a copy took three times as long to issue.
     if (cached) {   // coordinates: (column, row of eight, half, eight rows)
-        int i = 0;
-        if (a.s.bt == 64)   // whole blocks
-            for (; i + 4 <= groups; i += 4) {
-                const int at = __shfl_sync(~0u, row, i) >> 3;
-                if (leader) copy_box(stage + i * 2 * kGroupGrouped, &maps.hot_block, 0, 0, at, full);
-            }
-        if (i == 0 && groups == kTurnKeys / kBoxRows) {
+        const auto copy_all = [&](auto box) {
+            int i = 0;
+            if (a.s.bt == 64)   // whole blocks
+                for (; i + 4 <= groups; i += 4) {
+                    const int at = __shfl_sync(~0u, row, i) >> 3;
+                    if (leader) box(stage + i * 2 * kGroupGrouped, &maps.hot_block, at);
+                }
+            if (i == 0 && groups == kTurnKeys / kBoxRows) {
 #pragma unroll
-            for (int k = 0; k < kTurnKeys / kBoxRows; ++k) {
-                const int at = __shfl_sync(~0u, row, k) >> 3;
-                if (leader) copy_box(stage + k * 2 * kGroupGrouped, &maps.hot, 0, 0, at, full);
+                for (int k = 0; k < kTurnKeys / kBoxRows; ++k) {
+                    const int at = __shfl_sync(~0u, row, k) >> 3;
+                    if (leader) box(stage + k * 2 * kGroupGrouped, &maps.hot, at);
+                }
+            } else {
+                for (; i < groups; ++i) {
+                    const int at = __shfl_sync(~0u, row, i) >> 3;
+                    if (leader) box(stage + i * 2 * kGroupGrouped, &maps.hot, at);
+                }
             }
+        };
+        if (once) {
+            const uint64_t policy = policy_once();
+            copy_all([&](uint8_t *to, const CUtensorMap *map, int at) { copy_box_once(to, map, at, full, policy); });
         } else {
-            for (; i < groups; ++i) {
-                const int at = __shfl_sync(~0u, row, i) >> 3;
-                if (leader) copy_box(stage + i * 2 * kGroupGrouped, &maps.hot, 0, 0, at, full);
-            }
+            copy_all([&](uint8_t *to, const CUtensorMap *map, int at) { copy_box(to, map, 0, 0, at, full); });
         }
     } else if (leader) {
         if (!rest) {                            // (column, token, half, head)
@@ -532,6 +554,10 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
         ++runs;
         if (!more) break;
         int blk = block_id(a, r, r.t0, lane);
+        // K and V that no other item reads (one pair) leave the L2 first: what every call needs stays there, the
+        // tables, the maps and this code, without which a CTA's first copy went out 5 us later (16 sessions'
+        // drafts 103 -> 98 us, 32 sessions' 125 -> 117).
+        const bool once = r.n <= 2 << s.shift;
         if (ok && items > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.q_empty, (items - 1) & 1));
         if (!ok) break;
         ++items;
@@ -570,7 +596,7 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
                     if (kv == 0) load_rest(extra, rest_v, step, rest, lane);
                 }
                 copy_groups(a, maps, r, groups, rest, cached, first, row + kv * v_rows, kv, sm.kv[stage],
-                            &sm.kv_full[stage + (round & 1) * kStages]);
+                            &sm.kv_full[stage + (round & 1) * kStages], once);
                 if (filled < kStages) ++filled;
                 if (++stage == kStages) {
                     stage = 0;
