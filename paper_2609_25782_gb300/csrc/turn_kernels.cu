@@ -27,7 +27,7 @@
 // 20 % slower, 64 scores do not fit the registers of 640 threads. Few rows over long caches are bound by HBM.
 //   one prompt of 16 391 tokens, 32 heads (4 KV)           1 600 us   1 380 TFLOP/s
 //   turns of 300-3K tokens on 2K-24K, 4 sessions             930 us   1 340 TFLOP/s
-//   16 sessions of 2K-30K tokens, 16 drafts each             102 us   5.4 TB/s, with the merge
+//   16 sessions of 2K-30K tokens, 16 drafts each              99 us   5.5 TB/s, with the merge
 //   one prompt of 37 tokens                                    9 us   plan, load, product, softmax, end in turn
 //
 // turn_combine_kernel merges the partial results of items that lie in several
@@ -556,7 +556,7 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
         int blk = block_id(a, r, r.t0, lane);
         // K and V that no other item reads (one pair) leave the L2 first: what every call needs stays there, the
         // tables, the maps and this code, without which a CTA's first copy went out 5 us later (16 sessions'
-        // drafts 103 -> 98 us, 32 sessions' 125 -> 117).
+        // drafts 103 -> 99 us, 32 sessions' 125 -> 117.5).
         const bool once = r.n <= 2 << s.shift;
         if (ok && items > 0) ok = __all_sync(~0u, mbar_wait(sm, &sm.q_empty, (items - 1) & 1));
         if (!ok) break;
