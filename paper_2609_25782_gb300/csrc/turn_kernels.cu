@@ -564,7 +564,7 @@ __device__ void copy_role(const TurnArgs &a, const Maps &maps, Smem &sm, int lan
         pairs += !r.narrow;
         if (elected())   // coordinates: (column, head, token, half)
 #pragma unroll 1
-            for (int i = 0; i < (r.narrow ? 1 : 2); ++i) {
+            for (int i = 0; i < turn_q_tiles(r.narrow); ++i) {
                 mbar_expect(&sm.q_full[i], kTileBytes);
                 copy_box(sm.q[i], &maps.q, r.g << (7 - s.shift), r.lo + ((2 * r.pair + i) << s.shift), 0, &sm.q_full[i]);
             }
@@ -682,8 +682,9 @@ __device__ void mma_role(const TurnArgs &a, Smem &sm, int stream) {
             mma_commit(&sm.kv_empty[stage]);
             if (narrow) mma_commit(&sm.kv_empty[stage]);
         };
-        const int q = narrow ? 0 : stream;
-        wait(&sm.q_full[q], (q ? pairs : items) & 1);
+        const int q = narrow ? 0 : stream, q_waits = turn_q_waits(stream, narrow);
+        if (q_waits & 1) wait(&sm.q_full[0], items & 1);
+        if (ok && q_waits & 2) wait(&sm.q_full[1], pairs & 1);
         ++items;
         pairs += !narrow;
         // Place of the run's tile i in the ring's sequence: its stage, and the wait for it.

@@ -66,6 +66,13 @@ KVT_PLAN int turn_pairs(const TurnShape &s, const TurnSession &x) {
 KVT_PLAN bool turn_narrow(const TurnShape &s, const TurnSession &x, int pair) {
     return x.n - (pair << (s.shift + 1)) <= 1 << s.shift;
 }
+// Row tiles of q that an item loads, q[0] and (wide) q[1], and those whose copies a stream's products wait
+// for, a bit each. The barrier of a q tile is one parity: a wait for its phase k passes at once while phase
+// k - 1 is still on its way, unless that one has been waited for. So whoever waits for a barrier waits for
+// each of its phases: stream 1 for q[0] in wide items too, which it does not read there, since it reads it
+// in narrow ones, and a session's last item is often narrow.
+KVT_PLAN int turn_q_tiles(bool narrow) { return narrow ? 1 : 2; }
+KVT_PLAN int turn_q_waits(int stream, bool narrow) { return stream == 0 || narrow ? 1 : 3; }
 // Own tokens that the item's rows can see.
 KVT_PLAN int turn_own_keys(const TurnShape &s, const TurnSession &x, int pair) {
     const int64_t end = (static_cast<int64_t>(pair) + 1) << (s.shift + 1);

@@ -134,6 +134,22 @@ def test_many_calls_in_a_row(cuda_dev, kind, hq, hkv, bt):
     assert c.pool.check_device() == 0
 
 
+@pytest.mark.parametrize("hq,hkv,n", [(32, 4, 48), (32, 8, 70), (8, 4, 150)])
+def test_short_wide_items_before_narrow_ones(cuda_dev, hq, hkv, n):
+    """Each CTA goes through several items of one or two key tiles, a pair of row tiles and then a single one
+    in turn: q tiles of both kinds follow each other faster than a stream's products."""
+    c = Call("prefill", [n] * 60, [0] * 60, hq=hq, hkv=hkv, seed=30, q_std=2.0)
+    c.check()
+    first = c.out.clone()
+    outs = [torch.empty_like(c.out) for _ in range(8)]
+    for _ in range(25):
+        for o in outs:
+            c.out = o
+            c.run()
+        assert all(torch.equal(o, first) for o in outs)
+    assert c.pool.check_device() == 0
+
+
 def test_prefill_of_one_token_is_the_decode_step(cuda_dev):
     """n = 1 over the same cache: the decode kernel's result, both within their rounding."""
     p = [77, 1, 2000]

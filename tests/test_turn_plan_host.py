@@ -133,3 +133,25 @@ def test_cuts_of_work_past_32_bits():
         cuts = [x.cut(W, 152, c) for c in range(153)]
         assert cuts[0] == 0 and cuts[-1] == W
         assert max(b - a for a, b in zip(cuts, cuts[1:])) - min(b - a for a, b in zip(cuts, cuts[1:])) <= 1
+
+
+def test_no_wait_for_a_q_tile_passes_a_phase_early():
+    """A barrier of one parity lets a wait for phase k through after k phases less one, too. So in any order
+    of wide and narrow items, each wait of a stream for a q tile's phase k comes after its wait for k - 1;
+    and a stream waits for what it reads: its own tile in wide items, the only one in narrow ones."""
+    x, r = lib(), random.Random(5)
+    assert (x.q_tiles(0), x.q_tiles(1)) == (2, 1)
+    for stream in (0, 1):
+        assert x.q_waits(stream, 1) & 1 and x.q_waits(stream, 0) >> stream & 1
+        for _ in range(200):
+            loaded, done = [0, 0], [0, 0]                # phases begun; those that the stream knows to be over
+            for narrow in [r.random() < 0.4 for _ in range(12)]:
+                for tile in range(x.q_tiles(narrow)):
+                    phase = loaded[tile]
+                    loaded[tile] += 1
+                    if not x.q_waits(stream, narrow) >> tile & 1:
+                        continue
+                    least, most = done[tile], loaded[tile]
+                    passes = [n for n in range(least, most + 1) if n & 1 != phase & 1]   # phases over by then
+                    assert passes and all(n > phase for n in passes), "a wait that the phase before lets through"
+                    done[tile] = phase + 1

@@ -50,5 +50,7 @@ int32_t tile_cost(int many, int narrow) {
     const TurnCosts c = turn_costs(shape(16, 1, 1, many));
     return narrow ? c.narrow_tile : c.tile;
 }
+int32_t q_tiles(int narrow) { return turn_q_tiles(narrow != 0); }
+int32_t q_waits(int stream, int narrow) { return turn_q_waits(stream, narrow != 0); }
 int32_t item_cost(int many) { return turn_costs(shape(16, 1, 1, many)).item; }
 }
