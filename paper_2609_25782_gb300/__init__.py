@@ -171,16 +171,18 @@ class Pool:
 
     def _turn(self, q, k, v, out):
         """(token strides of q and of k and v, tokens, flags) of a call on packed tokens, checked:
-        bf16 [N][heads][D] each, heads contiguous, any token stride (k and v the same)."""
+        bf16 [N][heads][D] each, heads contiguous, any token stride (k and v the same) but 0, which
+        tokens that share storage have and which the library takes for contiguous rows."""
         total, D = q.shape[0], self.D
         kv_shape = (total, self.Hkv, D)
         q_stride, kv_stride = q.stride(), k.stride()
         if q.dtype is not self._bf16 or k.dtype is not self._bf16 or v.dtype is not self._bf16 or \
                 q.shape != (total, self.Hq, D) or k.shape != kv_shape or v.shape != kv_shape or \
                 q_stride[2] != 1 or (q_stride[1] != D and self.Hq > 1) or kv_stride != v.stride() or \
-                kv_stride[2] != 1 or (kv_stride[1] != D and self.Hkv > 1):
+                kv_stride[2] != 1 or (kv_stride[1] != D and self.Hkv > 1) or \
+                (total > 1 and (q_stride[0] == 0 or kv_stride[0] == 0)):
             raise ValueError(f"need bf16 q [{total}][{self.Hq}][{D}], k and v {list(kv_shape)} with contiguous heads "
-                             "and one token stride for k and v, got " +
+                             "and one token stride for k and v (not 0), got " +
                              ", ".join(f"{x.dtype} {tuple(x.shape)} strides {x.stride()}" for x in (q, k, v)))
         if out.shape != q.shape or not out.is_contiguous() or out.dtype not in self._out_flags:
             raise ValueError(f"out must be contiguous fp32 or bf16 [{total}][{self.Hq}][{D}]")

@@ -1,0 +1,68 @@
+"""What Pool.prefill_attention and Pool.tree_attention hand to the library, and what they refuse,
+without a GPU: tensors on the CPU and a library call that only notes its arguments."""
+import pytest
+import torch
+
+D = 128
+
+
+@pytest.fixture(scope="module")
+def package():
+    import __graft_entry__
+    __graft_entry__.build()
+    import paper_2609_25782_gb300
+    return paper_2609_25782_gb300
+
+
+def make_pool(package, hq=8, hkv=2):
+    """A pool without arenas or a handle."""
+    p = package.Pool.__new__(package.Pool)
+    p.device, p.handle, p.Hq, p.Hkv, p.D = torch.device("cpu"), None, hq, hkv, D
+    p._bf16 = torch.bfloat16
+    p._out_flags = {torch.float32: 0, torch.bfloat16: package.kvtier.KV_DECODE_OUT_BF16}
+    p._index = -1                      # the device number that tensors on the CPU give
+    p.calls = []
+    p._prefill = p._tree = lambda *a: p.calls.append(a) or 0
+    return p
+
+
+def arguments(pool, n, sessions=1, kind="prefill", **other):
+    a = dict(q=torch.zeros(n, pool.Hq, D).bfloat16(), k=torch.zeros(n, pool.Hkv, D).bfloat16(),
+             v=torch.zeros(n, pool.Hkv, D).bfloat16(), cu=torch.zeros(sessions + 1, dtype=torch.int32),
+             tables=torch.zeros(sessions, 4, dtype=torch.int32), lens=torch.zeros(sessions, dtype=torch.int32),
+             B=sessions, width=4, out=torch.zeros(n, pool.Hq, D), stream=None,
+             masks=torch.zeros(n, dtype=torch.int64))
+    a.update(other)
+    return a
+
+
+def call(pool, kind, a):
+    """The strides that reach the library: (q's, k's and v's)."""
+    pool.calls.clear()
+    if kind == "prefill":
+        pool.prefill_attention(0, a["q"], a["k"], a["v"], a["cu"], a["tables"], a["lens"], a["B"], a["width"], 0.1,
+                               a["out"], a["stream"])
+    else:
+        pool.tree_attention(0, a["q"], a["k"], a["v"], a["masks"], a["cu"], a["tables"], a["lens"], a["B"],
+                            a["width"], 0.1, a["out"], a["stream"])
+    (got,) = pool.calls
+    assert got[2] == a["q"].data_ptr() and got[4] == a["k"].data_ptr() and got[5] == a["v"].data_ptr()
+    return got[3], got[6]
+
+
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_tokens_that_share_storage_are_refused(package, kind):
+    """The library takes a stride of 0 for rows one after the other: eight tokens expanded from one would be
+    read from eight times their storage."""
+    pool = make_pool(package)
+    q, kv = torch.zeros(1, 8, D).bfloat16().expand(8, 8, D), torch.zeros(1, 2, D).bfloat16().expand(8, 2, D)
+    assert q.stride(0) == kv.stride(0) == 0
+    for other in (dict(q=q), dict(k=kv, v=kv), dict(q=q, k=kv, v=kv)):
+        with pytest.raises(ValueError):
+            call(pool, kind, arguments(pool, 8, **other))
+    assert not pool.calls
+    assert call(pool, kind, arguments(pool, 8)) == (8 * D, 2 * D)
+    qkv = torch.zeros(8, 12, D).bfloat16()
+    assert call(pool, kind, arguments(pool, 8, q=qkv[:, :8], k=qkv[:, 8:10], v=qkv[:, 10:])) == (12 * D, 12 * D)
+    # a single token's stride means nothing
+    call(pool, kind, arguments(pool, 1, q=q[:1], k=kv[:1], v=kv[:1]))
