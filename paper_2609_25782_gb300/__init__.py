@@ -175,20 +175,21 @@ class Pool:
         tokens that share storage have and which the library takes for contiguous rows."""
         total, D = q.shape[0], self.D
         kv_shape = (total, self.Hkv, D)
-        q_stride, kv_stride = q.stride(), k.stride()
+        q_stride, k_stride, v_stride = q.stride(), k.stride(), v.stride()
+        # (What a single token or head has for a stride means nothing.)
         if q.dtype is not self._bf16 or k.dtype is not self._bf16 or v.dtype is not self._bf16 or \
                 q.shape != (total, self.Hq, D) or k.shape != kv_shape or v.shape != kv_shape or \
-                q_stride[2] != 1 or (q_stride[1] != D and self.Hq > 1) or kv_stride != v.stride() or \
-                kv_stride[2] != 1 or (kv_stride[1] != D and self.Hkv > 1) or \
-                (total > 1 and (q_stride[0] == 0 or kv_stride[0] == 0)):
+                q_stride[2] != 1 or k_stride[2] != 1 or v_stride[2] != 1 or (q_stride[1] != D and self.Hq > 1) or \
+                (self.Hkv > 1 and (k_stride[1] != D or v_stride[1] != D)) or \
+                (total > 1 and (k_stride[0] != v_stride[0] or q_stride[0] == 0 or k_stride[0] == 0)):
             raise ValueError(f"need bf16 q [{total}][{self.Hq}][{D}], k and v {list(kv_shape)} with contiguous heads "
                              "and one token stride for k and v (not 0), got " +
                              ", ".join(f"{x.dtype} {tuple(x.shape)} strides {x.stride()}" for x in (q, k, v)))
         if out.shape != q.shape or not out.is_contiguous() or out.dtype not in self._out_flags:
             raise ValueError(f"out must be contiguous fp32 or bf16 [{total}][{self.Hq}][{D}]")
-        if total < 2:   # the stride of a single token says nothing
+        if total < 2:
             return 0, 0, total, self._out_flags[out.dtype]
-        return q_stride[0], kv_stride[0], total, self._out_flags[out.dtype]
+        return q_stride[0], k_stride[0], total, self._out_flags[out.dtype]
 
     def prefill_attention(self, layer: int, q, k_new, v_new, cu_new, block_tables, seq_lens, B: int,
                           max_blocks: int, scale: float, out, stream=None) -> None:

@@ -66,3 +66,25 @@ def test_tokens_that_share_storage_are_refused(package, kind):
     assert call(pool, kind, arguments(pool, 8, q=qkv[:, :8], k=qkv[:, 8:10], v=qkv[:, 10:])) == (12 * D, 12 * D)
     # a single token's stride means nothing
     call(pool, kind, arguments(pool, 1, q=q[:1], k=kv[:1], v=kv[:1]))
+
+
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_strides_that_mean_nothing_are_not_compared(package, kind):
+    """A single token's stride, and a single head's: k may be contiguous and v a view."""
+    pool = make_pool(package)
+    qkv = torch.zeros(8, 12, D).bfloat16()
+    call(pool, kind, arguments(pool, 1, v=qkv[:1, 10:]))
+    call(pool, kind, arguments(pool, 1, k=qkv[:1, 8:10]))
+    one = make_pool(package, hq=4, hkv=1)
+    whole = torch.zeros(8, 6 * D).bfloat16()
+    k = torch.as_strided(whole, (8, 1, D), (6 * D, D, 1), 4 * D)
+    v = torch.as_strided(whole, (8, 1, D), (6 * D, 6 * D, 1), 5 * D)
+    assert k.stride() != v.stride()
+    assert call(one, kind, arguments(one, 8, k=k, v=v))[1] == 6 * D
+    # strides that do mean something
+    two = torch.zeros(8, 2, 2 * D).bfloat16()
+    for other in (dict(v=qkv[:, 10:]), dict(v=two[:, :, :D]), dict(v=torch.zeros(8, 2, 2 * D).bfloat16()[:, :, ::2])):
+        with pytest.raises(ValueError):
+            call(pool, kind, arguments(pool, 8, **other))
+    with pytest.raises(ValueError):
+        call(pool, kind, arguments(pool, 1, v=two[:1, :, :D]))
