@@ -32,7 +32,8 @@ class Pool:
         # The calls that a model makes per layer go to the library by the shortest way: a call on a few
         # tokens takes the GPU about as long as the host.
         self._prefill, self._tree = kvtier.lib.prefill_attention, kvtier.lib.tree_attention
-        self._bf16 = torch.bfloat16
+        self._bf16, self._i32, self._masks, self._index = (torch.bfloat16, torch.int32,
+                                                           (torch.int64, torch.uint64), device)
         self._out_flags = {torch.float32: 0, torch.bfloat16: kvtier.KV_DECODE_OUT_BF16}
         probe = kvtier.make_config(num_layers=num_layers, num_q_heads=num_q_heads,
                                    num_kv_heads=num_kv_heads, head_dim=head_dim,
@@ -169,10 +170,11 @@ class Pool:
         kvtier.decode_append_attention(self.handle, layer, q, k_new, v_new, block_tables, seq_lens,
                                        B, max_blocks, scale, out, flags, stream)
 
-    def _turn(self, q, k, v, out):
-        """(token strides of q and of k and v, tokens, flags) of a call on packed tokens, checked:
-        bf16 [N][heads][D] each, heads contiguous, any token stride (k and v the same) but 0, which
-        tokens that share storage have and which the library takes for contiguous rows."""
+    def _turn(self, q, k, v, out, cu, tables, lens, B, max_blocks):
+        """(token strides of q and of k and v, tokens, flags) of a call on packed tokens, checked: all
+        on the pool's device; q, k and v bf16 [N][heads][D], heads contiguous, any token stride (k and
+        v the same) but 0, which tokens that share storage have and which the library takes for
+        contiguous rows; offsets, tables and lengths int32, contiguous, as long as the call reads."""
         total, D = q.shape[0], self.D
         kv_shape = (total, self.Hkv, D)
         q_stride, k_stride, v_stride = q.stride(), k.stride(), v.stride()
@@ -187,6 +189,17 @@ class Pool:
                              ", ".join(f"{x.dtype} {tuple(x.shape)} strides {x.stride()}" for x in (q, k, v)))
         if out.shape != q.shape or not out.is_contiguous() or out.dtype not in self._out_flags:
             raise ValueError(f"out must be contiguous fp32 or bf16 [{total}][{self.Hq}][{D}]")
+        i32, index = self._i32, self._index
+        if cu.dtype is not i32 or tables.dtype is not i32 or lens.dtype is not i32 or cu.numel() <= B or \
+                tables.numel() < B * max_blocks or lens.numel() < B or not cu.is_contiguous() or \
+                not tables.is_contiguous() or not lens.is_contiguous():
+            raise ValueError(f"need contiguous int32 offsets [{B + 1}], block tables [{B}][{max_blocks}] and lengths "
+                             f"[{B}], got " + ", ".join(f"{x.dtype} {tuple(x.shape)} strides {x.stride()}"
+                                                        for x in (cu, tables, lens)))
+        if q.get_device() != index or k.get_device() != index or v.get_device() != index or \
+                out.get_device() != index or cu.get_device() != index or tables.get_device() != index or \
+                lens.get_device() != index:
+            raise ValueError(f"all tensors must be on the pool's device, {self.device}")
         if total < 2:
             return 0, 0, total, self._out_flags[out.dtype]
         return q_stride[0], k_stride[0], total, self._out_flags[out.dtype]
@@ -197,7 +210,8 @@ class Pool:
         cu_new[b]..cu_new[b+1]-1 of q [N][Hq][D] and k_new, v_new [N][Hkv][D] (bf16, any token
         stride, so views of one projection will do), the newest of its seq_lens[b] tokens; K and V
         go into the slots that batch_reserve(counts=...) allocated. out: fp32 or bf16."""
-        q_stride, kv_stride, total, flags = self._turn(q, k_new, v_new, out)
+        q_stride, kv_stride, total, flags = self._turn(q, k_new, v_new, out, cu_new, block_tables, seq_lens, B,
+                                                       max_blocks)
         rc = self._prefill(self.handle, layer, q.data_ptr(), q_stride, k_new.data_ptr(),
                            v_new.data_ptr(), kv_stride, cu_new.data_ptr(), total,
                            block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, scale,
@@ -210,9 +224,11 @@ class Pool:
         """Attention of drafted tokens (at most 64 per session, packed by cu_draft) over the
         session's seq_lens[b] cached tokens and the drafts in ancestors [N] (64-bit masks over the
         session's own drafts). Nothing is written to the pool."""
-        q_stride, kv_stride, total, flags = self._turn(q, k_draft, v_draft, out)
-        if ancestors.numel() != total or ancestors.element_size() != 8 or not ancestors.is_contiguous():
-            raise ValueError("one contiguous 64-bit mask per draft")
+        q_stride, kv_stride, total, flags = self._turn(q, k_draft, v_draft, out, cu_draft, block_tables, seq_lens, B,
+                                                       max_blocks)
+        if ancestors.numel() != total or ancestors.dtype not in self._masks or not ancestors.is_contiguous() or \
+                ancestors.get_device() != self._index:
+            raise ValueError("need one contiguous 64-bit integer mask per draft, on the pool's device")
         rc = self._tree(self.handle, layer, q.data_ptr(), q_stride, k_draft.data_ptr(),
                         v_draft.data_ptr(), kv_stride, ancestors.data_ptr(), cu_draft.data_ptr(), total,
                         block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, scale,

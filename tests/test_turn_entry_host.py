@@ -18,7 +18,7 @@ def make_pool(package, hq=8, hkv=2):
     """A pool without arenas or a handle."""
     p = package.Pool.__new__(package.Pool)
     p.device, p.handle, p.Hq, p.Hkv, p.D = torch.device("cpu"), None, hq, hkv, D
-    p._bf16 = torch.bfloat16
+    p._bf16, p._i32, p._masks = torch.bfloat16, torch.int32, (torch.int64, torch.uint64)
     p._out_flags = {torch.float32: 0, torch.bfloat16: package.kvtier.KV_DECODE_OUT_BF16}
     p._index = -1                      # the device number that tensors on the CPU give
     p.calls = []
@@ -88,3 +88,53 @@ def test_strides_that_mean_nothing_are_not_compared(package, kind):
             call(pool, kind, arguments(pool, 8, **other))
     with pytest.raises(ValueError):
         call(pool, kind, arguments(pool, 1, v=two[:1, :, :D]))
+
+
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_offsets_tables_and_lengths_that_the_library_would_misread(package, kind):
+    """32-bit integers, contiguous, as many as the call reads; a wider or longer buffer is no fault."""
+    pool = make_pool(package)
+    i32 = torch.int32
+
+    def good(**other):
+        return call(pool, kind, arguments(pool, 6, 2, **other))
+
+    def bad(**other):
+        with pytest.raises(ValueError):
+            good(**other)
+        assert not pool.calls
+    good()
+    good(cu=torch.zeros(9, dtype=i32), lens=torch.zeros(5, dtype=i32), tables=torch.zeros(3, 9, dtype=i32))
+    good(tables=torch.zeros(8, dtype=i32))
+    good(cu=torch.zeros(6, dtype=i32)[1:4])
+    for name, n in (("cu", 3), ("lens", 2), ("tables", 8)):
+        bad(**{name: torch.zeros(n, dtype=torch.int64)})         # what cumsum of 32-bit integers gives
+        bad(**{name: torch.zeros(n, dtype=torch.float32)})
+        bad(**{name: torch.zeros(n - 1, dtype=i32)})
+        bad(**{name: torch.zeros(2 * n, dtype=i32)[::2]})
+        bad(**{name: torch.zeros(1, dtype=i32).expand(n)})
+    bad(tables=torch.zeros(2, 9, dtype=i32)[:, :4])              # columns of a wider table
+    if kind == "tree":
+        good(masks=torch.zeros(6, dtype=torch.uint64))
+        for masks in (torch.zeros(6, dtype=torch.float64), torch.zeros(5, dtype=torch.int64),
+                      torch.zeros(6, dtype=i32), torch.zeros(12, dtype=torch.int64)[::2]):
+            bad(masks=masks)
+
+
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_tensors_on_another_device_are_refused(package, kind):
+    """A host address would fault in the kernel: here the pool is on device 0, the tensors are not."""
+    pool = make_pool(package)
+    a = arguments(pool, 6, 2)
+    call(pool, kind, a)
+
+    class Elsewhere(torch.Tensor):
+        def get_device(self):
+            return 1
+    for name in ("q", "k", "v", "cu", "tables", "lens", "out") + (("masks",) if kind == "tree" else ()):
+        with pytest.raises(ValueError):
+            call(pool, kind, dict(a, **{name: a[name].as_subclass(Elsewhere)}))
+    pool._index = 0
+    with pytest.raises(ValueError):
+        call(pool, kind, a)
+    assert not pool.calls
