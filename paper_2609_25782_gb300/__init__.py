@@ -215,7 +215,7 @@ class Pool:
         rc = self._prefill(self.handle, layer, q.data_ptr(), q_stride, k_new.data_ptr(),
                            v_new.data_ptr(), kv_stride, cu_new.data_ptr(), total,
                            block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, scale,
-                           out.data_ptr(), flags, None if stream is None else stream.cuda_stream)
+                           out.data_ptr(), flags, kvtier._stream(stream))
         if rc:
             kvtier.raise_last(rc, "prefill_attention")
 
@@ -232,7 +232,7 @@ class Pool:
         rc = self._tree(self.handle, layer, q.data_ptr(), q_stride, k_draft.data_ptr(),
                         v_draft.data_ptr(), kv_stride, ancestors.data_ptr(), cu_draft.data_ptr(), total,
                         block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, scale,
-                        out.data_ptr(), flags, None if stream is None else stream.cuda_stream)
+                        out.data_ptr(), flags, kvtier._stream(stream))
         if rc:
             kvtier.raise_last(rc, "tree_attention")
 

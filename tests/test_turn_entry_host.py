@@ -138,3 +138,15 @@ def test_tensors_on_another_device_are_refused(package, kind):
     with pytest.raises(ValueError):
         call(pool, kind, a)
     assert not pool.calls
+
+
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_streams_as_in_the_other_calls(package, kind):
+    """None (the legacy default stream), a torch stream, or a stream's handle as an integer."""
+    pool = make_pool(package)
+
+    class Stream:
+        cuda_stream = 77
+    for stream, handle in ((None, None), (Stream(), 77), (1234, 1234), (0, 0)):
+        call(pool, kind, arguments(pool, 3, stream=stream))
+        assert pool.calls[0][-1] == handle
