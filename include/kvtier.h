@@ -312,7 +312,7 @@ int decode_append_attention(kv_pool *pool, int32_t layer, const void *q, const v
  *   total        rows of q, k_new, v_new and out; 0 does nothing
  *   block_tables device int32 [B][max_blocks]
  *   seq_lens     device int32 [B]: tokens of the session with the new ones, at
- *                most max_blocks * bt
+ *                most max_blocks * bt (and 2^31 - 513)
  *   out          device fp32 [total][Hq][D], or bf16 with KV_DECODE_OUT_BF16
  * out[lo + i][h] = sum over t <= seq_len - n + i of softmax_t(scale * q . K[g][t])
  * V[g][t] for the session's n new tokens at rows lo + i, g = h / (Hq/Hkv).

@@ -1318,8 +1318,7 @@ cudaError_t launch_turn(TurnArgs a, const CUtensorMap hot[2], cudaStream_t st) {
     a.token_shift = G == 8 ? 4 : G == 4 ? 5 : G == 2 ? 6 : 7;
     // No more CTAs than there can be pieces; items of at most two key tiles are not cut, which saves the
     // merge's launch (a prompt of 37 tokens: 9.9 us with it, 9.1 without).
-    const int64_t longest = static_cast<int64_t>(a.max_blocks) * a.s.bt;
-    a.longest = static_cast<int32_t>(std::min<int64_t>(longest, INT32_MAX));
+    const int64_t longest = a.longest = turn_longest(a.max_blocks, a.s.bt);
     const int64_t bound = turn_cost_bound(turn_shape(a), a.total, a.B, longest);
     const unsigned ctas = static_cast<unsigned>(
         std::max<int64_t>(1, std::min<int64_t>(bound / kCostsFew.piece, a.part_slots / 2)));

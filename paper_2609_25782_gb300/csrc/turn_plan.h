@@ -60,6 +60,12 @@ KVT_PLAN TurnCosts turn_costs(const TurnShape &s) {
 }
 
 KVT_PLAN int turn_tiles_of(int keys) { return static_cast<int>((static_cast<uint32_t>(keys) + kTurnKeys - 1) / kTurnKeys); }
+// The longest session that a call takes: what a table row holds, and so that a position in a last key tile,
+// or a group of 16 keys that a lane of a warp past it would have, still is a 32-bit one.
+KVT_PLAN int32_t turn_longest(int64_t max_blocks, int block_tokens) {
+    const int64_t holds = max_blocks * block_tokens, most = INT32_MAX - 4 * kTurnKeys;
+    return static_cast<int32_t>(holds < most ? holds : most);
+}
 KVT_PLAN int turn_pairs(const TurnShape &s, const TurnSession &x) {
     return static_cast<int>((static_cast<uint32_t>(x.n) + (2u << s.shift) - 1) >> (s.shift + 1));
 }

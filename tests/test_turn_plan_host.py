@@ -27,6 +27,7 @@ def lib():
         getattr(x, name).restype = None
         getattr(x, name).argtypes = [i32] * 6 + [i64, ctypes.POINTER(i32)]
     x.pieces.argtypes = [i32, i64, i32]
+    x.longest.argtypes = [i64, i32]
     x.is_many.argtypes = [i64, i32]
     x.cut.argtypes = x.cut_32.argtypes = [i64, i32, i32]
     x.cost_bound.argtypes = [i32, i32, i32, i64, i64, i64]
@@ -155,3 +156,13 @@ def test_no_wait_for_a_q_tile_passes_a_phase_early():
                     passes = [n for n in range(least, most + 1) if n & 1 != phase & 1]   # phases over by then
                     assert passes and all(n > phase for n in passes), "a wait that the phase before lets through"
                     done[tile] = phase + 1
+
+
+@pytest.mark.parametrize("bt", [16, 64])
+def test_positions_of_the_longest_session_fit_32_bits(bt):
+    """Tables may have rows of 2^26 blocks; a lane's group of 16 keys lies up to 496 past a tile's start."""
+    x = lib()
+    for blocks in (1, 7, 1 << 20, (1 << 25) - 1, 1 << 25, 1 << 26):
+        longest = x.longest(blocks, bt)
+        assert longest == blocks * bt or blocks * bt > longest > 2 ** 31 - 1024
+        assert (x.tiles_of(longest) - 1) * 128 + 31 * 16 < 2 ** 31

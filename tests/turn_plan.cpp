@@ -50,6 +50,8 @@ int32_t tile_cost(int many, int narrow) {
     const TurnCosts c = turn_costs(shape(16, 1, 1, many));
     return narrow ? c.narrow_tile : c.tile;
 }
+int32_t longest(int64_t max_blocks, int bt) { return turn_longest(max_blocks, bt); }
+int32_t tiles_of(int keys) { return turn_tiles_of(keys); }
 int32_t q_tiles(int narrow) { return turn_q_tiles(narrow != 0); }
 int32_t q_waits(int stream, int narrow) { return turn_q_waits(stream, narrow != 0); }
 int32_t item_cost(int many) { return turn_costs(shape(16, 1, 1, many)).item; }
