@@ -172,7 +172,8 @@ typedef struct kv_pool_stats {
  * Fisher-Yates driven by splitmix64 seeded with alloc_seed (draw
  * j = floor(r * (i+1) / 2^64) for i = n-1 .. 1); allocations pop from its
  * end. Allocates the pool's device metadata (tables, decode workspace, flag
- * word) with cudaMalloc. *out receives the pool. Errors: bad shape or null
+ * word) with cudaMalloc; later calls allocate nothing, but for the workspace of
+ * prefill_attention and tree_attention (see there). *out receives the pool. Errors: bad shape or null
  * or misaligned arenas -> KV_ERR_INVALID_ARG; a failing CUDA call ->
  * KV_ERR_CUDA (nothing is left allocated). */
 int kv_pool_create(const kv_pool_config *cfg, kv_pool **out);
@@ -325,9 +326,12 @@ int decode_append_attention(kv_pool *pool, int32_t layer, const void *q, const v
  * KV_DEVICE_BAD_LENGTH, and that session's rows are not written; a block id out
  * of range sets KV_DEVICE_BAD_BLOCK, a wait inside the kernel that runs out (2 s)
  * KV_DEVICE_TIMEOUT, and rows that they concern are wrong. Calls of this and
- * tree_attention on one pool share a workspace (0.27 MB per SM, allocated with the
- * pool): issue them in order on one stream, as decode_attention's. In residency
- * mode order them before the next call that may evict, as a decode. */
+ * tree_attention on one pool share a workspace: issue them in order on one
+ * stream, as decode_attention's. It has 0.27 MB per SM; the pool's first call
+ * with tables of more than 128 tokens allocates it with cudaMalloc (KV_ERR_CUDA
+ * where there is no room), also while a graph is recorded, and the pool keeps
+ * it. In residency mode order them before the next call that may evict, as a
+ * decode. */
 int prefill_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride,
                       const void *k_new, const void *v_new, int64_t kv_stride, const int32_t *cu_new,
                       int32_t total, const int32_t *block_tables, const int32_t *seq_lens, int32_t B,

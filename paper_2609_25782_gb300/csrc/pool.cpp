@@ -18,6 +18,7 @@
 #include "../../include/kvtier.h"
 #include "decode_launch.h"
 #include "kvt_internal.h"
+#include "turn_plan.h"
 
 static_assert(KV_DEVICE_BAD_BLOCK == kvt::kErrBadBlock && KV_DEVICE_BAD_LENGTH == kvt::kErrBadLength &&
                   KV_DEVICE_TIMEOUT == kvt::kErrTimeout,
@@ -131,8 +132,10 @@ struct kv_pool {
     int32_t *d_counters = nullptr;       // split arrivals per (layer-batch row, kv-head)
     int64_t counter_count = 0;
     int32_t *d_err = nullptr;
-    float *d_turn_part = nullptr;        // partial results of prefill_attention and tree_attention
-    CUtensorMap tmap{}, turn_maps[2]{};
+    CUtensorMap tmap{};
+    // prefill_attention and tree_attention (turn_setup)
+    CUtensorMap turn_maps[2]{};
+    float *d_turn_part = nullptr;        // partial results
 
     Fence fences[kFenceSlots];
     int next_fence = 0;
@@ -524,7 +527,6 @@ int kv_pool_create(const kv_pool_config *cfg, kv_pool **out) {
         const int64_t at_o = place(prow * kvt::kHeadDim * sizeof(float));
         const int64_t at_ml = place(prow * 2 * sizeof(float));
         const int64_t at_tables = place(tbl);
-        const int64_t at_turn = place(kvt::turn_part_floats(p->num_sms) * sizeof(float));
         const int64_t at_counters = place(p->counter_count * 4);
         const int64_t at_err = place(4);
         int rc = p->cuda("cudaMalloc(pool metadata)", [&] { return cudaMalloc(&p->d_slab, bytes); });
@@ -533,7 +535,6 @@ int kv_pool_create(const kv_pool_config *cfg, kv_pool **out) {
             p->d_part_o = reinterpret_cast<float *>(base + at_o);
             p->d_part_ml = reinterpret_cast<float *>(base + at_ml);
             p->d_tables = reinterpret_cast<int32_t *>(base + at_tables);
-            p->d_turn_part = reinterpret_cast<float *>(base + at_turn);
             p->d_counters = reinterpret_cast<int32_t *>(base + at_counters);
             p->d_err = reinterpret_cast<int32_t *>(base + at_err);
         }
@@ -571,6 +572,7 @@ int kv_pool_destroy(kv_pool *p) {
         for (auto &f : p->fences)
             if (f.ev) cudaEventDestroy(f.ev);
         cudaFree(p->d_slab);
+        cudaFree(p->d_turn_part);
     }
     delete p;
     return KV_OK;
@@ -984,6 +986,25 @@ int decode_append_attention(kv_pool *p, int32_t layer, const void *q, const void
                        out, flags, stream);
 }
 
+// What the calls below need besides, set up by the first of them: a pool that only decodes holds no
+// workspace for prompts (0.27 MB per SM), and a small one is created in 0.02 ms in place of 0.10 and destroyed
+// in 0.003 in place of 0.07. `cuts`: the call may leave partial results.
+static int turn_setup(kv_pool *p, bool cuts) {
+    if (p->d_turn_part || !cuts) return KV_OK;
+    // The call may be one that a graph records; the set-up is no part of the recording.
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    int rc = p->cuda("cudaMalloc(workspace of prompt and draft attention)", [&] {
+        void *part = nullptr;
+        const cudaError_t e = cudaMalloc(&part, kvt::turn_part_floats(p->num_sms) * sizeof(float));
+        if (e == cudaSuccess) p->d_turn_part = static_cast<float *>(part);
+        return e;
+    });
+    if (rc) cudaGetLastError();   // a later launch asks for its own
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    return rc;
+}
+
 // Several new tokens per session: a turn's context (masks == null) or drafts.
 static int turn_impl(kv_pool *p, int32_t layer, const void *q, int64_t q_stride, const void *k,
                      const void *v, int64_t kv_stride, const uint64_t *masks, const int32_t *cu,
@@ -1016,6 +1037,8 @@ static int turn_impl(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     if (p->host_only) return fail(KV_ERR_BAD_STATE, "attention on a host-logic-only pool");
     if (total == 0) return KV_OK;
     DeviceGuard dg(p->cfg.device, true);
+    int rc = turn_setup(p, kvt::turn_cuts(kvt::turn_longest(max_blocks, p->cfg.block_tokens)));
+    if (rc) return rc;
     kvt::TurnArgs a;
     a.q = static_cast<const uint16_t *>(q);
     a.k_new = static_cast<const uint16_t *>(k);
@@ -1041,7 +1064,7 @@ static int turn_impl(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     a.part_slots = 2 * p->num_sms;
     a.s = p->shape;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream_);
-    int rc = p->cuda("attention launch", [&] { return kvt::launch_turn(a, p->turn_maps, st); });
+    rc = p->cuda("attention launch", [&] { return kvt::launch_turn(a, p->turn_maps, st); });
     if (rc) return rc;
     p->inject_timeout = false;
     p->decoded = true;

@@ -66,6 +66,9 @@ KVT_PLAN int32_t turn_longest(int64_t max_blocks, int block_tokens) {
     const int64_t holds = max_blocks * block_tokens, most = INT32_MAX - 4 * kTurnKeys;
     return static_cast<int32_t>(holds < most ? holds : most);
 }
+// Whether items of such sessions may be cut: those of at most two key tiles are not, which saves the merge's
+// launch (a prompt of 37 tokens: 9.9 us with it, 9.1 without).
+KVT_PLAN bool turn_cuts(int64_t longest) { return longest > kTurnKeys; }
 KVT_PLAN int turn_pairs(const TurnShape &s, const TurnSession &x) {
     return static_cast<int>((static_cast<uint32_t>(x.n) + (2u << s.shift) - 1) >> (s.shift + 1));
 }

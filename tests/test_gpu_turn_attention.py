@@ -276,6 +276,29 @@ def test_capture_and_replay_with_longer_contexts(cuda_dev):
     assert torch.equal(c.out, want)
 
 
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_the_first_call_of_a_pool_is_recorded(cuda_dev, kind):
+    """The call that allocates the pool's workspace, while a graph is recorded; decodes need none of it."""
+    c = Call(kind, [16, 40], [2000, 900], seed=31)
+    refs = [c.reference(b) for b in range(2)]
+    c.pool.decode_attention(0, c.q[:1], c.tables, torch.tensor([5], dtype=torch.int32, device="cuda"), 1, 1, c.scale,
+                            torch.empty(1, c.hq, 128, device="cuda"))
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        c.run(side)
+        graph.capture_end()
+    for _ in range(2):
+        c.out.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for b, (ref, noise) in enumerate(refs):
+            c.assert_right(b, ref, noise)
+    assert c.pool.check_device() == 0
+
+
 @pytest.mark.slow
 @pytest.mark.parametrize("kind", ["prefill", "tree"])
 def test_arena_past_32_bit_offsets(cuda_dev, kind):
