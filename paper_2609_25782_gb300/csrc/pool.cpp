@@ -134,6 +134,7 @@ struct kv_pool {
     int32_t *d_err = nullptr;
     CUtensorMap tmap{};
     // prefill_attention and tree_attention (turn_setup)
+    bool turn_ready = false;             // the kernel and the maps
     CUtensorMap turn_maps[2]{};
     float *d_turn_part = nullptr;        // partial results
 
@@ -543,13 +544,10 @@ int kv_pool_create(const kv_pool_config *cfg, kv_pool **out) {
             return cudaMemset(p->d_counters, 0, bytes - at_counters);
         });
         if (!rc) rc = p->cuda("kernel attributes", [&] { return kvt::prepare_kernels(); });
-        if (!rc) rc = p->cuda("kernel attributes", [&] { return kvt::prepare_turn_kernel(); });
         if (rc) return bail(rc);
         const char *why = nullptr;
         if (!kvt::encode_hot_tensor_map(&p->tmap, c.hot_base, rows,
                                         static_cast<int64_t>(c.num_kv_heads) * c.block_tokens, &why))
-            return bail(fail(KV_ERR_CUDA, why));
-        if (!kvt::encode_turn_hot_maps(p->turn_maps, c.hot_base, rows, c.block_tokens, &why))
             return bail(fail(KV_ERR_CUDA, why));
         if (cudaDeviceSynchronize() != cudaSuccess)
             return bail(fail(KV_ERR_CUDA, "device synchronise after pool set-up failed"));
@@ -986,20 +984,30 @@ int decode_append_attention(kv_pool *p, int32_t layer, const void *q, const void
                        out, flags, stream);
 }
 
-// What the calls below need besides, set up by the first of them: a pool that only decodes holds no
-// workspace for prompts (0.27 MB per SM), and a small one is created in 0.02 ms in place of 0.10 and destroyed
-// in 0.003 in place of 0.07. `cuts`: the call may leave partial results.
+// What the calls below need besides, set up by the first of them: a pool that only decodes does not fail
+// over their kernel and holds no workspace for prompts (0.27 MB per SM), and a small one is created in
+// 0.02 ms in place of 0.10 and destroyed in 0.003 in place of 0.07. `cuts`: the call may leave partial results.
 static int turn_setup(kv_pool *p, bool cuts) {
-    if (p->d_turn_part || !cuts) return KV_OK;
+    if (p->turn_ready && (p->d_turn_part || !cuts)) return KV_OK;
     // The call may be one that a graph records; the set-up is no part of the recording.
     cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
     cudaThreadExchangeStreamCaptureMode(&mode);
-    int rc = p->cuda("cudaMalloc(workspace of prompt and draft attention)", [&] {
-        void *part = nullptr;
-        const cudaError_t e = cudaMalloc(&part, kvt::turn_part_floats(p->num_sms) * sizeof(float));
-        if (e == cudaSuccess) p->d_turn_part = static_cast<float *>(part);
-        return e;
-    });
+    int rc = KV_OK;
+    if (!p->turn_ready) {
+        rc = p->cuda("kernel of prompt and draft attention", [&] { return kvt::prepare_turn_kernel(); });
+        const char *why = nullptr;
+        const int64_t rows = p->cfg.num_hot_blocks * p->cfg.num_layers * 2 * p->cfg.num_kv_heads * p->cfg.block_tokens;
+        if (!rc && !kvt::encode_turn_hot_maps(p->turn_maps, p->cfg.hot_base, rows, p->cfg.block_tokens, &why))
+            rc = fail(KV_ERR_CUDA, why);
+        p->turn_ready = !rc;
+    }
+    if (!rc && cuts && !p->d_turn_part)
+        rc = p->cuda("cudaMalloc(workspace of prompt and draft attention)", [&] {
+            void *part = nullptr;
+            const cudaError_t e = cudaMalloc(&part, kvt::turn_part_floats(p->num_sms) * sizeof(float));
+            if (e == cudaSuccess) p->d_turn_part = static_cast<float *>(part);
+            return e;
+        });
     if (rc) cudaGetLastError();   // a later launch asks for its own
     cudaThreadExchangeStreamCaptureMode(&mode);
     return rc;

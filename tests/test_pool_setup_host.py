@@ -110,3 +110,18 @@ def test_a_first_call_that_a_graph_records(kv, fake, kind):
     assert turn(fake, pool, 32, kind) == kv.KV_OK and fake.fake_strict_mallocs() == before
     assert fake.fake_mode() == mode
     assert fake.kv_pool_destroy(pool) == kv.KV_OK
+
+
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_a_turn_kernel_that_cannot_run_does_not_keep_a_pool_from_decoding(kv, fake, kind):
+    """Its preparation fails where the compiler gave it other registers than its warps' shares presume."""
+    invalid_configuration = 9
+    fake.fake_turn_status(invalid_configuration)
+    pool = create(kv, fake)
+    assert decode(fake, pool) == kv.KV_OK
+    for width in (4, 32):
+        assert turn(fake, pool, width, kind) == kv.KV_ERR_CUDA
+        assert fake.fake_turns() == 0 and fake.fake_live() == 1 and fake.fake_last_error() == 0
+    fake.fake_turn_status(0)
+    assert turn(fake, pool, 32, kind) == kv.KV_OK and fake.fake_turns() == 1
+    assert fake.kv_pool_destroy(pool) == kv.KV_OK and fake.fake_live() == 0
