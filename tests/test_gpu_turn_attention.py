@@ -250,6 +250,100 @@ def test_reserve_then_prefill_then_decode(cuda_dev):
         assert pool.check_device() == 0
 
 
+@pytest.mark.parametrize("hq,hkv", [(24, 3), (5, 5), (24, 6), (14, 7)])
+@pytest.mark.parametrize("kind", ["prefill", "tree"])
+def test_every_number_of_kv_heads(cuda_dev, kind, hq, hkv):
+    """3, 5, 6 and 7 KV heads, in groups of 8, 1, 4 and 2; the powers of two are above."""
+    n = [5, 130, 260] if kind == "prefill" else [64, 9, 31]
+    Call(kind, n, [70, 0, 513], hq=hq, hkv=hkv, seed=hq + hkv, q_std=3.0, fused=True).check()
+
+
+@pytest.mark.parametrize("bad", [-1, 1 << 30])
+@pytest.mark.parametrize("place", [2, 7])
+def test_prefill_with_a_bad_block_id_writes_what_it_may(cuda_dev, place, bad):
+    """A block id out of range, of cached tokens (place 2) or of reserved slots (place 7, tokens 112 to 127):
+    it is flagged, no other row of the arena changes, and the other sessions come out right."""
+    from paper_2609_25782_gb300 import kvtier
+    c = Call("prefill", [20, 30, 40], [100, 100, 100], seed=32)
+    refs = [c.reference(b) for b in (0, 2)]
+    want = c.hot.clone()
+    for b, (n, p) in enumerate(zip(c.n, c.p)):
+        t = [x for x in range(p, p + n) if b != 1 or x // c.bt != place]
+        lo = sum(c.n[:b])
+        blk, slot = (x[t] for x in c.slots(b, 0, p + n))
+        rows = [lo + x - p for x in t]
+        want[blk, 0, 0, :, slot], want[blk, 0, 1, :, slot] = c.k[rows], c.v[rows]
+    c.tables[1, place] = bad
+    c.run()
+    assert c.pool.check_device() & kvtier.KV_DEVICE_BAD_BLOCK
+    assert torch.equal(c.hot.view(torch.int16), want.view(torch.int16))
+    for b, ref in zip((0, 2), refs):
+        c.assert_right(b, *ref)
+
+
+def attended(q, k, v, scale):
+    """(out, noise) of rows q [n][Hq][D], the newest of k, v [m][Hkv][D], in 64 bits: as Call.reference."""
+    n, m, G = q.shape[0], k.shape[0], q.shape[1] // k.shape[1]
+    k, v = (x.double().repeat_interleave(G, dim=1) for x in (k, v))
+    x = torch.einsum("nhd,mhd->nhm", q.double(), k) * scale
+    hidden = torch.arange(m, device=q.device)[None, :] > torch.arange(m - n, m, device=q.device)[:, None]
+    w = torch.softmax(x.masked_fill(hidden[:, None], float("-inf")), 2)
+    return torch.einsum("nhm,mhd->nhd", w, v), torch.sqrt(torch.einsum("nhm,mh->nh", w * w, (v * v).sum(2)))
+
+
+@pytest.mark.parametrize("lru", [False, True])
+def test_turns_and_a_decode_step_of_the_pools_own_sessions(cuda_dev, lru):
+    """Reserve and prefill twice, a pause and a resume between, then a reserved decode step: every output
+    against the session's whole history in 64 bits. (Decode rounds as these do, its result in 32 bits.)"""
+    from turn_cases import ROW
+    import __graft_entry__
+    __graft_entry__.build()
+    from paper_2609_25782_gb300 import Pool
+    L, B, width, scale = 2, 3, 25, 0.09
+    # 18 of the sessions' blocks at the end; in residency mode the other session's have to leave for them
+    pool = Pool(num_layers=L, num_hot_blocks=24, cold_bytes=1 << 24, max_sessions=5, max_batch=4, max_context=400,
+                alloc_seed=3, lru_residency=lru)
+    other = pool.session_create(400)
+    if lru:
+        x = torch.zeros(L, 200, 4, 128, dtype=torch.bfloat16, device="cuda")
+        pool.session_append(other, x, x)
+    sids = [pool.session_create(400) for _ in range(B)]
+    tables = torch.zeros(B, width, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    history = [torch.zeros(L, 2, 0, 4, 128, dtype=torch.bfloat16, device="cuda") for _ in sids]
+
+    def assert_right(layer, q, out, bounds):
+        for i, (lo, hi) in enumerate(bounds):
+            ref, noise = attended(q[lo:hi], history[i][layer, 0], history[i][layer, 1], scale)
+            assert ((out[lo:hi].double() - ref).norm(dim=2) <= ROW * (noise + ref.norm(dim=2))).all(), (layer, i)
+
+    for counts in ([37, 16, 90], [60, 1, 48]):
+        pool.batch_reserve(sids, tables, width, lens, counts=counts)
+        at = [sum(counts[:i]) for i in range(B + 1)]
+        cu = torch.tensor(at, dtype=torch.int32, device="cuda")
+        x = torch.randn(L, 2, at[-1], 4, 128, device="cuda", generator=g).bfloat16()
+        history = [torch.cat([h, x[:, :, lo:hi]], 2) for h, lo, hi in zip(history, at, at[1:])]
+        for layer in range(L):
+            q = torch.randn(at[-1], 32, 128, device="cuda", generator=g).bfloat16()
+            out = torch.empty(at[-1], 32, 128, device="cuda")
+            pool.prefill_attention(layer, q, x[layer, 0], x[layer, 1], cu, tables, lens, B, width, scale, out)
+            assert_right(layer, q, out, list(zip(at, at[1:])))
+        pool.session_pause(sids[1])
+        pool.session_resume(sids[1])
+    pool.batch_reserve(sids, tables, width, lens)
+    x = torch.randn(L, 2, B, 4, 128, device="cuda", generator=g).bfloat16()
+    history = [torch.cat([h, x[:, :, i:i + 1]], 2) for i, h in enumerate(history)]
+    for layer in range(L):
+        q = torch.randn(B, 32, 128, device="cuda", generator=g).bfloat16()
+        out = torch.empty(B, 32, 128, device="cuda")
+        pool.decode_append_attention(layer, q, x[layer, 0], x[layer, 1], tables, lens, B, width, scale, out)
+        assert_right(layer, q, out, [(i, i + 1) for i in range(B)])
+    assert lens.tolist() == [98, 18, 139] and pool.check_device() == 0
+    if lru:
+        assert pool.stats()["blocks_evicted"] > 0
+
+
 def test_capture_and_replay_with_longer_contexts(cuda_dev):
     """A draft verification recorded in a CUDA graph: lengths are read when it runs."""
     c = Call("tree", [16, 16], [2000, 900], seed=19)
