@@ -321,8 +321,10 @@ int decode_append_attention(kv_pool *pool, int32_t layer, const void *q, const v
  * of 8. Scores, softmax statistics and sums are held in 32 bits, the weights in
  * bf16 for the product with V. The new tokens' K and V have to be finite: a V
  * that is not may reach rows that come before it. Tokens past seq_len in a block
- * may hold anything. The result depends on the values, the lengths and the
- * batch, and is the same from run to run. Offsets or lengths out of range set
+ * may hold anything. The result is the same from run to run. Its last bits
+ * depend, beside the values, on what decides where the work is cut: the lengths
+ * of the whole batch, max_blocks and the device's number of SMs (so a graph
+ * recorded with wider tables than a call's own may round otherwise). Offsets or lengths out of range set
  * KV_DEVICE_BAD_LENGTH, and that session's rows are not written; a block id out
  * of range sets KV_DEVICE_BAD_BLOCK, a wait inside the kernel that runs out (2 s)
  * KV_DEVICE_TIMEOUT, and rows that they concern are wrong. Calls of this and

@@ -20,13 +20,14 @@
 //             memory, O += P V with P from tensor memory
 //   11        the new tokens' K and V, into the pool
 // The tensor cores work on one stream while the other's softmax runs. P lies in S's place, so a stream's
-// next scores wait for the product of its weights: a key tile of a pair takes 3 500 cycles, of which the
-// products need 2 050, and that chain bounds long prompts (tensor pipe 58 % active; no case got faster with
-// three quarters of the exponentials left out, or the maximum). Tensor memory has room for S beside P with
+// next scores wait for the product of its weights: a key tile of a pair takes 3 250 (turns) to 3 500 cycles
+// (one long prompt), of which the products need 2 050, and that chain bounds both (tensor pipe 63 and 58 %
+// active; no case got faster with three quarters of the exponentials left out, or the maximum). Tensor memory has room for S beside P with
 // key tiles of 80: 5 % slower, because a product of 80 columns takes 80 % of one of 128. Two threads a row:
 // 20 % slower, 64 scores do not fit the registers of 640 threads. Few rows over long caches are bound by HBM.
-//   one prompt of 16 391 tokens, 32 heads (4 KV)           1 600 us   1 380 TFLOP/s
-//   turns of 300-3K tokens on 2K-24K, 4 sessions             930 us   1 340 TFLOP/s
+// In a CUDA graph of twenty calls (called one by one: 1 600, 962, 103 and 12 us):
+//   one prompt of 16 391 tokens, 32 heads (4 KV)           1 590 us   1 385 TFLOP/s
+//   turns of 300-3K tokens on 2K-24K, 4 sessions             945 us   1 320 TFLOP/s
 //   16 sessions of 2K-30K tokens, 16 drafts each              99 us   5.5 TB/s, with the merge
 //   one prompt of 37 tokens                                    9 us   plan, load, product, softmax, end in turn
 //
