@@ -35,7 +35,7 @@ struct TurnCosts {
 // With little work the shortest piece counts, and items of one key tile have a CTA each (one prompt of 37
 // tokens 9.1 us; 12 with the other costs). With much, what the parts take: a wide item's tile 3 250 to 3 500
 // cycles, a narrow one's 2 500, an item's end and the next one's start 6 000. What that gave when it was
-// chosen, all in one run: 32 sessions of 20-60 drafts 140 -> 124 us, chunks of 1-200 tokens on 1K-40K
+// chosen (present times: turn_kernels.cu): 32 sessions of 20-60 drafts 140 -> 124 us, chunks of 1-200 tokens on 1K-40K
 // 282 -> 236, turns of 300-3K tokens 935 -> 910.
 constexpr TurnCosts kCostsFew = {4, 4, 4, 8}, kCostsMany = {4, 3, 8, 12};
 
