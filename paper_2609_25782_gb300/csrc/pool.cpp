@@ -6,18 +6,11 @@
 // write-on-evict watermark (cold_valid), and the CUDA events that order
 // migrations against decode. Device work goes to the kernels in
 // decode_kernels.cu and copy_kernels.cu.
-#include <algorithm>
 #include <cmath>
 #include <cstdio>
-#include <cstring>
-#include <map>
-#include <set>
-#include <string>
-#include <vector>
 
-#include "../../include/kvtier.h"
 #include "decode_launch.h"
-#include "kvt_internal.h"
+#include "pool_state.h"
 #include "turn_plan.h"
 
 static_assert(KV_DEVICE_BAD_BLOCK == kvt::kErrBadBlock && KV_DEVICE_BAD_LENGTH == kvt::kErrBadLength &&
@@ -27,11 +20,6 @@ static_assert(KV_DEVICE_BAD_BLOCK == kvt::kErrBadBlock && KV_DEVICE_BAD_LENGTH =
 namespace {
 
 thread_local std::string g_last_error;
-
-int fail(int code, const std::string &msg) {
-    g_last_error = msg;
-    return code;
-}
 
 // splitmix64 (Steele, Lea, Flood 2014): state += golden gamma, then mix.
 uint64_t splitmix64(uint64_t &st) {
@@ -51,388 +39,22 @@ void fisher_yates(std::vector<int32_t> &v, size_t n, uint64_t seed) {
     }
 }
 
-struct Session {
-    int32_t state = KV_SESSION_FREE;
-    int64_t T = 0, cap = 0, cold_valid = 0;
-    int64_t img_off = -1, img_bytes = 0;
-    std::vector<int32_t> blocks;      // per logical block: hot slot, or -1 (residency mode)
-    std::vector<int16_t> img_tok;     // residency mode: tokens of block j held by the image
-    int64_t hot_count = 0;            // residency mode: blocks with a hot slot
-    uint64_t last_use = 0;            // residency mode: recency stamp
-    cudaEvent_t ready = nullptr;
-    bool ready_recorded = false;
-    cudaEvent_t appended = nullptr;
-    bool appended_recorded = false;
-    cudaEvent_t packed = nullptr;     // residency mode: after the last eviction that wrote
-    bool packed_recorded = false;     // the image (it covers every earlier one)
-    int16_t pack_fence = -1;          // simple mode: fence slot and generation of the
-    uint64_t pack_gen = 0;            // last pause's pack (it reads the table row)
-};
-
-// A planned eviction: block j of session sid leaves hot slot `slot`; tokens
-// [t0, t1) are written to the image first (t0 == t1: the image has them).
-struct Victim {
-    int32_t sid, j, slot, t0, t1;
-};
-
-constexpr int kFenceSlots = 64;
-struct Fence {
-    cudaEvent_t ev = nullptr;
-    uint64_t gen = 0;
-};
-
-class DeviceGuard {
-  public:
-    DeviceGuard(int dev, bool active) : active_(active) {
-        if (active_ && cudaGetDevice(&prev_) == cudaSuccess && prev_ != dev) cudaSetDevice(dev);
-        else prev_ = -1;
-    }
-    ~DeviceGuard() {
-        if (active_ && prev_ >= 0) cudaSetDevice(prev_);
-    }
-
-  private:
-    bool active_;
-    int prev_ = -1;
-};
-
 }  // namespace
+
+int kvt::fail(int code, const std::string &msg) {
+    g_last_error = msg;
+    return code;
+}
 
 void kvt::set_last_error(const char *msg) { g_last_error = msg; }
 
-struct kv_pool {
-    kv_pool_config cfg{};
-    bool host_only = false;
-    int64_t block_bytes = 0, token_bytes = 0;
-    int64_t image_token_bytes = 0;       // of a token in a cold image
-    bool int8 = false;                   // KV_POOL_COLD_INT8
-    int32_t table_stride = 0;            // max blocks per session
-    int32_t max_splits = 0;              // split bound for max_context
-    int64_t part_rows = 0;               // decode workspace capacity (partial rows)
-    int64_t part_alloc = 0;              // partial rows allocated (at least part_rows)
-    int num_sms = 1;
-    int mig_ctas = 0;                    // cap on migration-kernel CTAs, 0 = none
-    // Stream of the last decode call: moves on another one may run beside
-    // decode. Compared only, and only to size a grid.
-    bool decoded = false;
-    cudaStream_t decode_stream = nullptr;
-    kvt::Shape shape{};
-
-    std::vector<int32_t> free_list;      // top = back
-    std::vector<int16_t> block_fence;    // fence slot of the pack that freed it, or -1
-    std::vector<uint64_t> block_fence_gen;
-    std::vector<Session> sessions;
-    std::map<int64_t, int64_t> cold_free;  // offset -> bytes
-    int64_t cold_used = 0;
-
-    void *d_slab = nullptr;              // the allocation behind the pointers below
-    int32_t *d_tables = nullptr;
-    float *d_part_o = nullptr;
-    float *d_part_ml = nullptr;
-    int32_t *d_counters = nullptr;       // split arrivals per (layer-batch row, kv-head)
-    int64_t counter_count = 0;
-    int32_t *d_err = nullptr;
-    CUtensorMap tmap{};
-    // prefill_attention and tree_attention (turn_setup)
-    bool turn_ready = false;             // the kernel and the maps
-    CUtensorMap turn_maps[2]{};
-    float *d_turn_part = nullptr;        // partial results
-
-    Fence fences[kFenceSlots];
-    int next_fence = 0;
-    uint64_t fence_gen = 0;
-
-    kv_pool_stats stats{};
-    int32_t inject_countdown = 0;
-    bool inject_timeout = false;   // kv_pool_inject_decode_timeout, next attention call only
-
-    // Residency mode (KV_POOL_LRU_RESIDENCY): sessions holding hot blocks,
-    // ordered by (last use, sid); the first one is the least recently used.
-    bool lru = false;
-    uint64_t clock = 0;
-    std::set<std::pair<uint64_t, int32_t>> lru_set;
-
-    // Every CUDA call of the pool goes through here: the failure-injection
-    // hook fires first, then (unless the pool is host-logic only) the call.
-    template <typename F>
-    int cuda(const char *what, F &&fn) {
-        if (inject_countdown > 0 && --inject_countdown == 0)
-            return fail(KV_ERR_CUDA, std::string(what) + ": injected CUDA failure");
-        if (host_only) return KV_OK;
-        cudaError_t e = fn();
-        if (e != cudaSuccess)
-            return fail(KV_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
-        return KV_OK;
-    }
-
-    bool beside_decode(cudaStream_t st) const { return decoded && st != decode_stream; }
-    int move_ctas(cudaStream_t st) const {
-        return kvt::migration_ctas(mig_ctas, beside_decode(st), num_sms);
-    }
-
-    Session *session(int32_t sid) {
-        if (sid < 0 || sid >= static_cast<int32_t>(sessions.size())) return nullptr;
-        Session &s = sessions[sid];
-        return s.state == KV_SESSION_FREE ? nullptr : &s;
-    }
-
-    int64_t image_bytes(int64_t cap) const {
-        return (cap * image_token_bytes + 255) / 256 * 256;
-    }
-
-    bool cold_alloc(int64_t bytes, int64_t *off) {
-        for (auto it = cold_free.begin(); it != cold_free.end(); ++it) {
-            if (it->second >= bytes) {
-                *off = it->first;
-                const int64_t rest = it->second - bytes;
-                const int64_t at = it->first + bytes;
-                cold_free.erase(it);
-                if (rest > 0) cold_free[at] = rest;
-                cold_used += bytes;
-                return true;
-            }
-        }
-        return false;
-    }
-
-    void cold_release(int64_t off, int64_t bytes) {
-        cold_used -= bytes;
-        auto it = cold_free.emplace(off, bytes).first;
-        auto nx = std::next(it);
-        if (nx != cold_free.end() && it->first + it->second == nx->first) {
-            it->second += nx->second;
-            cold_free.erase(nx);
-        }
-        if (it != cold_free.begin()) {
-            auto pv = std::prev(it);
-            if (pv->first + pv->second == it->first) {
-                pv->second += it->second;
-                cold_free.erase(it);
-            }
-        }
-    }
-
-    // Blocks popped for a session: make `st` wait for the packs that freed
-    // them, if those packs may still be running.
-    int wait_fences(const int32_t *blocks, size_t n, cudaStream_t st) {
-        bool need[kFenceSlots] = {};
-        for (size_t i = 0; i < n; ++i) {
-            const int f = block_fence[blocks[i]];
-            if (f >= 0 && fences[f].gen == block_fence_gen[blocks[i]]) need[f] = true;
-        }
-        for (int f = 0; f < kFenceSlots; ++f) {
-            if (!need[f]) continue;
-            int rc = cuda("cudaStreamWaitEvent", [&] { return cudaStreamWaitEvent(st, fences[f].ev, 0); });
-            if (rc) return rc;
-        }
-        return KV_OK;
-    }
-
-    void clear_fences(const int32_t *blocks, size_t n) {
-        for (size_t i = 0; i < n; ++i) block_fence[blocks[i]] = -1;
-    }
-
-    // Write entries [from, from+n) of a session's device table row.
-    int write_table(int32_t sid, const int32_t *vals, int64_t from, int64_t n, cudaStream_t st) {
-        for (int64_t i = 0; i < n; i += kvt::kTableWriteMax) {
-            kvt::TableWriteArgs a;
-            a.dst = d_tables + static_cast<int64_t>(sid) * table_stride + from + i;
-            a.n = static_cast<int32_t>(std::min<int64_t>(kvt::kTableWriteMax, n - i));
-            std::memcpy(a.vals, vals + i, sizeof(int32_t) * a.n);
-            int rc = cuda("table write launch", [&] { return kvt::launch_table_write(a, st); });
-            if (rc) return rc;
-        }
-        return KV_OK;
-    }
-
-    // Write n tokens at position s.T; the row gains blocks vals[0 .. fresh_n)
-    // at entry `from`, in the same launch where they fit its parameters.
-    int append_device(int32_t sid, const Session &s, const void *k, const void *v, int32_t n,
-                      const int32_t *vals, int64_t from, int64_t fresh_n, cudaStream_t st) {
-        kvt::AppendInlineArgs r;
-        kvt::AppendArgs &a = r.m;
-        a.k = static_cast<const uint8_t *>(k);
-        a.v = static_cast<const uint8_t *>(v);
-        a.table = d_tables + static_cast<int64_t>(sid) * table_stride;
-        a.hot = static_cast<uint8_t *>(cfg.hot_base);
-        a.pos0 = static_cast<int32_t>(s.T);
-        a.n = n;
-        a.err = d_err;
-        a.s = shape;
-        // the caller's bound is for migrations alone
-        const int ctas = kvt::migration_ctas(0, beside_decode(st), num_sms);
-        if (fresh_n > 0 && fresh_n <= kvt::kResumeInlineMax) {
-            r.from = static_cast<int32_t>(from);
-            r.n = static_cast<int32_t>(fresh_n);
-            std::memcpy(r.blocks, vals, sizeof(int32_t) * fresh_n);
-            return cuda("append launch", [&] { return kvt::launch_append_inline(r, ctas, st); });
-        }
-        int rc = fresh_n > 0 ? write_table(sid, vals, from, fresh_n, st) : KV_OK;
-        if (!rc) rc = cuda("append launch", [&] { return kvt::launch_append(a, ctas, st); });
-        return rc;
-    }
-
-    // ---- residency mode -------------------------------------------------
-    int32_t tokens_in_block(const Session &s, int64_t j) const {
-        const int64_t n = s.T - j * cfg.block_tokens;
-        return static_cast<int32_t>(n < cfg.block_tokens ? n : cfg.block_tokens);
-    }
-
-    void lru_out(int32_t sid) {
-        Session &s = sessions[sid];
-        if (s.hot_count > 0) lru_set.erase({s.last_use, sid});
-    }
-    void lru_in(int32_t sid) {
-        Session &s = sessions[sid];
-        if (s.hot_count > 0) lru_set.insert({s.last_use, sid});
-    }
-
-    // Least recently used hot blocks, outside `protect`, until `need` blocks
-    // would be free. Sessions in recency order; within one, ascending j.
-    bool plan_evict(int64_t need, const std::vector<int32_t> &protect, std::vector<Victim> &out) {
-        int64_t have = static_cast<int64_t>(free_list.size());
-        for (const auto &e : lru_set) {
-            if (have >= need) break;
-            const int32_t sid = e.second;
-            if (std::find(protect.begin(), protect.end(), sid) != protect.end()) continue;
-            const Session &s = sessions[sid];
-            for (size_t j = 0; j < s.blocks.size() && have < need; ++j) {
-                if (s.blocks[j] < 0) continue;
-                out.push_back({sid, static_cast<int32_t>(j), s.blocks[j], s.img_tok[j],
-                               tokens_in_block(s, static_cast<int64_t>(j))});
-                ++have;
-            }
-        }
-        return have >= need;
-    }
-
-    // The `need` slots the call will pop once the victims are pushed back:
-    // the free list grows by the victims (in order), pops come off its end.
-    std::vector<int32_t> peek_alloc(int64_t need, const std::vector<Victim> &v) const {
-        std::vector<int32_t> all(free_list);
-        for (const Victim &x : v) all.push_back(x.slot);
-        std::vector<int32_t> out(need);
-        for (int64_t i = 0; i < need; ++i) out[i] = all[all.size() - 1 - i];
-        return out;
-    }
-
-    // Device side of the victims: wait for their last writes, then write the
-    // tokens each image lacks. A session whose image this writes records its
-    // `packed` event after the writes; the stream first waits for the previous
-    // recording, so the event covers every eviction of the session so far.
-    // Whatever later fetches the session's blocks back waits on it
-    // (wait_packed), on whichever stream it runs.
-    int evict_device(const std::vector<Victim> &v, cudaStream_t st) {
-        std::vector<int32_t> seen, writes;
-        for (const Victim &x : v) {
-            if (x.t1 > x.t0 && std::find(writes.begin(), writes.end(), x.sid) == writes.end())
-                writes.push_back(x.sid);
-            if (std::find(seen.begin(), seen.end(), x.sid) != seen.end()) continue;
-            seen.push_back(x.sid);
-            Session &s = sessions[x.sid];
-            int rc = KV_OK;
-            if (s.appended_recorded)
-                rc = cuda("cudaStreamWaitEvent", [&] { return cudaStreamWaitEvent(st, s.appended, 0); });
-            if (!rc && s.ready_recorded)
-                rc = cuda("cudaStreamWaitEvent", [&] { return cudaStreamWaitEvent(st, s.ready, 0); });
-            if (!rc) rc = wait_packed(x.sid, st);
-            if (rc) return rc;
-        }
-        std::vector<kvt::BlockJob> jobs;
-        for (const Victim &x : v)
-            if (x.t1 > x.t0) jobs.push_back(job_for(x.sid, x.j, x.slot, x.t0, x.t1));
-        int rc = run_jobs(jobs, true, st);
-        for (size_t i = 0; !rc && !host_only && i < writes.size(); ++i) {
-            Session &s = sessions[writes[i]];
-            if (!s.packed)
-                rc = cuda("cudaEventCreate",
-                          [&] { return cudaEventCreateWithFlags(&s.packed, cudaEventDisableTiming); });
-            if (!rc) rc = cuda("cudaEventRecord", [&] { return cudaEventRecord(s.packed, st); });
-        }
-        if (rc) return rc;
-        for (int32_t sid : writes) sessions[sid].packed_recorded = !host_only;
-        return KV_OK;
-    }
-
-    // Before blocks of `sid` are fetched from its image on `st`: the image
-    // writes of its evictions (possibly on another stream) must be complete.
-    int wait_packed(int32_t sid, cudaStream_t st) {
-        const Session &s = sessions[sid];
-        if (!s.packed_recorded) return KV_OK;
-        return cuda("cudaStreamWaitEvent", [&] { return cudaStreamWaitEvent(st, s.packed, 0); });
-    }
-
-    void evict_commit(const std::vector<Victim> &v) {
-        for (const Victim &x : v) {
-            Session &s = sessions[x.sid];
-            lru_out(x.sid);
-            if (x.t1 > x.t0) stats.bytes_packed += static_cast<int64_t>(x.t1 - x.t0) * image_token_bytes;
-            s.img_tok[x.j] = static_cast<int16_t>(x.t1);
-            s.blocks[x.j] = -1;
-            s.hot_count -= 1;
-            lru_in(x.sid);
-            free_list.push_back(x.slot);
-            stats.blocks_evicted += 1;
-            stats.free_blocks += 1;
-            stats.used_blocks -= 1;
-        }
-    }
-
-    kvt::BlockJob job_for(int32_t sid, int32_t j, int32_t slot, int32_t t0, int32_t t1) const {
-        const Session &s = sessions[sid];
-        kvt::BlockJob b;
-        b.img = static_cast<uint8_t *>(cfg.cold_base) + s.img_off;
-        b.T_cap = static_cast<int32_t>(s.cap);
-        b.sid = -1;
-        b.slot = slot;
-        b.j = j;
-        b.t0 = t0;
-        b.t1 = t1;
-        return b;
-    }
-
-    // A fetch of block j into `slot`: the copy also writes the session's
-    // device table entry j.
-    kvt::BlockJob fetch_job(int32_t sid, int32_t j, int32_t slot, int32_t t0, int32_t t1) const {
-        kvt::BlockJob b = job_for(sid, j, slot, t0, t1);
-        b.sid = sid;
-        return b;
-    }
-
-    int run_jobs(const std::vector<kvt::BlockJob> &jobs, bool pack, cudaStream_t st) {
-        for (size_t i = 0; i < jobs.size(); i += kvt::kBlockJobsMax) {
-            kvt::BlockJobs a;
-            a.hot = static_cast<uint8_t *>(cfg.hot_base);
-            a.err = d_err;
-            a.tables = d_tables;
-            a.table_stride = table_stride;
-            a.s = shape;
-            a.n = static_cast<int32_t>(std::min<size_t>(kvt::kBlockJobsMax, jobs.size() - i));
-            a.once = 0;
-            a.int8 = int8;
-            std::copy(jobs.begin() + i, jobs.begin() + i + a.n, a.job);
-            int rc = cuda(pack ? "pack launch" : "unpack launch",
-                          [&] { return kvt::launch_block_jobs(a, pack, move_ctas(st), st); });
-            if (rc) return rc;
-        }
-        return KV_OK;
-    }
-
-    kvt::MigArgs mig_args(int32_t sid, const Session &s) const {
-        kvt::MigArgs m;
-        m.table = d_tables + static_cast<int64_t>(sid) * table_stride;
-        m.hot = static_cast<uint8_t *>(cfg.hot_base);
-        m.img = static_cast<uint8_t *>(cfg.cold_base) + s.img_off;
-        m.T_cap = s.cap;
-        m.t_begin = 0;
-        m.t_end = 0;
-        m.once = 0;
-        m.int8 = int8;
-        m.err = d_err;
-        m.s = shape;
-        return m;
-    }
-};
+using kvt::DeviceGuard;
+using kvt::ensure_event;
+using kvt::fail;
+using kvt::lru_fetch;
+using kvt::Session;
+using kvt::Victim;
+using kvt::wait_event;
 
 extern "C" {
 
@@ -499,6 +121,7 @@ int kv_pool_create(const kv_pool_config *cfg, kv_pool **out) {
     fisher_yates(p->free_list, p->free_list.size(), c.alloc_seed);
     p->block_fence.assign(c.num_hot_blocks, -1);
     p->block_fence_gen.assign(c.num_hot_blocks, 0);
+    p->block_extra.assign(c.num_hot_blocks, 0);
     p->sessions.resize(c.max_sessions);
     if (c.cold_bytes > 0) p->cold_free[0] = c.cold_bytes;
 
@@ -576,8 +199,10 @@ int kv_pool_destroy(kv_pool *p) {
     return KV_OK;
 }
 
-static int create_session(kv_pool *p, int64_t max_tokens, int64_t tokens, int32_t state,
-                          int32_t *sid_out) {
+}  // extern "C"
+
+int kvt::create_session(kv_pool *p, int64_t max_tokens, int64_t tokens, int32_t state,
+                        int32_t *sid_out) {
     if (!p || !sid_out) return fail(KV_ERR_INVALID_ARG, "null argument");
     if (max_tokens < 1 || max_tokens > p->cfg.max_context)
         return fail(KV_ERR_INVALID_ARG, "max_tokens must be in 1..max_context");
@@ -612,13 +237,15 @@ static int create_session(kv_pool *p, int64_t max_tokens, int64_t tokens, int32_
     return KV_OK;
 }
 
+extern "C" {
+
 int session_create(kv_pool *p, int64_t max_tokens, int32_t *sid_out) {
-    return create_session(p, max_tokens, 0, KV_SESSION_ACTIVE, sid_out);
+    return kvt::create_session(p, max_tokens, 0, KV_SESSION_ACTIVE, sid_out);
 }
 
 int session_create_paused(kv_pool *p, int64_t max_tokens, int64_t tokens, int32_t *sid_out) {
     if (tokens < 1) return fail(KV_ERR_INVALID_ARG, "a paused session needs tokens >= 1");
-    return create_session(p, max_tokens, tokens, KV_SESSION_PAUSED, sid_out);
+    return kvt::create_session(p, max_tokens, tokens, KV_SESSION_PAUSED, sid_out);
 }
 
 int session_destroy(kv_pool *p, int32_t sid) {
@@ -628,7 +255,7 @@ int session_destroy(kv_pool *p, int32_t sid) {
     if (p->lru) p->lru_out(sid);
     int64_t freed = 0;
     for (int32_t b : s->blocks)
-        if (b >= 0) {
+        if (b >= 0 && p->release(b)) {
             p->free_list.push_back(b);
             ++freed;
         }
@@ -652,7 +279,9 @@ static bool decode_pointers_aligned(const void *q, const void *tables, const voi
     return (a4 & 3) == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
 }
 
-static int ensure_event(kv_pool *p, cudaEvent_t *ev) {
+}  // extern "C"
+
+int kvt::ensure_event(kv_pool *p, cudaEvent_t *ev) {
     if (*ev || p->host_only) return KV_OK;
     return p->cuda("cudaEventCreate",
                    [&] { return cudaEventCreateWithFlags(ev, cudaEventDisableTiming); });
@@ -660,9 +289,11 @@ static int ensure_event(kv_pool *p, cudaEvent_t *ev) {
 
 // ---- residency mode (KV_POOL_LRU_RESIDENCY) --------------------------------
 
-static int wait_event(kv_pool *p, cudaStream_t st, cudaEvent_t ev) {
+int kvt::wait_event(kv_pool *p, cudaStream_t st, cudaEvent_t ev) {
     return p->cuda("cudaStreamWaitEvent", [&] { return cudaStreamWaitEvent(st, ev, 0); });
 }
+
+extern "C" {
 
 // Append with residency: a tail block that was evicted comes back first,
 // new blocks come from the free list or from evicting LRU blocks.
@@ -689,6 +320,7 @@ static int lru_append(kv_pool *p, int32_t sid, const void *k, const void *v, int
     DeviceGuard dg(p->cfg.device, !p->host_only);
     int rc = ensure_event(p, &s->appended);
     if (!rc && s->ready_recorded) rc = wait_event(p, st, s->ready);
+    if (!rc) rc = p->wait_fences(got.data(), got.size(), st);
     if (!rc) rc = p->evict_device(vic, st);
     if (!rc && refetch) rc = p->wait_packed(sid, st);
     if (!rc && refetch) {
@@ -702,6 +334,7 @@ static int lru_append(kv_pool *p, int32_t sid, const void *k, const void *v, int
 
     p->evict_commit(vic);
     p->free_list.resize(p->free_list.size() - need);
+    p->clear_fences(got.data(), got.size());
     p->lru_out(sid);
     if (refetch) {
         s->blocks[tail] = got[0];
@@ -748,6 +381,7 @@ static int lru_resume(kv_pool *p, int32_t sid, cudaStream_t st) {
 
     DeviceGuard dg(p->cfg.device, !p->host_only);
     int rc = ensure_event(p, &s->ready);
+    if (!rc) rc = p->wait_fences(got.data(), got.size(), st);
     if (!rc) rc = p->evict_device(vic, st);
     if (!rc && need > 0) rc = p->wait_packed(sid, st);
     if (!rc) rc = p->run_jobs(jobs, false, st);
@@ -756,6 +390,7 @@ static int lru_resume(kv_pool *p, int32_t sid, cudaStream_t st) {
 
     p->evict_commit(vic);
     p->free_list.resize(p->free_list.size() - need);
+    p->clear_fences(got.data(), got.size());
     p->lru_out(sid);
     s->blocks = row;
     s->hot_count += need;
@@ -772,15 +407,17 @@ static int lru_resume(kv_pool *p, int32_t sid, cudaStream_t st) {
     return KV_OK;
 }
 
+}  // extern "C"
+
 // Bring back every evicted block of the sessions `uniq` (no pinning: under
 // pressure even active blocks spill), with victims from sessions outside
 // `protect`, then stamp all of `uniq` with one new recency time. With
 // record_ready, each session that had a block fetched re-records its ready
 // event on `st` (a decode stream waits on it). *blocks receives the number
 // of blocks fetched.
-static int lru_fetch(kv_pool *p, const std::vector<int32_t> &uniq,
-                     const std::vector<int32_t> &protect, bool record_ready, cudaStream_t st,
-                     int64_t *blocks) {
+int kvt::lru_fetch(kv_pool *p, const std::vector<int32_t> &uniq,
+                   const std::vector<int32_t> &protect, bool record_ready, cudaStream_t st,
+                   int64_t *blocks) {
     std::vector<std::vector<int32_t>> miss(uniq.size());
     int64_t need = 0;
     for (size_t u = 0; u < uniq.size(); ++u) {
@@ -809,6 +446,7 @@ static int lru_fetch(kv_pool *p, const std::vector<int32_t> &uniq,
     int rc = KV_OK;
     for (size_t u = 0; !rc && record_ready && u < uniq.size(); ++u)
         if (!miss[u].empty()) rc = ensure_event(p, &p->sessions[uniq[u]].ready);
+    if (!rc) rc = p->wait_fences(got.data(), got.size(), st);
     if (!rc) rc = p->evict_device(vic, st);
     for (size_t u = 0; !rc && u < uniq.size(); ++u)
         if (!miss[u].empty()) rc = p->wait_packed(uniq[u], st);
@@ -822,6 +460,7 @@ static int lru_fetch(kv_pool *p, const std::vector<int32_t> &uniq,
 
     p->evict_commit(vic);
     p->free_list.resize(p->free_list.size() - need);
+    p->clear_fences(got.data(), got.size());
     const uint64_t stamp = ++p->clock;
     for (size_t u = 0; u < uniq.size(); ++u) {
         Session &s = p->sessions[uniq[u]];
@@ -838,6 +477,8 @@ static int lru_fetch(kv_pool *p, const std::vector<int32_t> &uniq,
     *blocks = need;
     return KV_OK;
 }
+
+extern "C" {
 
 static std::vector<int32_t> unique_ids(const int32_t *ids, int32_t n) {
     std::vector<int32_t> u;
@@ -1113,10 +754,8 @@ int session_pause(kv_pool *p, int32_t sid, kv_stream_t stream_) {
 
     // Fence slot that will mark the freed blocks; its previous pack must be
     // complete before the slot is re-recorded.
-    const int f = p->next_fence;
-    int rc = ensure_event(p, &p->fences[f].ev);
-    if (!rc && p->fences[f].gen != 0)
-        rc = p->cuda("cudaEventSynchronize", [&] { return cudaEventSynchronize(p->fences[f].ev); });
+    int f = 0;
+    int rc = p->open_fence(s->blocks.data(), s->blocks.size(), st, &f);
     if (!rc && s->appended_recorded)
         rc = p->cuda("cudaStreamWaitEvent", [&] { return cudaStreamWaitEvent(st, s->appended, 0); });
     if (!rc && s->ready_recorded)
@@ -1128,21 +767,13 @@ int session_pause(kv_pool *p, int32_t sid, kv_stream_t stream_) {
         m.t_end = static_cast<int32_t>(t1);
         rc = p->cuda("pack launch", [&] { return kvt::launch_pack(m, p->move_ctas(st), st); });
     }
-    if (!rc) rc = p->cuda("cudaEventRecord", [&] { return cudaEventRecord(p->fences[f].ev, st); });
+    if (!rc) rc = p->record_fence(f, st);
     if (rc) return rc;
 
-    p->next_fence = (f + 1) % kFenceSlots;
-    const uint64_t gen = ++p->fence_gen;
-    p->fences[f].gen = gen;
+    const uint64_t gen = p->commit_fence(f);
     s->pack_fence = static_cast<int16_t>(f);
     s->pack_gen = gen;
-    for (int32_t b : s->blocks) {
-        p->free_list.push_back(b);
-        p->block_fence[b] = static_cast<int16_t>(f);
-        p->block_fence_gen[b] = gen;
-    }
-    p->stats.free_blocks += static_cast<int64_t>(s->blocks.size());
-    p->stats.used_blocks -= static_cast<int64_t>(s->blocks.size());
+    for (int32_t b : s->blocks) p->give_back(b, f, gen);
     p->stats.bytes_packed += (t1 - t0) * p->image_token_bytes;
     p->stats.pauses += 1;
     s->blocks.clear();
