@@ -10,6 +10,7 @@
  *           (or kv_pool_batch_reserve + decode_append_attention: one
  *           token per session and step, written by the decode kernel;
  *           kv_pool_batch_reserve_tokens + prefill_attention: a turn's)
+ *           or read from another session's blocks (session_fork)
  *   path 4  eviction: hot blocks -> cold image .............. session_pause
  * The cold tier (high bandwidth flash in the paper) is a second device
  * allocation; its bandwidth, energy and endurance are not modelled.
@@ -24,6 +25,9 @@
  *              (KV_POOL_COLD_INT8: int8 codes and exponents, see there).
  *   block table: row of int32 physical block ids; logical block j of a
  *              session holds its tokens j*bt .. j*bt+bt-1.
+ *   bounds     of blocks' keys (kv_pool_block_bounds): int8
+ *              codes[L][Hkv][num_hot_blocks][2][D], then bf16
+ *              steps[L][Hkv][num_hot_blocks]
  *
  * Conventions for every call:
  *  - Return value 0 (KV_OK) or a negative KV_ERR_* code. On error nothing
@@ -357,6 +361,143 @@ int tree_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride
                    const int32_t *seq_lens, int32_t B, int32_t max_blocks, float scale, void *out,
                    uint32_t flags, kv_stream_t stream);
 
+/* Bytes of the bounds of a pool's blocks: L * Hkv * num_hot_blocks * (2 D + 2)
+ * (258 bytes for a block's 4 KiB of keys at 16 tokens, 16 KiB at 64). */
+int64_t kv_bounds_bytes(const kv_pool_config *cfg);
+
+/* Attention over a part of the cache (no passage; a session's decode step then
+ * reads `top` blocks and 258 bytes of every other one, per kv-head, in place of
+ * all of its KV). Three calls, since a selection may serve several layers, or be
+ * the caller's own:
+ *   kv_pool_block_bounds   channelwise bounds of the keys of each block
+ *   select_blocks          scores from the bounds, the `top` largest
+ *   sparse_attention       one new token per session over listed blocks
+ *
+ * Bounds: for each block of the B rows that holds tokens from since[b] on (and for
+ * every block of a row with since == NULL), each layer (layer = -1) or one, and
+ * each kv-head, hi[d] and lo[d], the largest and smallest K[t][d] over the block's
+ * tokens t < seq_lens[b], as codes of one step:
+ *   step = 2^(E - 133), E the biased exponent of the largest magnitude among
+ *   them (at least 1), one more if its seven fraction bits are all ones;
+ *   hi = step * codes[0][d], rounded up, lo = step * codes[1][d], rounded down,
+ *   codes in -127 .. 127. A block with a K that is not finite gets step = inf,
+ *   codes 127 and -127.
+ * A block's bounds go by its physical id, so forks share them with the blocks.
+ * They stay as they are until the call is made again: after tokens were
+ * written, blocks came back (resume) or a session was compacted, it is due for
+ * those blocks, unless select_blocks is told to take them anyway (first, last).
+ *   block_tables device int32 [B][max_blocks]
+ *   seq_lens     device int32 [B], 0 (nothing) .. max_blocks * bt (and 2^31 - 513)
+ *   since        device int32 [B] or NULL: tokens of the row whose bounds are
+ *                there already, 0 .. seq_len; a block that is partly among them
+ *                is done again (none is for since == seq_len)
+ *   bounds       device, kv_bounds_bytes(cfg), 256-byte aligned, the caller's
+ * B at most 4096, B * max_blocks at most 2^30. A length or since out of range sets KV_DEVICE_BAD_LENGTH and the row is
+ * skipped, a block id out of range KV_DEVICE_BAD_BLOCK. Two rows may name the
+ * same block: both write the same values, if their lengths cover it alike. */
+int kv_pool_block_bounds(kv_pool *pool, int32_t layer, const int32_t *block_tables,
+                         const int32_t *seq_lens, const int32_t *since, int32_t B,
+                         int32_t max_blocks, void *bounds, kv_stream_t stream);
+
+/* For each row and kv-head the blocks that its Hq/Hkv query heads may need most.
+ *   q            device bf16 [B][Hq][D], the next token q_stride elements on (0:
+ *                contiguous), 16-byte aligned, q_stride a multiple of 8
+ *   first, last  the row's first and last blocks that are always taken; their
+ *                bounds are not read (the last block of a session that grows has
+ *                none for its newest tokens). first + last <= top
+ *   selected     device int32 [B][Hkv][top]: logical block numbers, ascending, -1
+ *                behind the row's last
+ *   scores       device fp32 [B][Hkv][max_blocks] or NULL: the blocks' scores,
+ *                +inf for those always taken, -inf past the row's blocks
+ * score = step * sum_d (Qp[d] * codes[0][d] + Qn[d] * codes[1][d]), Qp and Qn the
+ * sums over the group's heads of the positive and the negative parts of
+ *   c[h][d] = round_to_even(q[h][d] * 2^(137 - E)),
+ * E the biased exponent of the group's largest finite |q| (at least 1); a q that is not
+ * finite counts as 0. So a score is at least 2^(137 - E) sum_h q_h . K[t] for every token t of
+ * the block, up to c's rounding. The sum is a whole number, rounded to fp32 once:
+ * scores, and with them the selection, do not depend on an order of sums. A block
+ * whose step is infinite scores +inf. Equal scores go to the lower block number;
+ * blocks always taken come before all others.
+ * Row b has ceil(seq_lens[b] / bt) blocks; 0 is none (all -1). A length out of
+ * range sets KV_DEVICE_BAD_LENGTH and its row gets -1 and no scores, a block id out of range
+ * KV_DEVICE_BAD_BLOCK (scored as block 0 is). max_blocks at most 49152. */
+int select_blocks(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride, const void *bounds,
+                  const int32_t *block_tables, const int32_t *seq_lens, int32_t B, int32_t max_blocks,
+                  int32_t first, int32_t last, int32_t top, int32_t *selected, float *scores,
+                  kv_stream_t stream);
+
+/* Attention of one new token per session, position seq_lens[b] - 1, over the
+ * tokens t < seq_lens[b] of the listed blocks of each kv-head:
+ * out[b][h] = sum_t softmax_t(scale * q . K[g][t]) V[g][t], g = h / (Hq/Hkv).
+ *   q            as in select_blocks
+ *   k_new, v_new device bf16 [B][Hkv][D], the next row kv_stride elements on (0:
+ *                contiguous), or both NULL. With them the token's K and V are written
+ *                into its pool slot (which kv_pool_batch_reserve allocated), listed or
+ *                not, and attended to if its block is listed (select_blocks with
+ *                last >= 1 lists it)
+ *   selected     device int32 [B][Hkv][top]: logical blocks in any order; negative
+ *                entries are skipped, a block that is named twice counts twice
+ *   out          device fp32 [B][Hq][D], or bf16 with KV_DECODE_OUT_BF16
+ * A row and head that sees nothing (no block listed, or seq_len 0) gets zeros.
+ * q, k_new, v_new and out 16-byte aligned, strides multiples of 8. Scores,
+ * softmax statistics and sums are held in 32 bits, weights in bf16 for the product
+ * with V. Tokens past seq_len in a block may hold anything. The result is the
+ * same from run to run; its last bits depend on the order of the list and on
+ * B x Hkv, top and the device's number of SMs, by which the work is cut. A length out of range
+ * sets KV_DEVICE_BAD_LENGTH and the row is not written; a listed block at or past the row's
+ * end, or a block id out of range, sets KV_DEVICE_BAD_BLOCK and is skipped; a wait
+ * inside the kernel that runs out (2 s) sets KV_DEVICE_TIMEOUT, the row is then wrong.
+ * No workspace: calls on several streams may overlap. */
+int sparse_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride, const void *k_new,
+                     const void *v_new, int64_t kv_stride, const int32_t *selected, int32_t top,
+                     const int32_t *block_tables, const int32_t *seq_lens, int32_t B, int32_t max_blocks,
+                     float scale, void *out, uint32_t flags, kv_stream_t stream);
+
+/* n new ACTIVE sessions of max_tokens each that begin with the first `tokens`
+ * tokens (0 .. T) of an ACTIVE session; sids_out (host) receives their ids. No
+ * passage; tokens are immutable (Section 3, "Memory hierarchy and write policy"),
+ * so full blocks are shared: they are held by all sessions that name them, only
+ * read, and go back to the free list with the last of them. The block that
+ * `tokens` ends in is copied into one block per new session. In residency mode a
+ * block has one owner, whom an eviction takes it from: there all blocks are
+ * copied, evicted ones read from the parent's image. A fork's image is its own
+ * and empty: its first pause writes all of its tokens.
+ * The stream first waits for the parent's last append and resume; order the call
+ * after the attention calls that write tokens which the parent has reserved. The
+ * parent's and the new sessions' ready events are recorded on the stream. Free-list pops go
+ * session by session, in logical order. Errors: KV_ERR_BAD_STATE (paused),
+ * KV_ERR_NO_HOT_BLOCKS, KV_ERR_NO_COLD_SPACE (n images), too many sessions ->
+ * KV_ERR_INVALID_ARG. All or nothing. */
+int session_fork(kv_pool *pool, int32_t sid, int64_t tokens, int64_t max_tokens, int32_t n,
+                 int32_t *sids_out, kv_stream_t stream);
+
+/* Forget all but the first `tokens` (0 .. T) tokens of a session in any state. No
+ * passage (the paper's contexts only grow). The blocks behind them are given
+ * back, the last one first, so that a session that grows again gets them again
+ * in order; they are reused only by work ordered after this call on the stream.
+ * If the block that `tokens` ends in is shared (session_fork), its part moves into
+ * a block of its own (KV_ERR_NO_HOT_BLOCKS). Tokens that the image holds stay
+ * valid there. The stream first waits for the session's last append and resume; the caller
+ * orders it after any other work that reads or writes the session. Where rows move,
+ * the session's ready event is recorded on the stream. */
+int session_truncate(kv_pool *pool, int32_t sid, int64_t tokens, kv_stream_t stream);
+
+/* Keep the first `prefix` tokens of an ACTIVE session and, behind them, n of the others: token
+ * prefix + i of layer l and kv-head g becomes the old token
+ *   keep[l * layer_stride + g * head_stride + i]
+ * (device int32, 4-byte aligned; strides in elements, 0 where lists are shared), K and V
+ * alike; T = prefix + n. No passage. A list ascends strictly within prefix .. T - 1. Rows move
+ * towards the front in place; blocks behind the new end are given back as by
+ * session_truncate, shared blocks are replaced by new ones (free-list pops in
+ * logical order). Of the image only the tokens before prefix stay valid: later
+ * ones are written again by the next pause. In residency mode evicted blocks are
+ * fetched back first. n = T - prefix keeps everything and moves nothing.
+ * A position out of range, or not above the one before it, sets KV_DEVICE_BAD_INDEX; that
+ * layer and head's rows from there on are then undefined. Waits and ordering as session_truncate. Errors:
+ * KV_ERR_BAD_STATE (paused), KV_ERR_NO_HOT_BLOCKS. */
+int session_compact(kv_pool *pool, int32_t sid, const int32_t *keep, int64_t layer_stride,
+                    int64_t head_stride, int32_t n, int64_t prefix, kv_stream_t stream);
+
 /* Data path 4 with write-on-evict (Section 3, "Memory hierarchy and write
  * policy"): copy tokens [cold_valid, T) of an ACTIVE session into its
  * image, set cold_valid = T, return its hot blocks to the end of the free
@@ -483,6 +624,7 @@ int kv_pool_get_stats(kv_pool *pool, kv_pool_stats *out);
 #define KV_DEVICE_BAD_LENGTH 2     /* seq_len < 1 or past its table row (row skipped) */
 #define KV_DEVICE_TIMEOUT 4        /* a tile wait gave up after 2 s (output undefined) */
 #define KV_DEVICE_STALE_COUNTERS 8 /* split-arrival counters not at zero (reset)       */
+#define KV_DEVICE_BAD_INDEX 16     /* a kept position out of range or out of order     */
 
 /* Synchronise the device and read the flags that kernels set when their own
  * bounds checks fire (a block id outside the pool, a length past a table

@@ -32,6 +32,7 @@ class Pool:
         # The calls that a model makes per layer go to the library by the shortest way: a call on a few
         # tokens takes the GPU about as long as the host.
         self._prefill, self._tree = kvtier.lib.prefill_attention, kvtier.lib.tree_attention
+        self._select, self._sparse = kvtier.lib.select_blocks, kvtier.lib.sparse_attention
         self._bf16, self._i32, self._masks, self._index = (torch.bfloat16, torch.int32,
                                                            (torch.int64, torch.uint64), device)
         self._out_flags = {torch.float32: 0, torch.bfloat16: kvtier.KV_DECODE_OUT_BF16}
@@ -40,6 +41,7 @@ class Pool:
                                    block_tokens=block_tokens, num_hot_blocks=num_hot_blocks)
         self.block_bytes = kvtier.kv_block_bytes(probe)
         self.token_bytes = kvtier.kv_token_bytes(probe)
+        self.bounds_bytes = kvtier.kv_bounds_bytes(probe)
         self.hot = torch.empty(num_hot_blocks * self.block_bytes // 2, dtype=torch.bfloat16,
                                device=self.device)
         self.cold_int8 = cold_int8
@@ -235,6 +237,134 @@ class Pool:
                         out.data_ptr(), flags, kvtier._stream(stream))
         if rc:
             kvtier.raise_last(rc, "tree_attention")
+
+    # attention over a part of the cache --------------------------------------------
+    def new_bounds(self):
+        """A buffer for the bounds of all blocks' keys (block_bounds), zeros."""
+        import torch
+        return torch.zeros(self.bounds_bytes, dtype=torch.int8, device=self.device)
+
+    def bounds_views(self, bounds):
+        """A buffer's int8 codes [L][Hkv][NB][2][D] (largest, smallest) and bf16 steps [L][Hkv][NB]
+        (views); bound = code * step."""
+        import torch
+        shape = (self.L, self.Hkv, self.num_hot_blocks)
+        n = self.L * self.Hkv * self.num_hot_blocks
+        return (bounds[:n * 2 * self.D].view(*shape, 2, self.D),
+                bounds[n * 2 * self.D:].view(torch.bfloat16).view(shape))
+
+    def _rows(self, tables, lens, B, max_blocks, *more):
+        """Block tables, lengths and other int32 tensors [B] of a call, checked."""
+        i32, index = self._i32, self._index
+        ok = tables.numel() >= B * max_blocks
+        for x in (tables, lens, *more):
+            ok = ok and x.dtype is i32 and x.numel() >= B and x.is_contiguous() and x.get_device() == index
+        if not ok:
+            raise ValueError(f"need contiguous int32 block tables [{B}][{max_blocks}] and lengths [{B}] on the "
+                             f"pool's device, {self.device}, got " +
+                             ", ".join(f"{x.dtype} {tuple(x.shape)} strides {x.stride()}" for x in (tables, lens, *more)))
+
+    def _heads(self, x, B, heads, name):
+        """The row stride of bf16 [B][heads][D] with contiguous heads, checked (0: one row)."""
+        stride, D = x.stride(), self.D
+        if x.dtype is not self._bf16 or x.shape != (B, heads, D) or stride[2] != 1 or \
+                (heads > 1 and stride[1] != D) or (B > 1 and stride[0] == 0) or x.get_device() != self._index:
+            raise ValueError(f"{name}: need bf16 [{B}][{heads}][{D}] with contiguous heads and a row stride that is "
+                             f"not 0 on the pool's device, {self.device}, got {x.dtype} {tuple(x.shape)} strides {stride}")
+        return stride[0] if B > 1 else 0
+
+    def _list(self, selected, B):
+        """Entries per row and head of a selection [B][Hkv][top], checked."""
+        if selected.dtype is not self._i32 or selected.dim() != 3 or selected.shape[0] != B or \
+                selected.shape[1] != self.Hkv or not selected.is_contiguous() or \
+                selected.get_device() != self._index:
+            raise ValueError(f"selected must be contiguous int32 [{B}][{self.Hkv}][top] on the pool's device, "
+                             f"got {selected.dtype} {tuple(selected.shape)} strides {selected.stride()}")
+        return selected.shape[2]
+
+    def _whole_bounds(self, bounds):
+        if bounds.numel() * bounds.element_size() < self.bounds_bytes or not bounds.is_contiguous() or \
+                bounds.get_device() != self._index:
+            raise ValueError(f"bounds must be a contiguous buffer of {self.bounds_bytes} bytes on the pool's "
+                             "device (new_bounds)")
+
+    def block_bounds(self, layer: int, block_tables, seq_lens, B: int, max_blocks: int, bounds, since=None,
+                     stream=None) -> None:
+        """Bounds of the keys of the rows' blocks that hold tokens from since[b] on (all without it), of
+        one layer or (-1) all."""
+        self._rows(block_tables, seq_lens, B, max_blocks, *(() if since is None else (since,)))
+        self._whole_bounds(bounds)
+        kvtier.kv_pool_block_bounds(self.handle, layer, block_tables, seq_lens, since, B, max_blocks, bounds,
+                                    stream)
+
+    def select_blocks(self, layer: int, q, bounds, block_tables, seq_lens, B: int, max_blocks: int, selected,
+                      first: int = 1, last: int = 1, scores=None, stream=None) -> None:
+        """The `top` blocks of each row and KV head that q's [B][Hq][D] heads (any row stride) may need
+        most, the row's `first` first and `last` last ones among them, into selected int32
+        [B][Hkv][top]: ascending, -1 behind. scores: fp32 [B][Hkv][max_blocks] or None."""
+        self._rows(block_tables, seq_lens, B, max_blocks)
+        self._whole_bounds(bounds)
+        top, q_stride, at = self._list(selected, B), self._heads(q, B, self.Hq, "q"), None
+        if scores is not None:
+            at = scores.data_ptr()
+            if str(scores.dtype) != "torch.float32" or scores.shape != (B, self.Hkv, max_blocks) or \
+                    not scores.is_contiguous() or scores.get_device() != self._index:
+                raise ValueError(f"scores must be contiguous fp32 [{B}][{self.Hkv}][{max_blocks}] on the pool's device")
+        rc = self._select(self.handle, layer, q.data_ptr(), q_stride, bounds.data_ptr(),
+                          block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, first, last, top,
+                          selected.data_ptr(), at, kvtier._stream(stream))
+        if rc:
+            kvtier.raise_last(rc, "select_blocks")
+
+    def sparse_attention(self, layer: int, q, selected, block_tables, seq_lens, B: int, max_blocks: int,
+                         scale: float, out, k_new=None, v_new=None, stream=None) -> None:
+        """Attention of one new token per session over the listed blocks of each KV head (selected, as
+        select_blocks leaves it, or any list). k_new, v_new: bf16 [B][Hkv][D] (any row stride), the
+        token at seq_lens[b] - 1, written to its pool slot as well. out: fp32 or bf16 [B][Hq][D]."""
+        self._rows(block_tables, seq_lens, B, max_blocks)
+        top, q_stride, kv_stride, k, v = self._list(selected, B), self._heads(q, B, self.Hq, "q"), 0, None, None
+        if (k_new is None) != (v_new is None):
+            raise ValueError("k_new and v_new come together")
+        if k_new is not None:
+            kv_stride = self._heads(k_new, B, self.Hkv, "k_new")
+            if self._heads(v_new, B, self.Hkv, "v_new") != kv_stride:
+                raise ValueError("k_new and v_new need the same row stride")
+            k, v = k_new.data_ptr(), v_new.data_ptr()
+        if out.shape != (B, self.Hq, self.D) or not out.is_contiguous() or out.dtype not in self._out_flags or \
+                out.get_device() != self._index:
+            raise ValueError(f"out must be contiguous fp32 or bf16 [{B}][{self.Hq}][{self.D}] on the pool's device")
+        rc = self._sparse(self.handle, layer, q.data_ptr(), q_stride, k, v, kv_stride, selected.data_ptr(), top,
+                          block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, scale, out.data_ptr(),
+                          self._out_flags[out.dtype], kvtier._stream(stream))
+        if rc:
+            kvtier.raise_last(rc, "sparse_attention")
+
+    # pages of sessions ---------------------------------------------------------------
+    def session_fork(self, sid: int, n: int = 1, tokens: int | None = None, max_tokens: int | None = None,
+                     stream=None) -> list[int]:
+        """n sessions of max_tokens (the parent's capacity) that begin with its first `tokens` (all):
+        full blocks are shared, the partly filled one copied (residency mode: all copied)."""
+        if tokens is None or max_tokens is None:
+            info = kvtier.session_info(self.handle, sid)
+            tokens = info.tokens if tokens is None else tokens
+            max_tokens = info.capacity if max_tokens is None else max_tokens
+        return kvtier.session_fork(self.handle, sid, tokens, max_tokens, n, stream)
+
+    def session_truncate(self, sid: int, tokens: int, stream=None) -> None:
+        """Forget all but the first `tokens` tokens."""
+        kvtier.session_truncate(self.handle, sid, tokens, stream)
+
+    def session_compact(self, sid: int, keep, prefix: int = 0, stream=None) -> None:
+        """Keep the first `prefix` tokens and, behind them, those that `keep` names: ascending positions,
+        int32 [n] for all heads, or [L][Hkv][n] (expanded dimensions will do)."""
+        if keep.dtype is not self._i32 or keep.get_device() != self._index or \
+                (keep.dim() != 1 and (keep.dim() != 3 or keep.shape[:2] != (self.L, self.Hkv))) or \
+                (keep.shape[-1] > 1 and keep.stride(-1) != 1):
+            raise ValueError(f"keep must be int32 [n] or [{self.L}][{self.Hkv}][n] with contiguous lists on the pool's "
+                             f"device, got {keep.dtype} {tuple(keep.shape)} strides {keep.stride()}")
+        strides = (0, 0) if keep.dim() == 1 else (keep.stride(0) if self.L > 1 else 0,
+                                                  keep.stride(1) if self.Hkv > 1 else 0)
+        kvtier.session_compact(self.handle, sid, keep, *strides, keep.shape[-1], prefix, stream)
 
     def shuffle_free(self, seed: int) -> None:
         kvtier.kv_pool_shuffle_free(self.handle, seed)

@@ -14,8 +14,10 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvtier.so")
-SOURCES = ["decode_kernels.cu", "turn_kernels.cu", "copy_kernels.cu", "pool.cpp", "noalloc.cu"]
-HEADERS = ["kvt_internal.h", "pool_state.h", "decode_launch.h", "turn_plan.h", "tile_ops.cuh", os.path.join("..", "..", "include", "kvtier.h")]
+SOURCES = ["decode_kernels.cu", "turn_kernels.cu", "copy_kernels.cu", "sparse_kernels.cu",
+           "page_kernels.cu", "pool.cpp", "pages.cpp", "sparse.cpp", "noalloc.cu"]
+HEADERS = ["kvt_internal.h", "pool_state.h", "decode_launch.h", "turn_plan.h", "tile_ops.cuh",
+           "cache_ops.h", os.path.join("..", "..", "include", "kvtier.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

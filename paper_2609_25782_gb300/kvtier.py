@@ -42,10 +42,13 @@ EXPORTS = [
     "decode_append_attention", "kv_pool_inject_decode_timeout", "kv_decode_splits",
     "session_block_table_device", "kv_pool_prefetch", "kv_pool_inject_stale_counter",
     "kv_image_token_bytes", "kv_pool_batch_reserve_tokens", "prefill_attention", "tree_attention",
+    "kv_bounds_bytes", "kv_pool_block_bounds", "select_blocks", "sparse_attention", "session_fork",
+    "session_truncate", "session_compact",
 ]
 
 KV_DEVICE_BAD_BLOCK, KV_DEVICE_BAD_LENGTH, KV_DEVICE_TIMEOUT = 1, 2, 4
 KV_DEVICE_STALE_COUNTERS = 8
+KV_DEVICE_BAD_INDEX = 16
 
 KV_DECODE_OVERLAP_PREVIOUS = 1
 KV_DECODE_OUT_BF16 = 2
@@ -108,6 +111,14 @@ def _load():
                               C.c_uint32, p],
         "tree_attention": [p, i32, p, i64, p, p, i64, p, p, i32, p, p, i32, i32, C.c_float, p,
                            C.c_uint32, p],
+        "kv_bounds_bytes": [C.POINTER(kv_pool_config)],
+        "kv_pool_block_bounds": [p, i32, p, p, p, i32, i32, p, p],
+        "select_blocks": [p, i32, p, i64, p, p, p, i32, i32, i32, i32, i32, p, p, p],
+        "sparse_attention": [p, i32, p, i64, p, p, i64, p, i32, p, p, i32, i32, C.c_float, p,
+                             C.c_uint32, p],
+        "session_fork": [p, i32, i64, i64, i32, p, p],
+        "session_truncate": [p, i32, i64, p],
+        "session_compact": [p, i32, p, i64, i64, i32, i64, p],
         "kv_pool_prefetch": [p, p, i32, p, i32, p],
         "decode_append_attention": [p, i32, p, p, p, p, p, i32, i32, C.c_float, p, C.c_uint32, p],
         "decode_attention": [p, i32, p, p, p, i32, i32, C.c_float, p, p],
@@ -138,6 +149,7 @@ def _load():
     L.kv_block_bytes.restype = i64
     L.kv_token_bytes.restype = i64
     L.kv_image_token_bytes.restype = i64
+    L.kv_bounds_bytes.restype = i64
     L.kv_last_error.restype = C.c_char_p
     return L
 
@@ -328,6 +340,50 @@ def tree_attention(pool: int, layer: int, q, q_stride: int, k_draft, v_draft, kv
                               kv_stride, _addr(ancestors), _addr(cu_draft), total,
                               _addr(block_tables), _addr(seq_lens), B, max_blocks, scale, _addr(out),
                               flags, _stream(stream)), "tree_attention")
+
+
+def kv_bounds_bytes(cfg: kv_pool_config) -> int:
+    return int(lib.kv_bounds_bytes(C.byref(cfg)))
+
+
+def kv_pool_block_bounds(pool: int, layer: int, block_tables, seq_lens, since, B: int, max_blocks: int,
+                         bounds, stream=None) -> None:
+    _check(lib.kv_pool_block_bounds(pool, layer, _addr(block_tables), _addr(seq_lens), _addr(since), B,
+                                    max_blocks, _addr(bounds), _stream(stream)),
+           "kv_pool_block_bounds")
+
+
+def select_blocks(pool: int, layer: int, q, q_stride: int, bounds, block_tables, seq_lens, B: int,
+                  max_blocks: int, first: int, last: int, top: int, selected, scores=None,
+                  stream=None) -> None:
+    _check(lib.select_blocks(pool, layer, _addr(q), q_stride, _addr(bounds), _addr(block_tables),
+                             _addr(seq_lens), B, max_blocks, first, last, top, _addr(selected),
+                             _addr(scores), _stream(stream)), "select_blocks")
+
+
+def sparse_attention(pool: int, layer: int, q, q_stride: int, k_new, v_new, kv_stride: int, selected,
+                     top: int, block_tables, seq_lens, B: int, max_blocks: int, scale: float, out,
+                     flags: int = 0, stream=None) -> None:
+    _check(lib.sparse_attention(pool, layer, _addr(q), q_stride, _addr(k_new), _addr(v_new), kv_stride,
+                                _addr(selected), top, _addr(block_tables), _addr(seq_lens), B,
+                                max_blocks, scale, _addr(out), flags, _stream(stream)),
+           "sparse_attention")
+
+
+def session_fork(pool: int, sid: int, tokens: int, max_tokens: int, n: int, stream=None) -> list[int]:
+    out = (C.c_int32 * max(1, n))()
+    _check(lib.session_fork(pool, sid, tokens, max_tokens, n, out, _stream(stream)), "session_fork")
+    return list(out)
+
+
+def session_truncate(pool: int, sid: int, tokens: int, stream=None) -> None:
+    _check(lib.session_truncate(pool, sid, tokens, _stream(stream)), "session_truncate")
+
+
+def session_compact(pool: int, sid: int, keep, layer_stride: int, head_stride: int, n: int, prefix: int,
+                    stream=None) -> None:
+    _check(lib.session_compact(pool, sid, _addr(keep), layer_stride, head_stride, n, prefix,
+                               _stream(stream)), "session_compact")
 
 
 def kv_pool_prefetch(pool: int, sids, busy=(), stream=None) -> None:
