@@ -1,7 +1,6 @@
 """Compile libkvtier.so in-tree with nvcc for sm_103a.
 
-The translation units (decode_kernels.cu, turn_kernels.cu,
-copy_kernels.cu, pool.cpp, noalloc.cu) compile in parallel and are linked with the static CUDA runtime,
+The translation units (SOURCES) compile in parallel and are linked with the static CUDA runtime,
 so the library needs only the driver at run time.
 """
 from __future__ import annotations
@@ -15,9 +14,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvtier.so")
 SOURCES = ["decode_kernels.cu", "turn_kernels.cu", "copy_kernels.cu", "sparse_kernels.cu",
-           "page_kernels.cu", "pool.cpp", "pages.cpp", "sparse.cpp", "noalloc.cu"]
+           "attend_kernels.cu", "page_kernels.cu", "pool.cpp", "pages.cpp", "sparse.cpp", "noalloc.cu"]
 HEADERS = ["kvt_internal.h", "pool_state.h", "decode_launch.h", "turn_plan.h", "tile_ops.cuh",
-           "cache_ops.h", os.path.join("..", "..", "include", "kvtier.h")]
+           "cluster.cuh", "cache_ops.h", os.path.join("..", "..", "include", "kvtier.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -1,5 +1,6 @@
 // Internal interface of the calls on parts of the cache: sparse.cpp with sparse_kernels.cu (bounds of blocks,
-// selection, attention over selected blocks), pages.cpp with page_kernels.cu (forks, compaction).
+// selection) and attend_kernels.cu (attention over listed blocks), pages.cpp with page_kernels.cu (forks,
+// compaction).
 #pragma once
 
 #include "kvt_internal.h"
@@ -35,6 +36,7 @@ struct SelectArgs {
     int32_t *err;
     int64_t q_stride;
     int32_t B, max_blocks, first, last, top;
+    int32_t group;            // Hq / Hkv
     Shape s;
 };
 
@@ -49,7 +51,9 @@ struct SparseArgs {
     int32_t *err;
     int64_t q_stride, kv_stride;
     int32_t B, max_blocks, layer, top, out_bf16;
+    int32_t group;            // Hq / Hkv
     float scale_log2;         // scale * log2(e)
+    int32_t inject_extra_tx;  // test hook: extra bytes expected on one tile (0 normally)
     Shape s;
 };
 
@@ -90,8 +94,10 @@ struct CompactArgs {
 };
 
 cudaError_t launch_bounds(const BoundsArgs &a, int num_sms, cudaStream_t st);
-cudaError_t launch_select(const SelectArgs &a, int num_sms, cudaStream_t st);
-cudaError_t launch_sparse(const CUtensorMap &map, const SparseArgs &a, int num_sms, cudaStream_t st);
+cudaError_t prepare_select_kernel(SelectFit *fit);
+cudaError_t launch_select(const SelectArgs &a, const SelectFit &fit, cudaStream_t st);
+cudaError_t prepare_sparse_kernels(SparseFit *fit);
+cudaError_t launch_sparse(const CUtensorMap &map, const SparseArgs &a, const SparseFit &fit, cudaStream_t st);
 cudaError_t launch_copy_jobs(const CopyJobs &a, int max_ctas, cudaStream_t st);
 cudaError_t launch_compact(const CompactArgs &a, int max_ctas, cudaStream_t st);
 

@@ -1,0 +1,65 @@
+// Clusters of thread blocks: their barrier, their blocks' shared memory, and launches (attend_kernels.cu,
+// sparse_kernels.cu).
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace kvt {
+namespace {
+
+__device__ __forceinline__ void cluster_arrive() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t remote(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+// A grid of (cluster, y, z) blocks, each row of it a cluster.
+template <typename... Args>
+cudaError_t launch_clusters(void (*kernel)(Args...), int cluster, int y, int z, int threads, int smem, cudaStream_t st,
+                            const Args &...args) {
+    cudaLaunchConfig_t c{};
+    cudaLaunchAttribute at[1];
+    c.gridDim = dim3(cluster, y, z);
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    c.attrs = at;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, kernel, args...);
+}
+
+// Prepares a kernel for clusters of up to 16 blocks and `most` bytes of shared memory, and tells how many clusters
+// of 1, 2, 4, 8 and 16 blocks of `smem` bytes the device holds at once.
+template <typename... Args>
+cudaError_t fit_clusters(void (*kernel)(Args...), int threads, int most, int smem, int (&fit)[5]) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    for (int i = 0; i < 5 && e == cudaSuccess; ++i) {
+        cudaLaunchConfig_t c{};
+        cudaLaunchAttribute at[1];
+        c.gridDim = dim3(1 << i);
+        c.blockDim = dim3(threads);
+        c.dynamicSmemBytes = smem;
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = 1 << i;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        c.attrs = at;
+        c.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&fit[i], kernel, &c);
+    }
+    return e;
+}
+
+}  // namespace
+}  // namespace kvt

@@ -231,6 +231,15 @@ struct GatherArgs {
     int32_t new_blk[kGatherMax];   // >= 0: also store it as the row's last entry (nblk-1)
 };
 
+// How many clusters of 1, 2, 4, 8 and 16 CTAs the device holds at once, for the kernels of select_blocks (one CTA per
+// SM in [1], two in [0]) and of sparse_attention (8 warps in [1], 4 in [0]).
+struct SelectFit {
+    int clusters[2][5];
+};
+struct SparseFit {
+    int clusters[2][5];
+};
+
 // Host launchers (decode_kernels.cu, turn_kernels.cu, copy_kernels.cu). Each returns the launch's CUDA status.
 // A bf16 tensor map with the 128-byte swizzle; strides in bytes, from the second dimension on.
 bool encode_bf16_map(CUtensorMap *map, void *base, int rank, const cuuint64_t *dims,

@@ -103,6 +103,10 @@ struct kv_pool {
     int64_t counter_count = 0;
     int32_t *d_err = nullptr;
     CUtensorMap tmap{};
+    bool select_ready = false;           // the kernels of select_blocks
+    bool sparse_ready = false;           // and of sparse_attention
+    kvt::SelectFit select_fit{};
+    kvt::SparseFit sparse_fit{};
     // prefill_attention and tree_attention (turn_setup)
     bool turn_ready = false;             // the kernel and the maps
     CUtensorMap turn_maps[2]{};

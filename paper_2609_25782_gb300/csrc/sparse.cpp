@@ -1,5 +1,5 @@
 // Attention over a part of the cache (include/kvtier.h): bounds of blocks' keys, the selection of blocks from
-// them, and attention over the selected ones. Kernels in sparse_kernels.cu.
+// them, and attention over the selected ones. Kernels in sparse_kernels.cu and attend_kernels.cu.
 #include <cmath>
 
 #include "cache_ops.h"
@@ -93,6 +93,11 @@ int select_blocks(kv_pool *p, int32_t layer, const void *q, int64_t q_stride, co
     if (rc) return rc;
     if (p->host_only) return fail(KV_ERR_BAD_STATE, "selection on a host-logic-only pool");
     DeviceGuard dg(p->cfg.device, true);
+    if (!p->select_ready) {
+        rc = p->cuda("kernel of the selection", [&] { return kvt::prepare_select_kernel(&p->select_fit); });
+        if (rc) return rc;
+        p->select_ready = true;
+    }
     const int64_t layer_records = static_cast<int64_t>(layer) * p->cfg.num_kv_heads * p->cfg.num_hot_blocks;
     kvt::SelectArgs a;
     a.q = static_cast<const uint16_t *>(q);
@@ -110,9 +115,10 @@ int select_blocks(kv_pool *p, int32_t layer, const void *q, int64_t q_stride, co
     a.first = first;
     a.last = last;
     a.top = top;
+    a.group = p->cfg.num_q_heads / p->cfg.num_kv_heads;
     a.s = p->shape;
     return p->cuda("selection launch", [&] {
-        return kvt::launch_select(a, p->num_sms, reinterpret_cast<cudaStream_t>(stream));
+        return kvt::launch_select(a, p->select_fit, reinterpret_cast<cudaStream_t>(stream));
     });
 }
 
@@ -136,6 +142,11 @@ int sparse_attention(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     if (!(scale == scale) || std::isinf(scale)) return fail(KV_ERR_INVALID_ARG, "scale not finite");
     if (p->host_only) return fail(KV_ERR_BAD_STATE, "attention on a host-logic-only pool");
     DeviceGuard dg(p->cfg.device, true);
+    if (!p->sparse_ready) {
+        rc = p->cuda("kernels of sparse attention", [&] { return kvt::prepare_sparse_kernels(&p->sparse_fit); });
+        if (rc) return rc;
+        p->sparse_ready = true;
+    }
     kvt::SparseArgs a;
     a.q = static_cast<const uint16_t *>(q);
     a.k_new = static_cast<const uint16_t *>(k_new);
@@ -152,12 +163,15 @@ int sparse_attention(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     a.max_blocks = max_blocks;
     a.layer = layer;
     a.top = top;
+    a.group = p->cfg.num_q_heads / p->cfg.num_kv_heads;
     a.out_bf16 = (flags & KV_DECODE_OUT_BF16) ? 1 : 0;
     a.scale_log2 = scale * 1.4426950408889634f;
+    a.inject_extra_tx = p->inject_timeout ? 16 : 0;
     a.s = p->shape;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    rc = p->cuda("attention launch", [&] { return kvt::launch_sparse(p->tmap, a, p->num_sms, st); });
+    rc = p->cuda("attention launch", [&] { return kvt::launch_sparse(p->tmap, a, p->sparse_fit, st); });
     if (rc) return rc;
+    p->inject_timeout = false;
     p->decoded = true;
     p->decode_stream = st;
     return KV_OK;

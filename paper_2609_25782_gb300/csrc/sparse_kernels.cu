@@ -1,11 +1,12 @@
-// Kernels of attention over a part of the cache, for sm_103a.
+// Kernels that choose the part of the cache that a step reads, for sm_103a.
 //
 //   bounds_kernel   channelwise bounds of the keys of blocks, in 8 bits
 //   select_kernel   scores of blocks from the bounds, and the `top` largest
-//   sparse_kernel   attention of one new token per session over listed blocks
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "cache_ops.h"
+#include "cluster.cuh"
 #include "tile_ops.cuh"
 
 namespace kvt {
@@ -153,235 +154,378 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const BoundsArgs
 
 // ---- selection ---------------------------------------------------------------------------------------
 
-constexpr int kSelectThreads = 256;
+// A row's blocks for one kv-head (a unit) are one cluster's. Each warp scores 16 blocks at a time with whole numbers,
+// codes times q's digits, as columns of an fp16 mma (int8 products are slow on this GPU: eight int8 mma of 16 blocks
+// took 1 500 cycles, a dp4a loop as long). The scores' keys go to the first CTA's shared memory, which alone finds the
+// key of the last block to be taken, by counts of the keys' leading bits within their range, and lists the blocks.
+//
+// A call of a few units is a chain of latencies and of instructions that run once: they come at some 8 cycles each,
+// so the code on the way is kept short, its loops rolled.
+constexpr int kSelectThreads = 512;
+constexpr int kSelectWarps = kSelectThreads / 32;
+constexpr int kBins = 4 * kSelectThreads;
+constexpr int kWarpBlocks = 16;                      // that a warp scores at a time
+constexpr int kDigits = 3;                           // of a sum over q's heads, in base 32
+constexpr int kDigitRow = kCodeRow + 16;             // halves from one digit's row to the next (banks)
 
-// Scores in an order of their bits: larger scores have larger keys. All NaN-free.
+constexpr int select_smem(int blocks) { return (blocks + 3) / 4 * 16; }
+
+// Scores in an order of their bits: larger scores have larger keys. NaN-free; no key is 0 or ~0.
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);   // one zero
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// The whole of a block of threads: the sum of x.
-__device__ __forceinline__ int block_sum(int x, int *scratch) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    x = __reduce_add_sync(~0u, x);
-    __syncthreads();
-    if (lane == 0) scratch[warp] = x;
-    __syncthreads();
-    int s = 0;
-    for (int w = 0; w < kSelectThreads / 32; ++w) s += scratch[w];
-    return s;
+// D = A(16x16 fp16, row) * B(16x8 fp16, col) + D in fp32.
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// One CTA per (row, kv-head).
-__global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectArgs a) {
-    extern __shared__ uint32_t keys[];
-    __shared__ int scratch[kSelectThreads / 32];
-    __shared__ int qp[kHeadDim], qn[kHeadDim];
+// Four codes c as fp16 numbers 1152 + c: 0x6400, which is 1024, and c + 128 in its last bits.
+__device__ __forceinline__ uint2 halves(uint32_t codes) {
+    const uint32_t u = codes ^ 0x80808080u;
+    return make_uint2(__byte_perm(u, 0x64646464u, 0x4140), __byte_perm(u, 0x64646464u, 0x4342));
+}
+constexpr int kCodeOffset = 1152;
+
+// Sum of the threads' values before this one's. (Two counts in a word's halves: each sums up to at most
+// kSelectBlocksMax.) One copy of its code: the second call finds it in the instruction cache.
+__device__ __noinline__ uint32_t scan_before(uint32_t x, uint32_t *scratch) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t y = x;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t z = __shfl_up_sync(~0u, y, d);
+        if (lane >= d) y += z;
+    }
+    __syncthreads();
+    if (lane == 31) scratch[warp] = y;
+    __syncthreads();
+    return y - x + __reduce_add_sync(~0u, lane < warp ? scratch[lane] : 0);
+}
+
+// Codes of the warp's 16 blocks, those of block `row` and of `row` + 8 (mma fragments), and a block's step per lane.
+struct Fetched {
+    uint4 x[4], y[4];
+    uint32_t step;
+};
+
+// kTwo: CTAs that have an SM each keep two fetches per warp on their way, 128 KiB in all; others one, two CTAs per SM.
+template <bool kTwo>
+__global__ void __launch_bounds__(kSelectThreads, kTwo ? 1 : 2) select_kernel(const SelectArgs a) {
+    extern __shared__ uint4 keys4[];                 // keys of the unit's blocks; used in the first CTA
+    uint32_t *keys = reinterpret_cast<uint32_t *>(keys4);
+    __shared__ alignas(16) uint32_t hist[kBins];
+    __shared__ uint32_t cand[kSelectThreads];
+    __shared__ uint32_t scratch[kSelectWarps];
+    __shared__ uint32_t least, most, found[4];
+    __shared__ int qsum[kCodeRow], qtotal;           // sums of q's positive parts, then of its negative ones
+    __shared__ alignas(16) __half digits[kDigits * kDigitRow];
     const Shape sh = a.s;
-    const int g = blockIdx.x % sh.Hkv, b = blockIdx.x / sh.Hkv;
-    const int G = sh.Hq / sh.Hkv;
+    const int C = gridDim.x, rank = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int T = a.seq_lens[b];
-    const bool bad = !good_length(T, a.max_blocks, sh.bt);
-    const int n = bad ? 0 : (T + sh.bt - 1) / sh.bt;
-    if (bad && tid == 0) atomicOr(a.err, kErrBadLength);
+    // The warp's blocks are j .. j + 15, then those `jump` on; lanes look up their places, the first ones before
+    // T is known (entries past a row's end are not used).
+    const int32_t *trow = a.tables + static_cast<int64_t>(b) * a.max_blocks;
+    const int jump = C * kSelectWarps * kWarpBlocks;
+    const int64_t start = a.first + static_cast<int64_t>(rank * kSelectWarps + warp) * kWarpBlocks;
+    auto block_of = [&](int64_t at) { return at + (lane & 15) < a.max_blocks ? trow[at + (lane & 15)] : 0; };
+    int blk0 = block_of(start), blk1 = kTwo ? block_of(start + jump) : 0;
+    // q as one dim of two heads per thread.
+    const int dim = tid & (kHeadDim - 1), head = tid / kHeadDim;
+    static_assert(kMaxGroup == 2 * kSelectThreads / kHeadDim, "two heads per thread");
+    const uint16_t *q = a.q + b * a.q_stride + static_cast<int64_t>(g * a.group + head) * kHeadDim + dim;
+    uint32_t v[2];
+    v[0] = head < a.group ? q[0] : 0;
+    v[1] = head + kMaxGroup / 2 < a.group ? q[kMaxGroup / 2 * kHeadDim] : 0;
     int32_t *selected = a.selected + (static_cast<int64_t>(b) * sh.Hkv + g) * a.top;
-    float *scores = a.scores ? a.scores + (static_cast<int64_t>(b) * sh.Hkv + g) * a.max_blocks : nullptr;
-
-    // q as whole numbers
-    const uint16_t *q = a.q + b * a.q_stride + static_cast<int64_t>(g) * G * kHeadDim;
-    int most = 0;
-    for (int i = tid; i < G * kHeadDim; i += kSelectThreads) {
-        const int m = q[i] & 0x7FFF;
-        if (m < static_cast<int>(kInfBits)) most = max(most, m);
-    }
-    most = __reduce_max_sync(~0u, most);
-    if (lane == 0) scratch[warp] = most;
-    __syncthreads();
-    for (int w = 0; w < kSelectThreads / 32; ++w) most = max(most, scratch[w]);
-    const int E = max(1, most >> 7);
-    const float s1 = pow2(min(254, 264 - E)), s2 = pow2(127 + max(0, 10 - E));   // 2^(137 - E)
-    for (int d = tid; d < kHeadDim; d += kSelectThreads) {
-        int p = 0, m = 0;
-        for (int h = 0; h < G; ++h) {
-            const uint32_t w = q[h * kHeadDim + d];
-            if ((w & 0x7FFF) >= kInfBits) continue;
-            const int c = __float2int_rn(__uint_as_float(w << 16) * s1 * s2);
-            p += max(c, 0);
-            m += min(c, 0);
+    if (!good_length(T, a.max_blocks, sh.bt)) {      // (the whole cluster leaves)
+        if (rank == 0) {
+            if (tid == 0) atomicOr(a.err, kErrBadLength);
+            for (int i = tid; i < a.top; i += kSelectThreads) selected[i] = -1;
         }
-        qp[d] = p;
-        qn[d] = m;
-    }
-    __syncthreads();
-
-    for (int j = warp; j < n; j += kSelectThreads / 32) {
-        uint32_t key = 0xFFFFFFFFu;
-        float x = INFINITY;
-        if (j >= a.first && j < n - a.last) {
-            int blk = a.tables[static_cast<int64_t>(b) * a.max_blocks + j];
-            if (blk < 0 || blk >= sh.num_blocks) {
-                if (lane == 0) atomicOr(a.err, kErrBadBlock);
-                blk = 0;
-            }
-            const int64_t rec = static_cast<int64_t>(g) * sh.num_blocks + blk;
-            const int8_t *codes = a.codes + rec * kCodeRow;
-            int sum = 0;
-            for (int d = lane; d < kHeadDim; d += 32) sum += qp[d] * codes[d] + qn[d] * codes[kHeadDim + d];
-            sum = __reduce_add_sync(~0u, sum);
-            const uint32_t step = a.steps[rec];
-            if (step < kInfBits) x = __fmul_rn(__int2float_rn(sum), __uint_as_float(step << 16));
-            key = key_of(x);
-        }
-        if (lane == 0) {
-            keys[j] = key;
-            if (scores) scores[j] = x;
-        }
-    }
-    if (scores && !bad)
-        for (int j = n + tid; j < a.max_blocks; j += kSelectThreads) scores[j] = -INFINITY;
-    __syncthreads();
-
-    // The key that the top-th largest has, bit by bit: the largest with at least `want` keys not below it.
-    const int want = min(a.top, n);
-    uint32_t edge = 0;
-    int above = 0;                                   // keys larger than edge
-    if (want > 0) {
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t probe = edge | 1u << bit;
-            int c = 0;
-            for (int j = tid; j < n; j += kSelectThreads) c += keys[j] >= probe;
-            c = block_sum(c, scratch);
-            if (c >= want) edge = probe;
-        }
-        int c = 0;
-        for (int j = tid; j < n; j += kSelectThreads) c += keys[j] > edge;
-        above = block_sum(c, scratch);
-    }
-    // In the blocks' order: all above the edge, and the first of those at it.
-    int done = 0, ties = 0;
-    for (int j0 = 0; j0 < n; j0 += kSelectThreads) {
-        const int j = j0 + tid;
-        const uint32_t key = j < n ? keys[j] : 0;
-        const bool gt = j < n && key > edge, eq = j < n && key == edge;
-        const unsigned mg = __ballot_sync(~0u, gt), me = __ballot_sync(~0u, eq);
-        __syncthreads();
-        if (lane == 0) scratch[warp] = __popc(mg) | __popc(me) << 16;
-        __syncthreads();
-        const unsigned below = (1u << lane) - 1;
-        int bg = __popc(mg & below), be = __popc(me & below), tg = 0, te = 0;
-        for (int w = 0; w < kSelectThreads / 32; ++w) {
-            const int s = scratch[w];
-            if (w < warp) {
-                bg += s & 0xFFFF;
-                be += s >> 16;
-            }
-            tg += s & 0xFFFF;
-            te += s >> 16;
-        }
-        const int rank = ties + be;                  // ties before this one
-        if (gt || (eq && rank < want - above)) selected[done + bg + min(rank, want - above)] = j;
-        done += tg;
-        ties += te;
-    }
-    for (int i = want + tid; i < a.top; i += kSelectThreads) selected[i] = -1;
-}
-
-// ---- attention ---------------------------------------------------------------------------------------
-
-constexpr int kSparseThreads = 128;
-
-// One CTA per (row, query head), a warp per token in turn, four dims a lane.
-__global__ void __launch_bounds__(kSparseThreads) sparse_kernel(const SparseArgs a) {
-    constexpr int kWarps = kSparseThreads / 32;
-    __shared__ float s_m[kWarps], s_l[kWarps];
-    __shared__ float4 s_o[kWarps][32];
-    const Shape sh = a.s;
-    const int h = blockIdx.x % sh.Hq, b = blockIdx.x / sh.Hq;
-    const int G = sh.Hq / sh.Hkv, g = h / G;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int T = a.seq_lens[b];
-    if (!good_length(T, a.max_blocks, sh.bt)) {
-        if (threadIdx.x == 0) atomicOr(a.err, kErrBadLength);
         return;
     }
-    const int32_t *trow = a.tables + static_cast<int64_t>(b) * a.max_blocks;
-    const int32_t *list = a.selected + (static_cast<int64_t>(b) * sh.Hkv + g) * a.top;
-    auto four = [&](const uint16_t *row) {
-        const uint2 w = reinterpret_cast<const uint2 *>(row)[lane];
-        return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u),
-                           __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
-    };
-    auto row_of = [&](int blk, int t, int kv) {
-        const int j = t / sh.bt;
-        return (((static_cast<int64_t>(blk) * sh.L + a.layer) * 2 + kv) * sh.Hkv + g) * sh.bt + t - j * sh.bt;
-    };
-    const uint16_t *k_new = a.k_new ? a.k_new + b * a.kv_stride + g * kHeadDim : nullptr;
-    const uint16_t *v_new = a.k_new ? a.v_new + b * a.kv_stride + g * kHeadDim : nullptr;
-    if (k_new && T > 0 && h == g * G && warp == 0) {
-        const int blk = trow[(T - 1) / sh.bt];
+    if (tid == 0) {
+        least = ~0u;
+        most = 0;
+        qtotal = 0;
+    }
+    if (C > 1) cluster_arrive();                     // the first CTA's memory may be written from here on
+    const int n = sh.bt == 16 ? (T + 15) >> 4 : (T + 63) >> 6;
+    const int want = min(a.top, n);
+    float *scores = a.scores ? a.scores + (static_cast<int64_t>(b) * sh.Hkv + g) * a.max_blocks : nullptr;
+    // Blocks [j0, j1) are scored: the others are always taken. Where all are taken, only for the caller's scores.
+    const int j0 = min(a.first, n), j1 = max(j0, n - a.last);
+    const bool choose = n > a.top;
+    const int end = choose || scores ? j1 : 0;
+    int j = static_cast<int>(start < end ? start : end);
+
+    const int quad = lane & 3, row = lane >> 2;
+    const int8_t *codes = a.codes + static_cast<int64_t>(g) * sh.num_blocks * kCodeRow;
+    const uint16_t *steps = a.steps + static_cast<int64_t>(g) * sh.num_blocks;
+    auto fetch = [&](Fetched &f, int at, int blk) {
+        if (at + (lane & 15) >= end) blk = 0;        // (not scored)
         if (blk < 0 || blk >= sh.num_blocks) {
-            if (lane == 0) atomicOr(a.err, kErrBadBlock);
-        } else {
-            reinterpret_cast<uint2 *>(a.hot + row_of(blk, T - 1, 0) * kHeadDim)[lane] = reinterpret_cast<const uint2 *>(k_new)[lane];
-            reinterpret_cast<uint2 *>(a.hot + row_of(blk, T - 1, 1) * kHeadDim)[lane] = reinterpret_cast<const uint2 *>(v_new)[lane];
+            atomicOr(a.err, kErrBadBlock);
+            blk = 0;
+        }
+        f.step = steps[blk];
+        const uint4 *px = reinterpret_cast<const uint4 *>(codes + static_cast<int64_t>(__shfl_sync(~0u, blk, row)) * kCodeRow) + quad;
+        const uint4 *py = reinterpret_cast<const uint4 *>(codes + static_cast<int64_t>(__shfl_sync(~0u, blk, row + 8)) * kCodeRow) + quad;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            f.x[c] = px[4 * c];
+            f.y[c] = py[4 * c];
+        }
+    };
+    Fetched f0, f1;
+    if (j < end) fetch(f0, j, blk0);
+    if (kTwo && j + jump < end) fetch(f1, j + jump, blk1);
+    if (j + jump < end) {
+        blk0 = block_of(j + (kTwo ? 2 : 1) * static_cast<int64_t>(jump));
+        if (kTwo) blk1 = block_of(j + 3 * static_cast<int64_t>(jump));
+    }
+
+    // q as whole numbers
+    int top_bits = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int m = v[h] & 0x7FFF;
+        if (m < static_cast<int>(kInfBits)) top_bits = max(top_bits, m);
+    }
+    top_bits = __reduce_max_sync(~0u, top_bits);
+    if (lane == 0) scratch[warp] = top_bits;
+    if (tid < kCodeRow) qsum[tid] = 0;
+    if (rank == 0) {
+        reinterpret_cast<uint4 *>(hist)[tid] = make_uint4(0u, 0u, 0u, 0u);
+        // Blocks that are always taken; what is read behind the last.
+        for (int i = tid; i < j0; i += kSelectThreads) keys[i] = ~0u;
+        for (int i = j1 + tid; i < ((n + 3) & ~3); i += kSelectThreads) keys[i] = i < n ? ~0u : 0;
+    }
+    __syncthreads();
+    top_bits = __reduce_max_sync(~0u, lane < kSelectWarps ? static_cast<int>(scratch[lane]) : 0);
+    const int E = max(1, top_bits >> 7);
+    const float s1 = pow2(min(254, 264 - E)), s2 = pow2(127 + max(0, 10 - E));   // 2^(137 - E)
+    int up = 0, down = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int c = (v[h] & 0x7FFF) < kInfBits ? __float2int_rn(__uint_as_float(v[h] << 16) * s1 * s2) : 0;
+        up += max(c, 0);
+        down += min(c, 0);
+    }
+    atomicAdd(&qsum[dim], up);
+    atomicAdd(&qsum[kHeadDim + dim], down);
+    __syncthreads();
+    if (tid < kCodeRow) {
+        int x = qsum[tid];                           // |x| <= 8 * 2040
+        const int total = __reduce_add_sync(~0u, x);
+        if (lane == 0) atomicAdd(&qtotal, total);
+#pragma unroll
+        for (int d = kDigits - 1; d >= 0; --d) {     // digits of -16 .. 15, the first one of -16 .. 16
+            const int low5 = d ? ((x + 16) & 31) - 16 : x;
+            digits[d * kDigitRow + tid] = __int2half_rn(low5);
+            x = (x - low5) >> 5;
         }
     }
-    const float4 q = four(a.q + b * a.q_stride + static_cast<int64_t>(h) * kHeadDim);
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int e = 0; e < a.top; ++e) {
-        const int j = list[e];
-        if (j < 0) continue;
-        const int blk = static_cast<int64_t>(j) * sh.bt < T ? trow[j] : -1;
-        if (blk < 0 || blk >= sh.num_blocks) {
-            if (threadIdx.x == 0) atomicOr(a.err, kErrBadBlock);
+    __syncthreads();
+    // B fragments: columns 0 to 2 are the digits, the others any. The order of the dims within a product is the
+    // loads': piece c of lane t (of four) is the record's 16 bytes t + 4 c.
+    const uint4 *weights = reinterpret_cast<const uint4 *>(digits + min(row, kDigits - 1) * kDigitRow) + 2 * quad;
+    const uint32_t offset = static_cast<uint32_t>(kCodeOffset * qtotal);
+    if (C > 1) cluster_wait();
+    const uint32_t keys_at = remote(smem_u32(keys), 0);
+    uint32_t low = ~0u, high = 0;
+    auto score = [&](const Fetched &f, int at) {
+        // 128 products of up to 1279 x 16 a sum: whole numbers below 2^24, exact in fp32.
+        float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint4 w0 = weights[8 * c], w1 = weights[8 * c + 1];
+            uint2 p = halves(f.x[c].x), o = halves(f.y[c].x);
+            mma_f16(d0, p.x, o.x, p.y, o.y, w0.x, w0.y);
+            p = halves(f.x[c].y), o = halves(f.y[c].y);
+            mma_f16(d1, p.x, o.x, p.y, o.y, w0.z, w0.w);
+            p = halves(f.x[c].z), o = halves(f.y[c].z);
+            mma_f16(d0, p.x, o.x, p.y, o.y, w1.x, w1.y);
+            p = halves(f.x[c].w), o = halves(f.y[c].w);
+            mma_f16(d1, p.x, o.x, p.y, o.y, w1.z, w1.w);
+        }
+        // Lanes of quad 0 have the first two digits' sums, of quad 1 the last one's, each for blocks row and row + 8:
+        // quad 0 keeps row. (Whole numbers modulo 2^32; the score's fits 32 bits.)
+        auto whole = [](float x, float y) { return static_cast<uint32_t>(__float2int_rn(x) + __float2int_rn(y)); };
+        uint32_t mine = whole(d0[0], d1[0]), other = whole(d0[2], d1[2]);
+        if (quad == 0) {
+            mine = mine * 1024 + whole(d0[1], d1[1]) * 32;
+            other = other * 1024 + whole(d0[3], d1[3]) * 32;
+        }
+        const uint32_t got = __shfl_xor_sync(~0u, quad == 0 ? other : mine, 1);
+        const int sum = static_cast<int>((quad == 0 ? mine : other) + got - offset);
+        const int r = row + 8 * quad;
+        const uint32_t st = __shfl_sync(~0u, f.step, r & 15);
+        const float z = st < kInfBits ? __fmul_rn(__int2float_rn(sum), __uint_as_float(st << 16)) : INFINITY;
+        if (quad < 2 && at + r < end) {
+            const uint32_t key = key_of(z);
+            low = min(low, key);
+            high = max(high, key);
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys_at + (at + r) * 4), "r"(key) : "memory");
+            if (scores) scores[at + r] = z;
+        }
+    };
+#pragma unroll 1
+    while (j < end) {
+        score(f0, j);
+        j += jump;
+        if (!kTwo) {
+            if (j >= end) break;
+            fetch(f0, j, blk0);
+            blk0 = block_of(j + static_cast<int64_t>(jump));
             continue;
         }
-        const int end = min(T, (j + 1) * sh.bt);
-        for (int t = j * sh.bt + warp; t < end; t += kWarps) {
-            const bool fresh = k_new && t == T - 1;
-            const float4 k = four(fresh ? k_new : a.hot + row_of(blk, t, 0) * kHeadDim);
-            const float4 v = four(fresh ? v_new : a.hot + row_of(blk, t, 1) * kHeadDim);
-            float x = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) x += __shfl_xor_sync(~0u, x, d);
-            x *= a.scale_log2;
-            const float mn = fmaxf(m, x), c = ex2(m - mn), w = ex2(x - mn);
-            m = mn;
-            l = l * c + w;
-            o = make_float4(o.x * c + w * v.x, o.y * c + w * v.y, o.z * c + w * v.z, o.w * c + w * v.w);
+        if (j >= end) break;
+        if (j + jump < end) {
+            fetch(f0, j + jump, blk0);
+            blk0 = block_of(j + 3 * static_cast<int64_t>(jump));
+        }
+        score(f1, j);
+        j += jump;
+        if (j + jump < end) {
+            fetch(f1, j + jump, blk1);
+            blk1 = block_of(j + 3 * static_cast<int64_t>(jump));
         }
     }
-    if (lane == 0) {
-        s_m[warp] = m;
-        s_l[warp] = l;
+    low = __reduce_min_sync(~0u, low);
+    high = __reduce_max_sync(~0u, high);
+    if (lane == 0 && low <= high) {
+        asm volatile("red.relaxed.cluster.shared::cluster.min.u32 [%0], %1;" ::"r"(remote(smem_u32(&least), 0)), "r"(low) : "memory");
+        asm volatile("red.relaxed.cluster.shared::cluster.max.u32 [%0], %1;" ::"r"(remote(smem_u32(&most), 0)), "r"(high) : "memory");
     }
-    s_o[warp][lane] = o;
-    __syncthreads();
-    if (warp != 0) return;
-    float M = -INFINITY;
-    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w]);
-    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-    for (int w = 0; w < kWarps; ++w) {
-        const float c = M == -INFINITY ? 0.f : ex2(s_m[w] - M);
-        const float4 y = s_o[w][lane];
-        sum += c * s_l[w];
-        r = make_float4(r.x + c * y.x, r.y + c * y.y, r.z + c * y.z, r.w + c * y.w);
+    if (C > 1) cluster_arrive();
+    if (scores) {
+        for (int i = rank * kSelectThreads + tid; i < a.max_blocks; i += C * kSelectThreads)
+            if (i < j0 || i >= j1) scores[i] = i < n ? INFINITY : -INFINITY;
     }
-    const float inv = sum > 0.f ? __frcp_rn(sum) : 0.f;
-    r = make_float4(r.x * inv, r.y * inv, r.z * inv, r.w * inv);
-    const int64_t row = static_cast<int64_t>(b) * sh.Hq + h;
-    if (a.out_bf16) {
-        float r0, r1;
-        uint2 pk;
-        pk.x = pack_bf16(r.x, r.y, r0, r1);
-        pk.y = pack_bf16(r.z, r.w, r0, r1);
-        reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row * kHeadDim)[lane] = pk;
-    } else {
-        reinterpret_cast<float4 *>(static_cast<float *>(a.out) + row * kHeadDim)[lane] = r;
+    if (C > 1) cluster_wait();
+    else __syncthreads();
+    if (rank != 0) return;
+
+    for (int i = want + tid; i < a.top; i += kSelectThreads) selected[i] = -1;
+    if (!choose) {
+        for (int i = tid; i < n; i += kSelectThreads) selected[i] = i;
+        return;
+    }
+    const int quads = (n + 3) >> 2;                  // of keys
+    // The largest key that is not taken whole, and how many of its blocks are: of the scored blocks `need`, the
+    // larger keys first. Those in question are lo + [0, span]: neither ~0 nor 0.
+    int need = want - (n - (j1 - j0));
+    uint32_t edge = ~0u - 1;
+    int ties = 0;
+    if (need > 0) {
+        uint32_t lo = least, span = most - lo;
+        int shift = max(0, 21 - __clz(span | 1));
+#pragma unroll 1
+        for (;;) {
+            auto count = [&](uint32_t key) {
+                if (key - lo <= span) atomicAdd(&hist[(key - lo) >> shift], 1u);
+            };
+#pragma unroll 1
+            for (int i = tid; i < quads; i += kSelectThreads) {
+                const uint4 k = keys4[i];
+                count(k.x), count(k.y), count(k.z), count(k.w);
+            }
+            __syncthreads();
+            // From the top: thread t has bins kBins - 4 - 4 t and on.
+            const uint4 h = reinterpret_cast<const uint4 *>(hist)[kSelectThreads - 1 - tid];
+            const int four = static_cast<int>(h.x + h.y + h.z + h.w);
+            const int above = static_cast<int>(scan_before(four, scratch));
+            if (above < need && need <= above + four) {
+                const int a1 = above + h.w, a2 = a1 + h.z, a3 = a2 + h.y;
+                const int at = need <= a1 ? 3 : need <= a2 ? 2 : need <= a3 ? 1 : 0;
+                found[0] = kBins - 4 - 4 * tid + at;
+                found[1] = at == 3 ? above : at == 2 ? a1 : at == 1 ? a2 : a3;     // above the bin
+                found[2] = at == 3 ? h.w : at == 2 ? h.z : at == 1 ? h.y : h.x;    // in it
+                found[3] = 0;
+            }
+            __syncthreads();
+            const int in = static_cast<int>(found[2]);
+            need -= static_cast<int>(found[1]);
+            lo += found[0] << shift;
+            if (in == need) {                        // the whole bin
+                edge = lo - 1;
+                break;
+            }
+            if (shift == 0) {                        // one key
+                edge = lo;
+                ties = need;
+                break;
+            }
+            span = (1u << shift) - 1;
+            if (in <= kSelectThreads) {              // each one's place among them
+                auto take = [&](uint32_t key) {
+                    if (key - lo <= span) cand[atomicAdd(&found[3], 1u)] = key;
+                };
+#pragma unroll 1
+                for (int i = tid; i < quads; i += kSelectThreads) {
+                    const uint4 k = keys4[i];
+                    take(k.x), take(k.y), take(k.z), take(k.w);
+                }
+                __syncthreads();
+                if (tid < in) {
+                    const uint32_t key = cand[tid];
+                    int more = 0, same = 0;
+#pragma unroll 4
+                    for (int i = 0; i < in; ++i) {
+                        more += cand[i] > key;
+                        same += cand[i] == key;
+                    }
+                    if (more < need && need <= more + same) {
+                        found[0] = key;              // (equal ones write the same)
+                        found[1] = need - more;
+                    }
+                }
+                __syncthreads();
+                edge = found[0];
+                ties = static_cast<int>(found[1]);
+                break;
+            }
+            shift = max(0, shift - 11);
+            reinterpret_cast<uint4 *>(hist)[tid] = make_uint4(0u, 0u, 0u, 0u);
+            __syncthreads();
+        }
+    }
+    // The list: each thread counts its blocks above the edge and at it, and places them behind the threads' before it.
+    // (An odd number of 16-byte pieces each: no bank conflicts.)
+    const int each = ((quads + kSelectThreads - 1) / kSelectThreads) | 1;
+    const int from = min(quads, tid * each), to = min(quads, from + each);
+    auto level = [&](uint32_t key) { return key > edge ? 1u << 16 : key == edge ? 1u : 0u; };
+    uint32_t count = 0;
+#pragma unroll 1
+    for (int i = from; i < to; ++i) {
+        const uint4 k = keys4[i];
+        count += level(k.x) + level(k.y) + level(k.z) + level(k.w);
+    }
+    const uint32_t before = scan_before(count, scratch);
+    if (count == 0) return;
+    int e = static_cast<int>(before & 0xFFFF), at = static_cast<int>(before >> 16) + min(e, ties);
+#pragma unroll 1
+    for (int i = from; i < to; i += 8) {             // a bit per block
+        uint32_t m = 0;
+#pragma unroll 1
+        for (int c = 0; c < 8 && i + c < to; ++c) {
+            const uint4 k = keys4[i + c];
+            m |= ((k.x >= edge) | (k.y >= edge) << 1 | (k.z >= edge) << 2 | (k.w >= edge) << 3) << (4 * c);
+        }
+#pragma unroll 1
+        for (; m != 0; m &= m - 1) {
+            const int block = 4 * i + __ffs(m) - 1;
+            const bool tie = keys[block] == edge;
+            if (!tie || e < ties) selected[at++] = block;
+            e += tie;
+        }
     }
 }
 
@@ -395,20 +539,29 @@ cudaError_t launch_bounds(const BoundsArgs &a, int num_sms, cudaStream_t st) {
     return cudaGetLastError();
 }
 
-cudaError_t launch_select(const SelectArgs &a, int, cudaStream_t st) {
-    const int bytes = a.max_blocks * 4;
-    if (bytes > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   kSelectBlocksMax * 4);
-        if (e != cudaSuccess) return e;
-    }
-    select_kernel<<<a.B * a.s.Hkv, kSelectThreads, bytes, st>>>(a);
-    return cudaGetLastError();
+cudaError_t prepare_select_kernel(SelectFit *fit) {
+    cudaError_t e = cudaSuccess;
+    for (int two = 0; two < 2 && e == cudaSuccess; ++two)
+        e = fit_clusters(two ? select_kernel<true> : select_kernel<false>, kSelectThreads, select_smem(kSelectBlocksMax),
+                         select_smem(8192), fit->clusters[two]);
+    return e;
 }
 
-cudaError_t launch_sparse(const CUtensorMap &, const SparseArgs &a, int, cudaStream_t st) {
-    sparse_kernel<<<a.B * a.s.Hq, kSparseThreads, 0, st>>>(a);
-    return cudaGetLastError();
+cudaError_t launch_select(const SelectArgs &a, const SelectFit &fit, cudaStream_t st) {
+    // The largest clusters that are all resident at once, of at least 64 blocks a CTA. us with the widest that fits
+    // and the next wider one (rotating inputs): 8 units of 1 250 blocks 6.5 (8 CTAs) and 10.0, 32 of up to 7 500 14.4
+    // (4) and 18.1, 64 of up to 1 875 9.0 (2) and 13.2. Too many units for two CTAs of an SM each: two to an SM, 512
+    // units of up to 1 250 28.4, by CTAs of an SM each 32.0.
+    const int64_t units = static_cast<int64_t>(a.B) * a.s.Hkv;
+    int two = 1, log = 4;
+    while (log > 0 && (units > fit.clusters[1][log] || a.max_blocks < 64 << log)) --log;
+    if (log == 0 && units > fit.clusters[1][0] / 2 && a.max_blocks >= 128) {
+        two = 0;
+        log = 4;
+        while (log > 0 && (units > fit.clusters[0][log] || a.max_blocks < 64 << log)) --log;
+    }
+    return launch_clusters(two ? select_kernel<true> : select_kernel<false>, 1 << log, a.s.Hkv, a.B, kSelectThreads,
+                           select_smem(a.max_blocks), st, a);
 }
 
 }  // namespace kvt

@@ -223,3 +223,40 @@ def test_numpy_int_arguments_are_plain_numbers(cuda_dev):
     c.random_lists(3, seed=1)
     c.pool.sparse_attention(0, c.q, c.selected, c.tables, c.lens, int(np.int64(1)), c.width, c.scale, c.out)
     assert c.pool.check_device() == 0
+
+
+def test_a_wait_that_runs_out(cuda_dev):
+    """The hook's one call reports it and ends, the next ones are right; a context that goes on."""
+    from paper_2609_25782_gb300 import kvtier
+    for T, top in (([1000], 40), ([2000] * 130, 20)):    # few units and many
+        c = Cache(T, seed=16)
+        c.random_lists(top, seed=2, holes=0.0)
+        kvtier.kv_pool_inject_decode_timeout(c.pool.handle, 1)
+        c.attend()
+        assert c.pool.check_device() == kvtier.KV_DEVICE_TIMEOUT
+        for b in range(1, c.B):
+            c.assert_right(b, *c.reference(b))
+        c.check(True)
+
+
+def test_infinite_keys_and_values(cuda_dev):
+    """A score of -inf has no weight, whatever came before it; of +inf or with an infinite value nothing is finite."""
+    c = Cache([400], seed=17, hq=8, hkv=1)
+    c.selected = torch.arange(25, device="cuda").int().view(1, 1, 25)
+    blk = [int(x) for x in c.tab[0]]
+    c.q[0] = c.q[0].abs() + 0.1
+    for j in (0, 1, 2, 13):
+        c.hot[blk[j], 0, 0, 0, :, 5] = -float("inf")     # q is positive there
+    c.hot[blk[14], 0, 0, 0, 3, 5] = -float("inf")
+    seen = torch.tensor([t for t in range(400) if t // 16 not in (0, 1, 2, 13) and t != 14 * 16 + 3], device="cuda")
+    k, v = (torch.stack([c.hot[blk[int(t) // 16], 0, w, 0, int(t) % 16] for t in seen]).double() for w in (0, 1))
+    w = torch.softmax(c.q[0].double() @ k.T * c.scale, 1)
+    c.attend()
+    c.assert_right(0, w @ v, torch.sqrt((w * w) @ (v * v).sum(1)))
+    c.hot[blk[9], 0, 1, 0, 2, 7] = float("inf")
+    c.attend()
+    assert (c.out[0, :, 7] == float("inf")).all() and torch.isfinite(c.out[0, :, 8]).all()
+    c.hot[blk[9], 0, 1, 0, 2, 7] = 0
+    c.hot[blk[9], 0, 0, 0, 2, 7] = float("inf")
+    c.attend()
+    assert c.out.isnan().all() and c.pool.check_device() == 0
