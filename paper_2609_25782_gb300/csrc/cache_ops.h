@@ -99,6 +99,6 @@ cudaError_t launch_select(const SelectArgs &a, const SelectFit &fit, cudaStream_
 cudaError_t prepare_sparse_kernels(SparseFit *fit);
 cudaError_t launch_sparse(const CUtensorMap &map, const SparseArgs &a, const SparseFit &fit, cudaStream_t st);
 cudaError_t launch_copy_jobs(const CopyJobs &a, int max_ctas, cudaStream_t st);
-cudaError_t launch_compact(const CompactArgs &a, int max_ctas, cudaStream_t st);
+cudaError_t launch_compact(const CompactArgs &a, int num_sms, cudaStream_t st);
 
 }  // namespace kvt

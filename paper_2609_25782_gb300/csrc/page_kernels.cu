@@ -55,58 +55,84 @@ __global__ void __launch_bounds__(kCopyThreads) copy_jobs_kernel(const __grid_co
     }
 }
 
-// A CTA per (layer, K|V, kv-head) run takes its tokens in chunks, in ascending order. Lists ascend, so token t
-// comes from a row at or behind t: a chunk's stores only overwrite rows that no later chunk reads, and the
-// barriers keep them behind the chunk's own loads.
+// A CTA per (layer, K|V, kv-head) run and column of its rows, 256 / kSplit bytes wide, takes the tokens in chunks, in
+// ascending order. Lists ascend, so token t comes from a row at or behind t: a chunk's stores only overwrite rows
+// that no later chunk reads, and a barrier keeps them behind the loads of all chunks up to it. A chunk's positions,
+// their blocks and their rows are each loaded while the chunk before is at the next of these steps.
 constexpr int kCompactThreads = 256;
-constexpr int kCompactRows = 64;
+constexpr int kCompactDeep = 4;                      // rows of a thread in a chunk
 
-__global__ void __launch_bounds__(kCompactThreads) compact_kernel(const __grid_constant__ CompactArgs a) {
+template <int kSplit>
+__global__ void __launch_bounds__(kCompactThreads, 4) compact_kernel(const __grid_constant__ CompactArgs a) {
+    constexpr int kUnits = kRowBytes / 16 / kSplit;  // threads of a row, 16 bytes each
+    constexpr int kRows = kCompactThreads / kUnits;
+    constexpr int kChunk = kRows * kCompactDeep;
     const Shape sh = a.s;
-    const int run = blockIdx.x;                      // (l * 2 + kv) * Hkv + g
+    const int run = blockIdx.x / kSplit;             // (l * 2 + kv) * Hkv + g
     const int runs = sh.L * 2 * sh.Hkv;
     const int g = run % sh.Hkv;
     const int l = run / (2 * sh.Hkv);
     const int32_t *keep = a.keep + l * a.layer_stride + g * a.head_stride;
-    const int u = threadIdx.x & 15;                  // 16-byte unit of a row
-    const int r0 = threadIdx.x >> 4;
-    auto row_of = [&](int blk, int t, int j) {
-        return (static_cast<int64_t>(blk) * runs + run) * sh.bt + (t - j * sh.bt);
+    const int u = (blockIdx.x % kSplit) * kUnits + threadIdx.x % kUnits;   // 16-byte unit of a row
+    const int r0 = threadIdx.x / kUnits;
+    const int shift = sh.bt == 16 ? 4 : 6;
+    uint4 *base = reinterpret_cast<uint4 *>(a.hot) + u;
+    auto at = [&](int blk, int t) {                  // the pool has fewer than 2^31 rows
+        return base + static_cast<int64_t>(((blk * runs + run) << shift) + (t & (sh.bt - 1))) * (kRowBytes / 16);
     };
-    for (int t0 = a.t_begin; t0 < a.t_end; t0 += kCompactRows) {
-        uint4 v[kCompactRows / 16];
-        uint4 *to[kCompactRows / 16];
+    int from[kCompactDeep], before[kCompactDeep];    // positions of the next chunk, and those they have to exceed
+    int src[kCompactDeep], dst[kCompactDeep];        // blocks
+    uint4 v[kCompactDeep];
+    uint4 *to[kCompactDeep];                         // places of the chunk that was loaded, or null
+    // (Nothing here waits for a value that is loaded: the loads are all on their way before the first is used.)
+    auto positions = [&](int t0) {
 #pragma unroll
-        for (int k = 0; k < kCompactRows / 16; ++k) {
-            const int t = t0 + k * 16 + r0;
-            to[k] = nullptr;
-            if (t >= a.t_end) continue;
-            int from = t;
-            if (t >= a.prefix) {
-                from = keep[t - a.prefix];
-                const int before = t > a.prefix ? keep[t - a.prefix - 1] : a.prefix - 1;
-                // (from >= t is what the order of loads and stores rests on.)
-                if (from >= a.T || from < t || from <= before) {
-                    if (u == 0) atomicOr(a.err, kErrBadIndex);
-                    continue;
-                }
-            }
-            const int js = from / sh.bt, jd = t / sh.bt;
-            const int bs = a.table[js];
-            int bd = a.fresh ? a.slot[jd - a.fresh_at] : -1;
-            if (bd < 0) bd = a.table[jd];
-            if (bs < 0 || bs >= sh.num_blocks || bd < 0 || bd >= sh.num_blocks) {
-                if (u == 0) atomicOr(a.err, kErrBadBlock);
-                continue;
-            }
-            v[k] = reinterpret_cast<const uint4 *>(a.hot + row_of(bs, from, js) * kRowBytes)[u];
-            to[k] = reinterpret_cast<uint4 *>(a.hot + row_of(bd, t, jd) * kRowBytes) + u;
+        for (int k = 0; k < kCompactDeep; ++k) {
+            const int t = t0 + k * kRows + r0;
+            from[k] = t;
+            before[k] = t < a.prefix ? t - 1 : a.prefix - 1;
+            if (t >= a.prefix && t < a.t_end) from[k] = keep[t - a.prefix];
+            if (t > a.prefix && t < a.t_end) before[k] = keep[t - a.prefix - 1];
         }
+    };
+    positions(a.t_begin);
+#pragma unroll
+    for (int k = 0; k < kCompactDeep; ++k) to[k] = nullptr;
+#pragma unroll 1
+    for (int t0 = a.t_begin;; t0 += kChunk) {
+        bool ok[kCompactDeep];
+        bool bad = false;
+#pragma unroll
+        for (int k = 0; k < kCompactDeep; ++k) {
+            const int t = t0 + k * kRows + r0;
+            // (from >= t is what the order of loads and stores rests on.)
+            const bool good = from[k] < a.T && from[k] >= t && from[k] > before[k];
+            ok[k] = t < a.t_end && good;
+            bad |= t < a.t_end && !good;
+            src[k] = ok[k] ? a.table[from[k] >> shift] : -1;
+            dst[k] = ok[k] ? (a.fresh ? a.slot[(t >> shift) - a.fresh_at] : -1) : -1;
+            if (ok[k] && dst[k] < 0) dst[k] = a.table[t >> shift];
+        }
+        if (bad && u == 0) atomicOr(a.err, kErrBadIndex);
+        int row[kCompactDeep];
+#pragma unroll
+        for (int k = 0; k < kCompactDeep; ++k) row[k] = from[k];
+        positions(t0 + kChunk);
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kCompactRows / 16; ++k)
+        for (int k = 0; k < kCompactDeep; ++k)
             if (to[k] != nullptr) *to[k] = v[k];
-        __syncthreads();
+        if (t0 >= a.t_end) return;
+        bad = false;
+#pragma unroll
+        for (int k = 0; k < kCompactDeep; ++k) {
+            const bool in = src[k] >= 0 && src[k] < sh.num_blocks && dst[k] >= 0 && dst[k] < sh.num_blocks;
+            bad |= ok[k] && !in;
+            ok[k] = ok[k] && in;
+            to[k] = ok[k] ? at(dst[k], t0 + k * kRows + r0) : nullptr;
+            if (ok[k]) v[k] = *at(src[k], row[k]);
+        }
+        if (bad && u == 0) atomicOr(a.err, kErrBadBlock);
     }
 }
 
@@ -120,9 +146,21 @@ cudaError_t launch_copy_jobs(const CopyJobs &a, int max_ctas, cudaStream_t st) {
     return cudaGetLastError();
 }
 
-cudaError_t launch_compact(const CompactArgs &a, int, cudaStream_t st) {
+template <int kSplit>
+static void start_compact(const CompactArgs &a, cudaStream_t st) {
+    compact_kernel<kSplit><<<a.s.L * 2 * a.s.Hkv * kSplit, kCompactThreads, 0, st>>>(a);
+}
+
+cudaError_t launch_compact(const CompactArgs &a, int num_sms, cudaStream_t st) {
     if (a.t_end <= a.t_begin) return cudaSuccess;
-    compact_kernel<<<a.s.L * 2 * a.s.Hkv, kCompactThreads, 0, st>>>(a);
+    // Narrower columns where there are few runs, for the latency of a chunk. us by columns 1, 2, 4 and 8: 384 runs of
+    // 2 040 tokens out of 8 200 79, 83, 76, 85; 256 runs (64-token blocks, one of three calls) 39.6, 29.7, 31.6, 36.1;
+    // 224 runs of 14 000 out of 24 000 434, 300, 314, 315; 32 runs of 2 700 out of 9 000 41.5, 21.7, 13.5, 12.2.
+    const int64_t runs = static_cast<int64_t>(a.s.L) * 2 * a.s.Hkv, want = 5ll * num_sms / 2;
+    if (runs >= want) start_compact<1>(a, st);
+    else if (runs * 2 >= want) start_compact<2>(a, st);
+    else if (runs * 4 >= want) start_compact<4>(a, st);
+    else start_compact<8>(a, st);
     return cudaGetLastError();
 }
 

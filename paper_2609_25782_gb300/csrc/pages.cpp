@@ -139,8 +139,9 @@ int session_fork(kv_pool *p, int32_t sid, int64_t tokens, int64_t max_tokens, in
     if (!rc) {
         std::vector<kvt::CopyJob> copies;
         std::vector<kvt::BlockJob> fetches;
-        for (int32_t c = 0; c < n; ++c)
-            for (int64_t j = shared; j < nb; ++j) {
+        // A block's copies one after the other: they read it from the L2.
+        for (int64_t j = shared; j < nb; ++j)
+            for (int32_t c = 0; c < n; ++c) {
                 const int32_t to = got[c * each + j - shared], from = parent->blocks[j];
                 const int32_t rows = static_cast<int32_t>(std::min<int64_t>(bt, tokens - j * bt));
                 const int32_t jj = static_cast<int32_t>(j);
@@ -305,7 +306,7 @@ int session_compact(kv_pool *p, int32_t sid, const int32_t *keep, int64_t layer_
         a.fresh_at = static_cast<int32_t>(j);
         if (need > 0) std::copy(slot.begin() + (j - j0), slot.begin() + (to - j0), a.slot);
         a.s = p->shape;
-        rc = p->cuda("compaction launch", [&] { return kvt::launch_compact(a, p->move_ctas(st), st); });
+        rc = p->cuda("compaction launch", [&] { return kvt::launch_compact(a, p->num_sms, st); });
     }
     std::vector<int32_t> row(s->blocks.begin() + j0, s->blocks.begin() + j1);
     for (int64_t j = 0; j < j1 - j0; ++j)

@@ -34,24 +34,40 @@ __device__ __forceinline__ int2 bounds_blocks(const BoundsArgs &a, int b) {
     return make_int2(from / a.s.bt, (T + a.s.bt - 1) / a.s.bt);
 }
 
-constexpr int kBoundsThreads = 256;
+__device__ __forceinline__ uint32_t max2(uint32_t x, uint32_t y) {   // of two bf16 each; a NaN stays
+    const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
+    return *reinterpret_cast<const uint32_t *>(&m);
+}
+__device__ __forceinline__ uint32_t min2(uint32_t x, uint32_t y) {
+    const __nv_bfloat162 m = __hmin2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
+    return *reinterpret_cast<const uint32_t *>(&m);
+}
 
-// A warp per (block, layer, kv-head). The rows' block counts are summed up by every CTA first, so that the
-// items are one line whatever the lengths; a warp finds its row in it by bisection.
-__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const BoundsArgs a) {
-    __shared__ int ends[kBoundsRowsMax];
+constexpr int kBoundsThreads = 256;
+constexpr uint32_t kNegate2 = 0x80008000u, kMinusInf2 = 0xFF80FF80u;
+
+// A warp per (block, layer, kv-head) in turn: the rows' block counts are summed up by every CTA first, so that the
+// items are one line whatever the lengths. 16 tokens at a time; the next ones are on their way while an item's codes
+// are made, and the item after that is looked up. Warps next to each other have items next to each other: in runs of
+// items, each warp at another block of 1.5 MiB, the call took 1.1 times as long. Bound by HBM, with the instructions
+// close behind (a first form spent 1 500 on an item of 4 KiB, and was bound by them at 2.4 TB/s).
+__global__ void __launch_bounds__(kBoundsThreads, 4) bounds_kernel(const BoundsArgs a) {
+    extern __shared__ int rows_smem[];               // [B] ends: items' blocks up to the row's; [B] its first block less those before
     __shared__ int sums[kBoundsThreads / 32];
+    int *ends = rows_smem, *shift = rows_smem + a.B;
     const Shape sh = a.s;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int total = 0;
     for (int b0 = 0; b0 < a.B; b0 += kBoundsThreads) {
         const int b = b0 + threadIdx.x;
-        int n = 0;
+        int n = 0, from = 0;
         if (b < a.B) {
             const int2 r = bounds_blocks(a, b);
             n = r.y - r.x;
+            from = r.x;
             if (r.x < 0 && blockIdx.x == 0) atomicOr(a.err, kErrBadLength);
         }
+        const int mine = n;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int y = __shfl_up_sync(~0u, n, d);
@@ -64,91 +80,143 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const BoundsArgs
             if (w < warp) before += sums[w];
             total += sums[w];
         }
-        if (b < a.B) ends[b] = before + n;
+        if (b < a.B) {
+            ends[b] = before + n;
+            shift[b] = from - (before + n - mine);
+        }
         __syncthreads();
     }
-    const int per = a.nlayers * sh.Hkv;              // items of a block
-    const int64_t items = static_cast<int64_t>(total) * per;
-    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kBoundsThreads / 32);
-    for (int64_t it = static_cast<int64_t>(blockIdx.x) * (kBoundsThreads / 32) + warp; it < items; it += warps) {
-        const int pair = static_cast<int>(it / per);
-        const int rest = static_cast<int>(it - static_cast<int64_t>(pair) * per);
-        const int l = a.layer0 + rest / sh.Hkv, g = rest % sh.Hkv;
-        int lo = 0, hi = a.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (ends[mid] > pair) hi = mid;
-            else lo = mid + 1;
+    // The warp's items are `warps` apart: blocks, layers and heads advance by these.
+    const int per = a.nlayers * sh.Hkv, warps = gridDim.x * (kBoundsThreads / 32);
+    const int dpair = warps / per, dl = (warps - dpair * per) / sh.Hkv, dg = warps - dpair * per - dl * sh.Hkv;
+    const int first = blockIdx.x * (kBoundsThreads / 32) + warp;
+    int pair = first / per, l = (first - pair * per) / sh.Hkv, g = first - pair * per - l * sh.Hkv;
+    int row = 0;
+    // An item: its records' and its keys' places, its block (-1: a bad id) and tokens.
+    struct Item {
+        int l, g, blk, tokens;
+    };
+    auto find = [&]() {                              // of `pair`, below `total`
+        while (ends[row] <= pair) ++row;
+        const int j = pair + shift[row];
+        return Item{l, g, a.tables[static_cast<int64_t>(row) * a.max_blocks + j], min(sh.bt, a.seq_lens[row] - j * sh.bt)};
+    };
+    auto advance = [&]() {                           // (2^30 blocks at most, and a step of at most 2^13: in int)
+        pair += dpair;
+        l += dl;
+        g += dg;
+        if (g >= sh.Hkv) {
+            g -= sh.Hkv;
+            ++l;
         }
-        const int2 r = bounds_blocks(a, lo);
-        const int j = r.x + pair - (lo ? ends[lo - 1] : 0);
-        const int blk = a.tables[static_cast<int64_t>(lo) * a.max_blocks + j];
-        if (blk < 0 || blk >= sh.num_blocks) {
-            if (lane == 0) atomicOr(a.err, kErrBadBlock);
-            continue;
+        if (l >= a.nlayers) {
+            l -= a.nlayers;
+            ++pair;
         }
-        const int tokens = min(sh.bt, a.seq_lens[lo] - j * sh.bt);
-        const int64_t row = ((static_cast<int64_t>(blk) * sh.L + l) * 2 * sh.Hkv + g) * sh.bt;
-        const uint4 *k = reinterpret_cast<const uint4 *>(a.hot + row * kHeadDim);
-        // Half a warp per token, eight channels a lane.
-        __nv_bfloat162 up[4], down[4];
-        uint32_t most = 0;
+    };
+    // Half a warp per token, eight channels a lane. Past the end the last token again.
+    uint4 v[8];
+    auto load = [&](const Item &x, int t0) {
+        if (x.blk < 0 || x.blk >= sh.num_blocks) return;
+        const int64_t at = ((static_cast<int64_t>(x.blk) * sh.L + a.layer0 + x.l) * 2 * sh.Hkv + x.g) * sh.bt + t0;
+        const uint4 *k = reinterpret_cast<const uint4 *>(a.hot + at * kHeadDim) + (lane & 15);
+        const int half = lane >> 4, last = x.tokens - t0 - 1;
+        if (last >= 15) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            up[i] = __float2bfloat162_rn(-INFINITY);
-            down[i] = __float2bfloat162_rn(INFINITY);
+            for (int i = 0; i < 8; ++i) v[i] = k[(2 * i + half) * 16];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k[min(2 * i + half, last) * 16];
         }
-        for (int t0 = 0; t0 < sh.bt; t0 += 16) {
-            uint4 v[8];
+    };
+    if (pair >= total) return;
+    Item now = find();
+    load(now, 0);
+    advance();
+    Item next{};
+    bool more = pair < total;
+    if (more) next = find();
+    int t0 = 0;
+    uint32_t up[4], down[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (t0 + 2 * i + (lane >> 4) < tokens) v[i] = k[(t0 + 2 * i) * 16 + lane];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (t0 + 2 * i + (lane >> 4) >= tokens) continue;
-                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&w[c]);
-                    up[c] = __hmax2(up[c], x);
-                    down[c] = __hmin2(down[c], x);
-                    most = __vmaxu2(most, w[c] & 0x7FFF7FFFu);
-                }
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const uint32_t u = __shfl_xor_sync(~0u, *reinterpret_cast<uint32_t *>(&up[c]), 16);
-            const uint32_t d = __shfl_xor_sync(~0u, *reinterpret_cast<uint32_t *>(&down[c]), 16);
-            up[c] = __hmax2(up[c], *reinterpret_cast<const __nv_bfloat162 *>(&u));
-            down[c] = __hmin2(down[c], *reinterpret_cast<const __nv_bfloat162 *>(&d));
-        }
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) most = __vmaxu2(most, __shfl_xor_sync(~0u, most, d));
-        const uint32_t top = max(most & 0xFFFFu, most >> 16);
-        const bool fine = top < kInfBits;
-        const int E = max(1, static_cast<int>(top >> 7)) + ((top & 0x7F) == 0x7F);
-        // 2^(133 - E) is up to 2^132: two factors. A value too small for the product still counts: it rounds outwards.
-        const float s1 = pow2(min(254, 260 - E)), s2 = pow2(127 + max(0, 6 - E));
-        uint32_t bytes[8];
+    for (int c = 0; c < 4; ++c) {
+        up[c] = kMinusInf2;
+        down[c] = kMinusInf2 ^ kNegate2;
+    }
+#pragma unroll 1
+    for (;;) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const __nv_bfloat162 p = lane < 16 ? up[i >> 1] : down[i >> 1];
-            float x = i & 1 ? __high2float(p) : __low2float(p);
-            if (lane >= 16) x = -x;
-            const float y = ceilf(x * s1 * s2);
-            int c = static_cast<int>(x > 0.f ? fmaxf(y, 1.f) : y);
-            if (!fine) c = 127;
-            bytes[i] = static_cast<uint32_t>(lane < 16 ? c : -c) & 0xFF;
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                up[c] = max2(up[c], w[c]);
+                down[c] = min2(down[c], w[c]);
+            }
         }
-        const int64_t rec = (static_cast<int64_t>(l) * sh.Hkv + g) * sh.num_blocks + blk;
-        uint2 out;
-        out.x = bytes[0] | bytes[1] << 8 | bytes[2] << 16 | bytes[3] << 24;
-        out.y = bytes[4] | bytes[5] << 8 | bytes[6] << 16 | bytes[7] << 24;
-        reinterpret_cast<uint2 *>(a.codes + rec * kCodeRow)[lane] = out;
-        // The step as a bf16: 2^(E - 133), below 2^-126 by its fraction bit.
-        if (lane == 0)
-            a.steps[rec] = static_cast<uint16_t>(!fine ? kInfBits : E > 6 ? (E - 6) << 7 : 1u << E);
+        t0 += 16;
+        if (t0 < now.tokens) {
+            load(now, t0);
+            continue;
+        }
+        t0 = 0;
+        const Item done = now;
+        const bool go = more;
+        if (go) {
+            load(next, 0);
+            now = next;
+            advance();
+            more = pair < total;
+            if (more) next = find();
+        }
+        // Lanes 0-15 get their channels' largest values, the others the smallest negated.
+        const bool high = lane < 16;
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t low = down[c] ^ kNegate2;
+            const uint32_t got = __shfl_xor_sync(~0u, high ? low : up[c], 16);
+            up[c] = max2(high ? up[c] : low, got);
+            top = max(top, max(up[c] & 0x7FFFu, up[c] >> 16 & 0x7FFFu));
+        }
+        top = __reduce_max_sync(~0u, top);
+        const bool fine = top < kInfBits;
+        const int E = max(1, static_cast<int>(top >> 7)) + ((top & 0x7F) == 0x7F);
+        if (done.blk >= 0 && done.blk < sh.num_blocks) {
+            // 2^(133 - E) is up to 2^132: two factors where E is below 6, which no real key's is. A value too small for
+            // the product still counts: it rounds outwards.
+            const float scale = pow2(min(254, 260 - E)), rest = E < 6 ? pow2(133 - E) : 1.f;
+            uint32_t out[2];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float x0 = __uint_as_float(up[c] << 16), x1 = __uint_as_float(up[c] & 0xFFFF0000u);
+                if (E < 6) {
+                    x0 *= rest;
+                    x1 *= rest;
+                }
+                int y0 = max(__float2int_ru(x0 * scale), x0 > 0.f ? 1 : -127);
+                int y1 = max(__float2int_ru(x1 * scale), x1 > 0.f ? 1 : -127);
+                if (!fine) y0 = y1 = 127;
+                if (!high) {
+                    y0 = -y0;
+                    y1 = -y1;
+                }
+                const uint32_t two = __byte_perm(static_cast<uint32_t>(y0), static_cast<uint32_t>(y1), 0x0040);
+                out[c >> 1] = c & 1 ? __byte_perm(out[c >> 1], two, 0x5410) : two;
+            }
+            const int64_t rec = (static_cast<int64_t>(a.layer0 + done.l) * sh.Hkv + done.g) * sh.num_blocks + done.blk;
+            reinterpret_cast<uint2 *>(a.codes + rec * kCodeRow)[lane] = make_uint2(out[0], out[1]);
+            // The step as a bf16: 2^(E - 133), below 2^-126 by its fraction bit.
+            if (lane == 0) a.steps[rec] = static_cast<uint16_t>(!fine ? kInfBits : E > 6 ? (E - 6) << 7 : 1u << E);
+        } else if (lane == 0) {
+            atomicOr(a.err, kErrBadBlock);
+        }
+        if (!go) break;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            up[c] = kMinusInf2;
+            down[c] = kMinusInf2 ^ kNegate2;
+        }
     }
 }
 
@@ -534,8 +602,8 @@ __global__ void __launch_bounds__(kSelectThreads, kTwo ? 1 : 2) select_kernel(co
 cudaError_t launch_bounds(const BoundsArgs &a, int num_sms, cudaStream_t st) {
     const int64_t most = (static_cast<int64_t>(a.B) * a.max_blocks * a.nlayers * a.s.Hkv + kBoundsThreads / 32 - 1) /
                          (kBoundsThreads / 32);
-    const int64_t ctas = 8ll * num_sms;
-    bounds_kernel<<<static_cast<unsigned>(most < ctas ? most : ctas), kBoundsThreads, 0, st>>>(a);
+    const int64_t ctas = 4ll * num_sms;               // all resident
+    bounds_kernel<<<static_cast<unsigned>(most < ctas ? most : ctas), kBoundsThreads, a.B * 8, st>>>(a);
     return cudaGetLastError();
 }
 
