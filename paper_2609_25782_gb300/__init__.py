@@ -35,6 +35,7 @@ class Pool:
         self._select, self._sparse = kvtier.lib.select_blocks, kvtier.lib.sparse_attention
         self._bf16, self._i32, self._masks, self._index = (torch.bfloat16, torch.int32,
                                                            (torch.int64, torch.uint64), device)
+        self._f32 = torch.float32
         self._out_flags = {torch.float32: 0, torch.bfloat16: kvtier.KV_DECODE_OUT_BF16}
         probe = kvtier.make_config(num_layers=num_layers, num_q_heads=num_q_heads,
                                    num_kv_heads=num_kv_heads, head_dim=head_dim,
@@ -253,16 +254,17 @@ class Pool:
         return (bounds[:n * 2 * self.D].view(*shape, 2, self.D),
                 bounds[n * 2 * self.D:].view(torch.bfloat16).view(shape))
 
-    def _rows(self, tables, lens, B, max_blocks, *more):
-        """Block tables, lengths and other int32 tensors [B] of a call, checked."""
+    def _rows(self, tables, lens, B, max_blocks, since=None):
+        """Block tables, lengths and (or None) another int32 [B] of a call, checked."""
         i32, index = self._i32, self._index
-        ok = tables.numel() >= B * max_blocks
-        for x in (tables, lens, *more):
-            ok = ok and x.dtype is i32 and x.numel() >= B and x.is_contiguous() and x.get_device() == index
-        if not ok:
-            raise ValueError(f"need contiguous int32 block tables [{B}][{max_blocks}] and lengths [{B}] on the "
-                             f"pool's device, {self.device}, got " +
-                             ", ".join(f"{x.dtype} {tuple(x.shape)} strides {x.stride()}" for x in (tables, lens, *more)))
+        if tables.dtype is i32 and lens.dtype is i32 and tables.numel() >= B * max_blocks and lens.numel() >= B and \
+                tables.is_contiguous() and lens.is_contiguous() and tables.get_device() == index == lens.get_device() \
+                and (since is None or (since.dtype is i32 and since.numel() >= B and since.is_contiguous() and
+                                       since.get_device() == index)):
+            return
+        raise ValueError(f"need contiguous int32 block tables [{B}][{max_blocks}] and lengths [{B}] on the pool's device, "
+                         f"{self.device}, got " + ", ".join(f"{x.dtype} {tuple(x.shape)} strides {x.stride()}"
+                                                            for x in (tables, lens, since) if x is not None))
 
     def _heads(self, x, B, heads, name):
         """The row stride of bf16 [B][heads][D] with contiguous heads, checked (0: one row)."""
@@ -275,12 +277,12 @@ class Pool:
 
     def _list(self, selected, B):
         """Entries per row and head of a selection [B][Hkv][top], checked."""
-        if selected.dtype is not self._i32 or selected.dim() != 3 or selected.shape[0] != B or \
-                selected.shape[1] != self.Hkv or not selected.is_contiguous() or \
-                selected.get_device() != self._index:
+        shape = selected.shape
+        if selected.dtype is not self._i32 or len(shape) != 3 or shape[0] != B or shape[1] != self.Hkv or \
+                not selected.is_contiguous() or selected.get_device() != self._index:
             raise ValueError(f"selected must be contiguous int32 [{B}][{self.Hkv}][top] on the pool's device, "
-                             f"got {selected.dtype} {tuple(selected.shape)} strides {selected.stride()}")
-        return selected.shape[2]
+                             f"got {selected.dtype} {tuple(shape)} strides {selected.stride()}")
+        return shape[2]
 
     def _whole_bounds(self, bounds):
         if bounds.numel() * bounds.element_size() < self.bounds_bytes or not bounds.is_contiguous() or \
@@ -292,7 +294,7 @@ class Pool:
                      stream=None) -> None:
         """Bounds of the keys of the rows' blocks that hold tokens from since[b] on (all without it), of
         one layer or (-1) all."""
-        self._rows(block_tables, seq_lens, B, max_blocks, *(() if since is None else (since,)))
+        self._rows(block_tables, seq_lens, B, max_blocks, since)
         self._whole_bounds(bounds)
         kvtier.kv_pool_block_bounds(self.handle, layer, block_tables, seq_lens, since, B, max_blocks, bounds,
                                     stream)
@@ -307,7 +309,7 @@ class Pool:
         top, q_stride, at = self._list(selected, B), self._heads(q, B, self.Hq, "q"), None
         if scores is not None:
             at = scores.data_ptr()
-            if str(scores.dtype) != "torch.float32" or scores.shape != (B, self.Hkv, max_blocks) or \
+            if scores.dtype is not self._f32 or scores.shape != (B, self.Hkv, max_blocks) or \
                     not scores.is_contiguous() or scores.get_device() != self._index:
                 raise ValueError(f"scores must be contiguous fp32 [{B}][{self.Hkv}][{max_blocks}] on the pool's device")
         rc = self._select(self.handle, layer, q.data_ptr(), q_stride, bounds.data_ptr(),

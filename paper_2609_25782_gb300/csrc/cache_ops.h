@@ -64,6 +64,8 @@ struct CopyJob {
     int32_t rows;
 };
 constexpr int kCopyJobsMax = 1300;   // keeps the parameter block under 32 KB
+constexpr int kCopyJobsFew = 24;     // and a small fork's under 1 KB
+template <int kMost>
 struct CopyJobs {
     uint8_t *hot;
     int32_t *err;
@@ -73,8 +75,8 @@ struct CopyJobs {
     int32_t n;
     // Sessions whose first `shared` table entries become those of `parent` (of any launch, one does it).
     int32_t parent, shared, children;
-    CopyJob job[kCopyJobsMax];
-    int32_t child[kCopyJobsMax];
+    CopyJob job[kMost];
+    int32_t child[kMost];
 };
 
 // Rows of a session that move towards its front: token t of [t_begin, t_end) of layer l and kv-head g is the old
@@ -98,7 +100,8 @@ cudaError_t prepare_select_kernel(SelectFit *fit);
 cudaError_t launch_select(const SelectArgs &a, const SelectFit &fit, cudaStream_t st);
 cudaError_t prepare_sparse_kernels(SparseFit *fit);
 cudaError_t launch_sparse(const CUtensorMap &map, const SparseArgs &a, const SparseFit &fit, cudaStream_t st);
-cudaError_t launch_copy_jobs(const CopyJobs &a, int max_ctas, cudaStream_t st);
+template <int kMost>
+cudaError_t launch_copy_jobs(const CopyJobs<kMost> &a, int max_ctas, cudaStream_t st);
 cudaError_t launch_compact(const CompactArgs &a, int num_sms, cudaStream_t st);
 
 }  // namespace kvt

@@ -14,7 +14,8 @@ constexpr int kChunkRows = 8;        // rows that a warp moves at a time, 2 KiB
 
 // One warp per chunk of a (job, layer, K|V, kv-head) run, as migrations move them: 16 bytes a lane, four loads
 // in flight. Bound by HBM where jobs are many.
-__global__ void __launch_bounds__(kCopyThreads) copy_jobs_kernel(const __grid_constant__ CopyJobs a) {
+template <int kMost>
+__global__ void __launch_bounds__(kCopyThreads) copy_jobs_kernel(const __grid_constant__ CopyJobs<kMost> a) {
     const Shape sh = a.s;
     const int nthreads = gridDim.x * blockDim.x;
     const int thread = blockIdx.x * blockDim.x + threadIdx.x;
@@ -138,13 +139,16 @@ __global__ void __launch_bounds__(kCompactThreads, 4) compact_kernel(const __gri
 
 }  // namespace
 
-cudaError_t launch_copy_jobs(const CopyJobs &a, int max_ctas, cudaStream_t st) {
+template <int kMost>
+cudaError_t launch_copy_jobs(const CopyJobs<kMost> &a, int max_ctas, cudaStream_t st) {
     if (a.n <= 0 && (a.shared <= 0 || a.children <= 0)) return cudaSuccess;
     const int64_t items = static_cast<int64_t>(a.n) * a.s.L * 2 * a.s.Hkv * (a.s.bt / kChunkRows);
     const int64_t entries = (a.shared + 31) / 32;
-    copy_jobs_kernel<<<item_grid(items > entries ? items : entries, max_ctas), kCopyThreads, 0, st>>>(a);
+    copy_jobs_kernel<kMost><<<item_grid(items > entries ? items : entries, max_ctas), kCopyThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
+template cudaError_t launch_copy_jobs(const CopyJobs<kCopyJobsFew> &, int, cudaStream_t);
+template cudaError_t launch_copy_jobs(const CopyJobs<kCopyJobsMax> &, int, cudaStream_t);
 
 template <int kSplit>
 static void start_compact(const CompactArgs &a, cudaStream_t st) {

@@ -33,12 +33,13 @@ int mark_moved(kv_pool *p, Session &s, cudaStream_t st) {
 }
 
 // Copies of blocks and the children's first table entries, as many launches as their parameters take.
-int run_copies(kv_pool *p, const std::vector<kvt::CopyJob> &jobs, int32_t parent, int32_t shared,
-               const std::vector<int32_t> &children, cudaStream_t st) {
+template <int kMost>
+int run_copies_by(kv_pool *p, const std::vector<kvt::CopyJob> &jobs, int32_t parent, int32_t shared,
+                  const std::vector<int32_t> &children, cudaStream_t st) {
     size_t j = 0, c = 0;
     const size_t nc = shared > 0 ? children.size() : 0;
     while (j < jobs.size() || c < nc) {
-        kvt::CopyJobs a;
+        kvt::CopyJobs<kMost> a;
         a.hot = static_cast<uint8_t *>(p->cfg.hot_base);
         a.err = p->d_err;
         a.tables = p->d_tables;
@@ -46,8 +47,8 @@ int run_copies(kv_pool *p, const std::vector<kvt::CopyJob> &jobs, int32_t parent
         a.s = p->shape;
         a.parent = parent;
         a.shared = shared;
-        a.n = static_cast<int32_t>(std::min<size_t>(kvt::kCopyJobsMax, jobs.size() - j));
-        a.children = static_cast<int32_t>(std::min<size_t>(kvt::kCopyJobsMax, nc - c));
+        a.n = static_cast<int32_t>(std::min<size_t>(kMost, jobs.size() - j));
+        a.children = static_cast<int32_t>(std::min<size_t>(kMost, nc - c));
         std::copy(jobs.begin() + j, jobs.begin() + j + a.n, a.job);
         std::copy(children.begin() + c, children.begin() + c + a.children, a.child);
         int rc = p->cuda("block copy launch", [&] { return kvt::launch_copy_jobs(a, p->move_ctas(st), st); });
@@ -56,6 +57,12 @@ int run_copies(kv_pool *p, const std::vector<kvt::CopyJob> &jobs, int32_t parent
         c += a.children;
     }
     return KV_OK;
+}
+int run_copies(kv_pool *p, const std::vector<kvt::CopyJob> &jobs, int32_t parent, int32_t shared,
+               const std::vector<int32_t> &children, cudaStream_t st) {
+    return std::max(jobs.size(), children.size()) <= kvt::kCopyJobsFew
+               ? run_copies_by<kvt::kCopyJobsFew>(p, jobs, parent, shared, children, st)
+               : run_copies_by<kvt::kCopyJobsMax>(p, jobs, parent, shared, children, st);
 }
 
 // `need` blocks that a simple pool's free list gives, in the order of their pops.

@@ -44,14 +44,17 @@ __device__ __forceinline__ uint32_t min2(uint32_t x, uint32_t y) {
 }
 
 constexpr int kBoundsThreads = 256;
+// CTAs per SM, each warp with 4 KiB on its way. us by 2, 3, 4, 5 and 6 of them, 48 layers, three sessions of 8K to 24K
+// tokens: 287, 285, 312, 530, 852 (of 64-token blocks 262, 263, 279, 352, 512); one of 2 100 22.6, 21.9, 23.1, 34.9, 54.5.
+constexpr int kBoundsPerSm = 3;
 constexpr uint32_t kNegate2 = 0x80008000u, kMinusInf2 = 0xFF80FF80u;
 
 // A warp per (block, layer, kv-head) in turn: the rows' block counts are summed up by every CTA first, so that the
 // items are one line whatever the lengths. 16 tokens at a time; the next ones are on their way while an item's codes
 // are made, and the item after that is looked up. Warps next to each other have items next to each other: in runs of
-// items, each warp at another block of 1.5 MiB, the call took 1.1 times as long. Bound by HBM, with the instructions
-// close behind (a first form spent 1 500 on an item of 4 KiB, and was bound by them at 2.4 TB/s).
-__global__ void __launch_bounds__(kBoundsThreads, 4) bounds_kernel(const BoundsArgs a) {
+// items, each warp at another block of 1.5 MiB, the call took 1.1 times as long. Bound by HBM: 6.6 TB/s over three
+// sessions of 8K to 24K tokens.
+__global__ void __launch_bounds__(kBoundsThreads, kBoundsPerSm) bounds_kernel(const BoundsArgs a) {
     extern __shared__ int rows_smem[];               // [B] ends: items' blocks up to the row's; [B] its first block less those before
     __shared__ int sums[kBoundsThreads / 32];
     int *ends = rows_smem, *shift = rows_smem + a.B;
@@ -602,7 +605,7 @@ __global__ void __launch_bounds__(kSelectThreads, kTwo ? 1 : 2) select_kernel(co
 cudaError_t launch_bounds(const BoundsArgs &a, int num_sms, cudaStream_t st) {
     const int64_t most = (static_cast<int64_t>(a.B) * a.max_blocks * a.nlayers * a.s.Hkv + kBoundsThreads / 32 - 1) /
                          (kBoundsThreads / 32);
-    const int64_t ctas = 4ll * num_sms;               // all resident
+    const int64_t ctas = static_cast<int64_t>(kBoundsPerSm) * num_sms;   // all resident
     bounds_kernel<<<static_cast<unsigned>(most < ctas ? most : ctas), kBoundsThreads, a.B * 8, st>>>(a);
     return cudaGetLastError();
 }

@@ -19,7 +19,7 @@ def make_pool(package, hq=8, hkv=2, layers=3, blocks=5):
     """A pool without arenas or a handle, and library calls that only note their arguments."""
     p = package.Pool.__new__(package.Pool)
     p.device, p.handle, p.Hq, p.Hkv, p.D, p.L, p.bt, p.num_hot_blocks = torch.device("cpu"), None, hq, hkv, D, layers, 16, blocks
-    p._bf16, p._i32 = BF, torch.int32
+    p._bf16, p._i32, p._f32 = BF, torch.int32, torch.float32
     p._out_flags = {torch.float32: 0, BF: package.kvtier.KV_DECODE_OUT_BF16}
     p._index = -1
     p.bounds_bytes = layers * hkv * blocks * (2 * D + 2)
