@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 8 ? 1 : 3)
     const int C = gridDim.x, rank = blockIdx.x, g = blockIdx.y, b = blockIdx.z;   // a row of the grid is a cluster
     const int G = a.group;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    after_previous();
     const int T = a.seq_lens[b];
     const int32_t *trow = a.tables + static_cast<int64_t>(b) * a.max_blocks;
     const int32_t *list = a.selected + (static_cast<int64_t>(b) * sh.Hkv + g) * a.top;
@@ -242,6 +243,7 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 8 ? 1 : 3)
         issue();
     }
 
+    next_may_come();
     // States into the warp's own ring, which no copy writes any more.
     {
 #pragma unroll

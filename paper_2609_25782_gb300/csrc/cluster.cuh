@@ -9,6 +9,10 @@
 namespace kvt {
 namespace {
 
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The kernel that comes next may be scheduled (it waits all the same for this one's end).
+__device__ __forceinline__ void next_may_come() { asm volatile("griddepcontrol.launch_dependents;"); }
+
 __device__ __forceinline__ void cluster_arrive() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
@@ -21,12 +25,14 @@ __device__ __forceinline__ uint32_t remote(uint32_t addr, uint32_t rank) {
     return r;
 }
 
-// A grid of (cluster, y, z) blocks, each row of it a cluster.
+// A grid of (cluster, y, z) blocks, each row of it a cluster. It is a programmatic dependent of the kernel before it on
+// the stream: its blocks may be there when that one ends, and every thread waits for its end (after_previous) before it
+// reads or writes anything.
 template <typename... Args>
 cudaError_t launch_clusters(void (*kernel)(Args...), int cluster, int y, int z, int threads, int smem, cudaStream_t st,
                             const Args &...args) {
     cudaLaunchConfig_t c{};
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     c.gridDim = dim3(cluster, y, z);
     c.blockDim = dim3(threads);
     c.dynamicSmemBytes = smem;
@@ -34,8 +40,10 @@ cudaError_t launch_clusters(void (*kernel)(Args...), int cluster, int y, int z, 
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = cluster;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     c.attrs = at;
-    c.numAttrs = 1;
+    c.numAttrs = 2;
     return cudaLaunchKernelEx(&c, kernel, args...);
 }
 

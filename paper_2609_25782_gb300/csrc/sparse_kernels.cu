@@ -298,6 +298,7 @@ __global__ void __launch_bounds__(kSelectThreads, kTwo ? 1 : 2) select_kernel(co
     const Shape sh = a.s;
     const int C = gridDim.x, rank = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    after_previous();
     const int T = a.seq_lens[b];
     // The warp's blocks are j .. j + 15, then those `jump` on; lanes look up their places, the first ones before
     // T is known (entries past a row's end are not used).
@@ -469,6 +470,7 @@ __global__ void __launch_bounds__(kSelectThreads, kTwo ? 1 : 2) select_kernel(co
             blk1 = block_of(j + 3 * static_cast<int64_t>(jump));
         }
     }
+    next_may_come();
     low = __reduce_min_sync(~0u, low);
     high = __reduce_max_sync(~0u, high);
     if (lane == 0 && low <= high) {

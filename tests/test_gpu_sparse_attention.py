@@ -260,3 +260,52 @@ def test_infinite_keys_and_values(cuda_dev):
     c.hot[blk[9], 0, 0, 0, 2, 7] = float("inf")
     c.attend()
     assert c.out.isnan().all() and c.pool.check_device() == 0
+
+
+def test_a_captured_step_behind_copies_and_two_streams(cuda_dev):
+    """What a step waits for: a copy, kernels of two streams that meet, the step before it."""
+    c = Cache([900, 333, 90], seed=18)
+    c.make_bounds()
+    c.selected = torch.zeros(3, 4, 12, dtype=torch.int32, device="cuda")
+    qs = [torch.randn_like(c.q.float()).bfloat16() for _ in range(2)]
+    source, big = qs[0].clone(), torch.zeros(64 << 20, device="cuda")
+    side = torch.cuda.Stream()
+
+    def step():
+        st = torch.cuda.current_stream()
+        side.wait_stream(st)
+        with torch.cuda.stream(side):                    # slow, and q comes from it
+            big.add_(1)
+            c.q.copy_(source)
+        big2 = big[:1 << 20] * 2
+        st.wait_stream(side)
+        c.pool.select_blocks(0, c.q, c.bounds, c.tables, c.lens, 3, c.width, c.selected, stream=st)
+        c.pool.sparse_attention(0, c.q, c.selected, c.tables, c.lens, 3, c.width, c.scale, c.out, stream=st)
+        c.q.copy_(-source)                               # the next step's begins with other values
+        c.pool.select_blocks(0, c.q, c.bounds, c.tables, c.lens, 3, c.width, c.selected, stream=st)
+        c.pool.sparse_attention(0, c.q, c.selected, c.tables, c.lens, 3, c.width, c.scale, c.out, stream=st)
+        return big2
+
+    first = torch.cuda.Stream()
+    with torch.cuda.stream(first):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=first):
+        step()
+    for q in qs:
+        source.copy_(q)
+        for replay in (False, True):
+            c.out.fill_(7.0)
+            if replay:
+                graph.replay()
+            else:
+                torch.cuda.synchronize()
+                with torch.cuda.stream(first):
+                    step()
+            torch.cuda.synchronize()
+            for b in range(3):
+                for g in range(4):
+                    assert c.selected[b, g].tolist() == c.reference_selection(b, g, 12)[0]
+                c.assert_right(b, *c.reference(b))
+    assert c.pool.check_device() == 0
