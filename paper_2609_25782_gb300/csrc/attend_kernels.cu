@@ -355,8 +355,8 @@ cudaError_t launch_sparse(const CUtensorMap &map, const SparseArgs &a, const Spa
     int log = 4;
     while (log > 0 && (units > fit.clusters[1][log] || tiles < 8 << log)) --log;
     const bool wide = units <= fit.clusters[1][0];
-    return wide ? launch_clusters(sparse_kernel<8, 3>, 1 << log, a.s.Hkv, a.B, 8 * 32, Layout<8, 3>::kBytes, st, map, a)
-                : launch_clusters(sparse_kernel<4, 2>, 1, a.s.Hkv, a.B, 4 * 32, Layout<4, 2>::kBytes, st, map, a);
+    return wide ? launch_behind(sparse_kernel<8, 3>, dim3(1 << log, a.s.Hkv, a.B), 1 << log, 8 * 32, Layout<8, 3>::kBytes, st, map, a)
+                : launch_behind(sparse_kernel<4, 2>, dim3(1, a.s.Hkv, a.B), 1, 4 * 32, Layout<4, 2>::kBytes, st, map, a);
 }
 
 }  // namespace kvt

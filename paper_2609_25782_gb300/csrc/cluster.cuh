@@ -1,5 +1,5 @@
-// Clusters of thread blocks: their barrier, their blocks' shared memory, and launches (attend_kernels.cu,
-// sparse_kernels.cu).
+// Clusters of thread blocks: their barrier, their blocks' shared memory, and launches behind the kernel before
+// (attend_kernels.cu, sparse_kernels.cu).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -25,25 +25,25 @@ __device__ __forceinline__ uint32_t remote(uint32_t addr, uint32_t rank) {
     return r;
 }
 
-// A grid of (cluster, y, z) blocks, each row of it a cluster. It is a programmatic dependent of the kernel before it on
-// the stream: its blocks may be there when that one ends, and every thread waits for its end (after_previous) before it
-// reads or writes anything.
+// A launch as a programmatic dependent of the kernel before it on the stream: its blocks may be there when that one
+// ends, and every thread waits for its end (after_previous) before it reads or writes anything. cluster > 0: each row
+// of the grid, of `cluster` blocks, is a cluster.
 template <typename... Args>
-cudaError_t launch_clusters(void (*kernel)(Args...), int cluster, int y, int z, int threads, int smem, cudaStream_t st,
-                            const Args &...args) {
+cudaError_t launch_behind(void (*kernel)(Args...), dim3 grid, int cluster, int threads, int smem, cudaStream_t st,
+                          const Args &...args) {
     cudaLaunchConfig_t c{};
     cudaLaunchAttribute at[2];
-    c.gridDim = dim3(cluster, y, z);
+    c.gridDim = grid;
     c.blockDim = dim3(threads);
     c.dynamicSmemBytes = smem;
     c.stream = st;
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = cluster;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     c.attrs = at;
-    c.numAttrs = 2;
+    c.numAttrs = cluster > 0 ? 2 : 1;
     return cudaLaunchKernelEx(&c, kernel, args...);
 }
 

@@ -60,6 +60,7 @@ __global__ void __launch_bounds__(kBoundsThreads, kBoundsPerSm) bounds_kernel(co
     int *ends = rows_smem, *shift = rows_smem + a.B;
     const Shape sh = a.s;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    after_previous();
     int total = 0;
     for (int b0 = 0; b0 < a.B; b0 += kBoundsThreads) {
         const int b = b0 + threadIdx.x;
@@ -280,9 +281,17 @@ __device__ __noinline__ uint32_t scan_before(uint32_t x, uint32_t *scratch) {
 
 // Codes of the warp's 16 blocks, those of block `row` and of `row` + 8 (mma fragments), and a block's step per lane.
 struct Fetched {
-    uint4 x[4], y[4];
+    uint32_t x[16], y[16];
     uint32_t step;
 };
+
+// 32 bytes at once: four lanes then read a whole 128-byte line of a record.
+__device__ __forceinline__ void load_32(const int8_t *p, uint32_t *v) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "l"(p)
+                 : "memory");
+}
 
 // kTwo: CTAs that have an SM each keep two fetches per warp on their way, 128 KiB in all; others one, two CTAs per SM.
 template <bool kTwo>
@@ -347,13 +356,12 @@ __global__ void __launch_bounds__(kSelectThreads, kTwo ? 1 : 2) select_kernel(co
             blk = 0;
         }
         f.step = steps[blk];
-        const uint4 *px = reinterpret_cast<const uint4 *>(codes + static_cast<int64_t>(__shfl_sync(~0u, blk, row)) * kCodeRow) + quad;
-        const uint4 *py = reinterpret_cast<const uint4 *>(codes + static_cast<int64_t>(__shfl_sync(~0u, blk, row + 8)) * kCodeRow) + quad;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            f.x[c] = px[4 * c];
-            f.y[c] = py[4 * c];
-        }
+        const int8_t *px = codes + static_cast<int64_t>(__shfl_sync(~0u, blk, row)) * kCodeRow + 32 * quad;
+        const int8_t *py = codes + static_cast<int64_t>(__shfl_sync(~0u, blk, row + 8)) * kCodeRow + 32 * quad;
+        load_32(px, f.x);
+        load_32(py, f.y);
+        load_32(px + 128, f.x + 8);
+        load_32(py + 128, f.y + 8);
     };
     Fetched f0, f1;
     if (j < end) fetch(f0, j, blk0);
@@ -406,34 +414,32 @@ __global__ void __launch_bounds__(kSelectThreads, kTwo ? 1 : 2) select_kernel(co
     }
     __syncthreads();
     // B fragments: columns 0 to 2 are the digits, the others any. The order of the dims within a product is the
-    // loads': piece c of lane t (of four) is the record's 16 bytes t + 4 c.
-    const uint4 *weights = reinterpret_cast<const uint4 *>(digits + min(row, kDigits - 1) * kDigitRow) + 2 * quad;
+    // loads': piece c of lane t (of four) is the record's 32 bytes t + 4 c.
+    const uint4 *weights = reinterpret_cast<const uint4 *>(digits + min(row, kDigits - 1) * kDigitRow) + 4 * quad;
     const uint32_t offset = static_cast<uint32_t>(kCodeOffset * qtotal);
     if (C > 1) cluster_wait();
     const uint32_t keys_at = remote(smem_u32(keys), 0);
     uint32_t low = ~0u, high = 0;
     auto score = [&](const Fetched &f, int at) {
-        // 128 products of up to 1279 x 16 a sum: whole numbers below 2^24, exact in fp32.
-        float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};
+        // 64 products of up to 1279 x 16 a sum: whole numbers below 2^24, exact in fp32.
+        float d[4][4] = {};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const uint4 w0 = weights[8 * c], w1 = weights[8 * c + 1];
-            uint2 p = halves(f.x[c].x), o = halves(f.y[c].x);
-            mma_f16(d0, p.x, o.x, p.y, o.y, w0.x, w0.y);
-            p = halves(f.x[c].y), o = halves(f.y[c].y);
-            mma_f16(d1, p.x, o.x, p.y, o.y, w0.z, w0.w);
-            p = halves(f.x[c].z), o = halves(f.y[c].z);
-            mma_f16(d0, p.x, o.x, p.y, o.y, w1.x, w1.y);
-            p = halves(f.x[c].w), o = halves(f.y[c].w);
-            mma_f16(d1, p.x, o.x, p.y, o.y, w1.z, w1.w);
-        }
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint4 w = weights[16 * c + i];
+                uint2 p = halves(f.x[8 * c + 2 * i]), o = halves(f.y[8 * c + 2 * i]);
+                mma_f16(d[2 * (i & 1)], p.x, o.x, p.y, o.y, w.x, w.y);
+                p = halves(f.x[8 * c + 2 * i + 1]), o = halves(f.y[8 * c + 2 * i + 1]);
+                mma_f16(d[2 * (i & 1) + 1], p.x, o.x, p.y, o.y, w.z, w.w);
+            }
+        auto whole = [&](int i) { return static_cast<uint32_t>(__float2int_rn((d[0][i] + d[1][i]) + (d[2][i] + d[3][i]))); };
         // Lanes of quad 0 have the first two digits' sums, of quad 1 the last one's, each for blocks row and row + 8:
         // quad 0 keeps row. (Whole numbers modulo 2^32; the score's fits 32 bits.)
-        auto whole = [](float x, float y) { return static_cast<uint32_t>(__float2int_rn(x) + __float2int_rn(y)); };
-        uint32_t mine = whole(d0[0], d1[0]), other = whole(d0[2], d1[2]);
+        uint32_t mine = whole(0), other = whole(2);
         if (quad == 0) {
-            mine = mine * 1024 + whole(d0[1], d1[1]) * 32;
-            other = other * 1024 + whole(d0[3], d1[3]) * 32;
+            mine = mine * 1024 + whole(1) * 32;
+            other = other * 1024 + whole(3) * 32;
         }
         const uint32_t got = __shfl_xor_sync(~0u, quad == 0 ? other : mine, 1);
         const int sum = static_cast<int>((quad == 0 ? mine : other) + got - offset);
@@ -608,8 +614,7 @@ cudaError_t launch_bounds(const BoundsArgs &a, int num_sms, cudaStream_t st) {
     const int64_t most = (static_cast<int64_t>(a.B) * a.max_blocks * a.nlayers * a.s.Hkv + kBoundsThreads / 32 - 1) /
                          (kBoundsThreads / 32);
     const int64_t ctas = static_cast<int64_t>(kBoundsPerSm) * num_sms;   // all resident
-    bounds_kernel<<<static_cast<unsigned>(most < ctas ? most : ctas), kBoundsThreads, a.B * 8, st>>>(a);
-    return cudaGetLastError();
+    return launch_behind(bounds_kernel, dim3(static_cast<unsigned>(most < ctas ? most : ctas)), 0, kBoundsThreads, a.B * 8, st, a);
 }
 
 cudaError_t prepare_select_kernel(SelectFit *fit) {
@@ -628,13 +633,13 @@ cudaError_t launch_select(const SelectArgs &a, const SelectFit &fit, cudaStream_
     const int64_t units = static_cast<int64_t>(a.B) * a.s.Hkv;
     int two = 1, log = 4;
     while (log > 0 && (units > fit.clusters[1][log] || a.max_blocks < 64 << log)) --log;
-    if (log == 0 && units > fit.clusters[1][0] / 2 && a.max_blocks >= 128) {
+    if (log == 0 && units > fit.clusters[1][0] / 2) {
         two = 0;
         log = 4;
         while (log > 0 && (units > fit.clusters[0][log] || a.max_blocks < 64 << log)) --log;
     }
-    return launch_clusters(two ? select_kernel<true> : select_kernel<false>, 1 << log, a.s.Hkv, a.B, kSelectThreads,
-                           select_smem(a.max_blocks), st, a);
+    return launch_behind(two ? select_kernel<true> : select_kernel<false>, dim3(1 << log, a.s.Hkv, a.B), 1 << log,
+                         kSelectThreads, select_smem(a.max_blocks), st, a);
 }
 
 }  // namespace kvt
