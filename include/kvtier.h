@@ -447,7 +447,9 @@ int select_blocks(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride,
  * sets KV_DEVICE_BAD_LENGTH and the row is not written; a listed block at or past the row's
  * end, or a block id out of range, sets KV_DEVICE_BAD_BLOCK and is skipped; a wait
  * inside the kernel that runs out (2 s) sets KV_DEVICE_TIMEOUT, the row is then wrong.
- * No workspace: calls on several streams may overlap. */
+ * No workspace: calls on several streams may overlap. Bounds, selections and this call are
+ * programmatic dependents of the kernel before them: they start while it ends, and wait for its
+ * end before they read anything. */
 int sparse_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride, const void *k_new,
                      const void *v_new, int64_t kv_stride, const int32_t *selected, int32_t top,
                      const int32_t *block_tables, const int32_t *seq_lens, int32_t B, int32_t max_blocks,
@@ -653,7 +655,8 @@ int kv_pool_inject_cuda_failure(kv_pool *pool, int32_t n);
 /* Test hook for the attention kernels' bounded waits: with on != 0, the next
  * decode call makes warp 0 of one CTA (split 0, kv-head 0, first row) expect
  * 16 bytes more than its first tile copy delivers; if prefill_attention or
- * tree_attention comes next, its first CTA does, for its first key tile. Every
+ * tree_attention comes next, its first CTA does, for its first key tile, and
+ * the first warp's first tile of sparse_attention, for the first row's kv-head 0. Every
  * copy still lands; that one wait runs out after its 2 s limit, the kernel sets
  * KV_DEVICE_TIMEOUT, waits (bounded) for the other copies and finishes. That
  * call's output for the rows concerned is undefined; the CUDA context stays

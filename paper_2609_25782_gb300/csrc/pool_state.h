@@ -29,6 +29,8 @@ struct Session {
     uint64_t last_use = 0;            // residency mode: recency stamp
     cudaEvent_t ready = nullptr;
     bool ready_recorded = false;
+    bool moved = false;               // `ready` marks a move of the session's rows (pages.cpp): who records it again
+                                      // waits for it first
     cudaEvent_t appended = nullptr;
     bool appended_recorded = false;
     cudaEvent_t packed = nullptr;     // residency mode: after the last eviction that wrote

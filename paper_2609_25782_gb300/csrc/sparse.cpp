@@ -139,7 +139,8 @@ int sparse_attention(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     rc = check_stride(&q_stride, static_cast<int64_t>(p->cfg.num_q_heads) * kvt::kHeadDim);
     if (!rc) rc = check_stride(&kv_stride, static_cast<int64_t>(p->cfg.num_kv_heads) * kvt::kHeadDim);
     if (rc) return rc;
-    if (!(scale == scale) || std::isinf(scale)) return fail(KV_ERR_INVALID_ARG, "scale not finite");
+    const float scale_log2 = scale * 1.4426950408889634f;
+    if (!std::isfinite(scale_log2)) return fail(KV_ERR_INVALID_ARG, "scale not finite, or above 2^127");
     if (p->host_only) return fail(KV_ERR_BAD_STATE, "attention on a host-logic-only pool");
     DeviceGuard dg(p->cfg.device, true);
     if (!p->sparse_ready) {
@@ -165,7 +166,7 @@ int sparse_attention(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     a.top = top;
     a.group = p->cfg.num_q_heads / p->cfg.num_kv_heads;
     a.out_bf16 = (flags & KV_DECODE_OUT_BF16) ? 1 : 0;
-    a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale_log2 = scale_log2;
     a.inject_extra_tx = p->inject_timeout ? 16 : 0;
     a.s = p->shape;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

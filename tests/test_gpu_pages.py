@@ -326,6 +326,32 @@ def test_other_streams_wait(cuda_dev, lru):
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("call", ["resume", "tables"])
+def test_residency_mode_still_waits_after_a_resume(cuda_dev, call):
+    """A compaction behind a spin; the session is paused and resumed on another stream (or has a block fetched
+    there), and then grows: its ready event still covers the compaction."""
+    m = Model(30, lru=True, seed=9)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    p, o = m.create(300), m.create(50)                   # 19 and 4 blocks
+    keep = m.lists(p, 120, 60, seed=1)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(a):
+        torch.cuda._sleep(20_000_000)
+    m.compact(p, keep, 60, stream=a)
+    if call == "resume":
+        m.pool.session_pause(p)
+        m.pool.session_resume(p, b)
+    else:
+        m.pool.prefetch([p], (), b)
+    x = m.tokens(40)
+    k, v = (x[:, i].transpose(1, 2).contiguous() for i in (0, 1))
+    b.wait_stream(torch.cuda.current_stream())
+    m.pool.session_append(p, k, v, b)
+    m.want[p] = torch.cat([m.want[p], x], 3)
+    torch.cuda.synchronize()
+    m.check(p, o)
+
+
 def test_random_calls(cuda_dev):
     import random
     from paper_2609_25782_gb300 import KVError, kvtier

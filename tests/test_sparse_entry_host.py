@@ -177,7 +177,7 @@ def test_what_the_library_refuses(package):
     for want, change in ((state, {}), (state, dict(k=None, v=None)), (state, dict(scale=-2.0)), (bad, dict(k=None)),
                          (bad, dict(v=None)), (bad, dict(q=8)), (bad, dict(k=8)), (bad, dict(out=8)), (bad, dict(out=None)),
                          (bad, dict(selected=None)), (bad, dict(top=0)), (bad, dict(kv_stride=4)), (bad, dict(kv_stride=128)),
-                         (bad, dict(scale=float("nan"))), (bad, dict(scale=float("inf"))), (bad, dict(flags=1)),
+                         (bad, dict(scale=float("nan"))), (bad, dict(scale=float("inf"))), (bad, dict(scale=-3e38)), (bad, dict(flags=1)),
                          (bad, dict(flags=4)), (bad, dict(layer=-1)), (bad, dict(width=0)), (bad, dict(B=0))):
         a = dict(good, **change)
         assert code(kv.sparse_attention, pool, *(a[x] for x in ("layer", "q", "q_stride", "k", "v", "kv_stride", "selected",
