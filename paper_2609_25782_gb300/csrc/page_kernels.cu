@@ -56,34 +56,36 @@ __global__ void __launch_bounds__(kCopyThreads) copy_jobs_kernel(const __grid_co
     }
 }
 
-// A CTA per (layer, K|V, kv-head) run and column of its rows, 256 / kSplit bytes wide, takes the tokens in chunks, in
-// ascending order. Lists ascend, so token t comes from a row at or behind t: a chunk's stores only overwrite rows
+// A CTA per (layer, kv-head) and column of its rows, 256 / kSplit bytes wide, takes the tokens in chunks, in ascending
+// order, K and V together (a list's positions and their blocks are looked up once; each alone took 79 us where both
+// take 65). Lists ascend, so token t comes from a row at or behind t: a chunk's stores only overwrite rows
 // that no later chunk reads, and a barrier keeps them behind the loads of all chunks up to it. A chunk's positions,
 // their blocks and their rows are each loaded while the chunk before is at the next of these steps.
 constexpr int kCompactThreads = 256;
+constexpr int kCompactPerSm = 3;
 constexpr int kCompactDeep = 4;                      // rows of a thread in a chunk
 
 template <int kSplit>
-__global__ void __launch_bounds__(kCompactThreads, 4) compact_kernel(const __grid_constant__ CompactArgs a) {
+__global__ void __launch_bounds__(kCompactThreads, kCompactPerSm) compact_kernel(const __grid_constant__ CompactArgs a) {
     constexpr int kUnits = kRowBytes / 16 / kSplit;  // threads of a row, 16 bytes each
     constexpr int kRows = kCompactThreads / kUnits;
     constexpr int kChunk = kRows * kCompactDeep;
     const Shape sh = a.s;
-    const int run = blockIdx.x / kSplit;             // (l * 2 + kv) * Hkv + g
-    const int runs = sh.L * 2 * sh.Hkv;
-    const int g = run % sh.Hkv;
-    const int l = run / (2 * sh.Hkv);
+    const int unit = blockIdx.x / kSplit;            // l * Hkv + g
+    const int g = unit % sh.Hkv, l = unit / sh.Hkv;
+    const int runs = sh.L * 2 * sh.Hkv, run = l * 2 * sh.Hkv + g;   // of K
     const int32_t *keep = a.keep + l * a.layer_stride + g * a.head_stride;
     const int u = (blockIdx.x % kSplit) * kUnits + threadIdx.x % kUnits;   // 16-byte unit of a row
     const int r0 = threadIdx.x / kUnits;
     const int shift = sh.bt == 16 ? 4 : 6;
     uint4 *base = reinterpret_cast<uint4 *>(a.hot) + u;
+    const int64_t values = static_cast<int64_t>(sh.Hkv) << shift << 4;     // from a K row to its V row, in 16 bytes
     auto at = [&](int blk, int t) {                  // the pool has fewer than 2^31 rows
         return base + static_cast<int64_t>(((blk * runs + run) << shift) + (t & (sh.bt - 1))) * (kRowBytes / 16);
     };
     int from[kCompactDeep], before[kCompactDeep];    // positions of the next chunk, and those they have to exceed
     int src[kCompactDeep], dst[kCompactDeep];        // blocks
-    uint4 v[kCompactDeep];
+    uint4 v[kCompactDeep][2];
     uint4 *to[kCompactDeep];                         // places of the chunk that was loaded, or null
     // (Nothing here waits for a value that is loaded: the loads are all on their way before the first is used.)
     auto positions = [&](int t0) {
@@ -122,7 +124,10 @@ __global__ void __launch_bounds__(kCompactThreads, 4) compact_kernel(const __gri
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kCompactDeep; ++k)
-            if (to[k] != nullptr) *to[k] = v[k];
+            if (to[k] != nullptr) {
+                *to[k] = v[k][0];
+                to[k][values] = v[k][1];
+            }
         if (t0 >= a.t_end) return;
         bad = false;
 #pragma unroll
@@ -131,7 +136,11 @@ __global__ void __launch_bounds__(kCompactThreads, 4) compact_kernel(const __gri
             bad |= ok[k] && !in;
             ok[k] = ok[k] && in;
             to[k] = ok[k] ? at(dst[k], t0 + k * kRows + r0) : nullptr;
-            if (ok[k]) v[k] = *at(src[k], row[k]);
+            if (ok[k]) {
+                const uint4 *x = at(src[k], row[k]);
+                v[k][0] = *x;
+                v[k][1] = x[values];
+            }
         }
         if (bad && u == 0) atomicOr(a.err, kErrBadBlock);
     }
@@ -152,19 +161,20 @@ template cudaError_t launch_copy_jobs(const CopyJobs<kCopyJobsMax> &, int, cudaS
 
 template <int kSplit>
 static void start_compact(const CompactArgs &a, cudaStream_t st) {
-    compact_kernel<kSplit><<<a.s.L * 2 * a.s.Hkv * kSplit, kCompactThreads, 0, st>>>(a);
+    compact_kernel<kSplit><<<a.s.L * a.s.Hkv * kSplit, kCompactThreads, 0, st>>>(a);
 }
 
 cudaError_t launch_compact(const CompactArgs &a, int num_sms, cudaStream_t st) {
     if (a.t_end <= a.t_begin) return cudaSuccess;
-    // Narrower columns where there are few runs, for the latency of a chunk. us by columns 1, 2, 4 and 8: 384 runs of
-    // 2 040 tokens out of 8 200 79, 83, 76, 85; 256 runs (64-token blocks, one of three calls) 39.6, 29.7, 31.6, 36.1;
-    // 224 runs of 14 000 out of 24 000 434, 300, 314, 315; 32 runs of 2 700 out of 9 000 41.5, 21.7, 13.5, 12.2.
-    const int64_t runs = static_cast<int64_t>(a.s.L) * 2 * a.s.Hkv, want = 5ll * num_sms / 2;
-    if (runs >= want) start_compact<1>(a, st);
-    else if (runs * 2 >= want) start_compact<2>(a, st);
-    else if (runs * 4 >= want) start_compact<4>(a, st);
-    else start_compact<8>(a, st);
+    // The narrowest columns whose CTAs are all resident: one chunk after another is a chain. us by columns 1, 2, 4 and 8:
+    // 192 units (48 layers, 4 heads), 2 040 tokens kept of 8 200: -, 65, 68, 85; 128 units (64-token blocks, one of three
+    // calls) 47, 30, 33, 34; 112 units, 14 000 of 24 000: 529, 315, 249, 298; 64 units, 8 100 of 9 000: 264, 158, 104,
+    // 124; 16 units, 2 700 of 9 000: 63, 29, 17, 12.
+    const int64_t units = static_cast<int64_t>(a.s.L) * a.s.Hkv, fit = static_cast<int64_t>(kCompactPerSm) * num_sms;
+    if (units * 8 <= fit) start_compact<8>(a, st);
+    else if (units * 4 <= fit) start_compact<4>(a, st);
+    else if (units * 2 <= fit) start_compact<2>(a, st);
+    else start_compact<1>(a, st);
     return cudaGetLastError();
 }
 
