@@ -384,7 +384,8 @@ int64_t kv_bounds_bytes(const kv_pool_config *cfg);
  *   codes 127 and -127.
  * A block's bounds go by its physical id, so forks share them with the blocks.
  * They stay as they are until the call is made again: after tokens were
- * written, blocks came back (resume) or a session was compacted, it is due for
+ * written, blocks came back (a resume; in residency mode any call that fetches,
+ * kv_pool_stats.batch_blocks_fetched) or a session was compacted, it is due for
  * those blocks, unless select_blocks is told to take them anyway (first, last).
  *   block_tables device int32 [B][max_blocks]
  *   seq_lens     device int32 [B], 0 (nothing) .. max_blocks * bt (and 2^31 - 513)
@@ -493,7 +494,7 @@ int session_truncate(kv_pool *pool, int32_t sid, int64_t tokens, kv_stream_t str
  * session_truncate, shared blocks are replaced by new ones (free-list pops in
  * logical order). Of the image only the tokens before prefix stay valid: later
  * ones are written again by the next pause. In residency mode evicted blocks are
- * fetched back first. n = T - prefix keeps everything and moves nothing.
+ * fetched back first (and stay, should a later step of the call fail). n = T - prefix keeps everything and moves nothing.
  * A position out of range, or not above the one before it, sets KV_DEVICE_BAD_INDEX; that
  * layer and head's rows from there on are then undefined. Waits and ordering as session_truncate. Errors:
  * KV_ERR_BAD_STATE (paused), KV_ERR_NO_HOT_BLOCKS. */

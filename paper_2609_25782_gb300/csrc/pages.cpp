@@ -257,7 +257,7 @@ int session_compact(kv_pool *p, int32_t sid, const int32_t *keep, int64_t layer_
     Session *s = p->session(sid);
     if (!s) return fail(KV_ERR_INVALID_ARG, "no such session");
     if (s->state != KV_SESSION_ACTIVE) return fail(KV_ERR_BAD_STATE, "compaction of a paused session");
-    if (n < 0 || prefix < 0 || prefix + n > s->T)
+    if (n < 0 || prefix < 0 || prefix > s->T || n > s->T - prefix)
         return fail(KV_ERR_INVALID_ARG, "prefix and kept tokens exceed the session's");
     if (layer_stride < 0 || head_stride < 0 || layer_stride > (int64_t(1) << 40) || head_stride > (int64_t(1) << 40))
         return fail(KV_ERR_INVALID_ARG, "strides of the lists out of range");

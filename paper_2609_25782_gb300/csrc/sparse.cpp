@@ -29,6 +29,19 @@ int check_rows(const kv_pool *p, int32_t layer, bool all_layers, const int32_t *
     return KV_OK;
 }
 
+// A pool's first call of a kind prepares its kernels. The call may be one that a graph records; the preparation is no
+// part of the recording.
+template <typename F>
+int prepare(kv_pool *p, bool *ready, const char *what, F &&fn) {
+    if (*ready) return KV_OK;
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    const int rc = p->cuda(what, fn);
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    *ready = !rc;
+    return rc;
+}
+
 int check_stride(int64_t *stride, int64_t row) {
     if (*stride == 0) *stride = row;
     if (*stride < row || *stride & 7 || *stride > (int64_t(1) << 32))
@@ -93,11 +106,8 @@ int select_blocks(kv_pool *p, int32_t layer, const void *q, int64_t q_stride, co
     if (rc) return rc;
     if (p->host_only) return fail(KV_ERR_BAD_STATE, "selection on a host-logic-only pool");
     DeviceGuard dg(p->cfg.device, true);
-    if (!p->select_ready) {
-        rc = p->cuda("kernel of the selection", [&] { return kvt::prepare_select_kernel(&p->select_fit); });
-        if (rc) return rc;
-        p->select_ready = true;
-    }
+    rc = prepare(p, &p->select_ready, "kernels of the selection", [&] { return kvt::prepare_select_kernel(&p->select_fit); });
+    if (rc) return rc;
     const int64_t layer_records = static_cast<int64_t>(layer) * p->cfg.num_kv_heads * p->cfg.num_hot_blocks;
     kvt::SelectArgs a;
     a.q = static_cast<const uint16_t *>(q);
@@ -143,11 +153,8 @@ int sparse_attention(kv_pool *p, int32_t layer, const void *q, int64_t q_stride,
     if (!std::isfinite(scale_log2)) return fail(KV_ERR_INVALID_ARG, "scale not finite, or above 2^127");
     if (p->host_only) return fail(KV_ERR_BAD_STATE, "attention on a host-logic-only pool");
     DeviceGuard dg(p->cfg.device, true);
-    if (!p->sparse_ready) {
-        rc = p->cuda("kernels of sparse attention", [&] { return kvt::prepare_sparse_kernels(&p->sparse_fit); });
-        if (rc) return rc;
-        p->sparse_ready = true;
-    }
+    rc = prepare(p, &p->sparse_ready, "kernels of sparse attention", [&] { return kvt::prepare_sparse_kernels(&p->sparse_fit); });
+    if (rc) return rc;
     kvt::SparseArgs a;
     a.q = static_cast<const uint16_t *>(q);
     a.k_new = static_cast<const uint16_t *>(k_new);

@@ -309,3 +309,37 @@ def test_a_captured_step_behind_copies_and_two_streams(cuda_dev):
                     assert c.selected[b, g].tolist() == c.reference_selection(b, g, 12)[0]
                 c.assert_right(b, *c.reference(b))
     assert c.pool.check_device() == 0
+
+
+FIRST_CALLS = """
+import sys
+sys.path[:0] = [ROOT, ROOT + "/tests"]
+import torch
+from sparse_cases import Cache
+c = Cache([700, 333, 90], seed=14)
+c.selected = torch.zeros(3, 4, 12, dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    st = torch.cuda.current_stream()
+    c.make_bounds(stream=st)
+    c.pool.select_blocks(0, c.q, c.bounds, c.tables, c.lens, 3, c.width, c.selected, stream=st)
+    c.pool.sparse_attention(0, c.q, c.selected, c.tables, c.lens, 3, c.width, c.scale, c.out, c.k, c.v, st)
+graph.replay()
+torch.cuda.synchronize()
+for b in range(3):
+    for g in range(4):
+        assert c.selected[b, g].tolist() == c.reference_selection(b, g, 12)[0]
+    c.assert_right(b, *c.reference(b, True))
+assert c.pool.check_device() == 0
+print("as they should be")
+"""
+
+
+def test_first_calls_of_a_process_in_a_capture(cuda_dev):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", FIRST_CALLS.replace("ROOT", repr(root))], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "as they should be" in run.stdout, run.stderr[-2000:]

@@ -295,7 +295,7 @@ def test_compact_refusals_change_nothing(kv):
     reserve(kv, pool, s, 100)
     before = state(kv, pool)
     for a in ((s, 256, 0, 0, -1, 0), (s, 256, 0, 0, 10, -1), (s, 256, 0, 0, 60, 41), (s, 256, -1, 0, 10, 0),
-              (s, 256, 0, -4, 10, 0), (s, 258, 0, 0, 10, 0), (5, 256, 0, 0, 10, 0), (s, 256, 1 << 41, 0, 10, 0)):
+              (s, 256, 0, -4, 10, 0), (s, 256, 0, 0, 1, 2 ** 63 - 1), (s, 258, 0, 0, 10, 0), (5, 256, 0, 0, 10, 0), (s, 256, 1 << 41, 0, 10, 0)):
         refused(kv, kv.KV_ERR_INVALID_ARG, kv.session_compact, pool, *a)
         assert state(kv, pool) == before, a
     kv.session_pause(pool, s, None)
