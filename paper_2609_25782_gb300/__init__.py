@@ -57,8 +57,13 @@ class Pool:
                                  (kvtier.KV_POOL_COLD_INT8 if cold_int8 else 0))
         self.handle = kvtier.kv_pool_create(cfg)
         self.max_context = max_context
+        self._calls = None
+        if kvtier._calls is not None and head_dim == 128:
+            self._calls = kvtier._calls.Calls(self.handle, device, num_q_heads, num_kv_heads, self.bounds_bytes, torch.bfloat16,
+                                              torch.int32, torch.float32, *map(kvtier.address, (self._select, self._sparse)))
 
     def close(self) -> None:
+        self._calls = None               # (it has the handle)
         if getattr(self, "handle", None):
             kvtier.kv_pool_destroy(self.handle)
             self.handle = None
@@ -304,17 +309,20 @@ class Pool:
         """The `top` blocks of each row and KV head that q's [B][Hq][D] heads (any row stride) may need
         most, the row's `first` first and `last` last ones among them, into selected int32
         [B][Hkv][top]: ascending, -1 behind. scores: fp32 [B][Hkv][max_blocks] or None."""
-        self._rows(block_tables, seq_lens, B, max_blocks)
-        self._whole_bounds(bounds)
-        top, q_stride, at = self._list(selected, B), self._heads(q, B, self.Hq, "q"), None
-        if scores is not None:
-            at = scores.data_ptr()
-            if scores.dtype is not self._f32 or scores.shape != (B, self.Hkv, max_blocks) or \
-                    not scores.is_contiguous() or scores.get_device() != self._index:
-                raise ValueError(f"scores must be contiguous fp32 [{B}][{self.Hkv}][{max_blocks}] on the pool's device")
-        rc = self._select(self.handle, layer, q.data_ptr(), q_stride, bounds.data_ptr(),
-                          block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, first, last, top,
-                          selected.data_ptr(), at, kvtier._stream(stream))
+        rc = self._calls and self._calls.select_blocks(layer, q, bounds, block_tables, seq_lens, B, max_blocks, selected, first,
+                                                       last, scores, stream)
+        if rc is None:                   # without the module, or something unusual about an argument
+            self._rows(block_tables, seq_lens, B, max_blocks)
+            self._whole_bounds(bounds)
+            top, q_stride, at = self._list(selected, B), self._heads(q, B, self.Hq, "q"), None
+            if scores is not None:
+                at = scores.data_ptr()
+                if scores.dtype is not self._f32 or scores.shape != (B, self.Hkv, max_blocks) or \
+                        not scores.is_contiguous() or scores.get_device() != self._index:
+                    raise ValueError(f"scores must be contiguous fp32 [{B}][{self.Hkv}][{max_blocks}] on the pool's device")
+            rc = self._select(self.handle, layer, q.data_ptr(), q_stride, bounds.data_ptr(),
+                              block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, first, last, top,
+                              selected.data_ptr(), at, kvtier._stream(stream))
         if rc:
             kvtier.raise_last(rc, "select_blocks")
 
@@ -323,21 +331,24 @@ class Pool:
         """Attention of one new token per session over the listed blocks of each KV head (selected, as
         select_blocks leaves it, or any list). k_new, v_new: bf16 [B][Hkv][D] (any row stride), the
         token at seq_lens[b] - 1, written to its pool slot as well. out: fp32 or bf16 [B][Hq][D]."""
-        self._rows(block_tables, seq_lens, B, max_blocks)
-        top, q_stride, kv_stride, k, v = self._list(selected, B), self._heads(q, B, self.Hq, "q"), 0, None, None
-        if (k_new is None) != (v_new is None):
-            raise ValueError("k_new and v_new come together")
-        if k_new is not None:
-            kv_stride = self._heads(k_new, B, self.Hkv, "k_new")
-            if self._heads(v_new, B, self.Hkv, "v_new") != kv_stride:
-                raise ValueError("k_new and v_new need the same row stride")
-            k, v = k_new.data_ptr(), v_new.data_ptr()
-        if out.shape != (B, self.Hq, self.D) or not out.is_contiguous() or out.dtype not in self._out_flags or \
-                out.get_device() != self._index:
-            raise ValueError(f"out must be contiguous fp32 or bf16 [{B}][{self.Hq}][{self.D}] on the pool's device")
-        rc = self._sparse(self.handle, layer, q.data_ptr(), q_stride, k, v, kv_stride, selected.data_ptr(), top,
-                          block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, scale, out.data_ptr(),
-                          self._out_flags[out.dtype], kvtier._stream(stream))
+        rc = self._calls and self._calls.sparse_attention(layer, q, selected, block_tables, seq_lens, B, max_blocks, scale, out,
+                                                          k_new, v_new, stream)
+        if rc is None:
+            self._rows(block_tables, seq_lens, B, max_blocks)
+            top, q_stride, kv_stride, k, v = self._list(selected, B), self._heads(q, B, self.Hq, "q"), 0, None, None
+            if (k_new is None) != (v_new is None):
+                raise ValueError("k_new and v_new come together")
+            if k_new is not None:
+                kv_stride = self._heads(k_new, B, self.Hkv, "k_new")
+                if self._heads(v_new, B, self.Hkv, "v_new") != kv_stride:
+                    raise ValueError("k_new and v_new need the same row stride")
+                k, v = k_new.data_ptr(), v_new.data_ptr()
+            if out.shape != (B, self.Hq, self.D) or not out.is_contiguous() or out.dtype not in self._out_flags or \
+                    out.get_device() != self._index:
+                raise ValueError(f"out must be contiguous fp32 or bf16 [{B}][{self.Hq}][{self.D}] on the pool's device")
+            rc = self._sparse(self.handle, layer, q.data_ptr(), q_stride, k, v, kv_stride, selected.data_ptr(), top,
+                              block_tables.data_ptr(), seq_lens.data_ptr(), B, max_blocks, scale, out.data_ptr(),
+                              self._out_flags[out.dtype], kvtier._stream(stream))
         if rc:
             kvtier.raise_last(rc, "sparse_attention")
 

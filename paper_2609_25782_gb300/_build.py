@@ -1,4 +1,5 @@
-"""Compile libkvtier.so in-tree with nvcc for sm_103a.
+"""Compile libkvtier.so in-tree with nvcc for sm_103a, and with the C compiler the
+module that Pool's calls per layer go through (_calls.so, where Python's headers are).
 
 The translation units (SOURCES) compile in parallel and are linked with the static CUDA runtime,
 so the library needs only the driver at run time.
@@ -9,10 +10,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvtier.so")
+CALLS = os.path.join(HERE, "_calls.so")
+PYTHON_H = os.path.join(sysconfig.get_paths()["include"], "Python.h")
 SOURCES = ["decode_kernels.cu", "turn_kernels.cu", "copy_kernels.cu", "sparse_kernels.cu",
            "attend_kernels.cu", "page_kernels.cu", "pool.cpp", "pages.cpp", "sparse.cpp", "noalloc.cu"]
 HEADERS = ["kvt_internal.h", "pool_state.h", "decode_launch.h", "turn_plan.h", "tile_ops.cuh",
@@ -28,10 +32,11 @@ def nvcc() -> str:
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    made = [LIB] + ([CALLS] if os.path.exists(PYTHON_H) else [])
+    if not all(os.path.exists(x) for x in made):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS] + [os.path.abspath(__file__)]
+    t = min(os.path.getmtime(x) for x in made)
+    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS + ["calls.c"]] + [os.path.abspath(__file__)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -53,10 +58,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
         procs.append((src, subprocess.Popen(common + extra + ["-c", os.path.join(CSRC, src), "-o", obj],
                                             stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
                                             text=True)))
+    if os.path.exists(PYTHON_H):
+        cmd = [os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-I", os.path.dirname(PYTHON_H),
+               os.path.join(CSRC, "calls.c"), "-o", CALLS + ".tmp"]
+        procs.append(("calls.c", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for src, p in procs:
         out, _ = p.communicate()
         if p.returncode != 0:
-            raise RuntimeError(f"nvcc failed on {src}:\n{out}")
+            raise RuntimeError(f"compiler failed on {src}:\n{out}")
         if verbose and out:
             sys.stderr.write(out)
     tmp = LIB + ".tmp"
@@ -64,6 +73,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if res.returncode != 0:
         raise RuntimeError(f"link failed:\n{res.stdout}{res.stderr}")
     os.replace(tmp, LIB)
+    if os.path.exists(PYTHON_H):
+        os.replace(CALLS + ".tmp", CALLS)
     return LIB
 
 

@@ -155,6 +155,10 @@ def _load():
 
 
 lib = _load()
+try:
+    from . import _calls        # checks and calls without ctypes (csrc/calls.c), where Python's headers were there
+except ImportError:
+    _calls = None
 
 
 def _addr(x) -> int | None:
@@ -175,6 +179,11 @@ def _stream(s) -> int | None:
     if isinstance(s, int):
         return s
     return s.cuda_stream
+
+
+def address(f) -> int:
+    """Where a function of the library is."""
+    return C.cast(f, C.c_void_p).value
 
 
 def raise_last(rc: int, where: str) -> None:

@@ -311,6 +311,19 @@ def test_a_captured_step_behind_copies_and_two_streams(cuda_dev):
     assert c.pool.check_device() == 0
 
 
+def test_calls_on_a_closed_pool_are_refused(cuda_dev):
+    from paper_2609_25782_gb300 import KVError
+    c = Cache([100], seed=19)
+    c.make_bounds()
+    c.select(4)
+    c.attend()
+    assert c.pool.check_device() == 0
+    c.pool.close()
+    for call in (lambda: c.select(4), c.attend, c.make_bounds):
+        with pytest.raises(KVError, match="null pool"):
+            call()
+
+
 FIRST_CALLS = """
 import sys
 sys.path[:0] = [ROOT, ROOT + "/tests"]

@@ -1,5 +1,7 @@
 """What the calls on bounds, selections and lists hand to the library, and what they and the library refuse,
 without a GPU."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -15,8 +17,9 @@ def package():
     return paper_2609_25782_gb300
 
 
-def make_pool(package, hq=8, hkv=2, layers=3, blocks=5):
-    """A pool without arenas or a handle, and library calls that only note their arguments."""
+def make_pool(package, native, hq=8, hkv=2, layers=3, blocks=5):
+    """A pool without arenas or a handle, and library calls that only note their arguments. native: through the module
+    in C, to functions that note theirs as well."""
     p = package.Pool.__new__(package.Pool)
     p.device, p.handle, p.Hq, p.Hkv, p.D, p.L, p.bt, p.num_hot_blocks = torch.device("cpu"), None, hq, hkv, D, layers, 16, blocks
     p._bf16, p._i32, p._f32 = BF, torch.int32, torch.float32
@@ -25,7 +28,25 @@ def make_pool(package, hq=8, hkv=2, layers=3, blocks=5):
     p.bounds_bytes = layers * hkv * blocks * (2 * D + 2)
     p.calls = []
     p._select = p._sparse = lambda *a: p.calls.append(a) or 0
+    p._calls, p.native = None, 0
+    if native:
+        if package.kvtier._calls is None:
+            pytest.skip("built without Python's headers")
+        i32, i64, ptr = C.c_int32, C.c_int64, C.c_void_p
+
+        def note(*a):
+            p.native += 1
+            return p.calls.append(a) or 0
+        select = C.CFUNCTYPE(C.c_int, ptr, i32, ptr, i64, ptr, ptr, ptr, i32, i32, i32, i32, i32, ptr, ptr, ptr)(note)
+        sparse = C.CFUNCTYPE(C.c_int, ptr, i32, ptr, i64, ptr, ptr, i64, ptr, i32, ptr, ptr, i32, i32, C.c_float, ptr,
+                             C.c_uint32, ptr)(note)
+        p.keep = select, sparse
+        p._calls = package.kvtier._calls.Calls(77, -1, hq, hkv, p.bounds_bytes, BF, torch.int32, torch.float32,
+                                               *map(package.kvtier.address, p.keep))
     return p
+
+
+BOTH = pytest.mark.parametrize("native", [False, True])
 
 
 def arguments(pool, B=3, top=4, **other):
@@ -61,8 +82,9 @@ def refused(pool, f, **other):
     assert not pool.calls, other
 
 
-def test_strides_and_shapes_reach_the_library(package):
-    pool = make_pool(package)
+@BOTH
+def test_strides_and_shapes_reach_the_library(package, native):
+    pool = make_pool(package, native)
     qkv = torch.zeros(3, 12, D, dtype=BF)
     q, k, v = qkv[:, :8], qkv[:, 8:10], qkv[:, 10:]
     got = select(pool, q=q)
@@ -76,11 +98,13 @@ def test_strides_and_shapes_reach_the_library(package):
     one = torch.zeros(1, 8, D, dtype=BF).expand(4, 8, D)[:1]
     assert attend(pool, B=1, q=one)[3] == 0
     for stream, handle in ((None, None), (1234, 1234), (0, 0)):
-        assert select(pool, stream=stream)[-1] == attend(pool, stream=stream)[-1] == handle
+        assert (select(pool, stream=stream)[-1] or 0) == (attend(pool, stream=stream)[-1] or 0) == (handle or 0)
+    assert pool.native == (12 if native else 0)
 
 
-def test_tensors_that_the_library_would_misread(package):
-    pool = make_pool(package)
+@BOTH
+def test_tensors_that_the_library_would_misread(package, native):
+    pool = make_pool(package, native)
     i32 = torch.int32
     wide = torch.zeros(3, 16, 2 * D, dtype=BF)
     for f in (select, attend):
@@ -110,8 +134,9 @@ def test_tensors_that_the_library_would_misread(package):
         refused(pool, attend, out=out)
 
 
-def test_tensors_on_another_device(package):
-    pool = make_pool(package)
+@BOTH
+def test_tensors_on_another_device(package, native):
+    pool = make_pool(package, native)
 
     class Elsewhere(torch.Tensor):
         def get_device(self):
@@ -124,7 +149,7 @@ def test_tensors_on_another_device(package):
 
 
 def test_lists_of_a_compaction(package, monkeypatch):
-    pool = make_pool(package)
+    pool = make_pool(package, False)
     calls = []
     monkeypatch.setattr(package.kvtier, "session_compact", lambda *a: calls.append(a))
     i32 = torch.int32
