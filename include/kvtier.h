@@ -393,9 +393,10 @@ int64_t kv_bounds_bytes(const kv_pool_config *cfg);
  *                there already, 0 .. seq_len; a block that is partly among them
  *                is done again (none is for since == seq_len)
  *   bounds       device, kv_bounds_bytes(cfg), 256-byte aligned, the caller's
- * B at most 4096, B * max_blocks at most 2^30. A length or since out of range sets KV_DEVICE_BAD_LENGTH and the row is
- * skipped, a block id out of range KV_DEVICE_BAD_BLOCK. Two rows may name the
- * same block: both write the same values, if their lengths cover it alike. */
+ * B at most 4096, B * max_blocks at most 2^30. A length or since out of range sets
+ * KV_DEVICE_BAD_LENGTH and the row is skipped, a block id out of range
+ * KV_DEVICE_BAD_BLOCK. Two rows may name the same block: both write the same
+ * values, if their lengths cover it alike. */
 int kv_pool_block_bounds(kv_pool *pool, int32_t layer, const int32_t *block_tables,
                          const int32_t *seq_lens, const int32_t *since, int32_t B,
                          int32_t max_blocks, void *bounds, kv_stream_t stream);
@@ -414,13 +415,13 @@ int kv_pool_block_bounds(kv_pool *pool, int32_t layer, const int32_t *block_tabl
  * sums over the group's heads of the positive and the negative parts of
  *   c[h][d] = round_to_even(q[h][d] * 2^(137 - E)),
  * E the biased exponent of the group's largest finite |q| (at least 1); a q that is not
- * finite counts as 0. So a score is at least 2^(137 - E) sum_h q_h . K[t] for every token t of
- * the block, up to c's rounding. The sum is a whole number, rounded to fp32 once:
- * scores, and with them the selection, do not depend on an order of sums. A block
- * whose step is infinite scores +inf. Equal scores go to the lower block number;
- * blocks always taken come before all others.
- * Row b has ceil(seq_lens[b] / bt) blocks; 0 is none (all -1). A length out of
- * range sets KV_DEVICE_BAD_LENGTH and its row gets -1 and no scores, a block id out of range
+ * finite counts as 0. So a score is at least 2^(137 - E) sum_h q_h . K[t] for every
+ * token t of the block, up to c's rounding. The sum is a whole number, rounded to
+ * fp32 once: scores, and with them the selection, do not depend on an order of
+ * sums. A block whose step is infinite scores +inf. Equal scores go to the lower
+ * block number; blocks always taken come before all others. Row b has
+ * ceil(seq_lens[b] / bt) blocks; 0 is none (all -1). A length out of range sets
+ * KV_DEVICE_BAD_LENGTH and its row gets -1 and no scores, a block id out of range
  * KV_DEVICE_BAD_BLOCK (scored as block 0 is). max_blocks at most 49152. */
 int select_blocks(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride, const void *bounds,
                   const int32_t *block_tables, const int32_t *seq_lens, int32_t B, int32_t max_blocks,
@@ -444,13 +445,14 @@ int select_blocks(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride,
  * softmax statistics and sums are held in 32 bits, weights in bf16 for the product
  * with V. Tokens past seq_len in a block may hold anything. The result is the
  * same from run to run; its last bits depend on the order of the list and on
- * B x Hkv, top and the device's number of SMs, by which the work is cut. A length out of range
- * sets KV_DEVICE_BAD_LENGTH and the row is not written; a listed block at or past the row's
- * end, or a block id out of range, sets KV_DEVICE_BAD_BLOCK and is skipped; a wait
- * inside the kernel that runs out (2 s) sets KV_DEVICE_TIMEOUT, the row is then wrong.
- * No workspace: calls on several streams may overlap. Bounds, selections and this call are
- * programmatic dependents of the kernel before them: they start while it ends, and wait for its
- * end before they read anything. */
+ * B x Hkv, top and the device's number of SMs, by which the work is cut. A length
+ * out of range sets KV_DEVICE_BAD_LENGTH and the row is not written; a listed block
+ * at or past the row's end, or a block id out of range, sets KV_DEVICE_BAD_BLOCK
+ * and is skipped; a wait inside the kernel that runs out (2 s) sets
+ * KV_DEVICE_TIMEOUT, the row is then wrong. No workspace: calls on several streams
+ * may overlap. Bounds, selections and this call are programmatic dependents of the
+ * kernel before them: they start while it ends, and wait for its end before they
+ * read anything. */
 int sparse_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stride, const void *k_new,
                      const void *v_new, int64_t kv_stride, const int32_t *selected, int32_t top,
                      const int32_t *block_tables, const int32_t *seq_lens, int32_t B, int32_t max_blocks,
@@ -467,8 +469,8 @@ int sparse_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stri
  * and empty: its first pause writes all of its tokens.
  * The stream first waits for the parent's last append and resume; order the call
  * after the attention calls that write tokens which the parent has reserved. The
- * parent's and the new sessions' ready events are recorded on the stream. Free-list pops go
- * session by session, in logical order. Errors: KV_ERR_BAD_STATE (paused),
+ * parent's and the new sessions' ready events are recorded on the stream. Free-list
+ * pops go session by session, in logical order. Errors: KV_ERR_BAD_STATE (paused),
  * KV_ERR_NO_HOT_BLOCKS, KV_ERR_NO_COLD_SPACE (n images), too many sessions ->
  * KV_ERR_INVALID_ARG. All or nothing. */
 int session_fork(kv_pool *pool, int32_t sid, int64_t tokens, int64_t max_tokens, int32_t n,
@@ -480,24 +482,25 @@ int session_fork(kv_pool *pool, int32_t sid, int64_t tokens, int64_t max_tokens,
  * in order; they are reused only by work ordered after this call on the stream.
  * If the block that `tokens` ends in is shared (session_fork), its part moves into
  * a block of its own (KV_ERR_NO_HOT_BLOCKS). Tokens that the image holds stay
- * valid there. The stream first waits for the session's last append and resume; the caller
- * orders it after any other work that reads or writes the session. Where rows move,
- * the session's ready event is recorded on the stream. */
+ * valid there. The stream first waits for the session's last append and resume; the
+ * caller orders it after any other work that reads or writes the session. Where
+ * rows move, the session's ready event is recorded on the stream. */
 int session_truncate(kv_pool *pool, int32_t sid, int64_t tokens, kv_stream_t stream);
 
 /* Keep the first `prefix` tokens of an ACTIVE session and, behind them, n of the others: token
  * prefix + i of layer l and kv-head g becomes the old token
  *   keep[l * layer_stride + g * head_stride + i]
  * (device int32, 4-byte aligned; strides in elements, 0 where lists are shared), K and V
- * alike; T = prefix + n. No passage. A list ascends strictly within prefix .. T - 1. Rows move
- * towards the front in place; blocks behind the new end are given back as by
- * session_truncate, shared blocks are replaced by new ones (free-list pops in
- * logical order). Of the image only the tokens before prefix stay valid: later
- * ones are written again by the next pause. In residency mode evicted blocks are
- * fetched back first (and stay, should a later step of the call fail). n = T - prefix keeps everything and moves nothing.
- * A position out of range, or not above the one before it, sets KV_DEVICE_BAD_INDEX; that
- * layer and head's rows from there on are then undefined. Waits and ordering as session_truncate. Errors:
- * KV_ERR_BAD_STATE (paused), KV_ERR_NO_HOT_BLOCKS. */
+ * alike; T = prefix + n. No passage. A list ascends strictly within prefix .. T -
+ * 1. Rows move towards the front in place; blocks behind the new end are given back
+ * as by session_truncate, shared blocks are replaced by new ones (free-list pops in
+ * logical order). Of the image only the tokens before prefix stay valid: later ones
+ * are written again by the next pause. In residency mode evicted blocks are fetched
+ * back first (and stay, should a later step of the call fail). n = T - prefix keeps
+ * everything and moves nothing. A position out of range, or not above the one
+ * before it, sets KV_DEVICE_BAD_INDEX; that layer and head's rows from there on are
+ * then undefined. Waits and ordering as session_truncate. Errors: KV_ERR_BAD_STATE
+ * (paused), KV_ERR_NO_HOT_BLOCKS. */
 int session_compact(kv_pool *pool, int32_t sid, const int32_t *keep, int64_t layer_stride,
                     int64_t head_stride, int32_t n, int64_t prefix, kv_stream_t stream);
 
