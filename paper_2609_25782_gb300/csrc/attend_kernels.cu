@@ -19,15 +19,13 @@ namespace kvt {
 namespace {
 
 constexpr int kItems = 64;           // places of tiles that a warp holds: two lists of 32
-constexpr int kMostCluster = 16;
 
-// Two shapes: few units get CTAs of 8 warps that have an SM each, so that a warp has few tiles one after
-// another; many get three CTAs of 4 warps per SM.
+// Two shapes: few units get clusters of CTAs of 8 warps that have an SM each, so that a warp has few tiles one after
+// another; many get a CTA of 4 warps each, three per SM.
 template <int kWarps, int kStages>
 struct Layout {
-    static constexpr int kMost = kWarps == 8 ? kMostCluster : 8;        // CTAs of a cluster
-    // Rows that a CTA receives: its ceil(8 / C) heads from C CTAs.
-    static constexpr int kRows = kWarps == 8 ? 16 : 14;
+    static constexpr bool kCluster = kWarps == 8;
+    static constexpr int kRows = kCluster ? 16 : 0;   // that a CTA receives: its ceil(8 / C) heads from C CTAs
     static constexpr int kRing = kWarps * kStages * kTileBytes;
     static constexpr int kRecvO = kRing;
     static constexpr int kRecvMl = kRecvO + kRows * kHeadDim * 4;
@@ -52,7 +50,8 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 8 ? 1 : 3)
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const Shape sh = a.s;
-    const int C = gridDim.x, rank = blockIdx.x, g = blockIdx.y, b = blockIdx.z;   // a row of the grid is a cluster
+    // A row of the grid is a cluster.
+    const int C = Lay::kCluster ? gridDim.x : 1, rank = Lay::kCluster ? blockIdx.x : 0, g = blockIdx.y, b = blockIdx.z;
     const int G = a.group;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     after_previous();
@@ -338,10 +337,8 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 8 ? 1 : 3)
 }  // namespace
 
 cudaError_t prepare_sparse_kernels(SparseFit *fit) {
-    cudaError_t e = fit_clusters(sparse_kernel<4, 2>, 4 * 32, Layout<4, 2>::kBytes, Layout<4, 2>::kBytes, fit->clusters[0]);
-    if (e == cudaSuccess)
-        e = fit_clusters(sparse_kernel<8, 3>, 8 * 32, Layout<8, 3>::kBytes, Layout<8, 3>::kBytes, fit->clusters[1]);
-    return e;
+    const cudaError_t e = cudaFuncSetAttribute(sparse_kernel<4, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<4, 2>::kBytes);
+    return e != cudaSuccess ? e : fit_clusters(sparse_kernel<8, 3>, 8 * 32, Layout<8, 3>::kBytes, Layout<8, 3>::kBytes, fit->clusters);
 }
 
 cudaError_t launch_sparse(const CUtensorMap &map, const SparseArgs &a, const SparseFit &fit, cudaStream_t st) {
@@ -353,10 +350,10 @@ cudaError_t launch_sparse(const CUtensorMap &map, const SparseArgs &a, const Spa
     // resident at once), (4, 8) 7.2; 64 units (8, 2) 16.2, (8, 1) 15.9, (4, 4) 15.9, (4, 8) 20.6; 256 units (4, 1) 43.9,
     // (8, 1) 45.9, (4, 2) 51.0; 384 units of 256 tiles (4, 1) 119.3, (8, 1) 116.9, (4, 4) 120.7.
     int log = 4;
-    while (log > 0 && (units > fit.clusters[1][log] || tiles < 8 << log)) --log;
-    const bool wide = units <= fit.clusters[1][0];
+    while (log > 0 && (units > fit.clusters[log] || tiles < 8 << log)) --log;
+    const bool wide = units <= fit.clusters[0];
     return wide ? launch_behind(sparse_kernel<8, 3>, dim3(1 << log, a.s.Hkv, a.B), 1 << log, 8 * 32, Layout<8, 3>::kBytes, st, map, a)
-                : launch_behind(sparse_kernel<4, 2>, dim3(1, a.s.Hkv, a.B), 1, 4 * 32, Layout<4, 2>::kBytes, st, map, a);
+                : launch_behind(sparse_kernel<4, 2>, dim3(1, a.s.Hkv, a.B), 0, 4 * 32, Layout<4, 2>::kBytes, st, map, a);
 }
 
 }  // namespace kvt

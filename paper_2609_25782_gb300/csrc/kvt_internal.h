@@ -232,12 +232,12 @@ struct GatherArgs {
 };
 
 // How many clusters of 1, 2, 4, 8 and 16 CTAs the device holds at once, for the kernels of select_blocks (one CTA per
-// SM in [1], two in [0]) and of sparse_attention (8 warps in [1], 4 in [0]).
+// SM in [1], two in [0]) and for that of sparse_attention with a CTA per SM.
 struct SelectFit {
     int clusters[2][5];
 };
 struct SparseFit {
-    int clusters[2][5];
+    int clusters[5];
 };
 
 // Host launchers (decode_kernels.cu, turn_kernels.cu, copy_kernels.cu). Each returns the launch's CUDA status.
