@@ -6,7 +6,7 @@ from sparse_cases import Cache
 
 pytestmark = pytest.mark.gpu
 
-HEADS = [(32, 4), (8, 8), (8, 4), (8, 2), (8, 1)]
+HEADS = [(32, 4), (8, 8), (8, 4), (8, 2), (8, 1), (64, 8), (6, 6)]
 
 
 @pytest.mark.parametrize("bt", [16, 64])

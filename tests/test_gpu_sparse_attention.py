@@ -7,7 +7,7 @@ from sparse_cases import Cache
 
 pytestmark = pytest.mark.gpu
 
-HEADS = [(32, 4), (8, 8), (8, 4), (8, 2), (8, 1)]
+HEADS = [(32, 4), (8, 8), (8, 4), (8, 2), (8, 1), (64, 8), (6, 6)]
 
 
 @pytest.mark.parametrize("bt", [16, 64])
@@ -309,6 +309,40 @@ def test_a_captured_step_behind_copies_and_two_streams(cuda_dev):
                     assert c.selected[b, g].tolist() == c.reference_selection(b, g, 12)[0]
                 c.assert_right(b, *c.reference(b))
     assert c.pool.check_device() == 0
+
+
+def test_as_many_rows_as_a_call_takes(cuda_dev):
+    """65 535 rows, each of one block of a few that they share, and their q rows apart."""
+    from paper_2609_25782_gb300 import KVError
+    c = Cache([16, 40, 5, 0], seed=20, hq=2, hkv=1)
+    c.make_bounds()
+    B, width = 65535, 3
+    which = torch.arange(B + 1, device="cuda") % 4
+    tables, lens = c.tables[:, :width][which].contiguous(), c.lens[which].contiguous()
+    q = torch.randn(B + 1, 4, 128, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).bfloat16()[:, 1:3]
+    selected = torch.zeros(B, 1, 2, dtype=torch.int32, device="cuda")
+    out = torch.zeros(B, 2, 128, device="cuda")
+    c.pool.select_blocks(0, q[:B], c.bounds, tables, lens, B, width, selected)
+    want = torch.tensor([[0, -1], [0, 2], [0, -1], [-1, -1]], dtype=torch.int32, device="cuda")
+    assert torch.equal(selected[:, 0], want[which[:B]])
+    c.pool.sparse_attention(0, q[:B], selected, tables, lens, B, width, c.scale, out)
+    for kind in range(4):
+        rows = torch.nonzero(which[:B] == kind)[:, 0]
+        pos = [t for t in range(c.T[kind]) if t // 16 in want[kind].tolist()]
+        if not pos:
+            assert (out[rows] == 0).all()
+            continue
+        at = torch.tensor(pos, device="cuda")
+        blk = torch.from_numpy(c.tab[kind]).cuda().long()[at // 16]
+        k, v = (c.hot[blk, 0, w, 0, at % 16].double() for w in (0, 1))
+        w = torch.softmax(q[rows].double() @ k.T * c.scale, -1)
+        ref, noise = w @ v, torch.sqrt((w * w) @ (v * v).sum(1))
+        from turn_cases import ROW
+        assert ((out[rows].double() - ref).norm(dim=2) <= ROW * (noise + ref.norm(dim=2))).all()
+    assert c.pool.check_device() == 0
+    with pytest.raises(KVError):
+        c.pool.sparse_attention(0, q, torch.zeros(B + 1, 1, 2, dtype=torch.int32, device="cuda"), tables, lens, B + 1, width, c.scale,
+                                torch.zeros(B + 1, 2, 128, device="cuda"))
 
 
 def test_calls_on_a_closed_pool_are_refused(cuda_dev):
