@@ -386,8 +386,8 @@ def _own_fork(s):
 
 def _own_compact(s):
     pool, st = s["pool"], torch.cuda.current_stream()
-    if s["gone"]:                           # the next turn's slots, after an earlier pass: the same ones, in turn
-        pool.batch_reserve(s["sids"][::-1], s["tables"], s["width"], s["lens"], st, counts=s["gone"][::-1])
+    if s["gone"]:                           # the next turn's slots, after an earlier pass
+        pool.batch_reserve(s["sids"], s["tables"], s["width"], s["lens"], st, counts=s["gone"])
     for sid, keep, (p, _) in zip(s["sids"], s["keep"], s["kept"]):
         pool.session_compact(sid, keep, prefix=p, stream=st)
     s["gone"] = [t - p - k for t, (p, k) in zip(s["n"], s["kept"])]
