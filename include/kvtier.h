@@ -478,8 +478,9 @@ int session_fork(kv_pool *pool, int32_t sid, int64_t tokens, int64_t max_tokens,
 
 /* Forget all but the first `tokens` (0 .. T) tokens of a session in any state. No
  * passage (the paper's contexts only grow). The blocks behind them are given
- * back, the last one first, so that a session that grows again gets them again
- * in order; they are reused only by work ordered after this call on the stream.
+ * back, the last one first, so that a session that grows again before any other
+ * takes or gives back blocks gets them again in order, and so do several that
+ * take them all by one reservation; they are reused only by work ordered after this call on the stream.
  * If the block that `tokens` ends in is shared (session_fork), its part moves into
  * a block of its own (KV_ERR_NO_HOT_BLOCKS). Tokens that the image holds stay
  * valid there. The stream first waits for the session's last append and resume; the
@@ -570,14 +571,15 @@ int kv_pool_batch_tables(kv_pool *pool, const int32_t *sids, int32_t B, int32_t 
  * mode the members' evicted blocks are fetched back first and victims come
  * only from sessions outside the batch; all members are stamped with one
  * recency time. Free-list pops go in batch order: a member's missing blocks
- * in ascending order, then its new block. The stream first waits for the
- * members' last resumes and for packs of popped blocks. Until the decode
- * has written the new tokens their slots hold stale data, so no call that
- * may pack these sessions (a pause, an eviction by a later allocation) may
- * come before it. Errors: a session twice, paused or at capacity, or
- * max_blocks too short -> KV_ERR_INVALID_ARG / KV_ERR_BAD_STATE;
- * KV_ERR_NO_HOT_BLOCKS. All or nothing. Host-logic-only pools do the
- * bookkeeping and ignore the outputs. */
+ * in ascending order, then its new block; where there are several members, new
+ * blocks that one of them gave back (session_truncate, session_compact) go to
+ * that one again, in order. The stream first waits for the members' last
+ * resumes and for packs of popped blocks. Until the decode has written the new
+ * tokens their slots hold stale data, so no call that may pack these sessions (a
+ * pause, an eviction by a later allocation) may come before it. Errors: a session
+ * twice, paused or at capacity, or max_blocks too short -> KV_ERR_INVALID_ARG /
+ * KV_ERR_BAD_STATE; KV_ERR_NO_HOT_BLOCKS. All or nothing. Host-logic-only pools
+ * do the bookkeeping and ignore the outputs. */
 int kv_pool_batch_reserve(kv_pool *pool, const int32_t *sids, int32_t B, int32_t *block_tables,
                           int32_t max_blocks, int32_t *seq_lens, kv_stream_t stream);
 

@@ -79,11 +79,13 @@ void take(kv_pool *p, const std::vector<int32_t> &v) {
     p->stats.used_blocks += static_cast<int64_t>(v.size());
 }
 
-// A session's blocks from logical block `from` on leave it, the last one first, behind the fence.
+// A session's blocks from logical block `from` on leave it, the last one first, behind the fence; those that are
+// free then keep its mark.
 void drop_tail(kv_pool *p, Session &s, int64_t from, int slot, uint64_t gen) {
+    if (s.home == 0) s.home = ++p->homes;
     for (int64_t j = static_cast<int64_t>(s.blocks.size()); j-- > from;)
         if (s.blocks[j] >= 0) {
-            p->give_back(s.blocks[j], slot, gen);
+            if (p->give_back(s.blocks[j], slot, gen)) p->block_home[s.blocks[j]] = s.home;
             if (p->lru) s.hot_count -= 1;
         }
     s.blocks.resize(from);

@@ -122,6 +122,7 @@ int kv_pool_create(const kv_pool_config *cfg, kv_pool **out) {
     p->block_fence.assign(c.num_hot_blocks, -1);
     p->block_fence_gen.assign(c.num_hot_blocks, 0);
     p->block_extra.assign(c.num_hot_blocks, 0);
+    p->block_home.assign(c.num_hot_blocks, 0);
     p->sessions.resize(c.max_sessions);
     if (c.cold_bytes > 0) p->cold_free[0] = c.cold_bytes;
 
@@ -951,11 +952,42 @@ int kv_pool_batch_tables(kv_pool *p, const int32_t *sids, int32_t B, int32_t *bl
     return gather_batch(p, sids, B, block_tables, max_blocks, seq_lens, st);
 }
 
+// The new blocks of a batch, grow[i] of member i behind its miss[i] others in `got`: a block that a member gave back
+// becomes that member's again, each one's in the order of their pops; the others fill the places left.
+static void deal_new_blocks(const kv_pool *p, const int32_t *sids, int32_t B,
+                            const std::vector<std::vector<int32_t>> &miss, const std::vector<int64_t> &grow,
+                            std::vector<int32_t> &got) {
+    std::map<uint64_t, int32_t> member;
+    for (int32_t i = 0; i < B; ++i)
+        if (p->sessions[sids[i]].home != 0) member[p->sessions[sids[i]].home] = i;
+    if (member.empty()) return;
+    std::vector<std::vector<int32_t>> own(B);
+    std::vector<int32_t> others;
+    size_t k = 0;
+    for (int32_t i = 0; i < B; ++i) {
+        k += miss[i].size();
+        for (int64_t j = 0; j < grow[i]; ++j, ++k) {
+            const auto m = member.find(p->block_home[got[k]]);
+            if (m != member.end() && static_cast<int64_t>(own[m->second].size()) < grow[m->second])
+                own[m->second].push_back(got[k]);
+            else
+                others.push_back(got[k]);
+        }
+    }
+    size_t o = k = 0;
+    for (int32_t i = 0; i < B; ++i) {
+        k += miss[i].size();
+        for (int64_t j = 0; j < grow[i]; ++j, ++k)
+            got[k] = j < static_cast<int64_t>(own[i].size()) ? own[i][j] : others[o++];
+    }
+}
+
 // Path 3 for one step: every member gets position T, or the next n (fresh
 // blocks where its tail block is full) and, in residency mode, its evicted blocks
 // back; victims come only from sessions outside the batch. The values
 // arrive with decode_append_attention. Free-list pops go in batch order:
-// a member's missing blocks (ascending), then its fresh blocks.
+// a member's missing blocks (ascending), then its fresh blocks; among several members a block that
+// one of them gave back goes to that one (deal_new_blocks).
 // counts: new positions per member, or null for one each.
 static int reserve_impl(kv_pool *p, const int32_t *sids, const int32_t *counts, int32_t B,
                         int32_t *block_tables, int32_t max_blocks, int32_t *seq_lens,
@@ -997,7 +1029,8 @@ static int reserve_impl(kv_pool *p, const int32_t *sids, const int32_t *counts, 
     if (p->lru ? !p->plan_evict(need, members, vic)
                : need > static_cast<int64_t>(p->free_list.size()))
         return fail(KV_ERR_NO_HOT_BLOCKS, "the batch's blocks and new positions do not fit in the hot pool");
-    const std::vector<int32_t> got = p->peek_alloc(need, vic);
+    std::vector<int32_t> got = p->peek_alloc(need, vic);
+    if (B > 1 && need > 1 && p->homes > 0) deal_new_blocks(p, sids, B, miss, grow, got);
     std::vector<std::vector<int32_t>> rows(B);
     std::vector<kvt::BlockJob> jobs;
     std::vector<int32_t> fresh;      // popped slots that are not eviction victims

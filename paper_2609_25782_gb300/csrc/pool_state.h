@@ -23,6 +23,7 @@ struct Session {
     int32_t state = KV_SESSION_FREE;
     int64_t T = 0, cap = 0, cold_valid = 0;
     int64_t img_off = -1, img_bytes = 0;
+    uint64_t home = 0;                // its mark on blocks that it gave back (kv_pool::block_home), 0 = on none
     std::vector<int32_t> blocks;      // per logical block: hot slot, or -1 (residency mode)
     std::vector<int16_t> img_tok;     // residency mode: tokens of block j held by the image
     int64_t hot_count = 0;            // residency mode: blocks with a hot slot
@@ -93,6 +94,8 @@ struct kv_pool {
     // is only read, and goes back to the free list with its last session.
     std::vector<int32_t> block_extra;
     bool forked = false;                 // some block has been shared
+    std::vector<uint64_t> block_home;    // of a free block: Session::home of who gave it back, 0 = nobody's
+    uint64_t homes = 0;                  // the last one of these marks
     std::vector<kvt::Session> sessions;
     std::map<int64_t, int64_t> cold_free;  // offset -> bytes
     int64_t cold_used = 0;
@@ -248,8 +251,12 @@ struct kv_pool {
         return true;
     }
 
+    // Blocks have been popped: what the free list knew of them is over.
     void clear_fences(const int32_t *blocks, size_t n) {
-        for (size_t i = 0; i < n; ++i) block_fence[blocks[i]] = -1;
+        for (size_t i = 0; i < n; ++i) {
+            block_fence[blocks[i]] = -1;
+            block_home[blocks[i]] = 0;
+        }
     }
 
     // Write entries [from, from+n) of a session's device table row.

@@ -333,6 +333,60 @@ def test_failing_device_calls_change_nothing(kv, lru):
 
 @pytest.mark.parametrize("lru", [False, True])
 @pytest.mark.parametrize("bt", [16, 64])
+@pytest.mark.parametrize("how", ["compact", "truncate", "mixed"])
+def test_sessions_that_grow_together_get_their_blocks_again(kv, lru, bt, how):
+    """Several sessions give back blocks; one reservation for all, in any order, returns each one's."""
+    pool = host_pool(kv, nb=40, lru=lru, bt=bt)
+    n = [9 * bt + 3, 12 * bt, 7 * bt + 1]
+    sids = [kv.session_create(pool, 1000) for _ in n]
+    kv.kv_pool_batch_reserve_tokens(pool, sids, n, None, 1 << 20, None)
+    rows, free = [kv.session_block_table(pool, s) for s in sids], kv.kv_pool_free_list(pool)
+    for order in ((0, 1, 2), (2, 1, 0), (1, 2, 0), (0, 2, 1)):
+        for i, s in enumerate(sids):
+            if how == "truncate" or how == "mixed" and i == 1:
+                kv.session_truncate(pool, s, 2 * bt + 5)
+            else:
+                kv.session_compact(pool, s, 256, 0, 0, 2 * bt, 5)
+        kv.kv_pool_batch_reserve_tokens(pool, [sids[i] for i in order], [n[i] - 2 * bt - 5 for i in order], None, 1 << 20, None)
+        assert [kv.session_block_table(pool, s) for s in sids] == rows and kv.kv_pool_free_list(pool) == free
+        check(kv, pool, 40, lru, bt)
+    kv.kv_pool_destroy(pool)
+
+
+def test_blocks_that_were_given_back_go_by_the_free_list_else(kv):
+    """A single session, sessions that gave nothing back, an ended one's id: the order of pops as it was."""
+    pool = host_pool(kv)
+    a, b = kv.session_create(pool, 400), kv.session_create(pool, 400)
+    kv.kv_pool_batch_reserve_tokens(pool, [a, b], [96, 96], None, 1 << 20, None)
+    rows = [kv.session_block_table(pool, s) for s in (a, b)]
+    kv.session_truncate(pool, a, 48)
+    kv.session_truncate(pool, b, 80)
+    free = kv.kv_pool_free_list(pool)[::-1]
+    assert free[:4] == rows[1][5:] + rows[0][3:]
+    c, d = kv.session_create(pool, 400), kv.session_create(pool, 400)
+    kv.kv_pool_batch_reserve_tokens(pool, [c, d], [16, 16], None, 1 << 20, None)
+    assert [kv.session_block_table(pool, s) for s in (c, d)] == [free[0:1], free[1:2]]
+    reserve(kv, pool, a, 32)
+    assert kv.session_block_table(pool, a) == rows[0][:3] + free[2:4]
+    kv.session_truncate(pool, a, 16)                     # four blocks with its mark
+    kv.session_destroy(pool, a)
+    assert kv.session_create(pool, 400) == a
+    free = kv.kv_pool_free_list(pool)[::-1]
+    kv.kv_pool_batch_reserve_tokens(pool, [b, a], [32, 32], None, 1 << 20, None)
+    assert kv.session_block_table(pool, b)[5:] == free[:2] and kv.session_block_table(pool, a) == free[2:4]
+    # fewer than were given back: what the free list has next, each one's own among it
+    kv.session_truncate(pool, b, 64)
+    kv.session_truncate(pool, a, 0)
+    free = kv.kv_pool_free_list(pool)[::-1]
+    mine = kv.session_block_table(pool, b)
+    kv.kv_pool_batch_reserve_tokens(pool, [b, a, c], [1, 33, 16], None, 1 << 20, None)
+    assert kv.session_block_table(pool, a)[:2] == free[:2] and kv.session_block_table(pool, b) == mine + [free[2]]
+    check(kv, pool, 60, False, 16)
+    kv.kv_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("lru", [False, True])
+@pytest.mark.parametrize("bt", [16, 64])
 @pytest.mark.parametrize("seed", range(4))
 def test_random_calls_keep_the_invariants(kv, lru, bt, seed):
     nb = 40 if bt == 16 else 14
