@@ -462,7 +462,10 @@ int sparse_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stri
  * tokens (0 .. T) of an ACTIVE session; sids_out (host) receives their ids. No
  * passage; tokens are immutable (Section 3, "Memory hierarchy and write policy"),
  * so full blocks are shared: they are held by all sessions that name them, only
- * read, and go back to the free list with the last of them. The block that
+ * read, and go back to the free list with the last of them; a session that alone
+ * holds such a block in the end writes it again (a compaction, tokens behind a
+ * truncation) only behind the moves by which the others left it, whatever streams
+ * those were on. The block that
  * `tokens` ends in is copied into one block per new session. In residency mode a
  * block has one owner, whom an eviction takes it from: there all blocks are
  * copied, evicted ones read from the parent's image. A fork's image is its own

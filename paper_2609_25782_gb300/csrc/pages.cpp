@@ -216,9 +216,11 @@ int session_truncate(kv_pool *p, int32_t sid, int64_t tokens, kv_stream_t stream
     const bool own = !p->lru && nb > 0 && tokens % bt != 0 && p->block_extra[s->blocks[nb - 1]] > 0;
     if (own && p->free_list.empty()) return fail(KV_ERR_NO_HOT_BLOCKS, "no free block for a shared block's part");
     const std::vector<int32_t> got = own ? next_free(p, 1) : std::vector<int32_t>{};
+    // One that was shared, and whose other holder may still be reading behind the cut: what comes there next waits.
+    const bool left = !p->lru && nb > 0 && tokens % bt != 0 && !own && p->live_fence(s->blocks[nb - 1]);
     std::vector<int32_t> gone(s->blocks.begin() + nb - (own ? 1 : 0), s->blocks.end());
     gone.erase(std::remove(gone.begin(), gone.end(), -1), gone.end());
-    if (!gone.empty()) {
+    if (left || !gone.empty()) {
         cudaStream_t st = reinterpret_cast<cudaStream_t>(stream_);
         DeviceGuard dg(p->cfg.device, !p->host_only);
         int f = 0;
@@ -229,8 +231,9 @@ int session_truncate(kv_pool *p, int32_t sid, int64_t tokens, kv_stream_t stream
             if (!rc)
                 rc = run_copies(p, {{s->blocks[nb - 1], got[0], sid, static_cast<int32_t>(nb - 1),
                                      static_cast<int32_t>(tokens % bt)}}, sid, 0, {}, st);
-            if (!rc) rc = mark_moved(p, *s, st);
         }
+        if (!rc && left) rc = p->wait_fences(&s->blocks[nb - 1], 1, st);
+        if (!rc && (own || left)) rc = mark_moved(p, *s, st);
         if (!rc) rc = p->record_fence(f, st);
         if (rc) return rc;
 
@@ -241,8 +244,8 @@ int session_truncate(kv_pool *p, int32_t sid, int64_t tokens, kv_stream_t stream
         if (own) {
             p->give_back(s->blocks[nb - 1], f, gen);
             s->blocks[nb - 1] = got[0];
-            s->ready_recorded = s->moved = !p->host_only;
         }
+        if (own || left) s->ready_recorded = s->moved = !p->host_only;
         if (p->lru) p->lru_in(sid);
     } else {
         s->blocks.resize(nb);                     // evicted ones, if any
@@ -288,14 +291,14 @@ int session_compact(kv_pool *p, int32_t sid, const int32_t *keep, int64_t layer_
     const std::vector<int32_t> got = next_free(p, need);
     for (int64_t j = j0, k = 0; need > 0 && j < j1; ++j)
         if (p->block_extra[s->blocks[j]] > 0) slot[j - j0] = got[k++];
-    std::vector<int32_t> gone(s->blocks.begin() + j1, s->blocks.end());
-    for (int64_t j = j0; j < j1; ++j)
-        if (slot[j - j0] >= 0) gone.push_back(s->blocks[j]);
+    std::vector<int32_t> gone(s->blocks.begin() + j1, s->blocks.end()), kept;
+    for (int64_t j = j0; j < j1; ++j) (slot[j - j0] >= 0 ? gone : kept).push_back(s->blocks[j]);
 
     int f = 0;
     int rc = p->open_fence(gone.data(), gone.size(), st, &f);
     if (!rc) rc = wait_written(p, *s, st);
     if (!rc) rc = p->wait_fences(got.data(), got.size(), st);
+    if (!rc && p->forked) rc = p->wait_fences(kept.data(), kept.size(), st);   // written in place
     const int64_t step = need > 0 ? kvt::kCompactFresh : j1 - j0;
     for (int64_t j = j0; !rc && j < j1; j += step) {
         kvt::CompactArgs a;

@@ -91,7 +91,8 @@ struct kv_pool {
     std::vector<int16_t> block_fence;    // fence slot of the pack that freed it, or -1
     std::vector<uint64_t> block_fence_gen;
     // Simple mode: sessions that hold a block beside its first one. Forks share full blocks; a shared block
-    // is only read, and goes back to the free list with its last session.
+    // is only read, and goes back to the free list with its last session. The session that stays with it may write
+    // it again behind the moves of those that left (live_fence).
     std::vector<int32_t> block_extra;
     bool forked = false;                 // some block has been shared
     std::vector<uint64_t> block_home;    // of a free block: Session::home of who gave it back, 0 = nobody's
@@ -191,13 +192,18 @@ struct kv_pool {
         }
     }
 
-    // Blocks popped for a session: make `st` wait for the packs that freed
-    // them, if those packs may still be running.
+    // Whether a move of a session that left the block may still be running.
+    bool live_fence(int32_t block) const {
+        const int f = block_fence[block];
+        return f >= 0 && fences[f].gen == block_fence_gen[block];
+    }
+
+    // Blocks popped for a session, or that it alone holds now and is about to write: make `st` wait for the moves of
+    // the sessions that left them, if those may still be running.
     int wait_fences(const int32_t *blocks, size_t n, cudaStream_t st) {
         bool need[kvt::kFenceSlots] = {};
         for (size_t i = 0; i < n; ++i) {
-            const int f = block_fence[blocks[i]];
-            if (f >= 0 && fences[f].gen == block_fence_gen[blocks[i]]) need[f] = true;
+            if (live_fence(blocks[i])) need[block_fence[blocks[i]]] = true;
         }
         for (int f = 0; f < kvt::kFenceSlots; ++f) {
             if (!need[f]) continue;

@@ -326,6 +326,42 @@ def test_other_streams_wait(cuda_dev, lru):
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("stay", ["compact", "truncate", "third stream"])
+@pytest.mark.parametrize("leave", ["pause", "compact", "truncate"])
+@pytest.mark.parametrize("bt", [16, 64])
+def test_who_keeps_a_shared_block_waits_for_who_left_it(cuda_dev, bt, leave, stay):
+    """A session leaves shared blocks behind a spin on one stream; its fork, the last holder, writes them in place on
+    another. Nothing waits between the calls but the pool's own events."""
+    m = Model(60, bt=bt, seed=17)
+    a, b, c = (torch.cuda.Stream() for _ in range(3))
+    n = 13 * bt if bt == 16 else 8 * bt
+    p = m.create(n)
+    kid, = m.fork(p)                                     # all blocks are shared
+    short = m.lists(p, n - 40, 3, seed=1)
+    most = m.lists(kid, n - 1, 0, seed=2)                # gives back no block
+    x = m.tokens(5)
+    k, v = (x[:, i].transpose(1, 2).contiguous() for i in (0, 1))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(a):
+        torch.cuda._sleep(20_000_000)
+    if leave == "pause":
+        m.pool.session_pause(p, a)
+    elif leave == "compact":
+        m.compact(p, short, 3, stream=a)
+    else:
+        m.truncate(p, n - 3, a)                          # copies the last block's part
+    if stay == "compact":
+        m.compact(kid, most, 0, stream=b)
+    else:
+        m.truncate(kid, n - 8, b)
+    m.pool.session_append(kid, k, v, c if stay == "third stream" else b)
+    m.want[kid] = torch.cat([m.want[kid], x], 3)
+    torch.cuda.synchronize()
+    if leave == "pause":
+        m.pool.session_resume(p)
+    m.check()
+
+
 @pytest.mark.parametrize("call", ["resume", "tables"])
 def test_residency_mode_still_waits_after_a_resume(cuda_dev, call):
     """A compaction behind a spin; the session is paused and resumed on another stream (or has a block fetched

@@ -1,0 +1,293 @@
+"""Which of the pool's moves wait for which, without a GPU: the pool runtime over a stand-in for the CUDA runtime
+(fake_streams.cpp) that notes launches, event records and waits. Each move's reads and writes of blocks' rows have to
+come behind those that they would disturb, whatever streams they are on."""
+import atexit
+import ctypes as C
+import functools
+import os
+import random
+import shutil
+import subprocess
+import tempfile
+
+import pytest
+
+from test_pool_setup_host import CSRC, HERE, cuda_include
+
+LAUNCH, RECORD, WAIT, HOST_WAIT = 1, 2, 3, 4
+BT = 16
+
+
+@pytest.fixture(scope="module")
+def kv():
+    import __graft_entry__
+    __graft_entry__.build()
+    from paper_2609_25782_gb300 import kvtier
+    return kvtier
+
+
+@functools.cache
+def built():
+    d = tempfile.mkdtemp()
+    so = os.path.join(d, "pool.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wl,-Bsymbolic", "-I", CSRC, "-I", cuda_include(),
+                    os.path.join(HERE, "fake_streams.cpp"), *(os.path.join(CSRC, x) for x in ("pool.cpp", "pages.cpp", "sparse.cpp")),
+                    "-o", so], check=True)
+    atexit.register(shutil.rmtree, d)
+    return so
+
+
+class Refused(Exception):
+    pass
+
+
+class Pool:
+    """A simple-mode pool, what its moves read and write, and when: a clock per stream, which a wait brings up to what
+    the event has seen."""
+
+    def __init__(self, kv, path, nb=60, sessions=10, **more):
+        x = self.x = C.CDLL(path)
+        for name in set(kv.EXPORTS) - {"decode_attention_noalloc"}:      # (a file of its own)
+            getattr(x, name).argtypes = getattr(kv.lib, name).argtypes
+        x.fake_calls.argtypes, x.fake_calls.restype, x.fake_events.restype = [C.c_void_p, C.c_int64], C.c_int64, C.c_int64
+        x.kv_last_error.restype = C.c_char_p
+        cfg = kv.make_config(num_layers=2, num_hot_blocks=nb, max_sessions=sessions, max_batch=sessions, max_context=1024,
+                             hot_base=1 << 20, cold_base=1 << 21, cold_bytes=1 << 30, block_tokens=BT, **more)
+        self.kv, self.h = kv, C.c_void_p()
+        assert x.kv_pool_create(C.byref(cfg), C.byref(self.h)) == kv.KV_OK
+        self.clocks, self.events, self.host = {}, {}, {}
+        self.past = {}                                   # block -> [(row from, to, writes, stream, tick, what)]
+        self.grown = {}                                  # session -> its stream of reservations' writes, with a clock
+
+    def call(self, name, *a):
+        rc = getattr(self.x, name)(self.h, *a)
+        self.replay()
+        if rc:
+            raise Refused(rc, self.x.kv_last_error())
+
+    def info(self, sid):
+        out = self.kv.kv_session_info()
+        assert self.x.session_info(self.h, sid, C.byref(out)) == 0
+        return out
+
+    def row(self, sid):
+        out, n = (C.c_int32 * 256)(), C.c_int32()
+        assert self.x.session_block_table(self.h, sid, out, 256, C.byref(n)) == 0
+        return list(out[:n.value])
+
+    # order ----------------------------------------------------------------------------
+    def clock(self, stream):
+        return self.clocks.setdefault(stream, {})
+
+    @staticmethod
+    def merge(into, other):
+        for s, t in other.items():
+            into[s] = max(into.get(s, 0), t)
+
+    def tick(self, stream):
+        c = self.clock(stream)
+        self.merge(c, self.host)
+        c[stream] = c.get(stream, 0) + 1
+
+    def replay(self):
+        out = (C.c_int64 * 3000)()
+        n = self.x.fake_calls(out, 1000)
+        assert n <= 1000
+        self.launches = 0
+        for what, stream, event in zip(out[0:3 * n:3], out[1:3 * n:3], out[2:3 * n:3]):
+            if what == LAUNCH:
+                self.tick(stream)
+                self.launches += 1
+            elif what == RECORD:
+                self.merge(self.clock(stream), self.host)
+                self.events[event] = dict(self.clock(stream))
+            elif what == WAIT:
+                self.merge(self.clock(stream), self.events[event])
+            else:
+                self.merge(self.host, self.events[event])
+
+    def synchronise(self):
+        for c in self.clocks.values():
+            self.merge(self.host, c)
+
+    def touch(self, stream, blocks, first, end, writes, what):
+        """Rows of tokens [first, end), which lie in `blocks` (the session's), by the stream's newest launch."""
+        c = self.clock(stream)
+        for j in range(first // BT, -(-end // BT)):
+            lo, hi = max(first, j * BT) - j * BT, min(end, (j + 1) * BT) - j * BT
+            past = self.past.setdefault(blocks[j], [])
+            for l, h, w, s, t, other in past:
+                if l < hi and lo < h and (w or writes):
+                    assert c.get(s, 0) >= t, f"{what} on stream {stream} does not wait for {other} on stream {s}"
+            past.append((lo, hi, writes, stream, c.get(stream, 0), what))
+
+    def caller_orders(self, sid, stream):
+        if sid in self.grown:
+            self.merge(self.clock(stream), self.grown[sid])
+
+    # the calls --------------------------------------------------------------------------
+    def create(self, n=512):
+        sid = C.c_int32()
+        self.call("session_create", n, C.byref(sid))
+        return sid.value
+
+    def append(self, sid, n, st):
+        T = self.info(sid).tokens
+        self.call("session_append", sid, 256, 256, n, st)
+        self.touch(st, self.row(sid), T, T + n, True, f"append({sid})")
+
+    def reserve(self, sids, n, st):
+        """A reservation and, behind it on the stream, the kernel that writes the tokens."""
+        T = [self.info(s).tokens for s in sids]
+        B = len(sids)
+        self.call("kv_pool_batch_reserve_tokens", (C.c_int32 * B)(*sids), (C.c_int32 * B)(*[n] * B), B, 256, 64, 256, st)
+        self.tick(st)
+        for s, t in zip(sids, T):
+            self.touch(st, self.row(s), t, t + n, True, f"reserved tokens({s})")
+            self.grown[s] = dict(self.clock(st))
+
+    def pause(self, sid, st):
+        self.caller_orders(sid, st)
+        i, row = self.info(sid), self.row(sid)
+        self.call("session_pause", sid, st)
+        if i.tokens > i.cold_valid:
+            self.touch(st, row, i.cold_valid, i.tokens, False, f"pause({sid})")
+
+    def resume(self, sid, st):
+        self.call("session_resume", sid, st)
+        self.touch(st, self.row(sid), 0, self.info(sid).tokens, True, f"resume({sid})")
+
+    def fork(self, sid, n, tokens, st):
+        self.caller_orders(sid, st)
+        out = (C.c_int32 * n)()
+        self.call("session_fork", sid, tokens, 512, n, out, st)
+        for k in out if tokens % BT else ():
+            self.touch(st, self.row(sid), tokens // BT * BT, tokens, False, f"fork of {sid}")
+            self.touch(st, self.row(k), tokens // BT * BT, tokens, True, f"fork to {k}")
+        return list(out)
+
+    def truncate(self, sid, tokens, st):
+        self.caller_orders(sid, st)
+        old = self.row(sid)
+        self.call("session_truncate", sid, tokens, st)
+        row = self.row(sid)
+        if row and row[-1] != old[len(row) - 1]:
+            self.touch(st, old, tokens // BT * BT, tokens, False, f"truncation of {sid}")
+            self.touch(st, row, tokens // BT * BT, tokens, True, f"truncation of {sid}")
+
+    def compact(self, sid, n, prefix, st):
+        self.caller_orders(sid, st)
+        T, old = self.info(sid).tokens, self.row(sid)
+        self.call("session_compact", sid, 256, 0, 0, n, prefix, st)
+        if not n or prefix + n == T:
+            return
+        row = self.row(sid)
+        first = prefix if row[prefix // BT] == old[prefix // BT] else prefix // BT * BT
+        past, self.past = self.past, {b: list(x) for b, x in self.past.items()}
+        self.touch(st, old, first, T, False, f"compaction of {sid}")
+        read, self.past = self.past, past
+        self.touch(st, row, first, prefix + n, True, f"compaction of {sid}")
+        for b, x in read.items():                        # (its own reads and writes are one kernel's)
+            self.past.setdefault(b, []).extend(y for y in x if y not in self.past[b])
+
+    def destroy(self, sid):
+        self.synchronise()
+        self.grown.pop(sid, None)
+        self.call("session_destroy", sid)
+
+
+@pytest.fixture()
+def pool(kv, tmp_path):
+    """A pool runtime of the test's own: a copy of the library has its variables at their start."""
+    return Pool(kv, shutil.copy(built(), tmp_path / "pool.so"))
+
+
+A, B, G, H = 11, 22, 33, 44              # streams
+
+
+def shared(pool, tokens=208):
+    """A session and a fork that shares all of its blocks."""
+    p = pool.create()
+    pool.append(p, tokens, G)
+    k, = pool.fork(p, 1, tokens, G)
+    pool.synchronise()
+    return p, k
+
+
+@pytest.mark.parametrize("n,prefix", [(207, 0), (100, 0), (20, 187), (60, 70)])
+def test_a_compaction_waits_for_a_former_holders_pause(pool, n, prefix):
+    p, k = shared(pool)
+    pool.pause(p, A)
+    pool.compact(k, n, prefix, B)
+    pool.append(k, 5, H)
+
+
+@pytest.mark.parametrize("n,prefix", [(207, 0), (100, 0), (20, 187), (60, 70)])
+def test_a_compaction_waits_for_a_former_holders_compaction(pool, n, prefix):
+    p, k = shared(pool)
+    pool.compact(p, 150, 10, A)
+    pool.compact(k, n, prefix, B)
+    pool.append(k, 5, H)
+
+
+@pytest.mark.parametrize("grow", ["append", "reserve"])
+@pytest.mark.parametrize("tokens", [200, 193, 100, 1])
+@pytest.mark.parametrize("leave", ["pause", "compact", "truncate"])
+def test_tokens_behind_a_cut_wait_for_a_former_holders_move(pool, leave, tokens, grow):
+    p, k = shared(pool)
+    if leave == "pause":
+        pool.pause(p, A)
+    elif leave == "compact":
+        pool.compact(p, 150, 0, A)
+    else:
+        pool.truncate(p, tokens, A)
+    pool.truncate(k, tokens, B)
+    pool.append(k, 8, H) if grow == "append" else pool.reserve([k], 8, H)
+    pool.append(k, 8, A)
+
+
+def test_a_fork_of_a_block_that_was_shared(pool):
+    """The fork reads a part of a block that a third session then writes."""
+    p, k = shared(pool)
+    f, = pool.fork(k, 1, 203, A)
+    pool.pause(k, B)
+    pool.truncate(p, 202, G)
+    pool.append(p, 9, H)
+    pool.append(f, 9, G)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_moves_on_several_streams(pool, seed):
+    r = random.Random(seed)
+    live, done = {}, {}                                  # session -> the stream that it grows on
+    for step in range(700):
+        st, op = r.choice([A, B, G, H]), r.choice(["create", "append", "append", "reserve", "pause", "resume", "fork", "fork",
+                                                   "truncate", "truncate", "compact", "destroy"])
+        sid = r.choice(list(live)) if live else None
+        try:
+            if op == "create" or sid is None:
+                live[pool.create()] = r.choice([A, B, G, H])
+            elif op == "append":
+                pool.append(sid, r.choice([1, 7, 16, 60]), live[sid])
+            elif op == "reserve":
+                pool.reserve([s for s in live if live[s] == live[sid] and (s == sid or r.random() < 0.5)], r.choice([1, 20]), live[sid])
+            elif op in ("pause", "resume"):
+                getattr(pool, op)(sid, st)
+            elif op == "fork":
+                T = pool.info(sid).tokens
+                for k in pool.fork(sid, r.choice([1, 2]), r.choice([T, T // BT * BT, r.randrange(T + 1)]), st):
+                    live[k] = r.choice([A, B, G, H])
+            elif op == "truncate":
+                T = pool.info(sid).tokens
+                pool.truncate(sid, max(0, T - r.choice([1, 5, 9, 30, 200])), st)
+            elif op == "compact":
+                T = pool.info(sid).tokens
+                prefix = r.randrange(T + 1)
+                pool.compact(sid, r.choice([T - prefix, max(0, T - prefix - 1), r.randrange(T - prefix + 1)]), prefix, st)
+            elif r.random() < 0.5:
+                pool.destroy(sid)
+                del live[sid]
+            done[op] = done.get(op, 0) + 1
+        except Refused:                                  # full, or in another state
+            pass
+    assert all(done.get(x, 0) > 5 for x in ("append", "reserve", "pause", "resume", "fork", "truncate", "compact"))
