@@ -136,6 +136,7 @@ int session_fork(kv_pool *p, int32_t sid, int64_t tokens, int64_t max_tokens, in
     if (p->lru ? !p->plan_evict(need, {sid}, vic) : need > static_cast<int64_t>(p->free_list.size()))
         return fail(KV_ERR_NO_HOT_BLOCKS, "hot pool has too few blocks for the fork");
     std::vector<int32_t> kids;
+    int64_t fetched = 0;                          // tokens out of the parent's image
     int rc = KV_OK;
     while (!rc && static_cast<int32_t>(kids.size()) < n) {
         int32_t id = -1;
@@ -160,6 +161,7 @@ int session_fork(kv_pool *p, int32_t sid, int64_t tokens, int64_t max_tokens, in
                     kvt::BlockJob b = p->job_for(sid, jj, to, 0, rows);   // out of the parent's image
                     b.sid = kids[c];
                     fetches.push_back(b);
+                    fetched += rows;
                 }
             }
         for (size_t c = 0; !rc && c < kids.size(); ++c) rc = ensure_event(p, &p->sessions[kids[c]].ready);
@@ -182,6 +184,7 @@ int session_fork(kv_pool *p, int32_t sid, int64_t tokens, int64_t max_tokens, in
 
     p->evict_commit(vic);
     take(p, got);
+    p->stats.bytes_unpacked += fetched * p->image_token_bytes;
     parent->ready_recorded = parent->moved = !p->host_only;
     for (int64_t j = 0; j < shared; ++j) p->block_extra[parent->blocks[j]] += n;
     p->forked = p->forked || shared > 0;

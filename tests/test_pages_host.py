@@ -133,6 +133,35 @@ def test_fork_in_residency_mode_owns_its_blocks(kv):
     kv.kv_pool_destroy(pool)
 
 
+@pytest.mark.parametrize("bt", [16, 64])
+@pytest.mark.parametrize("int8", [False, True])
+def test_what_a_fork_reads_from_an_image_counts(kv, int8, bt):
+    """bytes_unpacked: evicted blocks of the parent, once for each new session, by the image's bytes a token."""
+    cfg = kv.make_config(num_layers=2, num_hot_blocks=30, block_tokens=bt, alloc_seed=7, max_sessions=10, max_context=4096,
+                         cold_bytes=1 << 30, flags=kv.KV_POOL_HOST_LOGIC_ONLY | kv.KV_POOL_LRU_RESIDENCY |
+                         (kv.KV_POOL_COLD_INT8 if int8 else 0))
+    pool = kv.kv_pool_create(cfg)
+    token = 2 * 2 * 4 * (129 if int8 else 256)
+    p, o = kv.session_create(pool, 10 * bt), kv.session_create(pool, 30 * bt)
+    reserve(kv, pool, p, 6 * bt + 5)
+    kv.session_fork(pool, p, 6 * bt + 5, 7 * bt, 1)      # nothing has left yet
+    assert kv.kv_pool_get_stats(pool)["bytes_unpacked"] == 0
+    kv.session_truncate(pool, 2, 0)
+    reserve(kv, pool, o, 27 * bt)                        # 3 free: p's first four blocks leave
+    assert kv.session_block_table(pool, p)[:4] == [-1] * 4 and kv.session_info(pool, p).num_blocks == 3
+    kv.session_truncate(pool, o, 15 * bt)
+    kv.session_fork(pool, p, 6 * bt + 5, 7 * bt, 1)      # four blocks from the image
+    assert kv.kv_pool_get_stats(pool)["bytes_unpacked"] == 4 * bt * token
+    kv.session_truncate(pool, 3, 0)
+    kv.session_fork(pool, p, 2 * bt + 3, 7 * bt, 2)      # a part of the third one
+    assert kv.kv_pool_get_stats(pool)["bytes_unpacked"] == (4 * bt + 2 * (2 * bt + 3)) * token
+    before = kv.kv_pool_get_stats(pool)["bytes_unpacked"]
+    refused(kv, kv.KV_ERR_NO_HOT_BLOCKS, kv.session_fork, pool, p, 6 * bt + 5, 7 * bt, 5)
+    assert kv.kv_pool_get_stats(pool)["bytes_unpacked"] == before
+    check(kv, pool, 30, True, bt)
+    kv.kv_pool_destroy(pool)
+
+
 def test_fork_refusals_change_nothing(kv):
     pool = host_pool(kv, nb=8, sessions=4, cold=800 * 4096)       # images of 800 tokens
     p = kv.session_create(pool, 200)
