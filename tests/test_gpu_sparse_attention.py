@@ -225,6 +225,22 @@ def test_numpy_int_arguments_are_plain_numbers(cuda_dev):
     assert c.pool.check_device() == 0
 
 
+@pytest.mark.parametrize("kind", [np.int64, np.int32])
+def test_numpy_numbers_give_the_same_results(cuda_dev, kind):
+    c = Cache([400, 90], seed=15)
+    c.make_bounds()
+    c.select(6)
+    want = c.selected.clone(), c.scores.clone(), c.attend().clone()
+    c.selected.fill_(12345), c.scores.fill_(7.0), c.out.fill_(7.0)
+    c.pool.select_blocks(kind(0), c.q, c.bounds, c.tables, c.lens, kind(2), kind(c.width), c.selected, first=kind(1), last=kind(1),
+                         scores=c.scores)
+    c.pool.sparse_attention(kind(0), c.q, c.selected, c.tables, c.lens, kind(2), kind(c.width), np.float64(c.scale), c.out)
+    assert c.pool.check_device() == 0
+    assert torch.equal(c.selected, want[0]) and torch.equal(c.scores, want[1]) and torch.equal(c.out, want[2])
+    for b in range(2):
+        c.assert_right(b, *c.reference(b))
+
+
 def test_a_wait_that_runs_out(cuda_dev):
     """The hook's one call reports it and ends, the next ones are right; a context that goes on."""
     from paper_2609_25782_gb300 import kvtier

@@ -103,6 +103,27 @@ def test_strides_and_shapes_reach_the_library(package, native):
 
 
 @BOTH
+def test_numpy_numbers_are_numbers(package, native):
+    """The module in C leaves them to the checks in Python; the library gets the same numbers."""
+    import numpy as np
+    pool = make_pool(package, native)
+    a = arguments(pool)
+    for kind in (np.int64, np.int32):
+        pool.native = 0
+        for f in (select, attend):
+            assert f(pool, **dict(a, B=kind(3), width=kind(6)))[1:] == f(pool, **a)[1:]
+        pool.calls.clear()
+        pool.select_blocks(kind(1), a["q"], a["bounds"], a["tables"], a["lens"], kind(3), 6, a["selected"], kind(1), kind(2), a["scores"])
+        assert pool.calls[0][1:] == select(pool, **a)[1:]
+        pool.calls.clear()
+        pool.sparse_attention(kind(1), a["q"], a["selected"], a["tables"], a["lens"], 3, kind(6), np.float32(0.5), a["out"], a["k"], a["v"])
+        assert pool.calls[0][1:] == attend(pool, **a)[1:]
+        assert pool.native == (4 if native else 0)       # the plain calls
+        refused(pool, select, **dict(a, B=kind(2)))
+        refused(pool, attend, **dict(a, width=kind(7)))
+
+
+@BOTH
 def test_tensors_that_the_library_would_misread(package, native):
     pool = make_pool(package, native)
     i32 = torch.int32
