@@ -107,11 +107,7 @@ void unmake(kv_pool *p, int32_t sid) {
     Session &s = p->sessions[sid];
     p->cold_release(s.img_off, s.img_bytes);
     p->stats.cold_bytes_used = p->cold_used;
-    const cudaEvent_t ready = s.ready, appended = s.appended, packed = s.packed;
-    s = Session{};
-    s.ready = ready;
-    s.appended = appended;
-    s.packed = packed;
+    s.reset();
 }
 
 }  // namespace

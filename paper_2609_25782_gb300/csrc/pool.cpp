@@ -220,7 +220,7 @@ int kvt::create_session(kv_pool *p, int64_t max_tokens, int64_t tokens, int32_t 
     if (!p->cold_alloc(bytes, &off))
         return fail(KV_ERR_NO_COLD_SPACE, "cold arena cannot hold the session image");
     Session &s = p->sessions[sid];
-    s = Session{};
+    s.reset();
     s.state = state;
     s.cap = max_tokens;
     s.T = tokens;
@@ -264,11 +264,7 @@ int session_destroy(kv_pool *p, int32_t sid) {
     p->stats.used_blocks -= freed;
     p->cold_release(s->img_off, s->img_bytes);
     p->stats.cold_bytes_used = p->cold_used;
-    cudaEvent_t ready = s->ready, appended = s->appended, packed = s->packed;
-    *s = Session{};
-    s->ready = ready;   // events are kept for reuse by the next session in this slot
-    s->appended = appended;
-    s->packed = packed;
+    s->reset();
     return KV_OK;
 }
 

@@ -38,6 +38,15 @@ struct Session {
     bool packed_recorded = false;     // the image (it covers every earlier one)
     int16_t pack_fence = -1;          // simple mode: fence slot and generation of the
     uint64_t pack_gen = 0;            // last pause's pack (it reads the table row)
+
+    // Nobody's again. Its events stay, for the next session of this id.
+    void reset() {
+        Session fresh;
+        fresh.ready = ready;
+        fresh.appended = appended;
+        fresh.packed = packed;
+        *this = std::move(fresh);
+    }
 };
 
 // A planned eviction: block j of session sid leaves hot slot `slot`; tokens

@@ -94,6 +94,7 @@ class Pool:
         n = self.x.fake_calls(out, 1000)
         assert n <= 1000
         self.launches = 0
+        self.waits = out[0:3 * n:3].count(WAIT)
         for what, stream, event in zip(out[0:3 * n:3], out[1:3 * n:3], out[2:3 * n:3]):
             if what == LAUNCH:
                 self.tick(stream)
@@ -254,6 +255,35 @@ def test_a_fork_of_a_block_that_was_shared(pool):
     pool.truncate(p, 202, G)
     pool.append(p, 9, H)
     pool.append(f, 9, G)
+
+
+def test_a_sessions_events_serve_the_next_one_of_its_id(pool):
+    p = pool.create()
+    pool.append(p, 100, G)
+
+    def branches():
+        for k in pool.fork(p, 3, 90, A):
+            pool.append(k, 20, A)
+            pool.destroy(k)
+    branches()
+    made = pool.x.fake_events()
+    for _ in range(20):
+        branches()
+    assert pool.x.fake_events() == made
+    assert pool.x.kv_pool_destroy(pool.h) == 0 and pool.x.fake_events() == 0
+
+
+def test_a_new_session_waits_for_nothing_of_its_ids_last_one(pool):
+    p = pool.create()
+    pool.append(p, 30, G)
+    k, = pool.fork(p, 1, 20, A)
+    pool.append(k, 5, A)
+    pool.destroy(k)
+    assert pool.create() == k
+    ev = C.c_void_p(1)
+    assert pool.x.session_ready_event(pool.h, k, C.byref(ev)) == 0 and ev.value is None
+    pool.append(k, 5, B)
+    assert pool.waits == 0
 
 
 @pytest.mark.parametrize("seed", range(12))
