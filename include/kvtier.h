@@ -504,7 +504,8 @@ int session_truncate(kv_pool *pool, int32_t sid, int64_t tokens, kv_stream_t str
  * everything and moves nothing. A position out of range, or not above the one
  * before it, sets KV_DEVICE_BAD_INDEX; that layer and head's rows from there on are
  * then undefined. Waits and ordering as session_truncate. Errors: KV_ERR_BAD_STATE
- * (paused), KV_ERR_NO_HOT_BLOCKS. */
+ * (paused), KV_ERR_NO_HOT_BLOCKS; KV_ERR_CUDA by a launch or an event record that
+ * fails after a first launch leaves the tokens from prefix on undefined. */
 int session_compact(kv_pool *pool, int32_t sid, const int32_t *keep, int64_t layer_stride,
                     int64_t head_stride, int32_t n, int64_t prefix, kv_stream_t stream);
 

@@ -25,11 +25,10 @@ int wait_written(kv_pool *p, const Session &s, cudaStream_t st) {
 }
 
 // Behind work that reads or moves a session's rows: whatever the pool does with the session next, on any
-// stream, waits for it. The stream has waited for what the event marked before (wait_written).
+// stream, waits for it. The stream has waited for what the event marked before (wait_written); the event is made
+// before the work is launched, so that a call which cannot have one moves nothing.
 int mark_moved(kv_pool *p, Session &s, cudaStream_t st) {
-    int rc = ensure_event(p, &s.ready);
-    if (!rc) rc = p->cuda("cudaEventRecord", [&] { return cudaEventRecord(s.ready, st); });
-    return rc;
+    return p->cuda("cudaEventRecord", [&] { return cudaEventRecord(s.ready, st); });
 }
 
 // Copies of blocks and the children's first table entries, as many launches as their parameters take.
@@ -161,6 +160,7 @@ int session_fork(kv_pool *p, int32_t sid, int64_t tokens, int64_t max_tokens, in
                 }
             }
         for (size_t c = 0; !rc && c < kids.size(); ++c) rc = ensure_event(p, &p->sessions[kids[c]].ready);
+        if (!rc) rc = ensure_event(p, &parent->ready);
         if (!rc) rc = wait_written(p, *parent, st);
         if (!rc) rc = p->wait_fences(got.data(), got.size(), st);
         if (!rc) rc = p->evict_device(vic, st);
@@ -223,7 +223,8 @@ int session_truncate(kv_pool *p, int32_t sid, int64_t tokens, kv_stream_t stream
         cudaStream_t st = reinterpret_cast<cudaStream_t>(stream_);
         DeviceGuard dg(p->cfg.device, !p->host_only);
         int f = 0;
-        int rc = p->open_fence(gone.data(), gone.size(), st, &f);
+        int rc = own || left ? ensure_event(p, &s->ready) : KV_OK;
+        if (!rc) rc = p->open_fence(gone.data(), gone.size(), st, &f);
         if (!rc) rc = wait_written(p, *s, st);
         if (!rc && own) {
             rc = p->wait_fences(got.data(), got.size(), st);
@@ -294,7 +295,8 @@ int session_compact(kv_pool *p, int32_t sid, const int32_t *keep, int64_t layer_
     for (int64_t j = j0; j < j1; ++j) (slot[j - j0] >= 0 ? gone : kept).push_back(s->blocks[j]);
 
     int f = 0;
-    int rc = p->open_fence(gone.data(), gone.size(), st, &f);
+    int rc = ensure_event(p, &s->ready);
+    if (!rc) rc = p->open_fence(gone.data(), gone.size(), st, &f);
     if (!rc) rc = wait_written(p, *s, st);
     if (!rc) rc = p->wait_fences(got.data(), got.size(), st);
     if (!rc && p->forked) rc = p->wait_fences(kept.data(), kept.size(), st);   // written in place

@@ -273,6 +273,36 @@ def test_a_sessions_events_serve_the_next_one_of_its_id(pool):
     assert pool.x.kv_pool_destroy(pool.h) == 0 and pool.x.fake_events() == 0
 
 
+@pytest.mark.parametrize("call", ["fork", "truncate", "compact", "compact of shared blocks"])
+def test_calls_that_cannot_have_an_event_launch_nothing(pool, call):
+    p = pool.create()
+    pool.append(p, 200, G)
+    other = pool.create()
+    pool.append(other, 200, G)
+    if call != "compact":
+        f, = pool.fork(other, 1, 200, G)
+        g, = pool.fork(f, 1, 192, G)                     # 12 shared blocks; its events are made anew below
+        pool.destroy(f)
+        p = g if call != "fork" else p
+    calls = {"fork": lambda: pool.call("session_fork", p, 150, 512, 2, (C.c_int32 * 2)(), A),
+             "truncate": lambda: pool.call("session_truncate", p, 100, A)}
+    f = calls.get(call, lambda: pool.call("session_compact", p, 256, 0, 0, 100, 20, A))
+    failed = 0
+    while True:
+        before = [pool.info(s).tokens for s in (p, other)], pool.row(p), pool.row(other)
+        pool.x.fake_fail_create(failed + 1)
+        try:
+            f()
+            break
+        except Refused as e:
+            assert e.args[0] == pool.kv.KV_ERR_CUDA and b"EventCreate" in e.args[1]
+            assert pool.launches == 0
+            assert ([pool.info(s).tokens for s in (p, other)], pool.row(p), pool.row(other)) == before
+        failed += 1
+    pool.x.fake_fail_create(0)
+    assert failed >= 1 and pool.launches >= 1
+
+
 def test_a_new_session_waits_for_nothing_of_its_ids_last_one(pool):
     p = pool.create()
     pool.append(p, 30, G)
