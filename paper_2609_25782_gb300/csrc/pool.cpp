@@ -654,7 +654,6 @@ static int turn_setup(kv_pool *p, bool cuts) {
             if (e == cudaSuccess) p->d_turn_part = static_cast<float *>(part);
             return e;
         });
-    if (rc) cudaGetLastError();   // a later launch asks for its own
     cudaThreadExchangeStreamCaptureMode(&mode);
     return rc;
 }

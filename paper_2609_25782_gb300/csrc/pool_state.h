@@ -142,15 +142,18 @@ struct kv_pool {
     std::set<std::pair<uint64_t, int32_t>> lru_set;
 
     // Every CUDA call of the pool goes through here: the failure-injection
-    // hook fires first, then (unless the pool is host-logic only) the call.
+    // hook fires first, then (unless the pool is host-logic only) the call. A failing call is
+    // told of once, here.
     template <typename F>
     int cuda(const char *what, F &&fn) {
         if (inject_countdown > 0 && --inject_countdown == 0)
             return kvt::fail(KV_ERR_CUDA, std::string(what) + ": injected CUDA failure");
         if (host_only) return KV_OK;
         cudaError_t e = fn();
-        if (e != cudaSuccess)
+        if (e != cudaSuccess) {
+            cudaGetLastError();   // a later launch asks for its own
             return kvt::fail(KV_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
+        }
         return KV_OK;
     }
 

@@ -303,6 +303,25 @@ def test_calls_that_cannot_have_an_event_launch_nothing(pool, call):
     assert failed >= 1 and pool.launches >= 1
 
 
+@pytest.mark.parametrize("call", ["select", "attend", "append"])
+def test_a_failing_call_is_told_of_once(pool, call):
+    """The runtime's last error is gone: a launch that asks for it finds its own."""
+    p = pool.create()
+    calls = {"select": lambda: pool.call("select_blocks", 0, 256, 0, 256, 256, 256, 1, 4, 1, 1, 2, 256, None, A),
+             "attend": lambda: pool.call("sparse_attention", 0, 256, 0, None, None, 0, 256, 2, 256, 256, 1, 4, 1.0, 256, 0, A),
+             "append": lambda: pool.append(p, 5, A)}
+    no_resources = 101
+    pool.x.fake_prepare_status(no_resources)
+    pool.x.fake_fail_create(1)
+    with pytest.raises(Refused) as e:
+        calls[call]()
+    assert e.value.args[0] == pool.kv.KV_ERR_CUDA and pool.launches == 0 and pool.x.fake_last_error() == 0
+    pool.x.fake_prepare_status(0)
+    pool.x.fake_fail_create(0)
+    calls[call]()                                        # and it may go on
+    assert pool.launches >= 1
+
+
 def test_a_new_session_waits_for_nothing_of_its_ids_last_one(pool):
     p = pool.create()
     pool.append(p, 30, G)
