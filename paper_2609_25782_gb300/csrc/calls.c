@@ -3,7 +3,8 @@
  * GPU 5.7 us; a pass took 11.3 with the checks in Python, as the host needed that long, and takes 8.2 here.
  *
  * A method returns the library's code, or None where an argument is not plainly what the call takes: then nothing was
- * called, and Pool's own checks say what is wrong (or take what is unusual). */
+ * called, and Pool's own checks say what is wrong (or take what is unusual). An interrupt or a lack of memory that comes
+ * up meanwhile is passed on. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
@@ -123,6 +124,7 @@ static int stream_of(PyObject *x, void **to) {
 }
 
 static PyObject *declined(void) {
+    if (PyErr_Occurred() && (!PyErr_ExceptionMatches(PyExc_Exception) || PyErr_ExceptionMatches(PyExc_MemoryError))) return NULL;
     PyErr_Clear();
     Py_RETURN_NONE;
 }
@@ -167,7 +169,7 @@ static PyObject *calls_sparse(Calls *c, PyObject *const *a, Py_ssize_t n) {
         return declined();
     if (a[9] == Py_None && a[10] != Py_None) return declined();
     const int half = is_dtype(a[8], c->bf16);
-    if ((!half && !is_dtype(a[8], c->f32)) || !has_shape(a[8], B, c->Hq, kDim) || !is_contiguous(a[8]) || !place(c, a[8], &out))
+    if (PyErr_Occurred() || (!half && !is_dtype(a[8], c->f32)) || !has_shape(a[8], B, c->Hq, kDim) || !is_contiguous(a[8]) || !place(c, a[8], &out))
         return declined();
     if (!stream_of(a[11], &stream)) return declined();
     const float scale = (float)PyFloat_AS_DOUBLE(a[7]);

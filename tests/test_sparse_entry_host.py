@@ -103,6 +103,35 @@ def test_strides_and_shapes_reach_the_library(package, native):
 
 
 @BOTH
+@pytest.mark.parametrize("error", [KeyboardInterrupt, SystemExit, MemoryError])
+def test_an_interrupt_during_the_checks_is_not_lost(package, native, error):
+    """It comes up once, where a tensor is asked for something; an error of another kind is the checks' own to find."""
+    pool = make_pool(package, native)
+
+    class Once(torch.Tensor):
+        left = 0
+
+        @property
+        def dtype(self):
+            if Once.left:
+                Once.left -= 1
+                raise Once.error("once")
+            return super().dtype
+    a = arguments(pool)
+    for f, names in ((select, ("q", "tables", "lens", "selected", "scores")), (attend, ("q", "k", "v", "tables", "lens", "selected", "out"))):
+        for name in names:
+            x = a[name].as_subclass(Once)
+            Once.left, Once.error = 1, error
+            pool.calls.clear()
+            with pytest.raises(error):
+                f(pool, **dict(a, **{name: x}))
+            assert not pool.calls and not Once.left, name
+            if native:
+                Once.left, Once.error = 1, TypeError     # (without the module the checks pass it on)
+                assert f(pool, **dict(a, **{name: x}))[1:] == f(pool, **a)[1:] and not Once.left
+
+
+@BOTH
 def test_numpy_numbers_are_numbers(package, native):
     """The module in C leaves them to the checks in Python; the library gets the same numbers."""
     import numpy as np
