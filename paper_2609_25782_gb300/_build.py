@@ -1,5 +1,5 @@
 """Compile libkvtier.so in-tree with nvcc for sm_103a, and with the C compiler the
-module that Pool's calls per layer go through (_calls.so, where Python's headers are).
+module that Pool's calls per layer go through (_calls, where Python's headers are).
 
 The translation units (SOURCES) compile in parallel and are linked with the static CUDA runtime,
 so the library needs only the driver at run time.
@@ -7,6 +7,7 @@ so the library needs only the driver at run time.
 from __future__ import annotations
 
 import os
+import shlex
 import shutil
 import subprocess
 import sys
@@ -15,7 +16,8 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvtier.so")
-CALLS = os.path.join(HERE, "_calls.so")
+# Named for this Python: another one in the same tree builds its own and does not load it.
+CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 PYTHON_H = os.path.join(sysconfig.get_paths()["include"], "Python.h")
 SOURCES = ["decode_kernels.cu", "turn_kernels.cu", "copy_kernels.cu", "sparse_kernels.cu",
            "attend_kernels.cu", "page_kernels.cu", "pool.cpp", "pages.cpp", "sparse.cpp", "noalloc.cu"]
@@ -29,6 +31,11 @@ def nvcc() -> str:
         if cand and os.path.exists(cand):
             return cand
     raise RuntimeError("nvcc not found: the CUDA toolkit is required to build libkvtier.so")
+
+
+def calls_command(to: str) -> list[str]:
+    return [*shlex.split(os.environ.get("CC") or "gcc"), "-O2", "-shared", "-fPIC", "-I", os.path.dirname(PYTHON_H),
+            os.path.join(CSRC, "calls.c"), "-o", to]
 
 
 def _stale() -> bool:
@@ -59,9 +66,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
                                             stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
                                             text=True)))
     if os.path.exists(PYTHON_H):
-        cmd = [os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-I", os.path.dirname(PYTHON_H),
-               os.path.join(CSRC, "calls.c"), "-o", CALLS + ".tmp"]
-        procs.append(("calls.c", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+        procs.append(("calls.c", subprocess.Popen(calls_command(CALLS + ".tmp"), stdout=subprocess.PIPE,
+                                                  stderr=subprocess.STDOUT, text=True)))
     for src, p in procs:
         out, _ = p.communicate()
         if p.returncode != 0:

@@ -1,6 +1,7 @@
 """What the calls on bounds, selections and lists hand to the library, and what they and the library refuse,
 without a GPU."""
 import ctypes as C
+import os
 
 import pytest
 import torch
@@ -44,6 +45,24 @@ def make_pool(package, native, hq=8, hkv=2, layers=3, blocks=5):
         p._calls = package.kvtier._calls.Calls(77, -1, hq, hkv, p.bounds_bytes, BF, torch.int32, torch.float32,
                                                *map(package.kvtier.address, p.keep))
     return p
+
+
+@pytest.mark.parametrize("cc", [None, "", "gcc", "env gcc -g", "env 'CCACHE_DIR=/a b' gcc"])
+def test_the_module_is_built_by_any_compiler_command(package, monkeypatch, tmp_path, cc):
+    """CC as make and others take it, words and quotes; the file is named for this Python."""
+    import importlib.machinery
+    import subprocess
+
+    from paper_2609_25782_gb300 import _build
+    if not os.path.exists(_build.PYTHON_H):
+        pytest.skip("built without Python's headers")
+    monkeypatch.delenv("CC", raising=False)
+    if cc is not None:
+        monkeypatch.setenv("CC", cc)
+    subprocess.run(_build.calls_command(str(tmp_path / "calls.so")), check=True)
+    assert (tmp_path / "calls.so").exists()
+    tagged = importlib.machinery.EXTENSION_SUFFIXES[0]
+    assert _build.CALLS.endswith("_calls" + tagged) and package.kvtier._calls.__file__.endswith("_calls" + tagged)
 
 
 BOTH = pytest.mark.parametrize("native", [False, True])
