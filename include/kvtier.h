@@ -383,10 +383,15 @@ int64_t kv_bounds_bytes(const kv_pool_config *cfg);
  *   codes in -127 .. 127. A block with a K that is not finite gets step = inf,
  *   codes 127 and -127.
  * A block's bounds go by its physical id, so forks share them with the blocks.
- * They stay as they are until the call is made again: after tokens were
- * written, blocks came back (a resume; in residency mode any call that fetches,
- * kv_pool_stats.batch_blocks_fetched) or a session was compacted, it is due for
- * those blocks, unless select_blocks is told to take them anyway (first, last).
+ * They stay as they are until the call is made again. It is due, unless
+ * select_blocks is told to take the blocks anyway (first, last), for blocks that
+ *   - tokens were written to, or rows moved in (session_compact, from prefix on);
+ *   - came back into other slots: all of a session's by session_resume; in
+ *     residency mode those that a call fetched, whichever it was (kv_pool_stats:
+ *     bytes_unpacked grows);
+ *   - are copies: the one that a fork's tokens end in (in residency mode all of
+ *     a fork's), the one that a truncation into a shared block leaves.
+ * A truncation that copies nothing leaves bounds that still hold, if wider.
  *   block_tables device int32 [B][max_blocks]
  *   seq_lens     device int32 [B], 0 (nothing) .. max_blocks * bt (and 2^31 - 513)
  *   since        device int32 [B] or NULL: tokens of the row whose bounds are
@@ -465,17 +470,18 @@ int sparse_attention(kv_pool *pool, int32_t layer, const void *q, int64_t q_stri
  * read, and go back to the free list with the last of them; a session that alone
  * holds such a block in the end writes it again (a compaction, tokens behind a
  * truncation) only behind the moves by which the others left it, whatever streams
- * those were on. The block that
- * `tokens` ends in is copied into one block per new session. In residency mode a
- * block has one owner, whom an eviction takes it from: there all blocks are
- * copied, evicted ones read from the parent's image. A fork's image is its own
- * and empty: its first pause writes all of its tokens.
+ * those were on. The block that `tokens` ends in is copied into one block per new
+ * session. In residency mode a block has one owner, whom an eviction takes it
+ * from: there all blocks are copied, evicted ones read from the parent's image. A
+ * fork's image is its own and empty: its first pause writes all of its tokens.
  * The stream first waits for the parent's last append and resume; order the call
- * after the attention calls that write tokens which the parent has reserved. The
- * parent's and the new sessions' ready events are recorded on the stream. Free-list
- * pops go session by session, in logical order. Errors: KV_ERR_BAD_STATE (paused),
- * KV_ERR_NO_HOT_BLOCKS, KV_ERR_NO_COLD_SPACE (n images), too many sessions ->
- * KV_ERR_INVALID_ARG. All or nothing. */
+ * after the attention calls that write tokens which the parent has reserved and,
+ * in residency mode, after a kv_pool_batch_tables or kv_pool_batch_reserve call
+ * that fetches blocks of the parent. The parent's and the new sessions' ready
+ * events are recorded on the stream. Free-list pops go session by session, in
+ * logical order. Errors: KV_ERR_BAD_STATE (paused), KV_ERR_NO_HOT_BLOCKS,
+ * KV_ERR_NO_COLD_SPACE (n images), too many sessions -> KV_ERR_INVALID_ARG. All
+ * or nothing. */
 int session_fork(kv_pool *pool, int32_t sid, int64_t tokens, int64_t max_tokens, int32_t n,
                  int32_t *sids_out, kv_stream_t stream);
 
