@@ -232,9 +232,11 @@ struct GatherArgs {
 };
 
 // How many clusters of 1, 2, 4, 8 and 16 CTAs the device holds at once, for the kernels of select_blocks (one CTA per
-// SM in [1], two in [0]) and for that of sparse_attention with a CTA per SM.
+// SM in [1], two in [0], whose rows then have at most pair_blocks blocks) and for that of sparse_attention with a CTA
+// per SM.
 struct SelectFit {
     int clusters[2][5];
+    int pair_blocks;
 };
 struct SparseFit {
     int clusters[5];

@@ -622,6 +622,12 @@ cudaError_t prepare_select_kernel(SelectFit *fit) {
     for (int two = 0; two < 2 && e == cudaSuccess; ++two)
         e = fit_clusters(two ? select_kernel<true> : select_kernel<false>, kSelectThreads, select_smem(kSelectBlocksMax),
                          select_smem(8192), fit->clusters[two]);
+    // The longest rows of which two CTAs still share an SM: their keys are in shared memory.
+    fit->pair_blocks = 0;
+    for (int blocks = 8192, ctas = 2; e == cudaSuccess && ctas >= 2 && blocks <= kSelectBlocksMax; blocks += 1024) {
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, select_kernel<false>, kSelectThreads, select_smem(blocks));
+        if (e == cudaSuccess && ctas >= 2) fit->pair_blocks = blocks;
+    }
     return e;
 }
 
@@ -629,11 +635,13 @@ cudaError_t launch_select(const SelectArgs &a, const SelectFit &fit, cudaStream_
     // The largest clusters that are all resident at once, of at least 64 blocks a CTA. us with the widest that fits
     // and the next wider one (rotating inputs): 8 units of 1 250 blocks 6.5 (8 CTAs) and 10.0, 32 of up to 7 500 14.4
     // (4) and 18.1, 64 of up to 1 875 9.0 (2) and 13.2. Too many units for two CTAs of an SM each: two to an SM, 512
-    // units of up to 1 250 28.4, by CTAs of an SM each 32.0.
+    // units of up to 1 250 28.4, by CTAs of an SM each 32.0. Where the tables are too wide for two to an SM, CTAs of an
+    // SM each and no clusters: 152 units of 1 250 blocks in tables of 40 000 13.1, as if two still shared an SM 22.9;
+    // 512 units of 40 000 blocks 660 and 938.
     const int64_t units = static_cast<int64_t>(a.B) * a.s.Hkv;
     int two = 1, log = 4;
     while (log > 0 && (units > fit.clusters[1][log] || a.max_blocks < 64 << log)) --log;
-    if (log == 0 && units > fit.clusters[1][0] / 2) {
+    if (log == 0 && units > fit.clusters[1][0] / 2 && a.max_blocks <= fit.pair_blocks) {
         two = 0;
         log = 4;
         while (log > 0 && (units > fit.clusters[0][log] || a.max_blocks < 64 << log)) --log;

@@ -152,3 +152,16 @@ def test_many_rows_and_calls_at_once(cuda_dev):
             c.pool.select_blocks(0, c.q, c.bounds, c.tables, c.lens, c.B, c.width, o, first=1, last=1, stream=st)
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("width", [24000, 28000, 49152])
+@pytest.mark.parametrize("B", [20, 60])
+def test_many_units_in_wide_tables(cuda_dev, B, width):
+    """Tables too wide for two CTAs' keys on an SM, and just not; rows of one block to some thousands."""
+    T = [(37 * i * i) % 900 + 1 for i in range(B)]
+    T[3], T[B - 1], T[7] = 40000, 17, 0
+    c = Cache(T, seed=31, hq=8, hkv=4, extra_width=width - 2500)
+    assert c.width == width
+    c.make_bounds()
+    c.check_selection(9, 1, 2)
+    assert c.scores[3, 0, 2500:].eq(-float("inf")).all()
