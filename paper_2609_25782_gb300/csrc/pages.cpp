@@ -222,9 +222,10 @@ int session_truncate(kv_pool *p, int32_t sid, int64_t tokens, kv_stream_t stream
     if (left || !gone.empty()) {
         cudaStream_t st = reinterpret_cast<cudaStream_t>(stream_);
         DeviceGuard dg(p->cfg.device, !p->host_only);
+        const bool fence = !gone.empty();
         int f = 0;
         int rc = own || left ? ensure_event(p, &s->ready) : KV_OK;
-        if (!rc) rc = p->open_fence(gone.data(), gone.size(), st, &f);
+        if (!rc && fence) rc = p->open_fence(gone.data(), gone.size(), st, &f);
         if (!rc) rc = wait_written(p, *s, st);
         if (!rc && own) {
             rc = p->wait_fences(got.data(), got.size(), st);
@@ -234,10 +235,10 @@ int session_truncate(kv_pool *p, int32_t sid, int64_t tokens, kv_stream_t stream
         }
         if (!rc && left) rc = p->wait_fences(&s->blocks[nb - 1], 1, st);
         if (!rc && (own || left)) rc = mark_moved(p, *s, st);
-        if (!rc) rc = p->record_fence(f, st);
+        if (!rc && fence) rc = p->record_fence(f, st);
         if (rc) return rc;
 
-        const uint64_t gen = p->commit_fence(f);
+        const uint64_t gen = fence ? p->commit_fence(f) : 0;
         if (p->lru) p->lru_out(sid);
         take(p, got);
         drop_tail(p, *s, nb, f, gen);

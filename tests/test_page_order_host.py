@@ -57,7 +57,8 @@ class Pool:
         assert x.kv_pool_create(C.byref(cfg), C.byref(self.h)) == kv.KV_OK
         self.clocks, self.events, self.host = {}, {}, {}
         self.past = {}                                   # block -> [(row from, to, writes, stream, tick, what)]
-        self.grown = {}                                  # session -> its stream of reservations' writes, with a clock
+        self.grown = {}                                  # session -> the clock of its last reservation's writes
+        self.moves = {}                                  # session -> the clock of all that read or wrote for it
 
     def call(self, name, *a):
         rc = getattr(self.x, name)(self.h, *a)
@@ -111,9 +112,10 @@ class Pool:
         for c in self.clocks.values():
             self.merge(self.host, c)
 
-    def touch(self, stream, blocks, first, end, writes, what):
-        """Rows of tokens [first, end), which lie in `blocks` (the session's), by the stream's newest launch."""
+    def touch(self, stream, sid, blocks, first, end, writes, what):
+        """Rows of a session's tokens [first, end), which lie in `blocks`, by the stream's newest launch."""
         c = self.clock(stream)
+        self.merge(self.moves.setdefault(sid, {}), c)
         for j in range(first // BT, -(-end // BT)):
             lo, hi = max(first, j * BT) - j * BT, min(end, (j + 1) * BT) - j * BT
             past = self.past.setdefault(blocks[j], [])
@@ -135,7 +137,7 @@ class Pool:
     def append(self, sid, n, st):
         T = self.info(sid).tokens
         self.call("session_append", sid, 256, 256, n, st)
-        self.touch(st, self.row(sid), T, T + n, True, f"append({sid})")
+        self.touch(st, sid, self.row(sid), T, T + n, True, f"append({sid})")
 
     def reserve(self, sids, n, st):
         """A reservation and, behind it on the stream, the kernel that writes the tokens."""
@@ -144,7 +146,7 @@ class Pool:
         self.call("kv_pool_batch_reserve_tokens", (C.c_int32 * B)(*sids), (C.c_int32 * B)(*[n] * B), B, 256, 64, 256, st)
         self.tick(st)
         for s, t in zip(sids, T):
-            self.touch(st, self.row(s), t, t + n, True, f"reserved tokens({s})")
+            self.touch(st, s, self.row(s), t, t + n, True, f"reserved tokens({s})")
             self.grown[s] = dict(self.clock(st))
 
     def pause(self, sid, st):
@@ -152,19 +154,19 @@ class Pool:
         i, row = self.info(sid), self.row(sid)
         self.call("session_pause", sid, st)
         if i.tokens > i.cold_valid:
-            self.touch(st, row, i.cold_valid, i.tokens, False, f"pause({sid})")
+            self.touch(st, sid, row, i.cold_valid, i.tokens, False, f"pause({sid})")
 
     def resume(self, sid, st):
         self.call("session_resume", sid, st)
-        self.touch(st, self.row(sid), 0, self.info(sid).tokens, True, f"resume({sid})")
+        self.touch(st, sid, self.row(sid), 0, self.info(sid).tokens, True, f"resume({sid})")
 
     def fork(self, sid, n, tokens, st):
         self.caller_orders(sid, st)
         out = (C.c_int32 * n)()
         self.call("session_fork", sid, tokens, 512, n, out, st)
         for k in out if tokens % BT else ():
-            self.touch(st, self.row(sid), tokens // BT * BT, tokens, False, f"fork of {sid}")
-            self.touch(st, self.row(k), tokens // BT * BT, tokens, True, f"fork to {k}")
+            self.touch(st, sid, self.row(sid), tokens // BT * BT, tokens, False, f"fork of {sid}")
+            self.touch(st, k, self.row(k), tokens // BT * BT, tokens, True, f"fork to {k}")
         return list(out)
 
     def truncate(self, sid, tokens, st):
@@ -173,8 +175,8 @@ class Pool:
         self.call("session_truncate", sid, tokens, st)
         row = self.row(sid)
         if row and row[-1] != old[len(row) - 1]:
-            self.touch(st, old, tokens // BT * BT, tokens, False, f"truncation of {sid}")
-            self.touch(st, row, tokens // BT * BT, tokens, True, f"truncation of {sid}")
+            self.touch(st, sid, old, tokens // BT * BT, tokens, False, f"truncation of {sid}")
+            self.touch(st, sid, row, tokens // BT * BT, tokens, True, f"truncation of {sid}")
 
     def compact(self, sid, n, prefix, st):
         self.caller_orders(sid, st)
@@ -185,14 +187,15 @@ class Pool:
         row = self.row(sid)
         first = prefix if row[prefix // BT] == old[prefix // BT] else prefix // BT * BT
         past, self.past = self.past, {b: list(x) for b, x in self.past.items()}
-        self.touch(st, old, first, T, False, f"compaction of {sid}")
+        self.touch(st, sid, old, first, T, False, f"compaction of {sid}")
         read, self.past = self.past, past
-        self.touch(st, row, first, prefix + n, True, f"compaction of {sid}")
+        self.touch(st, sid, row, first, prefix + n, True, f"compaction of {sid}")
         for b, x in read.items():                        # (its own reads and writes are one kernel's)
             self.past.setdefault(b, []).extend(y for y in x if y not in self.past[b])
 
     def destroy(self, sid):
-        self.synchronise()
+        """The caller has waited for the session's own work, and for nothing else."""
+        self.merge(self.host, self.moves.pop(sid, {}))
         self.grown.pop(sid, None)
         self.call("session_destroy", sid)
 
@@ -245,6 +248,23 @@ def test_tokens_behind_a_cut_wait_for_a_former_holders_move(pool, leave, tokens,
     pool.truncate(k, tokens, B)
     pool.append(k, 8, H) if grow == "append" else pool.reserve([k], 8, H)
     pool.append(k, 8, A)
+
+
+@pytest.mark.parametrize("left", [1, 3])
+def test_a_cut_that_gives_back_no_block_takes_no_fence(pool, left):
+    """And the fence of who left stays on the block: who gets it after the session has ended waits for it."""
+    p, k = shared(pool)
+    pool.pause(p, A)
+    made = pool.x.fake_events()
+    for t in (206, 205, 204):
+        pool.truncate(k, t, B)
+        assert pool.waits > 0 and pool.launches == 0
+    assert pool.x.fake_events() == made                  # (the ready event is the fork's)
+    if left == 3:
+        pool.truncate(k, 48, B)
+    pool.destroy(k)
+    o = pool.create(512)
+    pool.append(o, 400, H)
 
 
 def test_a_fork_of_a_block_that_was_shared(pool):
