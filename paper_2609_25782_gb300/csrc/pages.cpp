@@ -181,7 +181,7 @@ int session_fork(kv_pool *p, int32_t sid, int64_t tokens, int64_t max_tokens, in
     p->evict_commit(vic);
     take(p, got);
     p->stats.bytes_unpacked += fetched * p->image_token_bytes;
-    parent->ready_recorded = parent->moved = !p->host_only;
+    parent->ready_recorded = !p->host_only;
     for (int64_t j = 0; j < shared; ++j) p->block_extra[parent->blocks[j]] += n;
     p->forked = p->forked || shared > 0;
     const uint64_t stamp = p->lru ? ++p->clock : 0;
@@ -190,7 +190,7 @@ int session_fork(kv_pool *p, int32_t sid, int64_t tokens, int64_t max_tokens, in
         s.T = tokens;
         s.blocks.assign(parent->blocks.begin(), parent->blocks.begin() + shared);
         s.blocks.insert(s.blocks.end(), got.begin() + c * each, got.begin() + (c + 1) * each);
-        s.ready_recorded = s.moved = !p->host_only;
+        s.ready_recorded = !p->host_only;
         if (p->lru) {
             s.img_tok.assign(nb, 0);
             s.hot_count = nb;
@@ -246,7 +246,7 @@ int session_truncate(kv_pool *p, int32_t sid, int64_t tokens, kv_stream_t stream
             p->give_back(s->blocks[nb - 1], f, gen);
             s->blocks[nb - 1] = got[0];
         }
-        if (own || left) s->ready_recorded = s->moved = !p->host_only;
+        if (own || left) s->ready_recorded = !p->host_only;
         if (p->lru) p->lru_in(sid);
     } else {
         s->blocks.resize(nb);                     // evicted ones, if any
@@ -341,7 +341,7 @@ int session_compact(kv_pool *p, int32_t sid, const int32_t *keep, int64_t layer_
         }
     if (p->lru) p->lru_in(sid);
     s->T = end;
-    s->ready_recorded = s->moved = !p->host_only;
+    s->ready_recorded = !p->host_only;
     forget_image(p, *s, prefix);
     return KV_OK;
 }

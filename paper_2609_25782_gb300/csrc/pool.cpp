@@ -378,7 +378,7 @@ static int lru_resume(kv_pool *p, int32_t sid, cudaStream_t st) {
 
     DeviceGuard dg(p->cfg.device, !p->host_only);
     int rc = ensure_event(p, &s->ready);
-    if (!rc && s->moved) rc = wait_event(p, st, s->ready);
+    if (!rc && s->ready_recorded) rc = wait_event(p, st, s->ready);
     if (!rc) rc = p->wait_fences(got.data(), got.size(), st);
     if (!rc) rc = p->evict_device(vic, st);
     if (!rc && need > 0) rc = p->wait_packed(sid, st);
@@ -396,7 +396,6 @@ static int lru_resume(kv_pool *p, int32_t sid, cudaStream_t st) {
     s->last_use = ++p->clock;
     p->lru_in(sid);
     s->ready_recorded = !p->host_only;
-    s->moved = false;
     p->stats.free_blocks -= need;
     p->stats.used_blocks += need;
     p->stats.bytes_unpacked += fetched * p->image_token_bytes;
@@ -446,7 +445,7 @@ int kvt::lru_fetch(kv_pool *p, const std::vector<int32_t> &uniq,
     for (size_t u = 0; !rc && record_ready && u < uniq.size(); ++u)
         if (!miss[u].empty()) {
             rc = ensure_event(p, &p->sessions[uniq[u]].ready);
-            if (!rc && p->sessions[uniq[u]].moved) rc = wait_event(p, st, p->sessions[uniq[u]].ready);
+            if (!rc && p->sessions[uniq[u]].ready_recorded) rc = wait_event(p, st, p->sessions[uniq[u]].ready);
         }
     if (!rc) rc = p->wait_fences(got.data(), got.size(), st);
     if (!rc) rc = p->evict_device(vic, st);
@@ -471,10 +470,7 @@ int kvt::lru_fetch(kv_pool *p, const std::vector<int32_t> &uniq,
         s.hot_count += static_cast<int64_t>(miss[u].size());
         s.last_use = stamp;
         p->lru_in(uniq[u]);
-        if (record_ready && !miss[u].empty()) {
-            s.ready_recorded = !p->host_only;
-            s.moved = false;
-        }
+        if (record_ready && !miss[u].empty()) s.ready_recorded = !p->host_only;
     }
     p->stats.free_blocks -= need;
     p->stats.used_blocks += need;
@@ -783,7 +779,7 @@ int session_pause(kv_pool *p, int32_t sid, kv_stream_t stream_) {
     s->blocks.clear();
     s->cold_valid = t1;
     s->state = KV_SESSION_PAUSED;
-    s->ready_recorded = s->moved = false;
+    s->ready_recorded = false;
     s->appended_recorded = false;
     return KV_OK;
 }

@@ -28,10 +28,8 @@ struct Session {
     std::vector<int16_t> img_tok;     // residency mode: tokens of block j held by the image
     int64_t hot_count = 0;            // residency mode: blocks with a hot slot
     uint64_t last_use = 0;            // residency mode: recency stamp
-    cudaEvent_t ready = nullptr;
-    bool ready_recorded = false;
-    bool moved = false;               // `ready` marks a move of the session's rows (pages.cpp): who records it again
-                                      // waits for it first
+    cudaEvent_t ready = nullptr;      // behind the last resume, fetch or move of its rows (pages.cpp); who records it
+    bool ready_recorded = false;      // again waits for it first, so that it covers those before as well
     cudaEvent_t appended = nullptr;
     bool appended_recorded = false;
     cudaEvent_t packed = nullptr;     // residency mode: after the last eviction that wrote

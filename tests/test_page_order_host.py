@@ -94,12 +94,13 @@ class Pool:
         out = (C.c_int64 * 3000)()
         n = self.x.fake_calls(out, 1000)
         assert n <= 1000
-        self.launches = 0
+        self.launches, self.first = 0, None              # the stream's clock behind the first launch
         self.waits = out[0:3 * n:3].count(WAIT)
         for what, stream, event in zip(out[0:3 * n:3], out[1:3 * n:3], out[2:3 * n:3]):
             if what == LAUNCH:
                 self.tick(stream)
                 self.launches += 1
+                self.first = self.first or dict(self.clock(stream))
             elif what == RECORD:
                 self.merge(self.clock(stream), self.host)
                 self.events[event] = dict(self.clock(stream))
@@ -112,9 +113,9 @@ class Pool:
         for c in self.clocks.values():
             self.merge(self.host, c)
 
-    def touch(self, stream, sid, blocks, first, end, writes, what):
-        """Rows of a session's tokens [first, end), which lie in `blocks`, by the stream's newest launch."""
-        c = self.clock(stream)
+    def touch(self, stream, sid, blocks, first, end, writes, what, clock=None):
+        """Rows of a session's tokens [first, end), which lie in `blocks`, by the stream's newest launch (or that of `clock`)."""
+        c = clock or self.clock(stream)
         self.merge(self.moves.setdefault(sid, {}), c)
         for j in range(first // BT, -(-end // BT)):
             lo, hi = max(first, j * BT) - j * BT, min(end, (j + 1) * BT) - j * BT
@@ -390,3 +391,194 @@ def test_random_moves_on_several_streams(pool, seed):
         except Refused:                                  # full, or in another state
             pass
     assert all(done.get(x, 0) > 5 for x in ("append", "reserve", "pause", "resume", "fork", "truncate", "compact"))
+
+
+# ---- residency mode -----------------------------------------------------------------------
+
+class Resident(Pool):
+    """A pool that evicts. Evictions and fetches of a call show in the sessions' tables; the model knows what each
+    image holds. An allocating call is ordered by its caller behind reservations and what they write, as the header
+    says."""
+
+    def __init__(self, kv, path, **more):
+        super().__init__(kv, path, flags=kv.KV_POOL_LRU_RESIDENCY, **more)
+        self.image = {}                                  # session -> tokens of each block that its image holds
+
+    def tokens_in(self, T, j):
+        return max(0, min(BT, T - j * BT))
+
+    def behind_reservations(self, st):
+        for c in self.grown.values():
+            self.merge(self.clock(st), c)
+
+    def moved(self, st, f, skip=()):
+        """Runs a call; notes its evictions and fetches."""
+        old = {s: (self.row(s), self.info(s).tokens) for s in self.image}
+        f()                                              # (evictions are its first launch)
+        for s, (row, T) in old.items():
+            now = self.row(s)
+            for j, (a, b) in enumerate(zip(row, now)):
+                if a >= 0 and b < 0:                     # out
+                    n = self.tokens_in(T, j)
+                    if n > self.image[s][j]:
+                        at = (self.image[s][j], n)
+                        self.touch(st, s, {0: a}, *at, False, f"eviction of {s}", self.first)
+                        self.touch(st, s, {0: ("image", s, j)}, *at, True, f"eviction of {s}", self.first)
+                        self.image[s][j] = n
+        for s, (row, T) in old.items():
+            now = self.row(s)
+            for j, (a, b) in enumerate(zip(row, now)):
+                if a < 0 and b >= 0 and s not in skip:   # back
+                    n = self.tokens_in(T, j)
+                    self.touch(st, s, {0: ("image", s, j)}, 0, n, False, f"fetch of {s}")
+                    self.touch(st, s, {0: b}, 0, n, True, f"fetch of {s}")
+
+    def shape(self, sid, T):
+        im = self.image[sid]
+        n = -(-T // BT)
+        self.image[sid] = [min(x, self.tokens_in(T, j)) for j, x in enumerate(im[:n])] + [0] * (n - len(im))
+
+    def create(self, n=512):
+        sid = super().create(n)
+        self.image[sid] = []
+        return sid
+
+    def append(self, sid, n, st):
+        self.behind_reservations(st)
+        T = self.info(sid).tokens
+        self.moved(st, lambda: self.call("session_append", sid, 256, 256, n, st))
+        self.touch(st, sid, self.row(sid), T, T + n, True, f"append({sid})")
+        self.shape(sid, T + n)
+
+    def reserve(self, sids, n, st):
+        self.behind_reservations(st)
+        T = [self.info(s).tokens for s in sids]
+        B = len(sids)
+        self.moved(st, lambda: self.call("kv_pool_batch_reserve_tokens", (C.c_int32 * B)(*sids), (C.c_int32 * B)(*[n] * B), B, 256,
+                                         64, 256, st))
+        self.tick(st)
+        for s, t in zip(sids, T):
+            self.touch(st, s, self.row(s), t, t + n, True, f"reserved tokens({s})")
+            self.grown[s] = dict(self.clock(st))
+            self.shape(s, t + n)
+
+    def pause(self, sid, st):
+        self.call("session_pause", sid, st)
+
+    def resume(self, sid, st):
+        self.behind_reservations(st)
+        self.moved(st, lambda: self.call("session_resume", sid, st))
+
+    def prefetch(self, sids, st):
+        self.behind_reservations(st)
+        a = (C.c_int32 * len(sids))(*sids)
+        self.moved(st, lambda: self.call("kv_pool_prefetch", a, len(sids), None, 0, st))
+
+    def fork(self, sid, n, tokens, st):
+        self.behind_reservations(st)
+        out, row = (C.c_int32 * n)(), self.row(sid)
+        self.moved(st, lambda: self.call("session_fork", sid, tokens, 512, n, out, st))
+        for k in out:
+            self.image[k] = [0] * -(-tokens // BT)
+            for j in range(-(-tokens // BT)):
+                rows = self.tokens_in(tokens, j)
+                self.touch(st, sid, {0: row[j] if row[j] >= 0 else ("image", sid, j)}, 0, rows, False, f"fork of {sid}")
+                self.touch(st, k, {0: self.row(k)[j]}, 0, rows, True, f"fork to {k}")
+        return list(out)
+
+    def truncate(self, sid, tokens, st):
+        self.caller_orders(sid, st)
+        self.call("session_truncate", sid, tokens, st)
+        self.shape(sid, tokens)
+
+    def compact(self, sid, n, prefix, st):
+        self.behind_reservations(st)
+        T = self.info(sid).tokens
+        self.moved(st, lambda: self.call("session_compact", sid, 256, 0, 0, n, prefix, st))
+        if n and prefix + n < T:
+            self.touch(st, sid, self.row(sid), prefix, prefix + n, True, f"compaction of {sid}")
+            self.shape(sid, prefix)
+        self.shape(sid, prefix + n)
+
+    def destroy(self, sid):
+        self.truncate(sid, 0, B)                         # its blocks may be others' next, behind a fence
+        super().destroy(sid)
+        del self.image[sid]
+        self.past = {b: x for b, x in self.past.items() if not (isinstance(b, tuple) and b[1] == sid)}
+
+
+@pytest.fixture()
+def resident(kv, tmp_path):
+    return Resident(kv, shutil.copy(built(), tmp_path / "pool.so"), nb=40)
+
+
+def out_and_back(pool):
+    """A session whose first ten blocks had left and came back on stream A, and one of 20 blocks."""
+    p, o = pool.create(), pool.create(1024)
+    pool.append(p, 16 * 12, G)
+    pool.append(o, 16 * 38, G)                           # 40 blocks: p's first ten leave
+    pool.pause(p, G)
+    pool.truncate(o, 16 * 20, G)
+    pool.synchronise()
+    pool.resume(p, A)
+    return p, o
+
+
+@pytest.mark.parametrize("then", ["compact", "fork", "append", "reserve", "evict"])
+def test_a_second_resume_still_stands_for_the_first_ones_fetches(resident, then):
+    pool = resident
+    p, o = out_and_back(pool)
+    pool.truncate(p, 16 * 11 + 9, B)
+    pool.pause(p, B)
+    pool.resume(p, B)                                    # nothing is missing: its event alone
+    if then == "compact":
+        pool.compact(p, 150, 5, H)
+    elif then == "fork":
+        pool.fork(p, 1, 100, H)
+    elif then == "evict":
+        pool.append(o, 16 * 18, H)
+    elif then == "append":
+        pool.truncate(p, 100, B)                         # into a block that was fetched
+        pool.append(p, 7, H)
+    else:
+        pool.truncate(p, 100, B)
+        pool.reserve([p], 7, H)
+
+
+@pytest.mark.parametrize("seed", [*range(12), 126, 129])
+def test_random_moves_on_several_streams_in_residency_mode(resident, seed):
+    r, pool = random.Random(seed), resident
+    live, done = {}, {}
+    for step in range(700):
+        st, op = r.choice([A, B, G, H]), r.choice(["create", "append", "append", "append", "reserve", "pause", "resume", "fork",
+                                                   "truncate", "truncate", "compact", "compact", "prefetch", "destroy"])
+        sid = r.choice(list(live)) if live else None
+        try:
+            if op == "create" or sid is None:
+                live[pool.create()] = r.choice([A, B, G, H])
+            elif op == "append":
+                pool.append(sid, r.choice([1, 7, 16, 60, 100]), live[sid])
+            elif op == "reserve":
+                pool.reserve([sid], r.choice([1, 20]), live[sid])
+            elif op in ("pause", "resume"):
+                getattr(pool, op)(sid, st)
+            elif op == "prefetch":
+                pool.prefetch([sid], st)
+            elif op == "fork":
+                T = pool.info(sid).tokens
+                for k in pool.fork(sid, r.choice([1, 2]), r.choice([T, T // BT * BT, r.randrange(T + 1)]), st):
+                    live[k] = r.choice([A, B, G, H])
+            elif op == "truncate":
+                T = pool.info(sid).tokens
+                pool.truncate(sid, max(0, T - r.choice([1, 5, 9, 30, 200])), st)
+            elif op == "compact":
+                T = pool.info(sid).tokens
+                prefix = r.randrange(T + 1)
+                pool.compact(sid, r.choice([T - prefix, max(0, T - prefix - 1), r.randrange(T - prefix + 1)]), prefix, st)
+            elif r.random() < 0.5:
+                pool.destroy(sid)
+                del live[sid]
+            done[op] = done.get(op, 0) + 1
+        except Refused:                                  # full, or in another state
+            pass
+    assert all(done.get(x, 0) > 2 for x in ("append", "reserve", "pause", "resume", "fork", "truncate", "compact", "prefetch"))
