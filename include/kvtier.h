@@ -532,7 +532,8 @@ int session_pause(kv_pool *pool, int32_t sid, kv_stream_t stream);
  * KV_ERR_NO_HOT_BLOCKS (nothing changes). */
 int session_resume(kv_pool *pool, int32_t sid, kv_stream_t stream);
 
-/* Event recorded after the session's last resume (NULL if none): a decode
+/* Event recorded after the session's last resume, prefetched blocks, fork or
+ * move of its rows (NULL if none); it covers those before as well. A decode
  * stream waits on it before reading the session's blocks (Section 3,
  * "Eviction, resume and decode": a resumed session decodes once its KV is
  * back in HBM; resume overlaps other work). The event is owned by the pool
@@ -569,7 +570,9 @@ int session_block_table_device(kv_pool *pool, int32_t sid, const int32_t **dev_r
 /* Build the decode inputs of a batch of ACTIVE sessions: block_tables
  * (device int32 [B][max_blocks], entries past a row's length set to -1) and
  * seq_lens (device int32 [B]) from the pool's tables. sids is a host array
- * of B ids. */
+ * of B ids. In residency mode the members' evicted blocks are fetched first, and
+ * the stream waits for the members' ready events (a resume's or a prefetch's
+ * fetches); otherwise the caller orders the call behind them. */
 int kv_pool_batch_tables(kv_pool *pool, const int32_t *sids, int32_t B, int32_t *block_tables,
                          int32_t max_blocks, int32_t *seq_lens, kv_stream_t stream);
 

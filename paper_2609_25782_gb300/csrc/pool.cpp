@@ -937,7 +937,10 @@ int kv_pool_batch_tables(kv_pool *p, const int32_t *sids, int32_t B, int32_t *bl
     DeviceGuard dg(p->cfg.device, true);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream_);
     if (p->lru) {
-        int rc = lru_fetch_batch(p, sids, B, st);
+        int rc = KV_OK;
+        for (int32_t i = 0; !rc && i < B; ++i)   // blocks that a prefetch or a resume is still bringing
+            if (p->sessions[sids[i]].ready_recorded) rc = wait_event(p, st, p->sessions[sids[i]].ready);
+        if (!rc) rc = lru_fetch_batch(p, sids, B, st);
         if (rc || p->host_only) return rc;   // host-logic pools: bookkeeping only
     }
     return gather_batch(p, sids, B, block_tables, max_blocks, seq_lens, st);

@@ -403,6 +403,7 @@ class Resident(Pool):
     def __init__(self, kv, path, **more):
         super().__init__(kv, path, flags=kv.KV_POOL_LRU_RESIDENCY, **more)
         self.image = {}                                  # session -> tokens of each block that its image holds
+        self.appended = {}                               # session -> the clock of its last append
 
     def tokens_in(self, T, j):
         return max(0, min(BT, T - j * BT))
@@ -448,6 +449,7 @@ class Resident(Pool):
         T = self.info(sid).tokens
         self.moved(st, lambda: self.call("session_append", sid, 256, 256, n, st))
         self.touch(st, sid, self.row(sid), T, T + n, True, f"append({sid})")
+        self.appended[sid] = dict(self.clock(st))
         self.shape(sid, T + n)
 
     def reserve(self, sids, n, st):
@@ -473,6 +475,19 @@ class Resident(Pool):
         self.behind_reservations(st)
         a = (C.c_int32 * len(sids))(*sids)
         self.moved(st, lambda: self.call("kv_pool_prefetch", a, len(sids), None, 0, st))
+
+    def tables(self, sids, st):
+        """A batch's tables and, behind them on the stream, a kernel that reads its tokens. (Appends are the caller's to
+        come behind.)"""
+        self.behind_reservations(st)
+        for s in sids:
+            self.merge(self.clock(st), self.appended.get(s, {}))
+        a = (C.c_int32 * len(sids))(*sids)
+        self.moved(st, lambda: self.call("kv_pool_batch_tables", a, len(sids), 256, 64, 256, st))
+        self.tick(st)
+        for s in sids:
+            self.touch(st, s, self.row(s), 0, self.info(s).tokens, False, f"decode of {s}")
+            self.grown[s] = dict(self.clock(st))
 
     def fork(self, sid, n, tokens, st):
         self.behind_reservations(st)
@@ -504,12 +519,30 @@ class Resident(Pool):
         self.truncate(sid, 0, B)                         # its blocks may be others' next, behind a fence
         super().destroy(sid)
         del self.image[sid]
+        self.appended.pop(sid, None)
         self.past = {b: x for b, x in self.past.items() if not (isinstance(b, tuple) and b[1] == sid)}
 
 
 @pytest.fixture()
 def resident(kv, tmp_path):
     return Resident(kv, shutil.copy(built(), tmp_path / "pool.so"), nb=40)
+
+
+@pytest.mark.parametrize("back", ["prefetch", "resume"])
+def test_a_batchs_tables_wait_for_what_is_being_fetched(resident, back):
+    pool = resident
+    p, o = out_and_back(pool)
+    pool.synchronise()
+    pool.append(o, 16 * 17, G)                           # 9 of p's leave again
+    assert pool.row(p)[:9] == [-1] * 9
+    pool.truncate(o, 16, G)
+    pool.synchronise()
+    if back == "prefetch":
+        pool.prefetch([p], A)
+    else:
+        pool.pause(p, A)
+        pool.resume(p, A)
+    pool.tables([p], B)
 
 
 def out_and_back(pool):
@@ -551,7 +584,7 @@ def test_random_moves_on_several_streams_in_residency_mode(resident, seed):
     live, done = {}, {}
     for step in range(700):
         st, op = r.choice([A, B, G, H]), r.choice(["create", "append", "append", "append", "reserve", "pause", "resume", "fork",
-                                                   "truncate", "truncate", "compact", "compact", "prefetch", "destroy"])
+                                                   "truncate", "truncate", "compact", "compact", "prefetch", "tables", "destroy"])
         sid = r.choice(list(live)) if live else None
         try:
             if op == "create" or sid is None:
@@ -562,8 +595,8 @@ def test_random_moves_on_several_streams_in_residency_mode(resident, seed):
                 pool.reserve([sid], r.choice([1, 20]), live[sid])
             elif op in ("pause", "resume"):
                 getattr(pool, op)(sid, st)
-            elif op == "prefetch":
-                pool.prefetch([sid], st)
+            elif op in ("prefetch", "tables"):
+                getattr(pool, op)([sid], st)
             elif op == "fork":
                 T = pool.info(sid).tokens
                 for k in pool.fork(sid, r.choice([1, 2]), r.choice([T, T // BT * BT, r.randrange(T + 1)]), st):
@@ -581,4 +614,4 @@ def test_random_moves_on_several_streams_in_residency_mode(resident, seed):
             done[op] = done.get(op, 0) + 1
         except Refused:                                  # full, or in another state
             pass
-    assert all(done.get(x, 0) > 2 for x in ("append", "reserve", "pause", "resume", "fork", "truncate", "compact", "prefetch"))
+    assert all(done.get(x, 0) > 2 for x in ("append", "reserve", "pause", "resume", "fork", "truncate", "compact", "prefetch", "tables"))
