@@ -513,3 +513,31 @@ def test_branches_decode_sparsely_and_shrink(cuda_dev, bt, lru):
     for _ in range(2):
         step([kids[2], kids[0], parent, kids[1]])
     m.check()
+
+
+@pytest.mark.parametrize("back", ["prefetch", "resume"])
+def test_tables_of_blocks_that_another_stream_is_bringing(cuda_dev, back):
+    """Fetches behind a spin on one stream; a kernel behind the batch's tables on another reads the blocks."""
+    m = Model(30, lru=True, seed=19)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    p, o = m.create(300), m.create(50)                   # 19 and 4 blocks
+    m.append(o, 330)                                     # 24: 13 of p's leave
+    m.truncate(o, 16)
+    assert m.pool.session_info(p).num_blocks < 19
+    rows = torch.zeros(1, 41, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(1, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(a):
+        torch.cuda._sleep(20_000_000)
+    if back == "prefetch":
+        m.pool.prefetch([p], (), a)
+    else:
+        m.pool.session_pause(p)
+        m.pool.session_resume(p, a)
+    m.pool.batch_tables([p], rows, 41, lens, b)
+    with torch.cuda.stream(b):
+        got = m.hot[rows[0, :19].long()]
+    torch.cuda.synchronize()
+    assert rows[0, :19].tolist() == m.pool.session_block_table(p) and int(lens[0]) == 300
+    assert torch.equal(got.permute(1, 2, 3, 0, 4, 5).flatten(3, 4)[:, :, :, :300], m.want[p])
+    m.check()
